@@ -255,6 +255,14 @@ hipError_t stage_to_device(void* dst, const void* src, size_t bytes, hipStream_t
 
 }  // namespace
 
+namespace c3 {
+
+hipError_t stage_bytes(void* dst, const void* src, size_t bytes, hipStream_t s) {
+    return stage_to_device(dst, src, bytes, s);
+}
+
+}  // namespace c3
+
 extern "C" {
 
 int c3_abi_version(void) { return C3_ABI_VERSION; }

@@ -1,0 +1,432 @@
+// What the attention kernels share: the work list, LDS tiles, fragments and the
+// masked product.
+//
+// Rows.  The query heads that share a key head are taken together: row r of a
+// sequence and key head is query r / group and head r % group of the group, so
+// a tile of rows reads a key tile once for all of them, and a token's row of a
+// group of 8 fills a quarter of a matrix operand.
+//
+// Matrix operands.  v_mfma_f32_32x32x16 takes, from lane l = 32 h + c, eight
+// elements k = 8 h .. 8 h + 7 of row c of A (of column c of B), and leaves in
+// register i row 8 (i / 4) + 4 h + i % 4 of column c.  A product whose 32 rows
+// are the next product's inner index therefore feeds it without any movement:
+// registers 8 j .. 8 j + 7, rounded, are its B operand for inner indices
+//     16 j + 4 h + {0 .. 3}  and  16 j + 8 + 4 h + {0 .. 3},
+// and the A operand is read in that order.  So scores are computed with keys as
+// rows where the next product sums over keys (forward, dq) and with queries as
+// rows where it sums over queries (dk, dv), and probabilities never leave the
+// registers.  A operands along a tile's rows are 16-byte LDS reads; those across
+// them (values in the forward, for instance) are ds_read_b64_tr_b16 reads, which
+// hand lane c elements of four rows of column c.
+//
+// LDS tiles hold rows of DP elements in 16-byte pieces, piece p of row r at
+// p ^ swizzle(r), which spreads both kinds of reads over all banks.  They are
+// filled by buffer loads straight to LDS; a piece outside the sequence or
+// behind the head size reads as zeros by the buffer's bound.
+#pragma once
+
+#include "c3_internal.h"
+#include "c3_replay_types.h"
+
+namespace c3 {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kAttnThreads = 256;
+constexpr int kAttnWaves = kAttnThreads / 64;
+
+struct AttnSeq {
+    int32_t b;              // sequence
+    int32_t q_start, q_len, k_start, k_len;
+    int32_t unit0;          // its first unit of work of one key head
+};
+
+// Sequences that go along as a kernel's argument (4,096 bytes at most in all);
+// longer lists are staged.
+constexpr int kAttnArgSeqs = 128;
+
+struct AttnTable {
+    int32_t n;              // 0: every sequence has q_tokens and k_tokens
+    const AttnSeq* staged;  // or null: seq
+    AttnSeq seq[kAttnArgSeqs];
+};
+
+struct AttnTensor {
+    char* ptr;
+    int64_t sb, st, sh;     // bytes: batch, token, head
+};
+
+struct AttnArgs {
+    AttnTensor q, k, v, o, d_o, dq, dk, dv;
+    float* lse;
+    float* lse2;            // per row, as lse: in powers of two, +inf where a row sees nothing
+    float* delta;           // per row: the sum of dout * out
+    float* part;            // partial results of split units
+    float* part_ml;         // their maxima and sums
+    FastDiv group;          // query heads of a key head
+    FastDiv units;          // units of work of one key head, all sequences
+    FastDiv seq_units;      // of one sequence, where n == 0
+    FastDiv splits;         // parts of one tile's walk, where fixed
+    int32_t heads, kv_heads, dim, causal, window, packed;
+    int32_t q_tokens, k_tokens;
+    int32_t split_keys;     // keys of a split, where splits go by the length
+    float scale;
+};
+
+// One unit: a sequence, a key head and the number of the unit in them.
+struct AttnUnit {
+    int32_t b, q_start, q_len, q_pad, k_start, k_len, hk;
+    uint32_t unit;
+};
+
+// Workgroups of one key head follow each other on one of the eight dies (which
+// take workgroups in turn), so that its keys and values are shared in the die's L2.
+__device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n) {
+    const uint32_t die = id & 7, each = n >> 3, rest = n & 7;
+    return die * each + min(die, rest) + (id >> 3);
+}
+
+__device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
+    AttnUnit w;
+    w.hk = (int32_t)a.units.quot(block);
+    const uint32_t u = block - (uint32_t)w.hk * a.units.d;
+    if (tab.n == 0) {
+        w.b = (int32_t)a.seq_units.quot(u);
+        w.unit = u - (uint32_t)w.b * a.seq_units.d;
+        w.q_start = w.k_start = 0;
+        w.q_len = a.q_tokens;
+        w.k_len = a.k_tokens;
+    } else {
+        int lo = 0, hi = tab.n - 1;             // the last sequence with unit0 <= u
+        AttnSeq s;
+        if (tab.staged != nullptr) {
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if ((uint32_t)tab.staged[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+            }
+            s = tab.staged[lo];
+        } else {
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if ((uint32_t)tab.seq[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+            }
+            s = tab.seq[lo];
+        }
+        w.b = s.b;
+        w.q_start = s.q_start;
+        w.q_len = s.q_len;
+        w.k_start = s.k_start;
+        w.k_len = s.k_len;
+        w.unit = u - (uint32_t)s.unit0;
+    }
+    // the same for every lane, kept in scalar registers
+    w.b = __builtin_amdgcn_readfirstlane(w.b);
+    w.q_start = __builtin_amdgcn_readfirstlane(w.q_start);
+    w.q_len = __builtin_amdgcn_readfirstlane(w.q_len);
+    w.k_start = __builtin_amdgcn_readfirstlane(w.k_start);
+    w.k_len = __builtin_amdgcn_readfirstlane(w.k_len);
+    w.unit = __builtin_amdgcn_readfirstlane(w.unit);
+    w.hk = __builtin_amdgcn_readfirstlane(w.hk);
+    w.q_pad = a.packed ? w.q_len : a.q_tokens;
+    return w;
+}
+
+// First token's head `head` of a sequence.
+__device__ __forceinline__ char* seq_base(const AttnTensor& t, int packed, int b, int start, int head) {
+    return t.ptr + (packed ? (int64_t)0 : (int64_t)b * t.sb) + (int64_t)start * t.st + (int64_t)head * t.sh;
+}
+
+// Index into lse of query 0, head 0 of a sequence, in rows of `heads`.
+__device__ __forceinline__ int64_t seq_row(const AttnArgs& a, const AttnUnit& w) {
+    return ((int64_t)(a.packed ? 0 : w.b) * a.q_tokens + w.q_start) * a.heads;
+}
+
+// ---------------------------------------------------------------------------
+// fragments
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c);
+template <>
+__device__ __forceinline__ f32x16 mfma<__bf16>(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x16 mfma<_Float16>(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Registers 8 j .. 8 j + 7 of a product as the B operand of the next: rounded to
+// the 16 bits that the matrix units take (nearest, ties to even); the sums that
+// they enter stay in fp32.
+template <typename T>
+__device__ __forceinline__ u32x4 operand(const f32x16& x, int j) {
+    T e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = (T)x[8 * j + i];
+    u32x4 r;
+    __builtin_memcpy(&r, e, 16);
+    return r;
+}
+
+// Pieces of a row of DP elements; the shift spreads rows over the 256 bytes that
+// the 64 banks span.
+template <int DP>
+__device__ __forceinline__ int swizzle(int row) {
+    if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+}
+
+// Byte offsets of a lane's reads in a tile; they repeat every 16 rows.
+template <int DP>
+struct TileReads {
+    int along[DP / 16];         // A operand along rows 0..31, inner step ks
+    int across[DP / 32][2];     // transposed: columns 32 db .., rows 4 h + .. and 8 + 4 h + ..
+    __device__ __forceinline__ TileReads() {
+        const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks)
+            along[ks] = c * DP * 2 + (((2 * ks + h) ^ swizzle<DP>(c)) << 4);
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int row = s * 8 + h * 4 + (i >> 2);
+                const int piece = db * 4 + g * 2 + ((i & 3) >> 1);
+                across[db][s] = row * DP * 2 + ((piece ^ swizzle<DP>(row)) << 4) + (i & 1) * 8;
+            }
+    }
+};
+
+__device__ __forceinline__ u32x4 read_along(const char* tile, int offset) {
+    return *reinterpret_cast<const u32x4*>(tile + offset);
+}
+__device__ __forceinline__ u32x2 read_tr(const char* p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(p)));
+}
+// Rows 16 j + .. of a 32-row tile as an A operand across its rows.
+__device__ __forceinline__ u32x4 read_across(const char* tile, const int offset[2], int rows_bytes) {
+    const u32x2 lo = read_tr(tile + rows_bytes + offset[0]), hi = read_tr(tile + rows_bytes + offset[1]);
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+}
+
+// A lane's 16-byte pieces 2 ks + h of one row, from memory; zeros behind the head
+// size or for a row that does not exist.
+template <int DP>
+__device__ __forceinline__ void load_row(u32x4 (&f)[DP / 16], const char* row, bool there, int dim) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) {
+        f[ks] = u32x4{0, 0, 0, 0};
+        if (there && (2 * ks + h) * 8 < dim) f[ks] = *reinterpret_cast<const u32x4*>(row + (2 * ks + h) * 16);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// tiles
+// ---------------------------------------------------------------------------
+// ROWS rows of DP elements to LDS, each wave its part.  The byte offsets of a
+// lane's pieces from the tile's first row are those of `Offsets`.
+template <int DP, int ROWS>
+struct TileLoads {
+    static constexpr int kPieces = DP / 8;                  // of a row
+    static constexpr int kStepRows = 64 / kPieces;          // rows of one load of a wave
+    static constexpr int kSteps = ROWS / kStepRows / kAttnWaves;
+    static constexpr int kBytes = ROWS * DP * 2;
+    static_assert(kSteps * kStepRows * kAttnWaves == ROWS, "rows of a tile");
+};
+
+// Offsets of pieces of consecutive tokens, `st` bytes apart.
+template <int DP, int ROWS>
+struct TokenOffsets {
+    uint32_t at[TileLoads<DP, ROWS>::kSteps];
+    __device__ __forceinline__ TokenOffsets(int64_t st, int dim) {
+        using L = TileLoads<DP, ROWS>;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int n = 0; n < L::kSteps; ++n) {
+            const int row = (wave * L::kSteps + n) * L::kStepRows + lane / L::kPieces;
+            const int piece = (lane % L::kPieces) ^ swizzle<DP>(row);
+            at[n] = piece * 8 < dim ? (uint32_t)((int64_t)row * st) + piece * 16 : 0xFFFFFF00u;
+        }
+    }
+};
+
+__device__ __forceinline__ void load_piece_lds(const char* base, uint32_t bytes, uint32_t offset, char* lds) {
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds), 16,
+                                             (int)offset, 0, 0, 0);
+}
+
+// Loads `rows` (those left of the sequence, any number) of a tile; `base` is its
+// first row's head.
+template <int DP, int ROWS>
+__device__ __forceinline__ void load_tile(const char* base, int64_t st, int dim, int rows,
+                                          const TokenOffsets<DP, ROWS>& off, char* lds) {
+    using L = TileLoads<DP, ROWS>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n_rows = min(rows, ROWS);
+    const uint32_t bytes = n_rows > 0 ? (uint32_t)((int64_t)(n_rows - 1) * st) + dim * 2 : 0;
+#pragma unroll
+    for (int n = 0; n < L::kSteps; ++n)
+        load_piece_lds(base, bytes, off.at[n], lds + (wave * L::kSteps + n) * 1024);
+}
+
+// The wave's loads to LDS have landed and every wave of the workgroup is here.
+__device__ __forceinline__ void tiles_ready() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------------------
+// the masked product
+// ---------------------------------------------------------------------------
+// Bits 15 and 31 where a half of x is an infinity or NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+    if constexpr (__is_same(T, __bf16)) return (x & 0x7F807F80u) + 0x00800080u;
+    return (x & 0x7C007C00u) + 0x04000400u;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t one_bits() {      // 1.0
+    if constexpr (__is_same(T, __bf16)) return 0x3F80u;
+    return 0x3C00u;
+}
+
+// A product acc[db] += A[db] B over 16 inner indices where a pair (inner index,
+// column) that the mask hides must add nothing, whatever A holds there: 0 times an
+// infinity or NaN is NaN.  B is 0 at hidden pairs; `seen` has a bit for each of
+// the lane's 8 elements of B that are not hidden.  A's elements that are not
+// finite (none, in training that goes well) are replaced by 0 here, and where
+// they meet pairs that are seen, which indicator products find, the infinities
+// that they would have added are noted in `special`: bit i of special[db] for
+// +inf in register i of acc[db], bit 16 + i for -inf, both for NaN.
+// Its own function, called once in a blue moon, so that its registers are not
+// the kernels'.
+template <typename T>
+__device__ __attribute__((noinline)) u32x4 finite_operand(u32x4 A, u32x4 B, uint32_t seen, uint32_t* special) {
+    u32x4 b_pos{0, 0, 0, 0}, b_neg{0, 0, 0, 0};       // 1 where seen, by B's sign
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if ((seen >> (2 * i + s)) & 1) {
+                if ((B[i] >> (16 * s + 15)) & 1)
+                    b_neg[i] |= one_bits<T>() << (16 * s);
+                else
+                    b_pos[i] |= one_bits<T>() << (16 * s);
+            }
+    u32x4 a_pos{0, 0, 0, 0}, a_neg{0, 0, 0, 0};       // 1 at +inf and NaN; at -inf and NaN
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = A[i], flags = not_finite<T>(x);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (!((flags >> (16 * s + 15)) & 1)) continue;
+            const uint32_t half = (x >> (16 * s)) & 0xFFFFu;
+            const bool nan = (half & 0x7FFFu) != (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u);
+            A[i] &= ~(0xFFFFu << (16 * s));
+            if (nan || !(half & 0x8000u)) a_pos[i] |= one_bits<T>() << (16 * s);
+            if (nan || (half & 0x8000u)) a_neg[i] |= one_bits<T>() << (16 * s);
+        }
+    }
+    uint32_t found = 0;
+    f32x16 n = {};
+    n = mfma<T>(a_pos, b_pos, n);
+    n = mfma<T>(a_neg, b_neg, n);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) found |= n[i] > 0.0f ? 1u << i : 0u;
+    n = f32x16{};
+    n = mfma<T>(a_neg, b_pos, n);
+    n = mfma<T>(a_pos, b_neg, n);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) found |= n[i] > 0.0f ? 0x10000u << i : 0u;
+    *special = found;
+    return A;
+}
+
+template <typename T, int NDB>
+__device__ __forceinline__ void finite_operands(u32x4 (&A)[NDB], u32x4 B, uint32_t seen,
+                                                uint32_t (&special)[NDB]) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bad |= not_finite<T>(A[db][i]);
+    if (__builtin_expect(!__any((bad & 0x80008000u) != 0), 1)) return;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+        uint32_t found;
+        A[db] = finite_operand<T>(A[db], B, seen, &found);
+        special[db] |= found;
+    }
+}
+
+// The infinities that finite_operands noted.
+template <int NDB>
+__device__ __forceinline__ void add_special(f32x16 (&acc)[NDB], const uint32_t (&special)[NDB]) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) any |= special[db];
+    if (__builtin_expect(!__any(any != 0), 1)) return;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if ((special[db] >> i) & 1) acc[db][i] += __builtin_inff();
+            if ((special[db] >> (16 + i)) & 1) acc[db][i] -= __builtin_inff();
+        }
+}
+
+// ---------------------------------------------------------------------------
+// host side (c3_attention.hip)
+// ---------------------------------------------------------------------------
+// Checked sizes of a call and the list of its sequences, longest first.
+struct AttnPlan {
+    AttnArgs args;
+    AttnTable table;
+    int64_t rows;               // query rows of all heads: entries of lse
+    int64_t key_rows;           // key rows of all key heads
+    int64_t max_q, max_k;       // the longest of each
+    int64_t work;               // sum of q_len * k_len
+    AttnSeq* seqs;              // heap copy where more than kAttnArgSeqs, else null
+    AttnPlan() : args(), table(), seqs(nullptr) {}
+    AttnPlan(const AttnPlan&) = delete;
+    ~AttnPlan() { delete[] seqs; }
+    AttnSeq* list() { return seqs != nullptr ? seqs : table.seq; }
+};
+
+int attn_plan(const c3_attention_t* a, AttnPlan& p);
+int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTensor& to);
+// Numbers the units of each sequence, of which `units_of(queries, k_len, keys)`
+// (queries and keys with the padding of a dense batch) gives the count, and
+// returns those of one key head, or -1 where there are too many.
+template <typename F>
+int64_t attn_number(AttnPlan& p, int batch, F units_of) {
+    int64_t n = 0;
+    if (p.table.n == 0) {
+        const int64_t u = units_of(p.args.q_tokens, p.args.k_tokens, p.args.k_tokens);
+        p.args.seq_units = FastDiv((uint32_t)(u < 1 ? 1 : u));
+        n = u * batch;
+    } else {
+        AttnSeq* s = p.list();
+        for (int i = 0; i < p.table.n; ++i) {
+            s[i].unit0 = (int32_t)n;
+            n += units_of(p.args.packed ? s[i].q_len : p.args.q_tokens, s[i].k_len,
+                          p.args.packed ? s[i].k_len : p.args.k_tokens);
+            if (n >= (1ll << 31)) return -1;
+        }
+    }
+    return n;
+}
+size_t attn_table_bytes(const c3_attention_t* a);
+
+}  // namespace c3

@@ -78,6 +78,11 @@ int plan_fetch_blocks(size_t bytes);
 hipError_t launch_plan_fetch(const void* host_src, void* dst, size_t bytes, hipStream_t stream,
                              uint64_t* seen = nullptr, uint64_t seq = 0);
 
+// Copies `bytes` of host memory to device memory on `stream` through the pinned
+// ring (c3_api.cpp); `src` may be freed when this returns, `dst` has room for the
+// bytes rounded up to 16.
+hipError_t stage_bytes(void* dst, const void* src, size_t bytes, hipStream_t stream);
+
 hipError_t launch_tensor_signature(const c3_chunk_record_t* records, int R, int64_t C, int T,
                                    uint64_t* out, hipStream_t stream);
 

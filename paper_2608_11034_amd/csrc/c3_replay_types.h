@@ -1,0 +1,47 @@
+// Element types, wide loads and small helpers of the replay operators.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/c3_replay.h"
+
+namespace c3 {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// V elements of one load: 16 bytes on the wide paths, one element otherwise.
+template <typename T, int V>
+struct Pack {
+    T v[V];
+};
+template <typename T, int V>
+struct alignas(sizeof(T) * V) AlignedPack {
+    T v[V];
+};
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
+__device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
+
+// Division by a run-time constant d of numbers below 2^31: q = (mulhi(n, m) +
+// n) >> s, with s = ceil(log2 d) and m = ceil(2^32 (2^s - d) / d) (Granlund and
+// Montgomery, division by invariant integers, 1994).
+struct FastDiv {
+    uint32_t d, m, s;
+    FastDiv() : d(1), m(0), s(0) {}
+    explicit FastDiv(uint32_t div) : d(div), s(0) {
+        while ((1ull << s) < div) ++s;
+        m = (uint32_t)((((1ull << 32) * ((1ull << s) - div)) + div - 1) / div);
+    }
+    __device__ __forceinline__ uint32_t quot(uint32_t n) const {
+        return (uint32_t)(((uint64_t)__umulhi(n, m) + n) >> s);
+    }
+};
+
+inline int replay_elem_size(int dtype) {
+    return dtype == C3_F32 ? 4 : dtype == C3_BF16 || dtype == C3_F16 ? 2 : 0;
+}
+
+}  // namespace c3

@@ -1,0 +1,450 @@
+"""Operators of a replayed transformer layer (include/c3_replay.h) for torch
+tensors on a ROCm device.
+
+A replay runs a layer again on every replica and votes on outputs and
+gradients bit by bit, so each operator's bits depend on its inputs alone: no
+atomics, sums in an order that the sizes fix.  Argument marshalling only;
+every step runs in the HIP kernels of libc3.so and there is no CPU fallback.
+
+* ``rotary(x, positions, freqs)``         rotary positions; ``inverse`` is the gradient
+* ``rotary_frequencies(rot, ...)``        their frequencies, scaled for long contexts
+* ``attention(q, k, v)``                  output and per-row log-sum-exp
+* ``attention_grad(dout, q, k, v, out, lse)`` gradients of queries, keys and values
+* ``expert_sort(ids, num_experts)``       choices sorted by expert
+* ``expert_dispatch(x, order)``           tokens to their experts' rows
+* ``expert_combine(y, order, weights)``   and back, weighted
+* ``expert_combine_grad``, ``expert_dispatch_grad``  their gradients
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple
+
+import torch
+
+from . import c3
+from .c3 import BF16, F16, F32, C3Error, _check, _dev_tensor, _empty, _ptr, _stream
+
+HALF, INTERLEAVED = 0, 1
+MAX_HEAD_DIM = 128
+MAX_EXPERTS, MAX_TOP = 512, 64
+
+_CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_LAYOUT = {"half": HALF, "interleaved": INTERLEAVED}
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("in_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
+                ("heads", ctypes.c_int64)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "dim", "causal", "window")] + [
+        ("scale", ctypes.c_float), ("batch", ctypes.c_int32), ("q_tokens", ctypes.c_int64),
+        ("k_tokens", ctypes.c_int64), ("packed", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p)]
+
+
+class AttnTensor(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3)]
+
+
+class ExpertRows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("top", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("hidden", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("sorted_stride", ctypes.c_int64), ("slot", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
+
+
+_ready = False
+
+
+def _lib():
+    global _ready
+    L = c3.lib()
+    if not _ready:
+        vp, i32, i64, sz, dbl = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t,
+                                 ctypes.c_double)
+        L.c3_rotary.restype = i32
+        L.c3_rotary.argtypes = [vp, i32, i32, i64, i64, i64, vp, i32, vp, vp, i64, i32, i32, dbl, vp]
+        for n in ("c3_attention_workspace_size", "c3_attention_grad_workspace_size"):
+            getattr(L, n).restype = sz
+            getattr(L, n).argtypes = [vp]
+        L.c3_attention.restype = i32
+        L.c3_attention.argtypes = [vp] * 7 + [sz, vp]
+        L.c3_attention_grad.restype = i32
+        L.c3_attention_grad.argtypes = [vp] * 11 + [sz, vp]
+        L.c3_expert_sort_workspace_size.restype = sz
+        L.c3_expert_sort_workspace_size.argtypes = [i64, i32]
+        L.c3_expert_sort.restype = i32
+        L.c3_expert_sort.argtypes = [vp, i64, i32, vp, vp, vp, vp, sz, vp]
+        L.c3_expert_dispatch.restype = i32
+        L.c3_expert_dispatch.argtypes = [vp] * 4
+        L.c3_expert_combine.restype = i32
+        L.c3_expert_combine.argtypes = [vp] * 5
+        L.c3_expert_combine_grad.restype = i32
+        L.c3_expert_combine_grad.argtypes = [vp] * 7
+        _ready = True
+    return L
+
+
+def _rows(t, name, dtype=None, device=None, dim=None):
+    """A device tensor whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise C3Error(f"{name} must be a tensor on a ROCm GPU device")
+    if t.dtype not in _CODE:
+        raise C3Error(f"{name}: unsupported dtype {t.dtype}")
+    if dtype is not None and t.dtype != dtype:
+        raise C3Error(f"{name} must be {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise C3Error(f"{name} must be on {device}")
+    if dim is not None and t.dim() not in dim:
+        raise C3Error(f"{name} must have {' or '.join(map(str, dim))} dimensions")
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise C3Error(f"{name}: the last dimension must be contiguous")
+    return t
+
+
+def _overlap(t):
+    """Whether an output's elements share memory."""
+    return any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride()))
+
+
+def _new_like(x):
+    return _empty(x.shape, x.dtype, x.device)
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, scaling: str = "none",
+                       trained: int = 4096, slow: float = 1.0, fast: float = 32.0, device="cuda"):
+    """Radians a position of each of the rot / 2 pairs, fp64 on the device:
+    base ** (-2 i / rot), for a context ``factor`` times the ``trained`` one
+    rescaled by
+
+    * ``"linear"``: every frequency divided by the factor;
+    * ``"base"``:   a base factor ** (rot / (rot - 2)) times as large, which
+      divides the slowest pair by the factor and leaves the fastest;
+    * ``"ramp"``:   pairs that make fewer than ``slow`` turns in the trained
+      context divided, those with more than ``fast`` left, a linear ramp in
+      the number of turns between."""
+    if rot < 2 or rot % 2:
+        raise C3Error("rot must be even and positive")
+    if not base > 0 or not factor > 0:
+        raise C3Error("base and factor must be positive")
+    if scaling not in ("none", "linear", "base", "ramp"):
+        raise C3Error(f"unknown scaling {scaling}")
+    if scaling == "base":
+        if rot == 2:
+            raise C3Error("scaling the base needs more than one pair")
+        base = base * factor ** (rot / (rot - 2))
+    f = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    elif scaling == "ramp":
+        if not fast > slow:
+            raise C3Error("fast must exceed slow")
+        keep = [min(1.0, max(0.0, (trained * x / (2 * math.pi) - slow) / (fast - slow))) for x in f]
+        f = [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)]
+    return torch.tensor(f, dtype=torch.float64, device=device)
+
+
+def _strides4(t):
+    """(batch, token, head) strides of [B, S, H, D] or [S, H, D]."""
+    s = t.stride()
+    return (s[0], s[1], s[2]) if t.dim() == 4 else (0, s[0], s[1])
+
+
+def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
+           amplitude: float = 1.0, out=None, stream=None):
+    """Rotary positions on the first 2 * len(freqs) elements of every head.
+
+    ``x`` is a tensor [B, S, H, D] or [S, H, D], or two of them (queries and
+    keys) with the same B, S and D; ``positions`` int32 or int64 [B, S] or [S].
+    ``inverse`` turns back, which is the gradient.  ``out`` (same structure as
+    ``x``) may be ``x`` itself.  Returns what ``out`` is, or new tensors."""
+    single = isinstance(x, torch.Tensor)
+    xs = [x] if single else list(x)
+    if len(xs) not in (1, 2):
+        raise C3Error("rotary takes one tensor or two")
+    for i, t in enumerate(xs):
+        _rows(t, f"x[{i}]", xs[0].dtype if i else None, xs[0].device if i else None, (3, 4))
+        if t.dim() != xs[0].dim() or t.shape[:-2] != xs[0].shape[:-2] or t.shape[-1] != xs[0].shape[-1]:
+            raise C3Error("the tensors must agree in all but their heads")
+    first = xs[0]
+    B, S = (first.shape[0], first.shape[1]) if first.dim() == 4 else (1, first.shape[0])
+    D, dev = first.shape[-1], first.device
+    outs = [_new_like(t) for t in xs] if out is None else [out] if single else list(out)
+    if len(outs) != len(xs):
+        raise C3Error("out must have one tensor for each of x")
+    for t, y in zip(xs, outs):
+        _rows(y, "out", t.dtype, dev)
+        if y.shape != t.shape or _overlap(y):
+            raise C3Error("out must have the shape of x and no repeated elements")
+    if not isinstance(positions, torch.Tensor) or positions.device != dev or positions.dtype not in (
+            torch.int32, torch.int64):
+        raise C3Error("positions must be int32 or int64 on the device of x")
+    if positions.dim() == 1 and positions.shape[0] == S:
+        pos = (0, positions.stride(0))
+    elif positions.dim() == 2 and tuple(positions.shape) == (B, S):
+        pos = (positions.stride(0), positions.stride(1))
+    else:
+        raise C3Error("positions must be [S] or [B, S]")
+    _dev_tensor(freqs, "freqs")
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or freqs.device != dev:
+        raise C3Error("freqs must be fp64 [rot / 2] on the device of x")
+    if layout not in _LAYOUT:
+        raise C3Error(f"unknown layout {layout}")
+    table = (Heads * len(xs))()
+    for h, t, y in zip(table, xs, outs):
+        h.in_, h.out, h.heads = t.data_ptr(), y.data_ptr(), t.shape[-2]
+        h.in_stride[:], h.out_stride[:] = _strides4(t), _strides4(y)
+    rc = _lib().c3_rotary(table, len(xs), _CODE[first.dtype], B, S, D, _ptr(positions),
+                          positions.element_size(), (ctypes.c_int64 * 2)(*pos), _ptr(freqs),
+                          2 * freqs.numel(), _LAYOUT[layout], int(bool(inverse)), float(amplitude),
+                          _stream(stream))
+    _check(rc, "c3_rotary")
+    return outs[0] if single else tuple(outs)
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+def _attn_tensor(t):
+    a = AttnTensor()
+    a.ptr = t.data_ptr()
+    a.stride[:] = _strides4(t)
+    return a
+
+
+def _attention_args(q, k, v, causal, window, scale, q_lens, k_lens):
+    _rows(q, "q", dim=(3, 4))
+    for t, n in ((k, "k"), (v, "v")):
+        _rows(t, n, q.dtype, q.device, (q.dim(),))
+    if k.shape != v.shape:
+        raise C3Error("k and v must have the same shape")
+    if q.shape[-1] != k.shape[-1]:
+        raise C3Error("q and k must have the same head size")
+    packed = q.dim() == 3
+    if (q_lens is None) != (k_lens is None):
+        raise C3Error("q_lens and k_lens go together")
+    if not packed and q.shape[0] != k.shape[0]:
+        raise C3Error("q and k must have the same batch")
+    if packed and q_lens is None:
+        q_lens, k_lens = [q.shape[0]], [k.shape[0]]
+    batch = len(q_lens) if packed else q.shape[0]
+    a = Attention()
+    keep = ()
+    if q_lens is not None:
+        if len(q_lens) != batch or len(k_lens) != batch:
+            raise C3Error("q_lens and k_lens need one length for each sequence")
+        try:
+            keep = tuple((ctypes.c_int32 * max(batch, 1))(*x) for x in (q_lens, k_lens))
+        except TypeError:
+            raise C3Error("q_lens and k_lens must be whole numbers on the host") from None
+        a.q_lens, a.k_lens = (ctypes.cast(x, ctypes.c_void_p) for x in keep)
+    a.dtype, a.heads, a.kv_heads, a.dim = _CODE[q.dtype], q.shape[-2], k.shape[-2], q.shape[-1]
+    a.causal, a.window, a.batch, a.packed = int(bool(causal)), int(window), batch, int(packed)
+    a.scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
+    a.q_tokens, a.k_tokens = (q.shape[0], k.shape[0]) if packed else (q.shape[1], k.shape[1])
+    return a, keep
+
+
+def _attn_out(t, like, name):
+    if t is None:
+        return _new_like(like)
+    _rows(t, name, like.dtype, like.device)
+    if t.shape != like.shape or _overlap(t):
+        raise C3Error(f"{name} must have the shape {tuple(like.shape)} and no repeated elements")
+    return t
+
+
+def _workspace(need, workspace, device, what):
+    if need == 0:
+        raise C3Error(f"invalid {what} sizes")
+    if workspace is None:
+        return _empty((need,), torch.uint8, device)
+    _dev_tensor(workspace, "workspace")
+    if workspace.numel() * workspace.element_size() < need:
+        raise C3Error(f"{what} workspace too small")
+    return workspace
+
+
+def _lse(t, q, name="lse"):
+    _dev_tensor(t, name)
+    if t.dtype != torch.float32 or t.shape != q.shape[:-1] or t.device != q.device:
+        raise C3Error(f"{name} must be fp32 {tuple(q.shape[:-1])}")
+    return t
+
+
+def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: float = None, q_lens=None,
+              k_lens=None, out=None, lse=None, workspace=None, stream=None):
+    """(out, lse) of softmax(scale q k^T) v.
+
+    Dense: q [B, Sq, H, D], k and v [B, Sk, Hk, D], optionally with the lengths
+    of each sequence (what lies behind them is padding: not looked at, zeros in
+    the output).  Packed: q [sum of q_lens, H, D], k and v alike.  bf16 or fp16,
+    D a multiple of 8 up to 128, H a multiple of Hk.  Lengths are host integers.
+    ``causal`` lines the last query up with the last key; ``window`` > 0 leaves
+    each query that many keys.  ``scale`` defaults to D ** -0.5.  lse is fp32
+    [.., H]; a row that sees no key has out 0 and lse -inf."""
+    a, keep = _attention_args(q, k, v, causal, window, scale, q_lens, k_lens)
+    out = _attn_out(out, q, "out")
+    lse = _empty(q.shape[:-1], torch.float32, q.device) if lse is None else _lse(lse, q)
+    ws = _workspace(_lib().c3_attention_workspace_size(ctypes.byref(a)), workspace, q.device,
+                    "attention")
+    t = [_attn_tensor(x) for x in (q, k, v, out)]
+    rc = _lib().c3_attention(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse), _ptr(ws),
+                             ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "c3_attention")
+    return out, lse
+
+
+def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int = 0,
+                   scale: float = None, q_lens=None, k_lens=None, dq=None, dk=None, dv=None,
+                   workspace=None, stream=None):
+    """(dq, dk, dv) of ``attention`` with the same arguments, from its ``out``
+    and ``lse`` and the output's gradient."""
+    a, keep = _attention_args(q, k, v, causal, window, scale, q_lens, k_lens)
+    for t, n in ((dout, "dout"), (out, "out")):
+        _rows(t, n, q.dtype, q.device)
+        if t.shape != q.shape:
+            raise C3Error(f"{n} must have the shape of q")
+    _lse(lse, q)
+    dq, dk, dv = _attn_out(dq, q, "dq"), _attn_out(dk, k, "dk"), _attn_out(dv, v, "dv")
+    ws = _workspace(_lib().c3_attention_grad_workspace_size(ctypes.byref(a)), workspace, q.device,
+                    "attention_grad")
+    t = [_attn_tensor(x) for x in (dout, q, k, v, out)]
+    d = [_attn_tensor(x) for x in (dq, dk, dv)]
+    rc = _lib().c3_attention_grad(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse),
+                                  *map(ctypes.byref, d), _ptr(ws), ws.numel() * ws.element_size(),
+                                  _stream(stream))
+    _check(rc, "c3_attention_grad")
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------------------
+# tokens to their experts and back
+# ---------------------------------------------------------------------------
+class ExpertOrder(NamedTuple):
+    """Choices sorted by expert (c3_expert_sort): expert e's rows are places
+    offsets[e] .. offsets[e + 1] - 1; source names the choice (token * top + i)
+    at each place, -1 behind the last; slot the place of each choice [T, top],
+    -1 where it was dropped."""
+    offsets: torch.Tensor
+    source: torch.Tensor
+    slot: torch.Tensor
+
+
+def expert_sort(ids: torch.Tensor, num_experts: int, *, workspace=None, stream=None) -> ExpertOrder:
+    """Sorts the choices ids [T, top] (int32; outside [0, num_experts): dropped)
+    by expert, stably."""
+    _dev_tensor(ids, "ids")
+    if ids.dtype != torch.int32 or ids.dim() != 2:
+        raise C3Error("ids must be int32 [tokens, top]")
+    if not 1 <= ids.shape[1] <= MAX_TOP:
+        raise C3Error(f"1 to {MAX_TOP} choices a token")
+    dev, n = ids.device, ids.numel()
+    order = ExpertOrder(_empty((max(int(num_experts), 0) + 1,), torch.int32, dev),
+                        _empty((n,), torch.int32, dev), _empty(ids.shape, torch.int32, dev))
+    ws = _workspace(_lib().c3_expert_sort_workspace_size(n, int(num_experts)), workspace, dev,
+                    "expert_sort")
+    rc = _lib().c3_expert_sort(_ptr(ids), n, int(num_experts), _ptr(order.offsets), _ptr(order.source),
+                               _ptr(order.slot), _ptr(ws), ws.numel() * ws.element_size(),
+                               _stream(stream))
+    _check(rc, "c3_expert_sort")
+    return order
+
+
+def _expert_rows(order, token_rows, sorted_rows, dtype):
+    """c3_expert_rows_t from tensors or None for either side."""
+    for t, n in zip(order, ("offsets", "source", "slot")):
+        _dev_tensor(t, n)
+        if t.dtype != torch.int32:
+            raise C3Error(f"{n} must be int32")
+    T, top = order.slot.shape
+    r = ExpertRows()
+    for t, n, rows in ((token_rows, "tokens' rows", T), (sorted_rows, "sorted rows", T * top)):
+        if t.dim() != 2 or t.shape[0] != rows:
+            raise C3Error(f"the {n} must be [{rows}, hidden]")
+        if t.dtype != dtype or t.device != order.slot.device:
+            raise C3Error("the rows must have one dtype and the order's device")
+    if token_rows.shape[1] != sorted_rows.shape[1]:
+        raise C3Error("the rows must have one hidden size")
+    H = token_rows.shape[1]
+    r.dtype, r.top, r.tokens, r.hidden = _CODE[dtype], top, T, H
+    # the stride of a single row says nothing
+    r.token_stride = token_rows.stride(0) if T > 1 else max(H, token_rows.stride(0))
+    r.sorted_stride = sorted_rows.stride(0) if T * top > 1 else max(H, sorted_rows.stride(0))
+    r.slot, r.kept = order.slot.data_ptr(), order.offsets.data_ptr() + 4 * (order.offsets.numel() - 1)
+    return r
+
+
+def _expert_out(t, shape, like):
+    if t is None:
+        return _empty(shape, like.dtype, like.device)
+    _rows(t, "out", like.dtype, like.device)
+    if tuple(t.shape) != tuple(shape) or _overlap(t):
+        raise C3Error(f"out must be {tuple(shape)} without repeated elements")
+    return t
+
+
+def _weights(weights, order):
+    if weights is None:
+        return None
+    _dev_tensor(weights, "weights")
+    if weights.dtype != torch.float32 or weights.shape != order.slot.shape:
+        raise C3Error("weights must be fp32 [tokens, top]")
+    return weights
+
+
+def expert_dispatch(x, order: ExpertOrder, *, out=None, stream=None):
+    """Rows [T * top, hidden] sorted by expert from tokens x [T, hidden]; the
+    rows behind the last kept choice are zeros."""
+    _rows(x, "x", dim=(2,))
+    out = _expert_out(out, (order.slot.numel(), x.shape[1]), x)
+    r = _expert_rows(order, x, out, x.dtype)
+    _check(_lib().c3_expert_dispatch(ctypes.byref(r), _ptr(x), _ptr(out), _stream(stream)),
+           "c3_expert_dispatch")
+    return out
+
+
+def expert_combine(y, order: ExpertOrder, weights=None, *, out=None, stream=None):
+    """out[t] = sum over t's choices of weight * y[their place]; y [T * top,
+    hidden], weights fp32 [T, top] or None (ones)."""
+    _rows(y, "y", dim=(2,))
+    out = _expert_out(out, (order.slot.shape[0], y.shape[1]), y)
+    weights = _weights(weights, order)
+    r = _expert_rows(order, out, y, y.dtype)
+    _check(_lib().c3_expert_combine(ctypes.byref(r), _ptr(y), _ptr(weights), _ptr(out),
+                                    _stream(stream)), "c3_expert_combine")
+    return out
+
+
+def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, stream=None):
+    """(dy [T * top, hidden], dweights fp32 [T, top]) of ``expert_combine``;
+    without weights dweights is None (and y may be)."""
+    _rows(dout, "dout", dim=(2,))
+    weights = _weights(weights, order)
+    dy = _expert_out(dy, (order.slot.numel(), dout.shape[1]), dout)
+    r = _expert_rows(order, dout, dy, dout.dtype)
+    dw = None
+    if weights is not None:
+        _rows(y, "y", dout.dtype, dout.device, (2,))
+        if y.shape != dy.shape:
+            raise C3Error(f"y must be {tuple(dy.shape)}")
+        if y.shape[0] > 1 and y.stride(0) != r.sorted_stride:
+            raise C3Error("y and dy must have the same row stride")
+        dw = _empty(order.slot.shape, torch.float32, dout.device)
+    _check(_lib().c3_expert_combine_grad(ctypes.byref(r), _ptr(dout), _ptr(y if dw is not None else None),
+                                         _ptr(weights), _ptr(dy), _ptr(dw), _stream(stream)),
+           "c3_expert_combine_grad")
+    return dy, dw
+
+
+def expert_dispatch_grad(dsorted, order: ExpertOrder, *, out=None, stream=None):
+    """Gradient [T, hidden] of ``expert_dispatch``: each token's sum over its
+    choices' rows of dsorted [T * top, hidden]."""
+    return expert_combine(dsorted, order, None, out=out, stream=stream)
