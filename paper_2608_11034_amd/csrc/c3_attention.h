@@ -67,6 +67,7 @@ struct AttnArgs {
     float* lse;
     float* lse2;            // per row, as lse: in powers of two, +inf where a row sees nothing
     float* delta;           // per row: the sum of dout * out
+    uint32_t* careful;      // per workgroup of the dkv pass: repeat it with care
     float* part;            // partial results of split units
     float* part_ml;         // their maxima and sums
     FastDiv group;          // query heads of a key head
@@ -176,47 +177,70 @@ __device__ __forceinline__ u32x4 operand(const f32x16& x, int j) {
     return r;
 }
 
-// Pieces of a row of DP elements; the shift spreads rows over the 256 bytes that
-// the 64 banks span.
-template <int DP>
-__device__ __forceinline__ int swizzle(int row) {
-    if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
-    return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
-}
-
-// Byte offsets of a lane's reads in a tile; they repeat every 16 rows.
-template <int DP>
-struct TileReads {
-    int along[DP / 16];         // A operand along rows 0..31, inner step ks
-    int across[DP / 32][2];     // transposed: columns 32 db .., rows 4 h + .. and 8 + 4 h + ..
-    __device__ __forceinline__ TileReads() {
-        const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks)
-            along[ks] = c * DP * 2 + (((2 * ks + h) ^ swizzle<DP>(c)) << 4);
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int row = s * 8 + h * 4 + (i >> 2);
-                const int piece = db * 4 + g * 2 + ((i & 3) >> 1);
-                across[db][s] = row * DP * 2 + ((piece ^ swizzle<DP>(row)) << 4) + (i & 1) * 8;
-            }
-    }
-};
-
-__device__ __forceinline__ u32x4 read_along(const char* tile, int offset) {
-    return *reinterpret_cast<const u32x4*>(tile + offset);
-}
 __device__ __forceinline__ u32x2 read_tr(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
         (__attribute__((address_space(3))) s16x4*)(p)));
 }
-// Rows 16 j + .. of a 32-row tile as an A operand across its rows.
-__device__ __forceinline__ u32x4 read_across(const char* tile, const int offset[2], int rows_bytes) {
-    const u32x2 lo = read_tr(tile + rows_bytes + offset[0]), hi = read_tr(tile + rows_bytes + offset[1]);
-    return u32x4{lo.x, lo.y, hi.x, hi.y};
+
+// Pieces of a row of DP elements; the shift spreads rows over the 256 bytes that
+// the 64 banks span.
+template <int DP>
+__host__ __device__ constexpr int swizzle(int row) {
+    if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
 }
+
+// A lane's reads in a tile.  The piece of a row that is read enters the address
+// only through the exclusive or, so each read is one of two base offsets with
+// constant bits flipped; fresh() keeps the compiler from holding every one of
+// them in a register for the whole walk.
+template <int DP>
+struct TileReads {
+    int row;            // A operand along rows: lane's row, piece h
+    int col;            // across rows: rows 4 h + .., columns 0 ..
+    __device__ __forceinline__ TileReads() {
+        const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
+        row = c * DP * 2 + ((h ^ swizzle<DP>(c)) << 4);
+        const int r = h * 4 + (i >> 2);
+        col = r * DP * 2 + (((g * 2 + ((i & 3) >> 1)) ^ swizzle<DP>(r)) << 4) + (i & 1) * 8;
+    }
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(col)); }
+    // Rows 0..31 of `tile`, inner step ks.
+    __device__ __forceinline__ u32x4 along(const char* tile, int ks) const {
+        return *reinterpret_cast<const u32x4*>(tile + (row ^ (ks << 5)));
+    }
+    // Columns 32 db .. of rows 0..15 of `tile`, as the A operand over them.
+    __device__ __forceinline__ u32x4 across(const char* tile, int db) const {
+        constexpr int kFlip = (swizzle<DP>(8) << 4) | (8 * DP * 2);
+        const u32x2 lo = read_tr(tile + (col ^ (db << 6))), hi = read_tr(tile + (col ^ (db << 6) ^ kFlip));
+        return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+};
+
+// The second layout: for each 32 rows and inner step ks 1 KiB with 32 bytes of
+// every row.  Every read then is one of two lane offsets plus a constant, without
+// bank conflicts and without a register for each; the loads that fill it take 32
+// bytes of a row at a time, half of what a compute unit's vector cache could
+// deliver.
+template <int DP>
+struct StepReads {
+    int row, col;
+    __device__ __forceinline__ StepReads() {
+        const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
+        row = c * 32 + h * 16;
+        col = g * 1024 + (h * 4 + (i >> 2)) * 32 + (i & 3) * 8;
+    }
+    // Rows 0..31 of the 32 rows at `sub`, inner step ks, as the A or B operand.
+    __device__ __forceinline__ u32x4 along(const char* sub, int ks) const {
+        return *reinterpret_cast<const u32x4*>(sub + row + ks * 1024);
+    }
+    // Columns 32 db .. of rows 16 j .. 16 j + 15, as the A operand over them.
+    __device__ __forceinline__ u32x4 across(const char* sub, int j, int db) const {
+        const char* p = sub + col + db * 2048 + j * 512;
+        const u32x2 lo = read_tr(p), hi = read_tr(p + 256);
+        return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+};
 
 // A lane's 16-byte pieces 2 ks + h of one row, from memory; zeros behind the head
 // size or for a row that does not exist.
@@ -296,6 +320,10 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t x) {
     return (x & 0x7C007C00u) + 0x04000400u;
 }
 template <typename T>
+__device__ __forceinline__ uint32_t not_finite(u32x4 x) {
+    return not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+}
+template <typename T>
 __device__ __forceinline__ uint32_t one_bits() {      // 1.0
     if constexpr (__is_same(T, __bf16)) return 0x3F80u;
     return 0x3C00u;
@@ -307,8 +335,8 @@ __device__ __forceinline__ uint32_t one_bits() {      // 1.0
 // the lane's 8 elements of B that are not hidden.  A's elements that are not
 // finite (none, in training that goes well) are replaced by 0 here, and where
 // they meet pairs that are seen, which indicator products find, the infinities
-// that they would have added are noted in `special`: bit i of special[db] for
-// +inf in register i of acc[db], bit 16 + i for -inf, both for NaN.
+// that they would have added are noted in LDS, in the lane's word of special[db]:
+// bit i for +inf in register i of acc[db], bit 16 + i for -inf, both for NaN.
 // Its own function, called once in a blue moon, so that its registers are not
 // the kernels'.
 template <typename T>
@@ -353,9 +381,19 @@ __device__ __attribute__((noinline)) u32x4 finite_operand(u32x4 A, u32x4 B, uint
     return A;
 }
 
-template <typename T, int NDB>
+// One lane's words of special[NS], kAttnThreads apart.
+template <int NS>
+struct Special {
+    uint32_t* word;
+    __device__ __forceinline__ explicit Special(uint32_t* lds) : word(lds + threadIdx.x) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) word[i * kAttnThreads] = 0;
+    }
+};
+
+template <typename T, int NDB, int NS>
 __device__ __forceinline__ void finite_operands(u32x4 (&A)[NDB], u32x4 B, uint32_t seen,
-                                                uint32_t (&special)[NDB]) {
+                                                const Special<NS>& special, int first = 0) {
     uint32_t bad = 0;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -366,23 +404,23 @@ __device__ __forceinline__ void finite_operands(u32x4 (&A)[NDB], u32x4 B, uint32
     for (int db = 0; db < NDB; ++db) {
         uint32_t found;
         A[db] = finite_operand<T>(A[db], B, seen, &found);
-        special[db] |= found;
+        special.word[(first + db) * kAttnThreads] |= found;
     }
 }
 
 // The infinities that finite_operands noted.
-template <int NDB>
-__device__ __forceinline__ void add_special(f32x16 (&acc)[NDB], const uint32_t (&special)[NDB]) {
-    uint32_t any = 0;
+template <int NDB, int NS>
+__device__ __forceinline__ void add_special(f32x16 (&acc)[NDB], const Special<NS>& special, int first = 0) {
+    uint32_t s[NDB], any = 0;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) any |= special[db];
+    for (int db = 0; db < NDB; ++db) any |= s[db] = special.word[(first + db) * kAttnThreads];
     if (__builtin_expect(!__any(any != 0), 1)) return;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            if ((special[db] >> i) & 1) acc[db][i] += __builtin_inff();
-            if ((special[db] >> (16 + i)) & 1) acc[db][i] -= __builtin_inff();
+            if ((s[db] >> i) & 1) acc[db][i] += __builtin_inff();
+            if ((s[db] >> (16 + i)) & 1) acc[db][i] -= __builtin_inff();
         }
 }
 
@@ -428,5 +466,10 @@ int64_t attn_number(AttnPlan& p, int batch, F units_of) {
     return n;
 }
 size_t attn_table_bytes(const c3_attention_t* a);
+
+// The passes of the gradient; the plan's units are numbered for the pass.
+hipError_t launch_attn_dq(const AttnPlan& p, bool bf16, hipStream_t s);
+hipError_t launch_attn_dkv(const AttnPlan& p, bool bf16, hipStream_t s);
+int attn_dkv_keys(int dim);         // keys of a unit of the second
 
 }  // namespace c3

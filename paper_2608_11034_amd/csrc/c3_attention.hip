@@ -26,6 +26,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     __shared__ __attribute__((aligned(1024))) char v0[L::kBytes];
     __shared__ __attribute__((aligned(1024))) char k1[L::kBytes];
     __shared__ __attribute__((aligned(1024))) char v1[L::kBytes];
+    __shared__ uint32_t special_words[NDB * kAttnThreads];
 
     const AttnUnit w = attn_unit(a, tab, die_order(blockIdx.x, gridDim.x));
     const int G = (int)a.group.d;
@@ -56,14 +57,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     u32x4 qf[KS];
     load_row<DP>(qf, seq_base(a.q, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.q.st, valid, a.dim);
 
-    const TileReads<DP> rd;
+    TileReads<DP> rd;
     const TokenOffsets<DP, kKeys> k_off(a.k.st, a.dim), v_off(a.v.st, a.dim);
     const char* kb = seq_base(a.k, a.packed, w.b, w.k_start, w.hk);
     const char* vb = seq_base(a.v, a.packed, w.b, w.k_start, w.hk);
     const float cs = a.scale * kLog2e;
 
     f32x16 acc[NDB] = {};
-    uint32_t special[NDB] = {};
+    const Special<NDB> special(special_words);
     float m = -__builtin_inff(), l = 0.0f;
 
     auto load = [&](int t, char* kt, char* vt) {
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                s[n] = mfma<T>(read_along(kt, rd.along[ks] + n * kSub), qf[ks], s[n]);
+                s[n] = mfma<T>(rd.along(kt + n * kSub, ks), qf[ks], s[n]);
         uint32_t seen[2] = {0, 0};
         if (masked) {
 #pragma unroll
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
                 u32x4 A[NDB];
 #pragma unroll
                 for (int db = 0; db < NDB; ++db)
-                    A[db] = read_across(vt + n * kSub, rd.across[db], j * 16 * DP * 2);
+                    A[db] = rd.across(vt + n * kSub + j * 16 * DP * 2, db);
                 if (masked) finite_operands<T, NDB>(A, p, seen[n] >> (8 * j), special);
 #pragma unroll
                 for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(A[db], p, acc[db]);

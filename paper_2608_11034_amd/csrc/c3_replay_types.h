@@ -36,7 +36,7 @@ struct FastDiv {
         m = (uint32_t)((((1ull << 32) * ((1ull << s) - div)) + div - 1) / div);
     }
     __device__ __forceinline__ uint32_t quot(uint32_t n) const {
-        return (uint32_t)(((uint64_t)__umulhi(n, m) + n) >> s);
+        return (__umulhi(n, m) + n) >> s;       // m < 2^32, so the sum is below 2 n
     }
 };
 
