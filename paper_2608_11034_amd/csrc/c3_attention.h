@@ -69,7 +69,8 @@ struct AttnArgs {
     float* delta;           // per row: the sum of dout * out
     uint32_t* careful;      // per workgroup of the dkv pass: repeat it with care
     float* part;            // partial results of split units
-    float* part_ml;         // their maxima and sums
+    float* part_ml;         // their maxima (scaled, in powers of two) and sums
+    int64_t part_rows;      // rows of one part
     FastDiv group;          // query heads of a key head
     FastDiv units;          // units of work of one key head, all sequences
     FastDiv seq_units;      // of one sequence, where n == 0

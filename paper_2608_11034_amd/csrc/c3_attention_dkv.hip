@@ -55,7 +55,8 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     const int G = (int)a.group.d;
     const int n_rows = w.q_len * G, off = w.k_len - w.q_len;
     const int k_pad = a.packed ? w.k_len : a.k_tokens;
-    const int key_block = (int)w.unit * kBlockKeys;
+    const int tile = (int)a.splits.quot(w.unit), part = (int)w.unit - tile * (int)a.splits.d;
+    const int key_block = tile * kBlockKeys;
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wkey = key_block + wave * kWaveKeys, key = wkey + c;      // and every 32nd from it
@@ -65,8 +66,13 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     if (a.causal) p_lo = max(0, key_block - off);
     if (a.window) p_hi = min(p_hi, key_block + kBlockKeys - 1 - off + a.window);
     if (key_block >= w.k_len) p_hi = 0;
-    const int t0 = p_lo * G / kTileRows;
-    const int t1 = p_hi > p_lo ? (p_hi * G + kTileRows - 1) / kTileRows : t0;
+    int t0 = p_lo * G / kTileRows;
+    int t1 = p_hi > p_lo ? (p_hi * G + kTileRows - 1) / kTileRows : t0;
+    if (a.splits.d > 1) {       // this workgroup's part of the walk
+        const int64_t n = t1 - t0;
+        t1 = t0 + (int)a.splits.quot((uint32_t)(n * (part + 1)));
+        t0 = t0 + (int)a.splits.quot((uint32_t)(n * part));
+    }
 
     const StepReads<DP> rd;
     const char* qb = seq_base(a.q, a.packed, w.b, w.q_start, w.hk * G);
@@ -253,6 +259,27 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
         const int k = key + 32 * m;
         if (k >= k_pad) continue;
         const bool valid = k < w.k_len;
+        if (a.splits.d > 1) {
+            // dk and dv of this part, in fp32 and not yet scaled
+            const int64_t keys = (int64_t)(a.packed ? 0 : w.b) * a.k_tokens + w.k_start + k;
+            float* to = a.part + (part * 2 * a.part_rows + keys * a.kv_heads + w.hk) * a.dim;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int d = db * 32 + q * 8 + h * 4;
+                    if (d >= a.dim) continue;
+                    f32x4 x, y;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = valid ? dk[m][db][4 * q + i] : 0.0f;
+                        y[i] = valid ? dv[m][db][4 * q + i] : 0.0f;
+                    }
+                    *reinterpret_cast<f32x4*>(to + d) = x;
+                    *reinterpret_cast<f32x4*>(to + a.part_rows * a.dim + d) = y;
+                }
+            continue;
+        }
         char* ok = seq_base(a.dk, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dk.st;
         char* ov = seq_base(a.dv, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dv.st;
 #pragma unroll

@@ -25,7 +25,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
     const int G = (int)a.group.d;
     const int n_rows = w.q_pad * G, off = w.k_len - w.q_len;
     const int tiles = (n_rows + kRows - 1) / kRows;
-    const int tile = a.causal ? tiles - 1 - (int)w.unit : (int)w.unit;
+    const int nth = (int)a.splits.quot(w.unit), part = (int)w.unit - nth * (int)a.splits.d;
+    const int tile = a.causal ? tiles - 1 - nth : nth;
     const int row0 = tile * kRows;
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = threadIdx.x >> 6;
@@ -36,7 +37,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
     if (a.causal) hi = min(hi, last + off + 1);
     if (a.window) lo = max(lo, first + off - a.window + 1);
     if (first >= w.q_len) hi = 0;
-    const int t0 = lo / kKeys, t1 = hi > lo ? (hi + kKeys - 1) / kKeys : t0;
+    int t0 = lo / kKeys, t1 = hi > lo ? (hi + kKeys - 1) / kKeys : t0;
+    if (a.splits.d > 1) {       // this workgroup's part of the walk
+        const int64_t n = t1 - t0;
+        t1 = t0 + (int)a.splits.quot((uint32_t)(n * (part + 1)));
+        t0 = t0 + (int)a.splits.quot((uint32_t)(n * part));
+    }
 
     const int row = row0 + wave * 32 + c;
     const int pos = (int)a.group.quot(row), head = w.hk * G + row - pos * G;
@@ -64,7 +70,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
             const float lse = a.lse[at];
             if (lse != -__builtin_inff()) lse2 = lse * kLog2e;
         }
-        if (there && h == 0) {
+        if (there && h == 0 && part == 0) {
             a.lse2[at] = lse2;
             a.delta[at] = delta;
         }
@@ -136,6 +142,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
 
     add_special<NDB>(acc, special);
     if (!there) return;
+    if (a.splits.d > 1) {
+        // this part's sum, in fp32 and not yet scaled
+        float* to = a.part + (part * a.part_rows + seq_row(a, w) + (int64_t)pos * a.heads + head) * a.dim;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int d = db * 32 + q * 8 + h * 4;
+                if (d >= a.dim) continue;
+                f32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = valid ? acc[db][4 * q + i] : 0.0f;
+                *reinterpret_cast<f32x4*>(to + d) = x;
+            }
+        return;
+    }
     char* out = seq_base(a.dq, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.dq.st;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
