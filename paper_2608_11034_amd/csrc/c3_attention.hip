@@ -17,6 +17,46 @@ namespace {
 
 constexpr int kKeys = 64;           // keys of a tile
 
+// Parts that a walk over k_len keys is divided into.
+__device__ __forceinline__ int key_parts(const AttnArgs& a, int k_len) {
+    return a.split_keys ? max(1, (k_len + a.split_keys - 1) / a.split_keys) : 1;
+}
+
+// Maximum (scaled, in powers of two) and sum of a row's part; the first part also
+// marks those that the row's sequence does not have.
+__device__ __forceinline__ void write_part_stats(const AttnArgs& a, int64_t row, int part, int parts, float mc,
+                                                 float l) {
+    float2* to = reinterpret_cast<float2*>(a.part_ml) + row;
+    to[part * a.part_rows] = make_float2(mc, l);
+    if (part == 0)
+        for (int p = parts; p < (int)a.splits.d; ++p) to[p * a.part_rows] = make_float2(0.0f, 0.0f);
+}
+// Columns 32 db .. of a row's part.
+__device__ __forceinline__ void write_part(const AttnArgs& a, int64_t row, int part, int db, int h,
+                                           const f32x16& x) {
+    float* to = a.part + (part * a.part_rows + row) * a.dim;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int d = db * 32 + q * 8 + h * 4;
+        if (d < a.dim) *reinterpret_cast<f32x4*>(to + d) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    }
+}
+// Columns 32 db .. of a row of the output; zeros where it saw nothing.
+template <typename T>
+__device__ __forceinline__ void write_out(char* out, int db, int h, int dim, const f32x16& x, float f, bool some) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int d = db * 32 + q * 8 + h * 4;
+        if (d >= dim) continue;
+        T e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = some ? (T)(x[4 * q + i] * f) : (T)0.0f;
+        u32x2 w;
+        __builtin_memcpy(&w, e, 8);
+        *reinterpret_cast<u32x2*>(out + d * 2) = w;
+    }
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs a, AttnTable tab) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
@@ -33,7 +73,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     const int n_rows = w.q_pad * G, off = w.k_len - w.q_len;
     const int tiles = (n_rows + kRows - 1) / kRows;
     // the last queries see the most keys: they go first
-    const int tile = a.causal ? tiles - 1 - (int)w.unit : (int)w.unit;
+    const int parts = key_parts(a, w.k_len), nth = parts > 1 ? (int)w.unit / parts : (int)w.unit;
+    const int part = (int)w.unit - nth * parts, tile = a.causal ? tiles - 1 - nth : nth;
     const int row0 = tile * kRows;
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = threadIdx.x >> 6;
@@ -45,6 +86,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     if (a.causal) hi = min(hi, last + off + 1);
     if (a.window) lo = max(lo, first + off - a.window + 1);
     if (first >= w.q_len) hi = 0;
+    if (a.split_keys) {
+        lo = max(lo, part * a.split_keys);
+        hi = min(hi, part * a.split_keys + a.split_keys);
+    }
     const int t0 = lo / kKeys, t1 = hi > lo ? (hi + kKeys - 1) / kKeys : t0;
 
     // the lane's row and the keys that it sees; a row that does not exist hides
@@ -152,38 +197,322 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     add_special<NDB>(acc, special);
     l += __shfl_xor(l, 32);
     if (!there) return;
+    const float mc = m == -__builtin_inff() ? 0.0f : m * cs;
+    const int64_t at = seq_row(a, w) + (int64_t)pos * a.heads + head;
+    if (a.split_keys) {
+        if (h == 0) write_part_stats(a, at, part, parts, mc, l);
+        if (l != 0.0f)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) write_part(a, at, part, db, h, acc[db]);
+        return;
+    }
     // a row that saw nothing (l = 0) and one of the padding: zeros and -inf
     const bool some = valid && l != 0.0f;
     const float f = some ? 1.0f / l : 0.0f;
     char* out = seq_base(a.o, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.o.st;
 #pragma unroll
+    for (int db = 0; db < NDB; ++db) write_out<T>(out, db, h, a.dim, acc[db], f, some);
+    if (h == 0) a.lse[at] = some ? (mc + __log2f(l)) * kLn2 : -__builtin_inff();
+}
+
+// Few rows against many keys, as new tokens against a cache: the keys are read
+// once and bound it.  The 32 rows of a workgroup stand in every one of its four
+// waves, which share out the keys 32 at a time, each through buffers of its own, so
+// that no wave waits for another before the end; there their maxima and sums are
+// joined in LDS.  Long caches are divided among workgroups as well.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a, AttnTable tab) {
+    constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
+    __shared__ __attribute__((aligned(1024))) char k0[kAttnWaves * kSub];
+    __shared__ __attribute__((aligned(1024))) char v0[kAttnWaves * kSub];
+    __shared__ __attribute__((aligned(1024))) char k1[kAttnWaves * kSub];
+    __shared__ __attribute__((aligned(1024))) char v1[kAttnWaves * kSub];
+    __shared__ uint32_t special_words[NDB * kAttnThreads];
+    __shared__ float stats[2][kAttnWaves][64];
+
+    const AttnUnit w = attn_unit(a, tab, blockIdx.x);
+    const int G = (int)a.group.d;
+    const int n_rows = w.q_pad * G, off = w.k_len - w.q_len;
+    const int parts = key_parts(a, w.k_len), tile = parts > 1 ? (int)w.unit / parts : (int)w.unit;
+    const int part = (int)w.unit - tile * parts, row0 = tile * 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    const int first = (int)a.group.quot(row0);
+    const int last = min((int)a.group.quot(min(row0 + 32, n_rows) - 1), w.q_len - 1);
+    int lo = 0, hi = w.k_len;
+    if (a.causal) hi = min(hi, last + off + 1);
+    if (a.window) lo = max(lo, first + off - a.window + 1);
+    if (first >= w.q_len) hi = 0;
+    if (a.split_keys) {
+        lo = max(lo, part * a.split_keys);
+        hi = min(hi, part * a.split_keys + a.split_keys);
+    }
+    // blocks of 32 keys, this wave's every fourth
+    const int t0 = lo / 32 + wave, t1 = hi > lo ? (hi + 31) / 32 : 0;
+
+    const int row = row0 + c;
+    const int pos = (int)a.group.quot(row), head = w.hk * G + row - pos * G;
+    const bool there = row < n_rows, valid = there && pos < w.q_len;
+    const int see_hi = !valid ? INT32_MAX : a.causal ? min(w.k_len, pos + off + 1) : w.k_len;
+    const int see_lo = valid && a.window ? pos + off - a.window + 1 : 0;
+    u32x4 qf[KS];
+    load_row<DP>(qf, seq_base(a.q, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.q.st, valid, a.dim);
+
+    const TileReads<DP> rd;
+    // byte offsets of the lane's pieces of 32 keys, as TokenOffsets for one wave
+    constexpr int kPieces = DP / 8, kStepRows = 64 / kPieces, kLoads = 32 / kStepRows;
+    uint32_t k_off[kLoads], v_off[kLoads];
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+        const int r = n * kStepRows + lane / kPieces, p = (lane % kPieces) ^ swizzle<DP>(r);
+        k_off[n] = p * 8 < a.dim ? (uint32_t)(r * (int)a.k.st + p * 16) : 0xFFFFFF00u;
+        v_off[n] = p * 8 < a.dim ? (uint32_t)(r * (int)a.v.st + p * 16) : 0xFFFFFF00u;
+    }
+    const char* kb = seq_base(a.k, a.packed, w.b, w.k_start, w.hk);
+    const char* vb = seq_base(a.v, a.packed, w.b, w.k_start, w.hk);
+    const float cs = a.scale * kLog2e;
+
+    f32x16 acc[NDB] = {};
+    const Special<NDB> special(special_words);
+    float m = -__builtin_inff(), l = 0.0f;
+
+    auto load = [&](int t, char* kt, char* vt) {
+        const int rows = min(w.k_len - t * 32, 32);
+        const uint32_t k_bytes = (uint32_t)((rows - 1) * (int)a.k.st) + a.dim * 2;
+        const uint32_t v_bytes = (uint32_t)((rows - 1) * (int)a.v.st) + a.dim * 2;
+        const char* kr = kb + (int64_t)t * 32 * a.k.st;
+        const char* vr = vb + (int64_t)t * 32 * a.v.st;
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) load_piece_lds(kr, k_bytes, k_off[n], kt + wave * kSub + n * 1024);
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) load_piece_lds(vr, v_bytes, v_off[n], vt + wave * kSub + n * 1024);
+    };
+    auto step = [&](int t, const char* kt, const char* vt) {
+        kt += wave * kSub;
+        vt += wave * kSub;
+        const int key0 = t * 32;
+        const bool masked = __any(key0 + 32 > see_hi || key0 < see_lo);
+        f32x16 s = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma<T>(rd.along(kt, ks), qf[ks], s);
+        uint32_t seen = 0;
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = key0 + (i >> 2) * 8 + h * 4 + (i & 3);
+                const bool see = key < see_hi && key >= see_lo;
+                seen |= see ? 1u << i : 0u;
+                s[i] = see ? s[i] : -__builtin_inff();
+            }
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any((top - m) * cs > 8.0f)) {         // as in the kernel above
+            const float next = fmaxf(m, top);
+            const float f = next == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - next) * cs);
+            m = next;
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] *= f;
+        }
+        const float mc = m == -__builtin_inff() ? 0.0f : m * cs;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -mc));
+            l += s[i];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const u32x4 p = operand<T>(s, j);
+            u32x4 A[NDB];
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) A[db] = rd.across(vt + j * 16 * DP * 2, db);
+            if (masked) finite_operands<T, NDB>(A, p, seen >> (8 * j), special);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(A[db], p, acc[db]);
+        }
+    };
+    // The wave's own loads, in order: all but the latest 2 kLoads have landed.
+    auto landed = [&](bool more) {
+        if (more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+
+    if (t0 < t1) load(t0, k0, v0);
+    for (int t = t0; t < t1; t += 2 * kAttnWaves) {
+        const int next = t + kAttnWaves, after = t + 2 * kAttnWaves;
+        if (next < t1) load(next, k1, v1);
+        landed(next < t1);
+        step(t, k0, v0);
+        if (next >= t1) break;
+        // reads of the buffer that is filled next have ended: their values are used
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (after < t1) load(after, k0, v0);
+        landed(after < t1);
+        step(next, k1, v1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    add_special<NDB>(acc, special);
+    l += __shfl_xor(l, 32);
+
+    // join the four waves: maxima and sums first, then the rescaled accumulators,
+    // block db of them by wave db, in the order of the waves
+    const float mine = m == -__builtin_inff() ? m : m * cs;
+    stats[0][wave][lane] = mine;
+    stats[1][wave][lane] = l;
+    __syncthreads();
+    float top = stats[0][0][lane];
+#pragma unroll
+    for (int v = 1; v < kAttnWaves; ++v) top = fmaxf(top, stats[0][v][lane]);
+    const float mc = top == -__builtin_inff() ? 0.0f : top;
+    float total = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kAttnWaves; ++v)
+        total = fmaf(stats[1][v][lane], __builtin_amdgcn_exp2f(stats[0][v][lane] - mc), total);
+    const float f = __builtin_amdgcn_exp2f(mine - mc);
+    // [wave][db][register / 4][lane] of four floats, over the buffers (a power of two
+    // apart in all: 32 KiB for 64 columns, 64 KiB for 128)
+    constexpr int kHalf = kAttnWaves * kSub / 16;       // four-float words of one buffer
+    auto cell = [&](int v, int db, int q) -> f32x4* {
+        const int i = ((v * NDB + db) * 4 + q) * 64 + lane;
+        return reinterpret_cast<f32x4*>(i < kHalf ? k0 : v0) + (i < kHalf ? i : i - kHalf);
+    };
+#pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int d = db * 32 + q * 8 + h * 4;
-            if (d >= a.dim) continue;
-            T e[4];
+            f32x4 x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = some ? (T)(acc[db][4 * q + i] * f) : (T)0.0f;
-            u32x2 x;
-            __builtin_memcpy(&x, e, 8);
-            *reinterpret_cast<u32x2*>(out + d * 2) = x;
+            for (int i = 0; i < 4; ++i) x[i] = acc[db][4 * q + i] * f;
+            *cell(wave, db, q) = x;
         }
-    if (h == 0) {
-        const float mc = m == -__builtin_inff() ? 0.0f : m * cs;
-        a.lse[seq_row(a, w) + (int64_t)pos * a.heads + head] =
-            some ? (mc + __log2f(l)) * kLn2 : -__builtin_inff();
+    __syncthreads();
+    const int64_t at = seq_row(a, w) + (int64_t)pos * a.heads + head;
+    const bool some = valid && total != 0.0f;
+    if (there && wave == 0 && h == 0) {
+        if (a.split_keys)
+            write_part_stats(a, at, part, parts, mc, total);
+        else
+            a.lse[at] = some ? (mc + __log2f(total)) * kLn2 : -__builtin_inff();
     }
+    if (wave >= NDB || !there) return;
+    f32x16 sum = {};
+#pragma unroll
+    for (int v = 0; v < kAttnWaves; ++v)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 x = *cell(v, wave, q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[4 * q + i] += x[i];
+        }
+    if (a.split_keys) {
+        if (total != 0.0f) write_part(a, at, part, wave, h, sum);
+        return;
+    }
+    char* out = seq_base(a.o, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.o.st;
+    write_out<T>(out, wave, h, a.dim, sum, some ? 1.0f / total : 0.0f, some);
+}
+
+// Joins the parts of divided walks.  A wave takes a row: lane p the maximum and sum
+// of part p (64 parts at most), then each lane two elements of the row.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_t rows, int parts, FastDiv tokens) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    float m = -__builtin_inff(), l = 0.0f;
+    if (lane < parts) {
+        const float2 x = reinterpret_cast<const float2*>(a.part_ml)[lane * rows + row];
+        m = x.x;
+        l = x.y;
+    }
+    if (l == 0.0f) m = -__builtin_inff();
+    float top = m;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const bool none = top == -__builtin_inff() && !__any(l != 0.0f);
+    const float f = none || l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    float total = f * l;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+    const int64_t token = row / a.heads, b = token / tokens.d;
+    const int head = (int)(row - token * a.heads);
+    if (lane == 0) a.lse[row] = none ? -__builtin_inff() : (top + __log2f(total)) * kLn2;
+    if (2 * lane >= a.dim) return;
+    float x = 0.0f, y = 0.0f;
+    const uint64_t full = __ballot(l != 0.0f);
+    for (int p = 0; p < parts; ++p) {
+        if (!((full >> p) & 1)) continue;
+        const float2 v = *reinterpret_cast<const float2*>(a.part + (p * rows + row) * a.dim + 2 * lane);
+        const float g = __shfl(f, p);
+        x = fmaf(v.x, g, x);
+        y = fmaf(v.y, g, y);
+    }
+    const float inv = none ? 0.0f : 1.0f / total;
+    T e[2] = {(T)(none ? 0.0f : x * inv), (T)(none ? 0.0f : y * inv)};
+    uint32_t two;
+    __builtin_memcpy(&two, e, 4);
+    *reinterpret_cast<uint32_t*>(a.o.ptr + b * a.o.sb + (token - b * tokens.d) * a.o.st + head * a.o.sh + lane * 4) = two;
 }
 
 template <typename T, int DP>
-hipError_t launch_forward(AttnPlan& p, hipStream_t s) {
-    const int64_t units = (int64_t)p.args.units.d * p.args.kv_heads;
-    attn_forward_kernel<T, DP><<<dim3((unsigned)units), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
+hipError_t launch_forward(const AttnPlan& p, bool tokens, hipStream_t s) {
+    const dim3 grid(p.args.units.d * (uint32_t)p.args.kv_heads), block(kAttnThreads);
+    if (tokens)
+        attn_tokens_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    else
+        attn_forward_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    if (p.args.split_keys)
+        attn_join_parts_kernel<T><<<dim3((unsigned)((p.rows + 3) / 4)), dim3(256), 0, s>>>(
+            p.args, p.rows, (int)p.args.splits.d, FastDiv((uint32_t)p.args.q_tokens));
     return hipGetLastError();
 }
 
 inline uint64_t align256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+// How a call's rows and keys are divided: 32 rows a workgroup where no sequence and
+// key head has more, 128 otherwise; and where that gives too few workgroups for the
+// compute units, keys in parts of split_keys, whose results a further kernel joins.
+struct ForwardShape {
+    bool tokens;
+    int64_t rows, split_keys, parts, table, part, part_ml, total;
+    ForwardShape(const c3_attention_t* a, AttnPlan& p) {
+        const int64_t group = p.args.group.d, kv = p.args.kv_heads;
+        tokens = p.max_q * group <= 32;
+        rows = tokens ? 32 : 32 * kAttnWaves;
+        auto units = [&](int64_t split) {
+            return kv * attn_number(p, a->batch, [&](int64_t nq, int64_t nk, int64_t) {
+                const int64_t t = (nq * group + rows - 1) / rows;
+                return split ? t * std::max<int64_t>(1, (nk + split - 1) / split) : t;
+            });
+        };
+        split_keys = 0;
+        parts = 1;
+        const int64_t want = tokens ? 768 : 512, least = tokens ? 256 : 512;
+        const int64_t n = units(0);
+        if (n > 0 && n < want && p.max_k > least) {
+            // as many keys to each of `want` workgroups, in whole tiles
+            const int64_t all = std::max<int64_t>(units(1), 1);        // keys times tiles of rows
+            split_keys = std::max(least, (all / want + 127) / 128 * 128);
+            split_keys = std::max(split_keys, ((p.max_k + 63) / 64 + 127) / 128 * 128);
+            parts = (p.max_k + split_keys - 1) / split_keys;
+            if (parts < 2) split_keys = 0, parts = 1;
+        }
+        uint64_t at = 0;
+        auto take = [&at](uint64_t bytes) { const uint64_t r = at; at = align256(at + bytes); return r; };
+        table = take(attn_table_bytes(a));
+        part = take(split_keys ? 4 * (uint64_t)(parts * p.rows * p.args.dim) : 0);
+        part_ml = take(split_keys ? 8 * (uint64_t)(parts * p.rows) : 0);
+        total = std::max<uint64_t>(at, 256);
+    }
+};
 
 }  // namespace
 
@@ -284,7 +613,7 @@ size_t c3_attention_workspace_size(const c3_attention_t* a) {
     try {
         c3::AttnPlan p;
         if (c3::attn_plan(a, p) != C3_OK) return 0;
-        return 256 + c3::attn_table_bytes(a);
+        return c3::ForwardShape(a, p).total;
     } catch (...) {
         return 0;
     }
@@ -304,26 +633,34 @@ int c3_attention(const c3_attention_t* a, const c3_attn_tensor_t* q, const c3_at
         if ((rc = attn_tensor(out, p, false, p.args.o)) != C3_OK) return rc;
         if (p.rows > 0 && lse == nullptr) return C3_E_INVAL;
         if ((uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
-        if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < 256 + attn_table_bytes(a))
-            return C3_E_WORKSPACE;
+        const ForwardShape f(a, p);
+        if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)f.total) return C3_E_WORKSPACE;
         if (p.rows == 0) return C3_OK;
         p.args.lse = lse;
-        const int64_t group = p.args.group.d, rows = 32 * kAttnWaves;
-        const int64_t units = attn_number(p, a->batch, [&](int64_t nq, int64_t, int64_t) {
-            return (nq * group + rows - 1) / rows;
+        const int64_t group = p.args.group.d;
+        const int64_t units = attn_number(p, a->batch, [&](int64_t nq, int64_t nk, int64_t) {
+            const int64_t t = (nq * group + f.rows - 1) / f.rows;
+            return f.split_keys ? t * std::max<int64_t>(1, (nk + f.split_keys - 1) / f.split_keys) : t;
         });
         if (units < 0 || units * p.args.kv_heads >= (1ll << 31)) return C3_E_UNSUPPORTED;
         p.args.units = FastDiv((uint32_t)units);
+        p.args.splits = FastDiv((uint32_t)f.parts);
+        p.args.split_keys = (int32_t)f.split_keys;
+        char* base = static_cast<char*>(ws);
+        p.args.part = reinterpret_cast<float*>(base + f.part);
+        p.args.part_ml = reinterpret_cast<float*>(base + f.part_ml);
+        p.args.part_rows = p.rows;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
         if (p.seqs != nullptr) {
-            if (stage_bytes(ws, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;
-            p.table.staged = static_cast<const AttnSeq*>(ws);
+            if (stage_bytes(base + f.table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;
+            p.table.staged = reinterpret_cast<const AttnSeq*>(base + f.table);
         }
         hipError_t e;
         if (a->dtype == C3_BF16)
-            e = a->dim > 64 ? launch_forward<__bf16, 128>(p, s) : launch_forward<__bf16, 64>(p, s);
+            e = a->dim > 64 ? launch_forward<__bf16, 128>(p, f.tokens, s) : launch_forward<__bf16, 64>(p, f.tokens, s);
         else
-            e = a->dim > 64 ? launch_forward<_Float16, 128>(p, s) : launch_forward<_Float16, 64>(p, s);
+            e = a->dim > 64 ? launch_forward<_Float16, 128>(p, f.tokens, s)
+                            : launch_forward<_Float16, 64>(p, f.tokens, s);
         return e == hipSuccess ? C3_OK : C3_E_HIP;
     } catch (...) {
         return C3_E_INVAL;
