@@ -44,12 +44,12 @@ constexpr int kAttnWaves = kAttnThreads / 64;
 struct AttnSeq {
     int32_t b;              // sequence
     int32_t q_start, q_len, k_start, k_len;
-    int32_t unit0;          // its first unit of work of one key head
+    int32_t unit0[2];       // its first unit of one key head, by rows and by keys
 };
 
 // Sequences that go along as a kernel's argument (4,096 bytes at most in all);
 // longer lists are staged.
-constexpr int kAttnArgSeqs = 128;
+constexpr int kAttnArgSeqs = 112;
 
 struct AttnTable {
     int32_t n;              // 0: every sequence has q_tokens and k_tokens
@@ -62,19 +62,24 @@ struct AttnTensor {
     int64_t sb, st, sh;     // bytes: batch, token, head
 };
 
+// How one pass divides its work.
+struct AttnSide {
+    FastDiv units;          // units of one key head, all sequences
+    FastDiv seq_units;      // of one sequence, where the table has none
+    FastDiv splits;         // parts of one unit's walk (the forward: at most)
+    uint32_t* marks;        // per workgroup: repeat it with care
+    float* part;            // results of the parts
+    int64_t part_rows;      // rows of one part
+};
+
 struct AttnArgs {
     AttnTensor q, k, v, o, d_o, dq, dk, dv;
     float* lse;
     float* lse2;            // per row, as lse: in powers of two, +inf where a row sees nothing
     float* delta;           // per row: the sum of dout * out
-    uint32_t* careful;      // per workgroup of the dkv pass: repeat it with care
-    float* part;            // partial results of split units
-    float* part_ml;         // their maxima (scaled, in powers of two) and sums
-    int64_t part_rows;      // rows of one part
+    float* part_ml;         // maxima (scaled, in powers of two) and sums of parts of the forward
     FastDiv group;          // query heads of a key head
-    FastDiv units;          // units of work of one key head, all sequences
-    FastDiv seq_units;      // of one sequence, where n == 0
-    FastDiv splits;         // parts of one tile's walk, where fixed
+    AttnSide side[2];       // units that are tiles of rows, and blocks of keys
     int32_t heads, kv_heads, dim, causal, window, packed;
     int32_t q_tokens, k_tokens;
     int32_t split_keys;     // keys of a split, where splits go by the length
@@ -94,13 +99,15 @@ __device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n) {
     return die * each + min(die, rest) + (id >> 3);
 }
 
-__device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
+__device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable& tab, int side,
+                                              uint32_t block) {
     AttnUnit w;
-    w.hk = (int32_t)a.units.quot(block);
-    const uint32_t u = block - (uint32_t)w.hk * a.units.d;
+    const AttnSide& d = a.side[side];
+    w.hk = (int32_t)d.units.quot(block);
+    const uint32_t u = block - (uint32_t)w.hk * d.units.d;
     if (tab.n == 0) {
-        w.b = (int32_t)a.seq_units.quot(u);
-        w.unit = u - (uint32_t)w.b * a.seq_units.d;
+        w.b = (int32_t)d.seq_units.quot(u);
+        w.unit = u - (uint32_t)w.b * d.seq_units.d;
         w.q_start = w.k_start = 0;
         w.q_len = a.q_tokens;
         w.k_len = a.k_tokens;
@@ -110,13 +117,13 @@ __device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable
         if (tab.staged != nullptr) {
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
-                if ((uint32_t)tab.staged[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+                if ((uint32_t)tab.staged[mid].unit0[side] <= u) lo = mid; else hi = mid - 1;
             }
             s = tab.staged[lo];
         } else {
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
-                if ((uint32_t)tab.seq[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+                if ((uint32_t)tab.seq[mid].unit0[side] <= u) lo = mid; else hi = mid - 1;
             }
             s = tab.seq[lo];
         }
@@ -125,7 +132,7 @@ __device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable
         w.q_len = s.q_len;
         w.k_start = s.k_start;
         w.k_len = s.k_len;
-        w.unit = u - (uint32_t)s.unit0;
+        w.unit = u - (uint32_t)s.unit0[side];
     }
     // the same for every lane, kept in scalar registers
     w.b = __builtin_amdgcn_readfirstlane(w.b);
@@ -210,6 +217,10 @@ struct TileReads {
     __device__ __forceinline__ u32x4 along(const char* tile, int ks) const {
         return *reinterpret_cast<const u32x4*>(tile + (row ^ (ks << 5)));
     }
+    // Elements d .. d + 3 of a row.
+    __device__ __forceinline__ const char* four(const char* tile, int r, int d) const {
+        return tile + r * DP * 2 + (((d >> 3) ^ swizzle<DP>(r)) << 4) + (d & 7) * 2;
+    }
     // Columns 32 db .. of rows 0..15 of `tile`, as the A operand over them.
     __device__ __forceinline__ u32x4 across(const char* tile, int db) const {
         constexpr int kFlip = (swizzle<DP>(8) << 4) | (8 * DP * 2);
@@ -234,6 +245,10 @@ struct StepReads {
     // Rows 0..31 of the 32 rows at `sub`, inner step ks, as the A or B operand.
     __device__ __forceinline__ u32x4 along(const char* sub, int ks) const {
         return *reinterpret_cast<const u32x4*>(sub + row + ks * 1024);
+    }
+    // Elements d .. d + 3 of a row.
+    __device__ __forceinline__ const char* four(const char* sub, int r, int d) const {
+        return sub + (d >> 4) * 1024 + r * 32 + (d & 15) * 2;
     }
     // Columns 32 db .. of rows 16 j .. 16 j + 15, as the A operand over them.
     __device__ __forceinline__ u32x4 across(const char* sub, int j, int db) const {
@@ -324,105 +339,70 @@ template <typename T>
 __device__ __forceinline__ uint32_t not_finite(u32x4 x) {
     return not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
 }
-template <typename T>
-__device__ __forceinline__ uint32_t one_bits() {      // 1.0
-    if constexpr (__is_same(T, __bf16)) return 0x3F80u;
-    return 0x3C00u;
-}
-
-// A product acc[db] += A[db] B over 16 inner indices where a pair (inner index,
-// column) that the mask hides must add nothing, whatever A holds there: 0 times an
-// infinity or NaN is NaN.  B is 0 at hidden pairs; `seen` has a bit for each of
-// the lane's 8 elements of B that are not hidden.  A's elements that are not
-// finite (none, in training that goes well) are replaced by 0 here, and where
-// they meet pairs that are seen, which indicator products find, the infinities
-// that they would have added are noted in LDS, in the lane's word of special[db]:
-// bit i for +inf in register i of acc[db], bit 16 + i for -inf, both for NaN.
-// Its own function, called once in a blue moon, so that its registers are not
-// the kernels'.
-template <typename T>
-__device__ __attribute__((noinline)) u32x4 finite_operand(u32x4 A, u32x4 B, uint32_t seen, uint32_t* special) {
-    u32x4 b_pos{0, 0, 0, 0}, b_neg{0, 0, 0, 0};       // 1 where seen, by B's sign
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if ((seen >> (2 * i + s)) & 1) {
-                if ((B[i] >> (16 * s + 15)) & 1)
-                    b_neg[i] |= one_bits<T>() << (16 * s);
-                else
-                    b_pos[i] |= one_bits<T>() << (16 * s);
-            }
-    u32x4 a_pos{0, 0, 0, 0}, a_neg{0, 0, 0, 0};       // 1 at +inf and NaN; at -inf and NaN
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t x = A[i], flags = not_finite<T>(x);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (!((flags >> (16 * s + 15)) & 1)) continue;
-            const uint32_t half = (x >> (16 * s)) & 0xFFFFu;
-            const bool nan = (half & 0x7FFFu) != (__is_same(T, __bf16) ? 0x7F80u : 0x7C00u);
-            A[i] &= ~(0xFFFFu << (16 * s));
-            if (nan || !(half & 0x8000u)) a_pos[i] |= one_bits<T>() << (16 * s);
-            if (nan || (half & 0x8000u)) a_neg[i] |= one_bits<T>() << (16 * s);
-        }
-    }
-    uint32_t found = 0;
-    f32x16 n = {};
-    n = mfma<T>(a_pos, b_pos, n);
-    n = mfma<T>(a_neg, b_neg, n);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) found |= n[i] > 0.0f ? 1u << i : 0u;
-    n = f32x16{};
-    n = mfma<T>(a_neg, b_pos, n);
-    n = mfma<T>(a_pos, b_neg, n);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) found |= n[i] > 0.0f ? 0x10000u << i : 0u;
-    *special = found;
-    return A;
-}
-
-// One lane's words of special[NS], kAttnThreads apart.
-template <int NS>
-struct Special {
-    uint32_t* word;
-    __device__ __forceinline__ explicit Special(uint32_t* lds) : word(lds + threadIdx.x) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i) word[i * kAttnThreads] = 0;
-    }
-};
-
-template <typename T, int NDB, int NS>
-__device__ __forceinline__ void finite_operands(u32x4 (&A)[NDB], u32x4 B, uint32_t seen,
-                                                const Special<NS>& special, int first = 0) {
+// Bits 15 and 31 set where the operands row(0 .. n - 1), which cover a tile, hold an
+// infinity or NaN.
+template <typename T, typename F>
+__device__ __forceinline__ uint32_t tile_not_finite(int n, F row) {
     uint32_t bad = 0;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bad |= not_finite<T>(A[db][i]);
-    if (__builtin_expect(!__any((bad & 0x80008000u) != 0), 1)) return;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-        uint32_t found;
-        A[db] = finite_operand<T>(A[db], B, seen, &found);
-        special.word[(first + db) * kAttnThreads] |= found;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) bad |= not_finite<T>(row(i));
+    return bad & 0x80008000u;
+}
+
+// Care for infinities and NaN that the mask hides takes registers that the walks
+// have none of to spare.  So a workgroup only notes whether a tile that its mask
+// cuts held one, and a further kernel repeats the noted units with care: hardly ever
+// any, and then it ends at once.  A thread looks at one mark at a time, so that few
+// workgroups look at all `blocks` of them.
+template <typename F>
+__device__ __forceinline__ void repeat_marked(const uint32_t* marks, uint32_t blocks, uint32_t group,
+                                              uint32_t groups, F unit) {
+    __shared__ uint32_t set[kAttnThreads];
+    for (uint32_t first = 0; first < blocks; first += groups * kAttnThreads) {
+        const uint32_t mine = first + threadIdx.x * groups + group;
+        const uint32_t mark = mine < blocks ? marks[mine] : 0;
+        if (!__syncthreads_or(mark != 0)) continue;
+        set[threadIdx.x] = mark;
+        __syncthreads();
+        for (int i = 0; i < kAttnThreads; ++i) {
+            if (set[i] == 0) continue;
+            unit(die_order(first + i * groups + group, blocks));
+            __syncthreads();
+        }
     }
 }
 
-// The infinities that finite_operands noted.
-template <int NDB, int NS>
-__device__ __forceinline__ void add_special(f32x16 (&acc)[NDB], const Special<NS>& special, int first = 0) {
-    uint32_t s[NDB], any = 0;
+// The product acc[db] += A[db] x over 32 inner indices with a mask, where A holds
+// infinities or NaN: a hidden pair must add nothing, and 0 times those is NaN in a
+// matrix product.  So each inner index in turn adds to the columns that see it, in
+// plain arithmetic on the operands rounded as ever.  `x` is a product's result, a
+// column per lane; bit i of `seen` says that its register i is not hidden; `words`
+// has room for 32 x 32 elements, the wave's own; four(k, d) are elements d .. d + 3
+// of A's inner index k.
+template <typename T, int NDB, typename F>
+__device__ __forceinline__ void masked_product(f32x16 (&acc)[NDB], const f32x16& x, uint32_t seen, T* words,
+                                               F four) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) any |= s[db] = special.word[(first + db) * kAttnThreads];
-    if (__builtin_expect(!__any(any != 0), 1)) return;
+    for (int i = 0; i < 16; ++i)        // -0 stands for a hidden pair
+        words[((i >> 2) * 8 + h * 4 + (i & 3)) * 32 + c] = (seen >> i) & 1 ? (T)(x[i] + 0.0f) : (T)-0.0f;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+    for (int k = 0; k < 32; ++k) {
+        const float p = to_f32(words[k * 32 + c]);
+        const bool hidden = __builtin_bit_cast(uint32_t, p) == 0x80000000u;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+        for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if ((s[db] >> i) & 1) acc[db][i] += __builtin_inff();
-            if ((s[db] >> (16 + i)) & 1) acc[db][i] -= __builtin_inff();
-        }
+            for (int q = 0; q < 4; ++q) {
+                T v[4];
+                __builtin_memcpy(v, four(k, db * 32 + q * 8 + h * 4), 8);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[db][4 * q + i] = fmaf(p, hidden ? 0.0f : to_f32(v[i]), acc[db][4 * q + i]);
+            }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // before the words are written again
 }
 
 // ---------------------------------------------------------------------------
@@ -445,30 +425,33 @@ struct AttnPlan {
 
 int attn_plan(const c3_attention_t* a, AttnPlan& p);
 int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTensor& to);
-// Numbers the units of each sequence, of which `units_of(queries, k_len, keys)`
-// (queries and keys with the padding of a dense batch) gives the count, and
+// Numbers the units of each sequence on one side, of which `units_of(queries, k_len,
+// keys)` (queries and keys with the padding of a dense batch) gives the count, and
 // returns those of one key head, or -1 where there are too many.
 template <typename F>
-int64_t attn_number(AttnPlan& p, int batch, F units_of) {
+int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
+    AttnSide& d = p.args.side[side];
     int64_t n = 0;
     if (p.table.n == 0) {
         const int64_t u = units_of(p.args.q_tokens, p.args.k_tokens, p.args.k_tokens);
-        p.args.seq_units = FastDiv((uint32_t)(u < 1 ? 1 : u));
+        d.seq_units = FastDiv((uint32_t)(u < 1 ? 1 : u));
         n = u * batch;
     } else {
         AttnSeq* s = p.list();
-        for (int i = 0; i < p.table.n; ++i) {
-            s[i].unit0 = (int32_t)n;
+        for (int i = 0; i < p.table.n && n >= 0; ++i) {
+            s[i].unit0[side] = (int32_t)n;
             n += units_of(p.args.packed ? s[i].q_len : p.args.q_tokens, s[i].k_len,
                           p.args.packed ? s[i].k_len : p.args.k_tokens);
             if (n >= (1ll << 31)) return -1;
         }
     }
+    if (n * p.args.kv_heads >= (1ll << 31)) return -1;
+    d.units = FastDiv((uint32_t)(n < 1 ? 1 : n));
     return n;
 }
 size_t attn_table_bytes(const c3_attention_t* a);
 
-// The passes of the gradient; the plan's units are numbered for the pass.
+// The passes of the gradient; the plan's units are numbered.
 hipError_t launch_attn_dq(const AttnPlan& p, bool bf16, hipStream_t s);
 hipError_t launch_attn_dkv(const AttnPlan& p, bool bf16, hipStream_t s);
 int attn_dkv_keys(int dim);         // keys of a unit of the second

@@ -27,14 +27,14 @@ __device__ __forceinline__ int key_parts(const AttnArgs& a, int k_len) {
 __device__ __forceinline__ void write_part_stats(const AttnArgs& a, int64_t row, int part, int parts, float mc,
                                                  float l) {
     float2* to = reinterpret_cast<float2*>(a.part_ml) + row;
-    to[part * a.part_rows] = make_float2(mc, l);
+    to[part * a.side[0].part_rows] = make_float2(mc, l);
     if (part == 0)
-        for (int p = parts; p < (int)a.splits.d; ++p) to[p * a.part_rows] = make_float2(0.0f, 0.0f);
+        for (int p = parts; p < (int)a.side[0].splits.d; ++p) to[p * a.side[0].part_rows] = make_float2(0.0f, 0.0f);
 }
 // Columns 32 db .. of a row's part.
 __device__ __forceinline__ void write_part(const AttnArgs& a, int64_t row, int part, int db, int h,
                                            const f32x16& x) {
-    float* to = a.part + (part * a.part_rows + row) * a.dim;
+    float* to = a.side[0].part + (part * a.side[0].part_rows + row) * a.dim;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int d = db * 32 + q * 8 + h * 4;
@@ -57,8 +57,11 @@ __device__ __forceinline__ void write_out(char* out, int db, int h, int dim, con
     }
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs a, AttnTable tab) {
+// A unit: the output of a tile of rows.  Returns whether a tile of keys that the mask
+// cuts held an infinity or NaN among its values, which only CAREFUL keeps from rows
+// that do not see it.
+template <typename T, int DP, bool CAREFUL>
+__device__ __forceinline__ bool forward_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
     constexpr int kRows = 32 * kAttnWaves;
     using L = TileLoads<DP, kKeys>;
@@ -66,9 +69,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     __shared__ __attribute__((aligned(1024))) char v0[L::kBytes];
     __shared__ __attribute__((aligned(1024))) char k1[L::kBytes];
     __shared__ __attribute__((aligned(1024))) char v1[L::kBytes];
-    __shared__ uint32_t special_words[NDB * kAttnThreads];
+    __shared__ T words[CAREFUL ? kAttnWaves : 1][32 * 32];        // for the masked product
 
-    const AttnUnit w = attn_unit(a, tab, die_order(blockIdx.x, gridDim.x));
+    const AttnUnit w = attn_unit(a, tab, 0, block);
     const int G = (int)a.group.d;
     const int n_rows = w.q_pad * G, off = w.k_len - w.q_len;
     const int tiles = (n_rows + kRows - 1) / kRows;
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
     const float cs = a.scale * kLog2e;
 
     f32x16 acc[NDB] = {};
-    const Special<NDB> special(special_words);
+    uint32_t bad = 0;
     float m = -__builtin_inff(), l = 0.0f;
 
     auto load = [&](int t, char* kt, char* vt) {
@@ -168,18 +171,28 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
                 sum += s[n][i];
             }
         l += sum;
+        if (masked) {
+            const uint32_t here =
+                tile_not_finite<T>(2 * KS, [&](int i) { return rd.along(vt + i / KS * kSub, i % KS); });
+            bad |= here;
+            if constexpr (CAREFUL) {
+                if (__any(here != 0)) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        masked_product<T, NDB>(acc, s[n], seen[n], words[wave],
+                                               [&](int k, int d) { return rd.four(vt + n * kSub, k, d); });
+                    return;
+                }
+            }
+        }
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const u32x4 p = operand<T>(s[n], j);
-                u32x4 A[NDB];
 #pragma unroll
                 for (int db = 0; db < NDB; ++db)
-                    A[db] = rd.across(vt + n * kSub + j * 16 * DP * 2, db);
-                if (masked) finite_operands<T, NDB>(A, p, seen[n] >> (8 * j), special);
-#pragma unroll
-                for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(A[db], p, acc[db]);
+                    acc[db] = mfma<T>(rd.across(vt + n * kSub + j * 16 * DP * 2, db), p, acc[db]);
             }
     };
 
@@ -194,9 +207,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
         step(t + 1, k1, v1);
     }
 
-    add_special<NDB>(acc, special);
     l += __shfl_xor(l, 32);
-    if (!there) return;
+    if (!there) return bad != 0;
     const float mc = m == -__builtin_inff() ? 0.0f : m * cs;
     const int64_t at = seq_row(a, w) + (int64_t)pos * a.heads + head;
     if (a.split_keys) {
@@ -204,7 +216,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
         if (l != 0.0f)
 #pragma unroll
             for (int db = 0; db < NDB; ++db) write_part(a, at, part, db, h, acc[db]);
-        return;
+        return bad != 0;
     }
     // a row that saw nothing (l = 0) and one of the padding: zeros and -inf
     const bool some = valid && l != 0.0f;
@@ -213,6 +225,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
 #pragma unroll
     for (int db = 0; db < NDB; ++db) write_out<T>(out, db, h, a.dim, acc[db], f, some);
     if (h == 0) a.lse[at] = some ? (mc + __log2f(l)) * kLn2 : -__builtin_inff();
+    return bad != 0;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs a, AttnTable tab) {
+    const bool bad = forward_unit<T, DP, false>(a, tab, die_order(blockIdx.x, gridDim.x));
+    if (a.causal || a.window) {
+        const int any = __syncthreads_or(bad);
+        if (threadIdx.x == 0) a.side[0].marks[blockIdx.x] = any;
+    }
+}
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 1) void attn_forward_careful_kernel(AttnArgs a, AttnTable tab,
+                                                                               uint32_t blocks) {
+    repeat_marked(a.side[0].marks, blocks, blockIdx.x, gridDim.x,
+                  [&](uint32_t unit) { forward_unit<T, DP, true>(a, tab, unit); });
 }
 
 // Few rows against many keys, as new tokens against a cache: the keys are read
@@ -221,16 +249,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs 
 // that no wave waits for another before the end; there their maxima and sums are
 // joined in LDS.  Long caches are divided among workgroups as well.
 template <typename T, int DP>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a, AttnTable tab) {
+__global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_kernel(AttnArgs a, AttnTable tab) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
     __shared__ __attribute__((aligned(1024))) char k0[kAttnWaves * kSub];
     __shared__ __attribute__((aligned(1024))) char v0[kAttnWaves * kSub];
     __shared__ __attribute__((aligned(1024))) char k1[kAttnWaves * kSub];
     __shared__ __attribute__((aligned(1024))) char v1[kAttnWaves * kSub];
-    __shared__ uint32_t special_words[NDB * kAttnThreads];
+    __shared__ T words[kAttnWaves][32 * 32];      // for the masked product
     __shared__ float stats[2][kAttnWaves][64];
 
-    const AttnUnit w = attn_unit(a, tab, blockIdx.x);
+    const AttnUnit w = attn_unit(a, tab, 0, blockIdx.x);
     const int G = (int)a.group.d;
     const int n_rows = w.q_pad * G, off = w.k_len - w.q_len;
     const int parts = key_parts(a, w.k_len), tile = parts > 1 ? (int)w.unit / parts : (int)w.unit;
@@ -274,7 +302,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a
     const float cs = a.scale * kLog2e;
 
     f32x16 acc[NDB] = {};
-    const Special<NDB> special(special_words);
     float m = -__builtin_inff(), l = 0.0f;
 
     auto load = [&](int t, char* kt, char* vt) {
@@ -326,15 +353,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a
             s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -mc));
             l += s[i];
         }
+        if (masked && __any(tile_not_finite<T>(KS, [&](int ks) { return rd.along(vt, ks); }) != 0)) {
+            masked_product<T, NDB>(acc, s, seen, words[wave], [&](int k, int d) { return rd.four(vt, k, d); });
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const u32x4 p = operand<T>(s, j);
-            u32x4 A[NDB];
 #pragma unroll
-            for (int db = 0; db < NDB; ++db) A[db] = rd.across(vt + j * 16 * DP * 2, db);
-            if (masked) finite_operands<T, NDB>(A, p, seen >> (8 * j), special);
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(A[db], p, acc[db]);
+            for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(rd.across(vt + j * 16 * DP * 2, db), p, acc[db]);
         }
     };
     // The wave's own loads, in order: all but the latest 2 kLoads have landed.
@@ -359,7 +386,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a
         step(next, k1, v1);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    add_special<NDB>(acc, special);
     l += __shfl_xor(l, 32);
 
     // join the four waves: maxima and sums first, then the rescaled accumulators,
@@ -450,7 +476,7 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
     const uint64_t full = __ballot(l != 0.0f);
     for (int p = 0; p < parts; ++p) {
         if (!((full >> p) & 1)) continue;
-        const float2 v = *reinterpret_cast<const float2*>(a.part + (p * rows + row) * a.dim + 2 * lane);
+        const float2 v = *reinterpret_cast<const float2*>(a.side[0].part + (p * rows + row) * a.dim + 2 * lane);
         const float g = __shfl(f, p);
         x = fmaf(v.x, g, x);
         y = fmaf(v.y, g, y);
@@ -464,14 +490,16 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
 
 template <typename T, int DP>
 hipError_t launch_forward(const AttnPlan& p, bool tokens, hipStream_t s) {
-    const dim3 grid(p.args.units.d * (uint32_t)p.args.kv_heads), block(kAttnThreads);
+    const dim3 grid(p.args.side[0].units.d * (uint32_t)p.args.kv_heads), block(kAttnThreads);
     if (tokens)
         attn_tokens_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
     else
         attn_forward_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    if (!tokens && (p.args.causal || p.args.window) && p.key_rows > 0)
+        attn_forward_careful_kernel<T, DP><<<dim3(32), block, 0, s>>>(p.args, p.table, grid.x);
     if (p.args.split_keys)
         attn_join_parts_kernel<T><<<dim3((unsigned)((p.rows + 3) / 4)), dim3(256), 0, s>>>(
-            p.args, p.rows, (int)p.args.splits.d, FastDiv((uint32_t)p.args.q_tokens));
+            p.args, p.rows, (int)p.args.side[0].splits.d, FastDiv((uint32_t)p.args.q_tokens));
     return hipGetLastError();
 }
 
@@ -482,13 +510,15 @@ inline uint64_t align256(uint64_t x) { return (x + 255) / 256 * 256; }
 // compute units, keys in parts of split_keys, whose results a further kernel joins.
 struct ForwardShape {
     bool tokens;
-    int64_t rows, split_keys, parts, table, part, part_ml, total;
+    int64_t rows, split_keys, parts;
+    uint64_t table, marks, part, part_ml, total;
+    bool fits;
     ForwardShape(const c3_attention_t* a, AttnPlan& p) {
         const int64_t group = p.args.group.d, kv = p.args.kv_heads;
         tokens = p.max_q * group <= 32;
         rows = tokens ? 32 : 32 * kAttnWaves;
         auto units = [&](int64_t split) {
-            return kv * attn_number(p, a->batch, [&](int64_t nq, int64_t nk, int64_t) {
+            return kv * attn_number(p, a->batch, 0, [&](int64_t nq, int64_t nk, int64_t) {
                 const int64_t t = (nq * group + rows - 1) / rows;
                 return split ? t * std::max<int64_t>(1, (nk + split - 1) / split) : t;
             });
@@ -505,9 +535,12 @@ struct ForwardShape {
             parts = (p.max_k + split_keys - 1) / split_keys;
             if (parts < 2) split_keys = 0, parts = 1;
         }
+        const int64_t blocks = units(split_keys);
+        fits = blocks >= 0;
         uint64_t at = 0;
         auto take = [&at](uint64_t bytes) { const uint64_t r = at; at = align256(at + bytes); return r; };
         table = take(attn_table_bytes(a));
+        marks = take(fits && !tokens ? 4 * (uint64_t)blocks : 0);
         part = take(split_keys ? 4 * (uint64_t)(parts * p.rows * p.args.dim) : 0);
         part_ml = take(split_keys ? 8 * (uint64_t)(parts * p.rows) : 0);
         total = std::max<uint64_t>(at, 256);
@@ -566,7 +599,7 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
         const int64_t q = a->q_lens[i], k = a->k_lens[i];
         if (q < 0 || k < 0 || (!a->packed && (q > a->q_tokens || k > a->k_tokens))) return C3_E_INVAL;
         if (a->packed && (nq + q > a->q_tokens || nk + k > a->k_tokens)) return C3_E_INVAL;
-        s[i] = AttnSeq{i, a->packed ? (int32_t)nq : 0, (int32_t)q, a->packed ? (int32_t)nk : 0, (int32_t)k, 0};
+        s[i] = AttnSeq{i, a->packed ? (int32_t)nq : 0, (int32_t)q, a->packed ? (int32_t)nk : 0, (int32_t)k, {0, 0}};
         nq += q;
         nk += k;
         p.max_q = std::max(p.max_q, q);
@@ -613,7 +646,8 @@ size_t c3_attention_workspace_size(const c3_attention_t* a) {
     try {
         c3::AttnPlan p;
         if (c3::attn_plan(a, p) != C3_OK) return 0;
-        return c3::ForwardShape(a, p).total;
+        const c3::ForwardShape f(a, p);
+        return f.fits ? f.total : 0;
     } catch (...) {
         return 0;
     }
@@ -634,22 +668,18 @@ int c3_attention(const c3_attention_t* a, const c3_attn_tensor_t* q, const c3_at
         if (p.rows > 0 && lse == nullptr) return C3_E_INVAL;
         if ((uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
         const ForwardShape f(a, p);
+        if (!f.fits) return C3_E_UNSUPPORTED;
         if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)f.total) return C3_E_WORKSPACE;
         if (p.rows == 0) return C3_OK;
         p.args.lse = lse;
-        const int64_t group = p.args.group.d;
-        const int64_t units = attn_number(p, a->batch, [&](int64_t nq, int64_t nk, int64_t) {
-            const int64_t t = (nq * group + f.rows - 1) / f.rows;
-            return f.split_keys ? t * std::max<int64_t>(1, (nk + f.split_keys - 1) / f.split_keys) : t;
-        });
-        if (units < 0 || units * p.args.kv_heads >= (1ll << 31)) return C3_E_UNSUPPORTED;
-        p.args.units = FastDiv((uint32_t)units);
-        p.args.splits = FastDiv((uint32_t)f.parts);
-        p.args.split_keys = (int32_t)f.split_keys;
         char* base = static_cast<char*>(ws);
-        p.args.part = reinterpret_cast<float*>(base + f.part);
+        AttnSide& side = p.args.side[0];
+        side.splits = FastDiv((uint32_t)f.parts);
+        side.marks = reinterpret_cast<uint32_t*>(base + f.marks);
+        side.part = reinterpret_cast<float*>(base + f.part);
+        side.part_rows = p.rows;
+        p.args.split_keys = (int32_t)f.split_keys;
         p.args.part_ml = reinterpret_cast<float*>(base + f.part_ml);
-        p.args.part_rows = p.rows;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
         if (p.seqs != nullptr) {
             if (stage_bytes(base + f.table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;

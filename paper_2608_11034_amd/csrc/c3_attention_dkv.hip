@@ -1,346 +1,22 @@
-// Second pass of attention's gradient (c3_attention_grad.hip): dk and dv.
-//
-// A wave holds 32 NT keys and values and walks the rows of the query heads that
-// share them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
-#include <type_traits>
-
-#include "c3_attention.h"
+// Second pass of attention's gradient (c3_attention_dkv.h).
+#include "c3_attention_dkv.h"
 
 namespace c3 {
 namespace {
 
-constexpr int kDkvTiles = 1;
-
-// acc[m] += A x[m] over inner indices 16 j .., for the wave's NT blocks of columns.
-// Where the mask hides some pairs each block has its own finite operands.
-template <typename T, int NT, int NDB, bool MASKED, int NS>
-__device__ __forceinline__ void add_product(f32x16 (&acc)[NT][NDB], const u32x4 (&A)[NDB],
-                                            const f32x16 (&x)[NT], int j,
-                                            const uint32_t (&seen)[NT], const Special<NS>& special) {
-#pragma unroll
-    for (int m = 0; m < NT; ++m) {
-        const u32x4 B = operand<T>(x[m], j);
-        u32x4 C[NDB];
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) C[db] = A[db];
-        if constexpr (MASKED) finite_operands<T, NDB>(C, B, seen[m] >> (8 * j), special, m * NDB);
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) acc[m][db] = mfma<T>(C[db], B, acc[m][db]);
-    }
-}
-
-// One unit: dk and dv of a block of keys.  The plain form notes whether a tile that
-// the mask cuts holds an infinity or NaN and returns it; the careful one keeps such
-// values from pairs that the mask hides.  They are kernels of their own because the
-// care costs registers that the plain walk has none of to spare.
-template <typename T, int DP, int NT, bool CAREFUL>
-__device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
-    constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
-    constexpr int kWaveKeys = 32 * NT, kBlockKeys = kWaveKeys * kAttnWaves;
-    // Heads over 64: the values lie in LDS and tiles have 32 rows, so that two
-    // workgroups fit a compute unit's registers (256 a lane) and LDS (160 KiB).
-    constexpr bool kValuesLds = DP > 64;
-    constexpr int kTileRows = kValuesLds ? 32 : 64;
-    constexpr int kTileBytes = kTileRows * DP * 2, kSteps = kTileRows / 32 * KS / kAttnWaves;
-    __shared__ __attribute__((aligned(1024))) char q0[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) char g0[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) float s0[2 * 64];      // lse2, delta: 64 lanes' words each
-    __shared__ __attribute__((aligned(1024))) char q1[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) char g1[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) float s1[2 * 64];
-    __shared__ __attribute__((aligned(1024))) char v_tile[kValuesLds ? kBlockKeys * DP * 2 : 16];
-    __shared__ uint32_t special_words[CAREFUL ? 2 * NT * NDB * kAttnThreads : 1];
-
-    const AttnUnit w = attn_unit(a, tab, block);
-    const int G = (int)a.group.d;
-    const int n_rows = w.q_len * G, off = w.k_len - w.q_len;
-    const int k_pad = a.packed ? w.k_len : a.k_tokens;
-    const int tile = (int)a.splits.quot(w.unit), part = (int)w.unit - tile * (int)a.splits.d;
-    const int key_block = tile * kBlockKeys;
-    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wkey = key_block + wave * kWaveKeys, key = wkey + c;      // and every 32nd from it
-
-    // queries that see any of the block's keys
-    int p_lo = 0, p_hi = w.q_len;
-    if (a.causal) p_lo = max(0, key_block - off);
-    if (a.window) p_hi = min(p_hi, key_block + kBlockKeys - 1 - off + a.window);
-    if (key_block >= w.k_len) p_hi = 0;
-    int t0 = p_lo * G / kTileRows;
-    int t1 = p_hi > p_lo ? (p_hi * G + kTileRows - 1) / kTileRows : t0;
-    if (a.splits.d > 1) {       // this workgroup's part of the walk
-        const int64_t n = t1 - t0;
-        t1 = t0 + (int)a.splits.quot((uint32_t)(n * (part + 1)));
-        t0 = t0 + (int)a.splits.quot((uint32_t)(n * part));
-    }
-
-    const StepReads<DP> rd;
-    const char* qb = seq_base(a.q, a.packed, w.b, w.q_start, w.hk * G);
-    const char* gb = seq_base(a.d_o, a.packed, w.b, w.q_start, w.hk * G);
-    const int64_t stat_row = seq_row(a, w) + w.hk * G;
-    const float cs = a.scale * kLog2e;
-
-    f32x16 dk[NT][NDB], dv[NT][NDB];
-    constexpr int kSpecial = CAREFUL ? NT * NDB : 0;
-    const Special<kSpecial> dk_special(special_words), dv_special(special_words + kSpecial * kAttnThreads);
-    uint32_t bad = 0;
-
-    auto load = [&](int t, char* qt, char* gt, float* st) {
-        const int row0 = t * kTileRows, rows = min(kTileRows, n_rows - row0);
-        const int p0 = __builtin_amdgcn_readfirstlane((int)a.group.quot(row0));
-        const int p1 = __builtin_amdgcn_readfirstlane((int)a.group.quot(row0 + rows - 1)) - p0;
-        const char* qr = qb + (int64_t)p0 * a.q.st;
-        const char* gr = gb + (int64_t)p0 * a.d_o.st;
-        const uint32_t q_bytes = (uint32_t)(p1 * a.q.st + (G - 1) * a.q.sh) + a.dim * 2;
-        const uint32_t g_bytes = (uint32_t)(p1 * a.d_o.st + (G - 1) * a.d_o.sh) + a.dim * 2;
-        // the wave's steps lie in one of the tile's 32 rows; a lane takes half a row's
-        // 32 bytes of each
-        const int first = wave * kSteps, i = first / KS * 32 + (lane >> 1);
-        const int r = row0 + i, p = (int)a.group.quot(r), g = r - p * G;
-        const uint32_t qo = (uint32_t)((p - p0) * (int)a.q.st + g * (int)a.q.sh);
-        const uint32_t go = (uint32_t)((p - p0) * (int)a.d_o.st + g * (int)a.d_o.sh);
-#pragma unroll
-        for (int n = 0; n < kSteps; ++n) {
-            const int piece = 2 * ((first + n) % KS) + (lane & 1);
-            const bool ok = i < rows && piece * 8 < a.dim;
-            load_piece_lds(qr, q_bytes, ok ? qo + piece * 16 : 0xFFFFFF00u, qt + (first + n) * 1024);
-            load_piece_lds(gr, g_bytes, ok ? go + piece * 16 : 0xFFFFFF00u, gt + (first + n) * 1024);
-        }
-        if (wave < 2) {         // a lane for each row: lse2 by the first wave, delta by the second
-            const float* from = (wave == 0 ? a.lse2 : a.delta) + stat_row + (int64_t)p0 * a.heads;
-            const int r = row0 + lane, p = (int)a.group.quot(r), g = r - p * G;
-            const uint32_t bytes = (uint32_t)(p1 * a.heads + G) * 4;
-            const uint32_t at = lane < rows ? (uint32_t)((p - p0) * a.heads + g) * 4 : 0xFFFFFF00u;
-            const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, (int)bytes, 0x00027000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rs, (__attribute__((address_space(3))) void*)(st + wave * 64), 4, (int)at, 0, 0, 0);
-        }
-    };
-#pragma unroll
-    for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) dk[m][db] = dv[m][db] = f32x16{};
-        u32x4 kf[NT][KS], vf[kValuesLds ? 1 : NT][KS];
-        {
-            const char* kb = seq_base(a.k, a.packed, w.b, w.k_start, w.hk);
-            const char* vb = seq_base(a.v, a.packed, w.b, w.k_start, w.hk);
-#pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                load_row<DP>(kf[m], kb + (int64_t)(key + 32 * m) * a.k.st, key + 32 * m < w.k_len, a.dim);
-                if constexpr (!kValuesLds)
-                    load_row<DP>(vf[m], vb + (int64_t)(key + 32 * m) * a.v.st, key + 32 * m < w.k_len, a.dim);
-            }
-            if constexpr (kValuesLds) {
-                // each wave its own keys'
-                const int rows = min(w.k_len - wkey, kWaveKeys);
-                const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * a.v.st) + a.dim * 2 : 0;
-#pragma unroll
-                for (int n = 0; n < NT * KS; ++n) {
-                    const int i = n / KS * 32 + (lane >> 1), piece = 2 * (n % KS) + (lane & 1);
-                    const bool ok = i < rows && piece * 8 < a.dim;
-                    load_piece_lds(vb + (int64_t)wkey * a.v.st, bytes,
-                                   ok ? (uint32_t)(i * (int)a.v.st + piece * 16) : 0xFFFFFF00u,
-                                   v_tile + (wave * NT * KS + n) * 1024);
-                }
-            }
-        }
-
-        // The four parts of 32 rows' work: scores and dP; P and dS; what they add to
-        // dv and dk.
-        auto scores = [&](int n, const char* qt, const char* gt, f32x16 (&s)[NT], f32x16 (&dp)[NT]) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const u32x4 x = rd.along(qt + n * kSub, ks);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) s[m] = mfma<T>(x, kf[m][ks], s[m]);
-            }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const u32x4 x = rd.along(gt + n * kSub, ks);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    if constexpr (kValuesLds)
-                        dp[m] = mfma<T>(x, rd.along(v_tile + (wave * NT + m) * kSub, ks), dp[m]);
-                    else
-                        dp[m] = mfma<T>(x, vf[m][ks], dp[m]);
-                }
-            }
-        };
-        auto probabilities = [&](int n, const float* st, f32x16 (&s)[NT], f32x16 (&dp)[NT]) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 l2 = *reinterpret_cast<const f32x4*>(st + n * 32 + q * 8 + h * 4);
-                const f32x4 de = *reinterpret_cast<const f32x4*>(st + 64 + n * 32 + q * 8 + h * 4);
-#pragma unroll
-                for (int m = 0; m < NT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s[m][4 * q + i] = __builtin_amdgcn_exp2f(fmaf(s[m][4 * q + i], cs, -l2[i]));
-                        dp[m][4 * q + i] = s[m][4 * q + i] * (dp[m][4 * q + i] - de[i]);
-                    }
-            }
-        };
-        auto gradients = [&](int n, const char* qt, const char* gt, const f32x16 (&s)[NT], const f32x16 (&dp)[NT],
-                             const uint32_t (&seen)[NT]) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4 A[NDB];
-#pragma unroll
-                for (int db = 0; db < NDB; ++db) A[db] = rd.across(gt + n * kSub, j, db);
-                add_product<T, NT, NDB, CAREFUL>(dv, A, s, j, seen, dv_special);
-#pragma unroll
-                for (int db = 0; db < NDB; ++db) A[db] = rd.across(qt + n * kSub, j, db);
-                add_product<T, NT, NDB, CAREFUL>(dk, A, dp, j, seen, dk_special);
-            }
-        };
-        auto step = [&](int t, const char* qt, const char* gt, const float* st) {
-#pragma unroll
-            for (int n = 0; n < kTileRows / 32; ++n) {
-                const int row0 = t * kTileRows + n * 32;
-                if (row0 >= n_rows) continue;
-                const int pa = (int)a.group.quot(row0) + off;
-                const int pb = (int)a.group.quot(min(row0 + 31, n_rows - 1)) + off;
-                if (a.causal && wkey > pb) continue;
-                if (a.window && wkey + kWaveKeys - 1 <= pa - a.window) continue;
-                const bool masked = (a.causal && wkey + kWaveKeys - 1 > pa) || (a.window && wkey <= pb - a.window);
-                f32x16 s[NT] = {}, dp[NT] = {};
-                uint32_t seen[NT] = {};
-                scores(n, qt, gt, s, dp);
-                probabilities(n, st, s, dp);
-                if (masked) {
-                    // formed here, not held in registers through the walk
-                    int k_ = key, h_ = h * 4;
-                    asm volatile("" : "+v"(k_), "+v"(h_));
-#pragma unroll
-                    for (int m = 0; m < NT; ++m) {
-                        // rows from r_lo to below r_hi of these 32 see the lane's key
-                        const int64_t at = (int64_t)(k_ + 32 * m - off) * G - row0, all = (int64_t)a.window * G;
-                        const int r_lo = a.causal ? (int)min(max(at, (int64_t)0), (int64_t)32) : 0;
-                        const int r_hi = a.window ? (int)min(max(at + all, (int64_t)0), (int64_t)32) : 32;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = (i >> 2) * 8 + h_ + (i & 3);
-                            const bool see = r >= r_lo && r < r_hi;
-                            seen[m] |= see ? 1u << i : 0u;
-                            s[m][i] = see ? s[m][i] : 0.0f;
-                            dp[m][i] = see ? dp[m][i] : 0.0f;
-                        }
-                    }
-                    if constexpr (!CAREFUL) {
-#pragma unroll 1
-                        for (int ks = 0; ks < KS; ++ks)
-                            bad |= not_finite<T>(rd.along(qt + n * kSub, ks)) | not_finite<T>(rd.along(gt + n * kSub, ks));
-                    }
-                }
-                if (!masked)
-#pragma unroll
-                    for (int m = 0; m < NT; ++m) seen[m] = 0xFFFFu;
-                gradients(n, qt, gt, s, dp, seen);
-            }
-        };
-
-        if (t0 < t1) load(t0, q0, g0, s0);
-        for (int t = t0; t < t1; t += 2) {
-            tiles_ready();
-                if (t + 1 < t1) load(t + 1, q1, g1, s1);
-            step(t, q0, g0, s0);
-            if (t + 1 >= t1) break;
-            tiles_ready();
-                if (t + 2 < t1) load(t + 2, q0, g0, s0);
-            step(t + 1, q1, g1, s1);
-        }
-
-#pragma unroll
-    for (int m = 0; m < NT; ++m) {
-        if constexpr (CAREFUL) {
-            add_special<NDB>(dk[m], dk_special, m * NDB);
-            add_special<NDB>(dv[m], dv_special, m * NDB);
-        }
-        const int k = key + 32 * m;
-        if (k >= k_pad) continue;
-        const bool valid = k < w.k_len;
-        if (a.splits.d > 1) {
-            // dk and dv of this part, in fp32 and not yet scaled
-            const int64_t keys = (int64_t)(a.packed ? 0 : w.b) * a.k_tokens + w.k_start + k;
-            float* to = a.part + (part * 2 * a.part_rows + keys * a.kv_heads + w.hk) * a.dim;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int d = db * 32 + q * 8 + h * 4;
-                    if (d >= a.dim) continue;
-                    f32x4 x, y;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[i] = valid ? dk[m][db][4 * q + i] : 0.0f;
-                        y[i] = valid ? dv[m][db][4 * q + i] : 0.0f;
-                    }
-                    *reinterpret_cast<f32x4*>(to + d) = x;
-                    *reinterpret_cast<f32x4*>(to + a.part_rows * a.dim + d) = y;
-                }
-            continue;
-        }
-        char* ok = seq_base(a.dk, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dk.st;
-        char* ov = seq_base(a.dv, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dv.st;
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int d = db * 32 + q * 8 + h * 4;
-                if (d >= a.dim) continue;
-                T e[4], f[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e[i] = valid ? (T)(dk[m][db][4 * q + i] * a.scale) : (T)0.0f;
-                    f[i] = valid ? (T)dv[m][db][4 * q + i] : (T)0.0f;
-                }
-                u32x2 x, y;
-                __builtin_memcpy(&x, e, 8);
-                __builtin_memcpy(&y, f, 8);
-                *reinterpret_cast<u32x2*>(ok + d * 2) = x;
-                *reinterpret_cast<u32x2*>(ov + d * 2) = y;
-            }
-    }
-    return (bad & 0x80008000u) != 0;
-}
-
-template <typename T, int DP, int NT>
+template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, AttnTable tab) {
-    const bool bad = dkv_unit<T, DP, NT, false>(a, tab, die_order(blockIdx.x, gridDim.x));
+    const bool bad = dkv_unit<T, DP, kDkvTiles, false>(a, tab, die_order(blockIdx.x, gridDim.x));
     if (a.causal || a.window) {
         const int any = __syncthreads_or(bad);
-        if (threadIdx.x == 0) a.careful[blockIdx.x] = any;
-    }
-}
-
-// Repeats the units that the plain kernel, of `blocks` workgroups, marked: hardly
-// ever any.  A lane looks at one mark at a time, so a few workgroups look at all.
-template <typename T, int DP, int NT>
-__global__ __launch_bounds__(kAttnThreads, 1) void attn_dkv_careful_kernel(AttnArgs a, AttnTable tab,
-                                                                           uint32_t blocks) {
-    __shared__ uint32_t marks[kAttnThreads];
-    for (uint32_t first = 0; first < blocks; first += gridDim.x * kAttnThreads) {
-        const uint32_t mine = first + threadIdx.x * gridDim.x + blockIdx.x;
-        const uint32_t mark = mine < blocks ? a.careful[mine] : 0;
-        if (!__syncthreads_or(mark != 0)) continue;
-        marks[threadIdx.x] = mark;
-        __syncthreads();
-        for (int i = 0; i < kAttnThreads; ++i) {
-            if (marks[i] == 0) continue;
-            dkv_unit<T, DP, NT, true>(a, tab, die_order(first + i * gridDim.x + blockIdx.x, blocks));
-            __syncthreads();
-        }
-        __syncthreads();
+        if (threadIdx.x == 0) a.side[1].marks[blockIdx.x] = any;
     }
 }
 
 template <typename T, int DP>
 hipError_t launch(const AttnPlan& p, hipStream_t s) {
-    const uint32_t blocks = p.args.units.d * (uint32_t)p.args.kv_heads;
-    attn_dkv_kernel<T, DP, kDkvTiles><<<dim3(blocks), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
-    if (p.args.causal || p.args.window)
-        attn_dkv_careful_kernel<T, DP, kDkvTiles>
-            <<<dim3(blocks < 64 ? blocks : 64), dim3(kAttnThreads), 0, s>>>(p.args, p.table, blocks);
+    const uint32_t blocks = p.args.side[1].units.d * (uint32_t)p.args.kv_heads;
+    attn_dkv_kernel<T, DP><<<dim3(blocks), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
     return hipGetLastError();
 }
 

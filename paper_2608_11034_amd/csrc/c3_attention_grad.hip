@@ -7,7 +7,8 @@
 // change from run to run.  Matrix products bound both.
 #include <algorithm>
 
-#include "c3_attention.h"
+#include "c3_attention_dkv.h"
+#include "c3_attention_dq.h"
 
 namespace c3 {
 namespace {
@@ -40,16 +41,39 @@ __global__ __launch_bounds__(256) void attn_sum_parts_kernel(const float* part, 
     *reinterpret_cast<u32x2*>(out.ptr + b * out.sb + (token - b * tokens.d) * out.st + head * out.sh + d * 2) = x;
 }
 
-hipError_t sum_parts(const AttnPlan& p, bool bf16, const float* part, int64_t stride, int64_t rows, int heads,
+hipError_t sum_parts(const AttnPlan& p, bool bf16, const AttnSide& side, int which, int of, int heads,
                      int64_t tokens, const AttnTensor& out, float factor, hipStream_t s) {
     const FastDiv quads((uint32_t)p.args.dim / 4), h((uint32_t)heads), t((uint32_t)tokens);
-    const int64_t blocks = (rows * quads.d + 255) / 256;
+    const int64_t blocks = (side.part_rows * quads.d + 255) / 256, n = side.part_rows * p.args.dim;
+    const dim3 grid((unsigned)blocks), block(256);
     if (bf16)
-        attn_sum_parts_kernel<__bf16><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(
-            part, stride, (int)p.args.splits.d, rows, quads, h, t, out, factor);
+        attn_sum_parts_kernel<__bf16><<<grid, block, 0, s>>>(side.part + which * n, of * n, (int)side.splits.d,
+                                                              side.part_rows, quads, h, t, out, factor);
     else
-        attn_sum_parts_kernel<_Float16><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(
-            part, stride, (int)p.args.splits.d, rows, quads, h, t, out, factor);
+        attn_sum_parts_kernel<_Float16><<<grid, block, 0, s>>>(side.part + which * n, of * n, (int)side.splits.d,
+                                                                side.part_rows, quads, h, t, out, factor);
+    return hipGetLastError();
+}
+
+// Repeats with care the units that either pass marked: the first half of the
+// workgroups those of the first.
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 1) void attn_grad_careful_kernel(AttnArgs a, AttnTable tab,
+                                                                            uint32_t q_blocks, uint32_t k_blocks) {
+    const uint32_t half = gridDim.x / 2;
+    if (blockIdx.x < half)
+        repeat_marked(a.side[0].marks, q_blocks, blockIdx.x, half,
+                      [&](uint32_t unit) { dq_unit<T, DP, true>(a, tab, unit); });
+    else
+        repeat_marked(a.side[1].marks, k_blocks, blockIdx.x - half, half,
+                      [&](uint32_t unit) { dkv_unit<T, DP, kDkvTiles, true>(a, tab, unit); });
+}
+
+template <typename T, int DP>
+hipError_t launch_careful(const AttnPlan& p, hipStream_t s) {
+    const uint32_t q = p.rows > 0 ? p.args.side[0].units.d * (uint32_t)p.args.kv_heads : 0;
+    const uint32_t k = p.key_rows > 0 ? p.args.side[1].units.d * (uint32_t)p.args.kv_heads : 0;
+    attn_grad_careful_kernel<T, DP><<<dim3(64), dim3(kAttnThreads), 0, s>>>(p.args, p.table, q, k);
     return hipGetLastError();
 }
 
@@ -66,57 +90,39 @@ inline uint64_t align256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int64_t kDqRows = 32 * kAttnWaves;        // rows of a unit of the first pass
 
-// Units of one key head, all sequences, of either pass before its walks are
-// divided.
-int64_t tiles_of(const c3_attention_t* a, AttnPlan& p, bool keys) {
-    const int64_t group = p.args.group.d, block_keys = attn_dkv_keys(a->dim);
-    return attn_number(p, a->batch, [&](int64_t nq, int64_t, int64_t nk) {
-        return keys ? (nk + block_keys - 1) / block_keys : (nq * group + kDqRows - 1) / kDqRows;
-    });
-}
-
-// Workspace: lse2 and delta of every row, the marks of the second pass, the tables
-// of both, parts of sums; and how the walks are divided.
+// Divides the work of both passes and lays out the workspace: lse2 and delta of every
+// row, marks, the table of sequences, parts of sums.
 struct GradSpace {
-    uint64_t lse2, delta, careful, table_q, table_k, part, total;
-    int64_t parts_q, parts_k;
+    uint64_t lse2, delta, marks[2], table, part[2], total;
+    int64_t parts[2];
+    bool fits;
     GradSpace(const c3_attention_t* a, AttnPlan& p) {
-        const int64_t group = p.args.group.d, kv = p.args.kv_heads;
-        const int64_t units_k = tiles_of(a, p, true) * kv;
-        parts_q = walk_parts(tiles_of(a, p, false) * kv, 512, p.max_k / 64);
+        const int64_t group = p.args.group.d, kv = p.args.kv_heads, block_keys = attn_dkv_keys(a->dim);
+        auto number = [&](int side, int64_t times) {
+            return kv * attn_number(p, a->batch, side, [&](int64_t nq, int64_t, int64_t nk) {
+                return times * (side ? (nk + block_keys - 1) / block_keys : (nq * group + kDqRows - 1) / kDqRows);
+            });
+        };
+        parts[0] = walk_parts(number(0, 1), 512, p.max_k / kDqKeys);
         // walks under a causal mask differ in length: more of them even that out
-        parts_k = walk_parts(units_k, a->causal ? 1024 : 512, p.max_q * group / 64);
+        parts[1] = walk_parts(number(1, 1), a->causal ? 1024 : 512, p.max_q * group / 64);
+        const int64_t units[2] = {number(0, parts[0]), number(1, parts[1])};
+        fits = units[0] >= 0 && units[1] >= 0;
         uint64_t at = 0;
-        auto take = [&at](uint64_t bytes) { const uint64_t r = at; at = align256(at + bytes); return r; };
-        lse2 = take(4 * (uint64_t)p.rows);
-        delta = take(4 * (uint64_t)p.rows);
-        careful = take(4 * (uint64_t)std::max<int64_t>(units_k * parts_k, 0));
-        table_q = take(attn_table_bytes(a));
-        table_k = take(attn_table_bytes(a));
-        uint64_t bytes = 0;     // the passes follow each other
-        if (parts_q > 1) bytes = 4 * (uint64_t)(parts_q * p.rows * p.args.dim);
-        if (parts_k > 1) bytes = std::max(bytes, 8 * (uint64_t)(parts_k * p.key_rows * p.args.dim));
-        part = take(bytes);
+        auto take = [&at](int64_t bytes) { const uint64_t r = at; at = align256(at + (uint64_t)bytes); return r; };
+        lse2 = take(4 * p.rows);
+        delta = take(4 * p.rows);
+        table = take((int64_t)attn_table_bytes(a));
+        for (int i = 0; i < 2; ++i) {
+            const int64_t rows = i ? p.key_rows : p.rows;
+            p.args.side[i].splits = FastDiv((uint32_t)parts[i]);
+            p.args.side[i].part_rows = rows;
+            marks[i] = take(fits ? 4 * units[i] : 0);
+            part[i] = take(parts[i] > 1 ? 4 * (i + 1) * parts[i] * rows * p.args.dim : 0);
+        }
         total = std::max<uint64_t>(at, 256);
     }
 };
-
-// Numbers the sequences' units for one pass and stages the list if it is long.
-int number_units(const c3_attention_t* a, AttnPlan& p, char* table, bool keys, int64_t parts, hipStream_t s) {
-    const int64_t group = p.args.group.d, block_keys = attn_dkv_keys(a->dim);
-    const int64_t units = attn_number(p, a->batch, [&](int64_t nq, int64_t, int64_t nk) {
-        return parts * (keys ? (nk + block_keys - 1) / block_keys : (nq * group + kDqRows - 1) / kDqRows);
-    });
-    if (units < 0 || units * p.args.kv_heads >= (1ll << 31)) return C3_E_UNSUPPORTED;
-    p.args.units = FastDiv((uint32_t)(units < 1 ? 1 : units));
-    p.args.splits = FastDiv((uint32_t)parts);
-    p.args.part_rows = keys ? p.key_rows : p.rows;
-    if (units > 0 && p.seqs != nullptr) {
-        if (stage_bytes(table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;
-        p.table.staged = reinterpret_cast<const AttnSeq*>(table);
-    }
-    return C3_OK;
-}
 
 }  // namespace
 }  // namespace c3
@@ -127,7 +133,8 @@ size_t c3_attention_grad_workspace_size(const c3_attention_t* a) {
     try {
         c3::AttnPlan p;
         if (c3::attn_plan(a, p) != C3_OK) return 0;
-        return c3::GradSpace(a, p).total;
+        const c3::GradSpace sp(a, p);
+        return sp.fits ? sp.total : 0;
     } catch (...) {
         return 0;
     }
@@ -155,32 +162,38 @@ int c3_attention_grad(const c3_attention_t* a, const c3_attn_tensor_t* dout,
         if (p.rows > 0 && lse == nullptr) return C3_E_INVAL;
         if ((uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
         const GradSpace sp(a, p);
+        if (!sp.fits) return C3_E_UNSUPPORTED;
         if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < sp.total) return C3_E_WORKSPACE;
         char* base = static_cast<char*>(ws);
         g.lse = const_cast<float*>(lse);
         g.lse2 = reinterpret_cast<float*>(base + sp.lse2);
         g.delta = reinterpret_cast<float*>(base + sp.delta);
-        g.part = reinterpret_cast<float*>(base + sp.part);
-        g.careful = reinterpret_cast<uint32_t*>(base + sp.careful);
+        for (int i = 0; i < 2; ++i) {
+            g.side[i].marks = reinterpret_cast<uint32_t*>(base + sp.marks[i]);
+            g.side[i].part = reinterpret_cast<float*>(base + sp.part[i]);
+        }
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        const bool bf16 = a->dtype == C3_BF16;
-        if (p.rows > 0) {
-            if ((rc = number_units(a, p, base + sp.table_q, false, sp.parts_q, s)) != C3_OK) return rc;
-            if (launch_attn_dq(p, bf16, s) != hipSuccess) return C3_E_HIP;
-            if (sp.parts_q > 1 &&
-                sum_parts(p, bf16, g.part, p.rows * g.dim, p.rows, g.heads, g.q_tokens, g.dq, g.scale, s) != hipSuccess)
+        const bool bf16 = a->dtype == C3_BF16, wide = a->dim > 64;
+        if (p.seqs != nullptr && p.rows + p.key_rows > 0) {
+            if (stage_bytes(base + sp.table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess)
                 return C3_E_HIP;
+            p.table.staged = reinterpret_cast<const AttnSeq*>(base + sp.table);
         }
-        if (p.key_rows > 0) {
-            if ((rc = number_units(a, p, base + sp.table_k, true, sp.parts_k, s)) != C3_OK) return rc;
-            if (launch_attn_dkv(p, bf16, s) != hipSuccess) return C3_E_HIP;
-            if (sp.parts_k > 1) {
-                const int64_t n = p.key_rows * g.dim;
-                if (sum_parts(p, bf16, g.part, 2 * n, p.key_rows, g.kv_heads, g.k_tokens, g.dk, g.scale, s) != hipSuccess ||
-                    sum_parts(p, bf16, g.part + n, 2 * n, p.key_rows, g.kv_heads, g.k_tokens, g.dv, 1.0f, s) != hipSuccess)
-                    return C3_E_HIP;
-            }
+        if (p.rows > 0 && launch_attn_dq(p, bf16, s) != hipSuccess) return C3_E_HIP;
+        if (p.key_rows > 0 && launch_attn_dkv(p, bf16, s) != hipSuccess) return C3_E_HIP;
+        if ((g.causal || g.window) && p.rows > 0 && p.key_rows > 0) {
+            const hipError_t e =
+                bf16 ? (wide ? launch_careful<__bf16, 128>(p, s) : launch_careful<__bf16, 64>(p, s))
+                     : (wide ? launch_careful<_Float16, 128>(p, s) : launch_careful<_Float16, 64>(p, s));
+            if (e != hipSuccess) return C3_E_HIP;
         }
+        if (p.rows > 0 && sp.parts[0] > 1 &&
+            sum_parts(p, bf16, g.side[0], 0, 1, g.heads, g.q_tokens, g.dq, g.scale, s) != hipSuccess)
+            return C3_E_HIP;
+        if (p.key_rows > 0 && sp.parts[1] > 1 &&
+            (sum_parts(p, bf16, g.side[1], 0, 2, g.kv_heads, g.k_tokens, g.dk, g.scale, s) != hipSuccess ||
+             sum_parts(p, bf16, g.side[1], 1, 2, g.kv_heads, g.k_tokens, g.dv, 1.0f, s) != hipSuccess))
+            return C3_E_HIP;
         return C3_OK;
     } catch (...) {
         return C3_E_INVAL;
