@@ -415,7 +415,6 @@ struct AttnPlan {
     int64_t rows;               // query rows of all heads: entries of lse
     int64_t key_rows;           // key rows of all key heads
     int64_t max_q, max_k;       // the longest of each
-    int64_t work;               // sum of q_len * k_len
     AttnSeq* seqs;              // heap copy where more than kAttnArgSeqs, else null
     AttnPlan() : args(), table(), seqs(nullptr) {}
     AttnPlan(const AttnPlan&) = delete;

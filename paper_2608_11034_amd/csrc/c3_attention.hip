@@ -211,15 +211,15 @@ __device__ __forceinline__ bool forward_unit(const AttnArgs& a, const AttnTable&
     if (!there) return bad != 0;
     const float mc = m == -__builtin_inff() ? 0.0f : m * cs;
     const int64_t at = seq_row(a, w) + (int64_t)pos * a.heads + head;
+    // a row that saw nothing (l = 0) and one of the padding: zeros and -inf
+    const bool some = valid && l != 0.0f;
     if (a.split_keys) {
-        if (h == 0) write_part_stats(a, at, part, parts, mc, l);
-        if (l != 0.0f)
+        if (h == 0) write_part_stats(a, at, part, parts, mc, some ? l : 0.0f);
+        if (some)
 #pragma unroll
             for (int db = 0; db < NDB; ++db) write_part(a, at, part, db, h, acc[db]);
         return bad != 0;
     }
-    // a row that saw nothing (l = 0) and one of the padding: zeros and -inf
-    const bool some = valid && l != 0.0f;
     const float f = some ? 1.0f / l : 0.0f;
     char* out = seq_base(a.o, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.o.st;
 #pragma unroll
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
     const bool some = valid && total != 0.0f;
     if (there && wave == 0 && h == 0) {
         if (a.split_keys)
-            write_part_stats(a, at, part, parts, mc, total);
+            write_part_stats(a, at, part, parts, mc, some ? total : 0.0f);
         else
             a.lse[at] = some ? (mc + __log2f(total)) * kLn2 : -__builtin_inff();
     }
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
             for (int i = 0; i < 4; ++i) sum[4 * q + i] += x[i];
         }
     if (a.split_keys) {
-        if (total != 0.0f) write_part(a, at, part, wave, h, sum);
+        if (some) write_part(a, at, part, wave, h, sum);
         return;
     }
     char* out = seq_base(a.o, a.packed, w.b, w.q_start, head) + (int64_t)pos * a.o.st;
@@ -581,7 +581,6 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
     p.table.staged = nullptr;
     p.max_q = a->q_tokens;
     p.max_k = a->k_tokens;
-    p.work = a->batch * a->q_tokens * a->k_tokens;
     const int64_t seqs = a->packed ? 1 : a->batch;
     if (seqs > 0 && (a->q_tokens * a->heads >= (1ll << 40) / seqs || a->k_tokens * a->kv_heads >= (1ll << 40) / seqs))
         return C3_E_UNSUPPORTED;
@@ -594,7 +593,7 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
     }
     AttnSeq* s = p.list();
     int64_t nq = 0, nk = 0;
-    p.max_q = p.max_k = p.work = 0;
+    p.max_q = p.max_k = 0;
     for (int i = 0; i < a->batch; ++i) {
         const int64_t q = a->q_lens[i], k = a->k_lens[i];
         if (q < 0 || k < 0 || (!a->packed && (q > a->q_tokens || k > a->k_tokens))) return C3_E_INVAL;
@@ -604,7 +603,6 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
         nk += k;
         p.max_q = std::max(p.max_q, q);
         p.max_k = std::max(p.max_k, k);
-        p.work += q * k;
     }
     if (a->packed && (nq != a->q_tokens || nk != a->k_tokens)) return C3_E_INVAL;
     // the longest walks first, so that short ones fill the end

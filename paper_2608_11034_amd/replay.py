@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 from typing import NamedTuple
 
 import torch
@@ -111,8 +112,24 @@ def _overlap(t):
     return any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride()))
 
 
-def _new_like(x):
-    return _empty(x.shape, x.dtype, x.device)
+def _new(shape, dtype, device, stream):
+    """Memory of the stream that the call runs on: memory of another one could still be in
+    use there, or be given out again before the call has ended."""
+    if stream is None:
+        return _empty(shape, dtype, device)
+    with torch.cuda.stream(stream):
+        return _empty(shape, dtype, device)
+
+
+def _int32(x, name):
+    """A whole number that fits the call's field, which would cut it off without a word."""
+    try:
+        x = operator.index(x)
+    except TypeError:
+        raise C3Error(f"{name} must be a whole number") from None
+    if not 0 <= x < 2 ** 31:
+        raise C3Error(f"{name} must be in [0, 2^31)")
+    return x
 
 
 # ---------------------------------------------------------------------------
@@ -176,7 +193,7 @@ def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
     first = xs[0]
     B, S = (first.shape[0], first.shape[1]) if first.dim() == 4 else (1, first.shape[0])
     D, dev = first.shape[-1], first.device
-    outs = [_new_like(t) for t in xs] if out is None else [out] if single else list(out)
+    outs = [_new(t.shape, t.dtype, dev, stream) for t in xs] if out is None else [out] if single else list(out)
     if len(outs) != len(xs):
         raise C3Error("out must have one tensor for each of x")
     for t, y in zip(xs, outs):
@@ -240,32 +257,30 @@ def _attention_args(q, k, v, causal, window, scale, q_lens, k_lens):
     if q_lens is not None:
         if len(q_lens) != batch or len(k_lens) != batch:
             raise C3Error("q_lens and k_lens need one length for each sequence")
-        try:
-            keep = tuple((ctypes.c_int32 * max(batch, 1))(*x) for x in (q_lens, k_lens))
-        except TypeError:
-            raise C3Error("q_lens and k_lens must be whole numbers on the host") from None
+        keep = tuple((ctypes.c_int32 * max(batch, 1))(*[_int32(n, "a length") for n in x])
+                     for x in (q_lens, k_lens))
         a.q_lens, a.k_lens = (ctypes.cast(x, ctypes.c_void_p) for x in keep)
     a.dtype, a.heads, a.kv_heads, a.dim = _CODE[q.dtype], q.shape[-2], k.shape[-2], q.shape[-1]
-    a.causal, a.window, a.batch, a.packed = int(bool(causal)), int(window), batch, int(packed)
+    a.causal, a.window, a.batch, a.packed = int(bool(causal)), _int32(window, "window"), batch, int(packed)
     a.scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
     a.q_tokens, a.k_tokens = (q.shape[0], k.shape[0]) if packed else (q.shape[1], k.shape[1])
     return a, keep
 
 
-def _attn_out(t, like, name):
+def _attn_out(t, like, name, stream):
     if t is None:
-        return _new_like(like)
+        return _new(like.shape, like.dtype, like.device, stream)
     _rows(t, name, like.dtype, like.device)
     if t.shape != like.shape or _overlap(t):
         raise C3Error(f"{name} must have the shape {tuple(like.shape)} and no repeated elements")
     return t
 
 
-def _workspace(need, workspace, device, what):
+def _workspace(need, workspace, device, what, stream):
     if need == 0:
         raise C3Error(f"invalid {what} sizes")
     if workspace is None:
-        return _empty((need,), torch.uint8, device)
+        return _new((need,), torch.uint8, device, stream)
     _dev_tensor(workspace, "workspace")
     if workspace.numel() * workspace.element_size() < need:
         raise C3Error(f"{what} workspace too small")
@@ -291,10 +306,10 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: float = 
     each query that many keys.  ``scale`` defaults to D ** -0.5.  lse is fp32
     [.., H]; a row that sees no key has out 0 and lse -inf."""
     a, keep = _attention_args(q, k, v, causal, window, scale, q_lens, k_lens)
-    out = _attn_out(out, q, "out")
-    lse = _empty(q.shape[:-1], torch.float32, q.device) if lse is None else _lse(lse, q)
+    out = _attn_out(out, q, "out", stream)
+    lse = _new(q.shape[:-1], torch.float32, q.device, stream) if lse is None else _lse(lse, q)
     ws = _workspace(_lib().c3_attention_workspace_size(ctypes.byref(a)), workspace, q.device,
-                    "attention")
+                    "attention", stream)
     t = [_attn_tensor(x) for x in (q, k, v, out)]
     rc = _lib().c3_attention(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse), _ptr(ws),
                              ws.numel() * ws.element_size(), _stream(stream))
@@ -313,9 +328,9 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
         if t.shape != q.shape:
             raise C3Error(f"{n} must have the shape of q")
     _lse(lse, q)
-    dq, dk, dv = _attn_out(dq, q, "dq"), _attn_out(dk, k, "dk"), _attn_out(dv, v, "dv")
+    dq, dk, dv = (_attn_out(t, x, n, stream) for t, x, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
     ws = _workspace(_lib().c3_attention_grad_workspace_size(ctypes.byref(a)), workspace, q.device,
-                    "attention_grad")
+                    "attention_grad", stream)
     t = [_attn_tensor(x) for x in (dout, q, k, v, out)]
     d = [_attn_tensor(x) for x in (dq, dk, dv)]
     rc = _lib().c3_attention_grad(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse),
@@ -346,12 +361,15 @@ def expert_sort(ids: torch.Tensor, num_experts: int, *, workspace=None, stream=N
         raise C3Error("ids must be int32 [tokens, top]")
     if not 1 <= ids.shape[1] <= MAX_TOP:
         raise C3Error(f"1 to {MAX_TOP} choices a token")
+    num_experts = _int32(num_experts, "num_experts")
+    if not 1 <= num_experts <= MAX_EXPERTS:
+        raise C3Error(f"1 to {MAX_EXPERTS} experts")
     dev, n = ids.device, ids.numel()
-    order = ExpertOrder(_empty((max(int(num_experts), 0) + 1,), torch.int32, dev),
-                        _empty((n,), torch.int32, dev), _empty(ids.shape, torch.int32, dev))
-    ws = _workspace(_lib().c3_expert_sort_workspace_size(n, int(num_experts)), workspace, dev,
-                    "expert_sort")
-    rc = _lib().c3_expert_sort(_ptr(ids), n, int(num_experts), _ptr(order.offsets), _ptr(order.source),
+    order = ExpertOrder(_new((num_experts + 1,), torch.int32, dev, stream),
+                        _new((n,), torch.int32, dev, stream), _new(ids.shape, torch.int32, dev, stream))
+    ws = _workspace(_lib().c3_expert_sort_workspace_size(n, num_experts), workspace, dev,
+                    "expert_sort", stream)
+    rc = _lib().c3_expert_sort(_ptr(ids), n, num_experts, _ptr(order.offsets), _ptr(order.source),
                                _ptr(order.slot), _ptr(ws), ws.numel() * ws.element_size(),
                                _stream(stream))
     _check(rc, "c3_expert_sort")
@@ -382,9 +400,9 @@ def _expert_rows(order, token_rows, sorted_rows, dtype):
     return r
 
 
-def _expert_out(t, shape, like):
+def _expert_out(t, shape, like, stream):
     if t is None:
-        return _empty(shape, like.dtype, like.device)
+        return _new(shape, like.dtype, like.device, stream)
     _rows(t, "out", like.dtype, like.device)
     if tuple(t.shape) != tuple(shape) or _overlap(t):
         raise C3Error(f"out must be {tuple(shape)} without repeated elements")
@@ -395,8 +413,9 @@ def _weights(weights, order):
     if weights is None:
         return None
     _dev_tensor(weights, "weights")
-    if weights.dtype != torch.float32 or weights.shape != order.slot.shape:
-        raise C3Error("weights must be fp32 [tokens, top]")
+    if weights.dtype != torch.float32 or (
+            weights.shape != order.slot.shape or weights.device != order.slot.device):
+        raise C3Error("weights must be fp32 [tokens, top] on the order's device")
     return weights
 
 
@@ -404,7 +423,7 @@ def expert_dispatch(x, order: ExpertOrder, *, out=None, stream=None):
     """Rows [T * top, hidden] sorted by expert from tokens x [T, hidden]; the
     rows behind the last kept choice are zeros."""
     _rows(x, "x", dim=(2,))
-    out = _expert_out(out, (order.slot.numel(), x.shape[1]), x)
+    out = _expert_out(out, (order.slot.numel(), x.shape[1]), x, stream)
     r = _expert_rows(order, x, out, x.dtype)
     _check(_lib().c3_expert_dispatch(ctypes.byref(r), _ptr(x), _ptr(out), _stream(stream)),
            "c3_expert_dispatch")
@@ -415,7 +434,7 @@ def expert_combine(y, order: ExpertOrder, weights=None, *, out=None, stream=None
     """out[t] = sum over t's choices of weight * y[their place]; y [T * top,
     hidden], weights fp32 [T, top] or None (ones)."""
     _rows(y, "y", dim=(2,))
-    out = _expert_out(out, (order.slot.shape[0], y.shape[1]), y)
+    out = _expert_out(out, (order.slot.shape[0], y.shape[1]), y, stream)
     weights = _weights(weights, order)
     r = _expert_rows(order, out, y, y.dtype)
     _check(_lib().c3_expert_combine(ctypes.byref(r), _ptr(y), _ptr(weights), _ptr(out),
@@ -428,7 +447,7 @@ def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, s
     without weights dweights is None (and y may be)."""
     _rows(dout, "dout", dim=(2,))
     weights = _weights(weights, order)
-    dy = _expert_out(dy, (order.slot.numel(), dout.shape[1]), dout)
+    dy = _expert_out(dy, (order.slot.numel(), dout.shape[1]), dout, stream)
     r = _expert_rows(order, dout, dy, dout.dtype)
     dw = None
     if weights is not None:
@@ -437,7 +456,7 @@ def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, s
             raise C3Error(f"y must be {tuple(dy.shape)}")
         if y.shape[0] > 1 and y.stride(0) != r.sorted_stride:
             raise C3Error("y and dy must have the same row stride")
-        dw = _empty(order.slot.shape, torch.float32, dout.device)
+        dw = _new(order.slot.shape, torch.float32, dout.device, stream)
     _check(_lib().c3_expert_combine_grad(ctypes.byref(r), _ptr(dout), _ptr(y if dw is not None else None),
                                          _ptr(weights), _ptr(dy), _ptr(dw), _stream(stream)),
            "c3_expert_combine_grad")

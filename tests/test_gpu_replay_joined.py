@@ -1,0 +1,87 @@
+"""Attention walks that are divided among workgroups, in padded batches, and the
+memory and arguments of calls on another stream, against the plain 64-bit forms
+(replay_plain)."""
+import math
+
+import pytest
+import torch
+
+import replay_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+replay = pytest.importorskip("paper_2608_11034_amd.replay")
+DEV = "cuda"
+BF = torch.bfloat16
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("S,M,H,Hk,D,q_lens,k_lens", [
+    (4, 4099, 8, 2, 128, [4, 2, 0], [4099, 900, 700]),        # 16 rows of a key head
+    (7, 2500, 4, 4, 64, [1, 7, 3], [2500, 2500, 5]),
+    (200, 4096, 8, 2, 128, [200, 50, 0], [4096, 3000, 100]),  # tiles of 128 rows, cut by the padding
+    (300, 3001, 2, 2, 64, [299, 1, 130], [3001, 2900, 0]),
+])
+def test_divided_walks_and_padding(S, M, H, Hk, D, q_lens, k_lens, causal):
+    """Padding that shares a tile with queries comes back as zeros and -inf also
+    where the walk over the keys is divided; what it holds does not matter."""
+    print("CASE", S, M, H, Hk, D, causal, flush=True)
+    B = len(q_lens)
+    gen = torch.Generator().manual_seed(31)
+    q, g = (torch.full((B, S, H, D), math.nan, dtype=BF) for _ in range(2))
+    k, v = (torch.full((B, M, Hk, D), math.nan, dtype=BF) for _ in range(2))
+    for b in range(B):
+        for t, n in ((q, q_lens), (g, q_lens), (k, k_lens), (v, k_lens)):
+            t[b, :n[b]] = torch.randn(t[b, :n[b]].shape, generator=gen).to(BF)
+    Q, K, V, Gd = (x.to(DEV) for x in (q, k, v, g))
+    how = dict(causal=causal, q_lens=q_lens, k_lens=k_lens)
+    out, lse = replay.attention(Q, K, V, **how)
+    dq, dk, dv = replay.attention_grad(Gd, Q, K, V, out, lse, **how)
+    torch.cuda.synchronize()
+
+    def packed(t, n):
+        return torch.cat([t[b, :n[b]] for b in range(B)]).cpu()
+    want = plain.attention(packed(q, q_lens), packed(k, k_lens), packed(v, k_lens), q_lens, k_lens, causal, 0,
+                           D ** -0.5, packed(g, q_lens), BF)
+    for n, t, lens in (("out", out, q_lens), ("lse", lse, q_lens), ("dq", dq, q_lens), ("dk", dk, k_lens),
+                       ("dv", dv, k_lens)):
+        plain.within(packed(t, lens), want[n], want[n + "_bound"], n)
+    for b in range(B):
+        for t, n in ((out, q_lens), (dq, q_lens), (dk, k_lens), (dv, k_lens)):
+            assert not bool(t[b, n[b]:].any())
+        assert bool((lse[b, q_lens[b]:] == -math.inf).all())
+
+
+def test_memory_comes_from_the_stream_of_the_call():
+    """Results and workspaces that a call on another stream makes belong to that
+    stream: memory freed there is not given to the current one."""
+    gen = torch.Generator().manual_seed(32)
+    q = torch.randn((64, 2, 64), generator=gen).to(BF).to(DEV)
+    want = replay.attention(q, q, q, causal=True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out, lse = replay.attention(q, q, q, causal=True, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    at = out.data_ptr()
+    del out, lse
+    here = [torch.empty_like(q) for _ in range(64)]
+    assert at not in [t.data_ptr() for t in here]
+
+
+def test_argument_ranges():
+    """Numbers that the call's 32-bit fields cannot hold are refused, not cut off."""
+    q = torch.zeros((8, 2, 64), dtype=BF, device=DEV)
+    bad = pytest.raises(replay.C3Error)
+    for window in (2 ** 32, 2 ** 32 + 5, 2.5, "1", None):
+        with bad:
+            replay.attention(q, q, q, causal=True, window=window)
+    for lens in ([2 ** 32 + 8], [8.0], [-(2 ** 32) + 8], ["8"]):
+        with bad:
+            replay.attention(q, q, q, q_lens=lens, k_lens=[8])
+        with bad:
+            replay.attention(q, q, q, q_lens=[8], k_lens=lens)
+    ids = torch.zeros((4, 2), dtype=torch.int32, device=DEV)
+    for n in (2 ** 32 + 4, 0, -1, replay.MAX_EXPERTS + 1, 4.0, "4"):
+        with bad:
+            replay.expert_sort(ids, n)
