@@ -75,7 +75,7 @@ typedef struct {
     int32_t dim;            /* multiple of 8, at most 128                      */
     int32_t causal;         /* query i sees key j only if j <= i + k_len - q_len*/
     int32_t window;         /* > 0: also j > i + k_len - q_len - window        */
-    float scale;            /* factor of q . k, finite                         */
+    float scale;            /* factor of q . k, positive and finite            */
     int32_t batch;          /* sequences                                       */
     int64_t q_tokens;       /* per sequence, or of all where packed            */
     int64_t k_tokens;
@@ -167,7 +167,8 @@ int c3_expert_sort(const int32_t *ids, int64_t choices, int experts, int32_t *of
  * elements, `top` choices a token, slot [tokens][top] and `kept` (device, one
  * i32, offsets + experts) as c3_expert_sort wrote them.  Token-side rows are
  * token_stride elements apart, the tokens * top sorted rows sorted_stride.
- * Rows from *kept on hold no token: they are written as zeros and never read. */
+ * Rows from *kept on hold no token: they are written as zeros, and what they
+ * hold enters no result. */
 typedef struct {
     int32_t dtype;
     int32_t top;            /* 1..C3_MAX_EXPERT_TOP */

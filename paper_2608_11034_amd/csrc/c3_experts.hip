@@ -71,10 +71,17 @@ __global__ __launch_bounds__(kSortThreads) void expert_place_kernel(
     int32_t total = 0, before = 0;
     if (tid < experts) {
         if (gridDim.x > 1) {
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const int32_t c = counts[(int64_t)b * experts + tid];
-                if (b < (int)blockIdx.x) before += c;
-                total += c;
+            // sixteen counts in flight: one after the other their latencies add up
+            const int runs = gridDim.x;
+            for (int b = 0; b < runs; b += 16) {
+                int32_t c[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) c[j] = counts[(int64_t)min(b + j, runs - 1) * experts + tid];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    before += b + j < (int)blockIdx.x ? c[j] : 0;
+                    total += b + j < runs ? c[j] : 0;
+                }
             }
         } else {
             for (int w = 0; w < kSortWaves; ++w) total += lds[w * experts + tid];
@@ -201,20 +208,21 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowArgs a, const T*
     float my_weight = 1.0f;
     if (a.weights != nullptr && lane < a.top) my_weight = a.weights[token * a.top + lane];
     float acc[U][V] = {};
+    // Pieces behind the row's end are the last one again, and a choice without a row
+    // takes row 0: the loads stand without a branch between them, four rows at a time.
+    int64_t at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) at[u] = min(c0 + u * 64, a.pieces - 1) * V;
     for (int k0 = 0; k0 < a.top; k0 += 4) {
-        // four rows in flight; a dropped choice or one past the last adds nothing
-        Piece<T, V> p[4][U] = {};
+        Piece<T, V> p[4][U];
         bool there[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int32_t s = k0 + q < a.top ? __builtin_amdgcn_readlane(my_slot, (k0 + q) & 63) : -1;
             there[q] = (uint32_t)s < rows;
-            if (!there[q]) continue;
-            const T* row = sorted + (int64_t)s * a.sorted_stride;
+            const T* row = sorted + (there[q] ? (int64_t)s : 0) * a.sorted_stride;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c0 + u * 64 < a.pieces)
-                    p[q][u] = *reinterpret_cast<const Piece<T, V>*>(row + (c0 + u * 64) * V);
+            for (int u = 0; u < U; ++u) p[q][u] = *reinterpret_cast<const Piece<T, V>*>(row + at[u]);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
