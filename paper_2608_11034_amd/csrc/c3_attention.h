@@ -64,8 +64,7 @@ struct AttnTensor {
 
 // How one pass divides its work.
 struct AttnSide {
-    FastDiv units;          // units of one key head, all sequences
-    FastDiv seq_units;      // of one sequence, where the table has none
+    uint32_t units;         // units of one key head, all sequences
     FastDiv splits;         // parts of one unit's walk (the forward: at most)
     uint32_t* marks;        // per workgroup: repeat it with care
     float* part;            // results of the parts
@@ -79,6 +78,7 @@ struct AttnArgs {
     float* delta;           // per row: the sum of dout * out
     float* part_ml;         // maxima (scaled, in powers of two) and sums of parts of the forward
     FastDiv group;          // query heads of a key head
+    FastDiv kv, batch;      // key heads and sequences
     AttnSide side[2];       // units that are tiles of rows, and blocks of keys
     int32_t heads, kv_heads, dim, causal, window, packed;
     int32_t q_tokens, k_tokens;
@@ -92,22 +92,20 @@ struct AttnUnit {
     uint32_t unit;
 };
 
-// Workgroups of one key head follow each other on one of the eight dies (which
-// take workgroups in turn), so that its keys and values are shared in the die's L2.
-__device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n) {
-    const uint32_t die = id & 7, each = n >> 3, rest = n & 7;
-    return die * each + min(die, rest) + (id >> 3);
-}
-
+// Key heads and sequences run fastest, units slowest.  Units are numbered from the
+// longest walk under a causal mask, so that the short ones fill the end; and workgroups
+// go to the eight dies in turn, so that where heads times sequences are a multiple of
+// eight (or divide it) a die meets the keys of an eighth of them only and shares them in
+// its L2.  With a head's units in one run on a die instead, 16,384 causal tokens of 2 key
+// heads gave one die 1.75 times its share.
 __device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& a, const AttnTable& tab, int side,
                                               uint32_t block) {
     AttnUnit w;
-    const AttnSide& d = a.side[side];
-    w.hk = (int32_t)d.units.quot(block);
-    const uint32_t u = block - (uint32_t)w.hk * d.units.d;
+    const uint32_t u = a.kv.quot(block);
+    w.hk = (int32_t)(block - u * a.kv.d);
     if (tab.n == 0) {
-        w.b = (int32_t)d.seq_units.quot(u);
-        w.unit = u - (uint32_t)w.b * d.seq_units.d;
+        w.unit = a.batch.quot(u);
+        w.b = (int32_t)(u - w.unit * a.batch.d);
         w.q_start = w.k_start = 0;
         w.q_len = a.q_tokens;
         w.k_len = a.k_tokens;
@@ -230,30 +228,42 @@ struct TileReads {
 };
 
 // The second layout: for each 32 rows and inner step ks 1 KiB with 32 bytes of
-// every row.  Every read then is one of two lane offsets plus a constant, without
-// bank conflicts and without a register for each; the loads that fill it take 32
-// bytes of a row at a time, half of what a compute unit's vector cache could
-// deliver.
+// every row.  Every read then is one of a few lane offsets plus a constant, without a
+// register for each; the loads that fill it take 32 bytes of a row at a time, half of
+// what a compute unit's vector cache could deliver.  Plainly laid out, every read
+// would meet its banks twice (half of the reads' cycles in the gradient's second
+// pass): so the two pieces of rows 8 .. 15 and 24 .. 31 change places, which parts 16
+// rows' reads of one piece, and rows r of odd steps stand at r ^ 4, which parts the
+// two steps that a read across rows takes together.
 template <int DP>
 struct StepReads {
-    int row, col;
+    int row[2], col[2];
     __device__ __forceinline__ StepReads() {
         const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
-        row = c * 32 + h * 16;
-        col = g * 1024 + (h * 4 + (i >> 2)) * 32 + (i & 3) * 8;
+        row[0] = piece(c, 0, h);
+        row[1] = piece(c, 1, h);
+        col[0] = g * 1024 + piece(h * 4 + (i >> 2), g, (i & 3) >> 1) + (i & 1) * 8;
+        col[1] = g * 1024 + piece(h * 4 + (i >> 2) + 8, g, (i & 3) >> 1) + (i & 1) * 8;
     }
+    // Where a row's piece stands in a step's 1 KiB.
+    static __device__ __forceinline__ int piece(int row, int ks, int half) {
+        return (row ^ ((ks & 1) << 2)) * 32 + ((half ^ ((row >> 3) & 1)) << 4);
+    }
+    // The row and the half that a lane loads of a step.
+    static __device__ __forceinline__ int load_row(int lane, int ks) { return (lane >> 1) ^ ((ks & 1) << 2); }
+    static __device__ __forceinline__ int load_half(int lane) { return (lane & 1) ^ ((lane >> 4) & 1); }
     // Rows 0..31 of the 32 rows at `sub`, inner step ks, as the A or B operand.
     __device__ __forceinline__ u32x4 along(const char* sub, int ks) const {
-        return *reinterpret_cast<const u32x4*>(sub + row + ks * 1024);
+        return *reinterpret_cast<const u32x4*>(sub + row[ks & 1] + ks * 1024);
     }
     // Elements d .. d + 3 of a row.
     __device__ __forceinline__ const char* four(const char* sub, int r, int d) const {
-        return sub + (d >> 4) * 1024 + r * 32 + (d & 15) * 2;
+        return sub + (d >> 4) * 1024 + piece(r, d >> 4, (d >> 3) & 1) + (d & 7) * 2;
     }
     // Columns 32 db .. of rows 16 j .. 16 j + 15, as the A operand over them.
     __device__ __forceinline__ u32x4 across(const char* sub, int j, int db) const {
-        const char* p = sub + col + db * 2048 + j * 512;
-        const u32x2 lo = read_tr(p), hi = read_tr(p + 256);
+        const char* p = sub + db * 2048 + j * 512;
+        const u32x2 lo = read_tr(p + col[0]), hi = read_tr(p + col[1]);
         return u32x4{lo.x, lo.y, hi.x, hi.y};
     }
 };
@@ -366,7 +376,7 @@ __device__ __forceinline__ void repeat_marked(const uint32_t* marks, uint32_t bl
         __syncthreads();
         for (int i = 0; i < kAttnThreads; ++i) {
             if (set[i] == 0) continue;
-            unit(die_order(first + i * groups + group, blocks));
+            unit(first + i * groups + group);
             __syncthreads();
         }
     }
@@ -433,7 +443,6 @@ int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
     int64_t n = 0;
     if (p.table.n == 0) {
         const int64_t u = units_of(p.args.q_tokens, p.args.k_tokens, p.args.k_tokens);
-        d.seq_units = FastDiv((uint32_t)(u < 1 ? 1 : u));
         n = u * batch;
     } else {
         AttnSeq* s = p.list();
@@ -445,7 +454,7 @@ int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
         }
     }
     if (n * p.args.kv_heads >= (1ll << 31)) return -1;
-    d.units = FastDiv((uint32_t)(n < 1 ? 1 : n));
+    d.units = (uint32_t)(n < 1 ? 1 : n);
     return n;
 }
 size_t attn_table_bytes(const c3_attention_t* a);

@@ -230,7 +230,7 @@ __device__ __forceinline__ bool forward_unit(const AttnArgs& a, const AttnTable&
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(AttnArgs a, AttnTable tab) {
-    const bool bad = forward_unit<T, DP, false>(a, tab, die_order(blockIdx.x, gridDim.x));
+    const bool bad = forward_unit<T, DP, false>(a, tab, blockIdx.x);
     if (a.causal || a.window) {
         const int any = __syncthreads_or(bad);
         if (threadIdx.x == 0) a.side[0].marks[blockIdx.x] = any;
@@ -490,7 +490,7 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
 
 template <typename T, int DP>
 hipError_t launch_forward(const AttnPlan& p, bool tokens, hipStream_t s) {
-    const dim3 grid(p.args.side[0].units.d * (uint32_t)p.args.kv_heads), block(kAttnThreads);
+    const dim3 grid(p.args.side[0].units * (uint32_t)p.args.kv_heads), block(kAttnThreads);
     if (tokens)
         attn_tokens_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
     else
@@ -577,6 +577,8 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
     g.k_tokens = (int32_t)a->k_tokens;
     g.scale = a->scale;
     g.group = FastDiv((uint32_t)(a->heads / a->kv_heads));
+    g.kv = FastDiv((uint32_t)a->kv_heads);
+    g.batch = FastDiv((uint32_t)std::max(a->batch, 1));
     p.table.n = 0;
     p.table.staged = nullptr;
     p.max_q = a->q_tokens;

@@ -20,7 +20,8 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     // workgroups fit a compute unit's registers (256 a lane) and LDS (160 KiB).
     constexpr bool kValuesLds = DP > 64;
     constexpr int kTileRows = kValuesLds ? 32 : 64;
-    constexpr int kTileBytes = kTileRows * DP * 2, kSteps = kTileRows / 32 * KS / kAttnWaves;
+    constexpr int kTileBytes = kTileRows * DP * 2, kSteps = 2;
+    static_assert(kTileRows / 32 * KS == kSteps * kAttnWaves, "two steps of a tile to each wave");
     __shared__ __attribute__((aligned(1024))) char q0[kTileBytes];
     __shared__ __attribute__((aligned(1024))) char g0[kTileBytes];
     __shared__ __attribute__((aligned(1024))) float s0[2 * 64];      // lse2, delta: 64 lanes' words each
@@ -71,18 +72,18 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
         const char* gr = gb + (int64_t)p0 * a.d_o.st;
         const uint32_t q_bytes = (uint32_t)(p1 * a.q.st + (G - 1) * a.q.sh) + a.dim * 2;
         const uint32_t g_bytes = (uint32_t)(p1 * a.d_o.st + (G - 1) * a.d_o.sh) + a.dim * 2;
-        // the wave's steps lie in one of the tile's 32 rows; a lane takes half a row's
-        // 32 bytes of each
-        const int first = wave * kSteps, i = first / KS * 32 + (lane >> 1);
+        // the wave's steps, all odd or all even, lie in one of the tile's 32 rows; a lane
+        // takes half a row's 32 bytes of each
+        const int first = wave / 2 * 4 + (wave & 1), i = first / KS * 32 + rd.load_row(lane, first);
         const int r = row0 + i, p = (int)a.group.quot(r), g = r - p * G;
         const uint32_t qo = (uint32_t)((p - p0) * (int)a.q.st + g * (int)a.q.sh);
         const uint32_t go = (uint32_t)((p - p0) * (int)a.d_o.st + g * (int)a.d_o.sh);
 #pragma unroll
         for (int n = 0; n < kSteps; ++n) {
-            const int piece = 2 * ((first + n) % KS) + (lane & 1);
+            const int at = first + 2 * n, piece = 2 * (at % KS) + rd.load_half(lane);
             const bool ok = i < rows && piece * 8 < a.dim;
-            load_piece_lds(qr, q_bytes, ok ? qo + piece * 16 : 0xFFFFFF00u, qt + (first + n) * 1024);
-            load_piece_lds(gr, g_bytes, ok ? go + piece * 16 : 0xFFFFFF00u, gt + (first + n) * 1024);
+            load_piece_lds(qr, q_bytes, ok ? qo + piece * 16 : 0xFFFFFF00u, qt + at * 1024);
+            load_piece_lds(gr, g_bytes, ok ? go + piece * 16 : 0xFFFFFF00u, gt + at * 1024);
         }
         if (wave < 2) {         // a lane for each row: lse2 by the first wave, delta by the second
             const float* from = (wave == 0 ? a.lse2 : a.delta) + stat_row + (int64_t)p0 * a.heads;
@@ -110,7 +111,7 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
             const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * a.v.st) + a.dim * 2 : 0;
 #pragma unroll
             for (int n = 0; n < NT * KS; ++n) {
-                const int i = n / KS * 32 + (lane >> 1), piece = 2 * (n % KS) + (lane & 1);
+                const int i = n / KS * 32 + rd.load_row(lane, n), piece = 2 * (n % KS) + rd.load_half(lane);
                 const bool ok = i < rows && piece * 8 < a.dim;
                 load_piece_lds(vb + (int64_t)wkey * a.v.st, bytes,
                                ok ? (uint32_t)(i * (int)a.v.st + piece * 16) : 0xFFFFFF00u,

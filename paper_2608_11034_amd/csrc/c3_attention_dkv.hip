@@ -6,7 +6,7 @@ namespace {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, AttnTable tab) {
-    const bool bad = dkv_unit<T, DP, kDkvTiles, false>(a, tab, die_order(blockIdx.x, gridDim.x));
+    const bool bad = dkv_unit<T, DP, kDkvTiles, false>(a, tab, blockIdx.x);
     if (a.causal || a.window) {
         const int any = __syncthreads_or(bad);
         if (threadIdx.x == 0) a.side[1].marks[blockIdx.x] = any;
@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, A
 
 template <typename T, int DP>
 hipError_t launch(const AttnPlan& p, hipStream_t s) {
-    const uint32_t blocks = p.args.side[1].units.d * (uint32_t)p.args.kv_heads;
+    const uint32_t blocks = p.args.side[1].units * (uint32_t)p.args.kv_heads;
     attn_dkv_kernel<T, DP><<<dim3(blocks), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
     return hipGetLastError();
 }

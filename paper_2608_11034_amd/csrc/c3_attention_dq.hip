@@ -6,7 +6,7 @@ namespace {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, AttnTable tab) {
-    const bool bad = dq_unit<T, DP, false>(a, tab, die_order(blockIdx.x, gridDim.x));
+    const bool bad = dq_unit<T, DP, false>(a, tab, blockIdx.x);
     if (a.causal || a.window) {
         const int any = __syncthreads_or(bad);
         if (threadIdx.x == 0) a.side[0].marks[blockIdx.x] = any;
@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
 
 template <typename T, int DP>
 hipError_t launch(const AttnPlan& p, hipStream_t s) {
-    attn_dq_kernel<T, DP><<<dim3(p.args.side[0].units.d * p.args.kv_heads), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
+    attn_dq_kernel<T, DP><<<dim3(p.args.side[0].units * p.args.kv_heads), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
     return hipGetLastError();
 }
 
