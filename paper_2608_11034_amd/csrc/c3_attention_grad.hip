@@ -13,45 +13,71 @@
 namespace c3 {
 namespace {
 
-// out = factor * the sum of the parts, in their order.  A thread takes four elements
-// of a row; `rows` rows [tokens][heads] of `dim`.
+// One gradient's parts: out = factor * their sum, in their order.
+struct PartSum {
+    const float* part;      // `rows` rows [tokens][heads] of `dim` each
+    int64_t stride;         // elements from one part to the next
+    int64_t rows;
+    FastDiv heads, tokens;
+    AttnTensor out;
+    int32_t parts;
+    float factor;
+};
+struct PartSums {
+    PartSum of[3];
+};
+
+// All the divided gradients in one launch (blockIdx.y); a thread takes four elements
+// of a row.
 template <typename T>
-__global__ __launch_bounds__(256) void attn_sum_parts_kernel(const float* part, int64_t stride, int parts,
-                                                             int64_t rows, FastDiv quads, FastDiv heads,
-                                                             FastDiv tokens, AttnTensor out, float factor) {
+__global__ __launch_bounds__(256) void attn_sum_parts_kernel(PartSums sums, FastDiv quads) {
+    const PartSum& j = sums.of[blockIdx.y];
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * quads.d) return;
+    if (i >= j.rows * quads.d) return;
     const int64_t row = i / quads.d;
     const int d = (int)(i - row * quads.d) * 4;
-    const float* from = part + row * quads.d * 4 + d;
+    const float* from = j.part + row * quads.d * 4 + d;
     f32x4 sum = *reinterpret_cast<const f32x4*>(from);
 #pragma unroll 4
-    for (int p = 1; p < parts; ++p) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(from + p * stride);
+    for (int p = 1; p < j.parts; ++p) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(from + p * j.stride);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] += x[j];
+        for (int n = 0; n < 4; ++n) sum[n] += x[n];
     }
-    const int64_t token = row / heads.d, b = token / tokens.d;
-    const int head = (int)(row - token * heads.d);
+    const int64_t token = row / j.heads.d, b = token / j.tokens.d;
+    const int head = (int)(row - token * j.heads.d);
     T e[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = (T)(sum[j] * factor);
+    for (int n = 0; n < 4; ++n) e[n] = (T)(sum[n] * j.factor);
     u32x2 x;
     __builtin_memcpy(&x, e, 8);
-    *reinterpret_cast<u32x2*>(out.ptr + b * out.sb + (token - b * tokens.d) * out.st + head * out.sh + d * 2) = x;
+    *reinterpret_cast<u32x2*>(j.out.ptr + b * j.out.sb + (token - b * j.tokens.d) * j.out.st + head * j.out.sh +
+                              d * 2) = x;
 }
 
-hipError_t sum_parts(const AttnPlan& p, bool bf16, const AttnSide& side, int which, int of, int heads,
-                     int64_t tokens, const AttnTensor& out, float factor, hipStream_t s) {
-    const FastDiv quads((uint32_t)p.args.dim / 4), h((uint32_t)heads), t((uint32_t)tokens);
-    const int64_t blocks = (side.part_rows * quads.d + 255) / 256, n = side.part_rows * p.args.dim;
-    const dim3 grid((unsigned)blocks), block(256);
+hipError_t sum_parts(const AttnPlan& p, bool bf16, hipStream_t s) {
+    const AttnArgs& g = p.args;
+    PartSums sums{};
+    int n = 0;
+    int64_t most = 0;
+    auto add = [&](const AttnSide& side, int which, int of, int heads, int64_t tokens, const AttnTensor& out,
+                   float factor) {
+        if (side.splits.d < 2 || side.part_rows == 0) return;
+        const int64_t size = side.part_rows * g.dim;
+        sums.of[n++] = PartSum{side.part + which * size, of * size, side.part_rows, FastDiv((uint32_t)heads),
+                               FastDiv((uint32_t)tokens), out, (int32_t)side.splits.d, factor};
+        most = std::max(most, side.part_rows);
+    };
+    add(g.side[0], 0, 1, g.heads, g.q_tokens, g.dq, g.scale);
+    add(g.side[1], 0, 2, g.kv_heads, g.k_tokens, g.dk, g.scale);
+    add(g.side[1], 1, 2, g.kv_heads, g.k_tokens, g.dv, 1.0f);
+    if (n == 0) return hipSuccess;
+    const FastDiv quads((uint32_t)g.dim / 4);
+    const dim3 grid((unsigned)((most * quads.d + 255) / 256), (unsigned)n), block(256);
     if (bf16)
-        attn_sum_parts_kernel<__bf16><<<grid, block, 0, s>>>(side.part + which * n, of * n, (int)side.splits.d,
-                                                              side.part_rows, quads, h, t, out, factor);
+        attn_sum_parts_kernel<__bf16><<<grid, block, 0, s>>>(sums, quads);
     else
-        attn_sum_parts_kernel<_Float16><<<grid, block, 0, s>>>(side.part + which * n, of * n, (int)side.splits.d,
-                                                                side.part_rows, quads, h, t, out, factor);
+        attn_sum_parts_kernel<_Float16><<<grid, block, 0, s>>>(sums, quads);
     return hipGetLastError();
 }
 
@@ -80,7 +106,7 @@ hipError_t launch_careful(const AttnPlan& p, hipStream_t s) {
 // Parts of a walk.  A pass whose tiles give fewer than `want` workgroups divides
 // each tile's walk, of `steps` tiles on the other side at most, into parts of at
 // least kPartSteps, whose fp32 sums a further kernel adds up in order.
-constexpr int64_t kPartSteps = 4, kMostParts = 16;
+constexpr int64_t kPartSteps = 2, kMostParts = 16;
 int64_t walk_parts(int64_t units, int64_t want, int64_t steps) {
     if (units < 1 || units >= want) return 1;
     return std::max<int64_t>(1, std::min({(want + units - 1) / units, steps / kPartSteps, kMostParts}));
@@ -187,13 +213,7 @@ int c3_attention_grad(const c3_attention_t* a, const c3_attn_tensor_t* dout,
                      : (wide ? launch_careful<_Float16, 128>(p, s) : launch_careful<_Float16, 64>(p, s));
             if (e != hipSuccess) return C3_E_HIP;
         }
-        if (p.rows > 0 && sp.parts[0] > 1 &&
-            sum_parts(p, bf16, g.side[0], 0, 1, g.heads, g.q_tokens, g.dq, g.scale, s) != hipSuccess)
-            return C3_E_HIP;
-        if (p.key_rows > 0 && sp.parts[1] > 1 &&
-            (sum_parts(p, bf16, g.side[1], 0, 2, g.kv_heads, g.k_tokens, g.dk, g.scale, s) != hipSuccess ||
-             sum_parts(p, bf16, g.side[1], 1, 2, g.kv_heads, g.k_tokens, g.dv, 1.0f, s) != hipSuccess))
-            return C3_E_HIP;
+        if (sum_parts(p, bf16, s) != hipSuccess) return C3_E_HIP;
         return C3_OK;
     } catch (...) {
         return C3_E_INVAL;

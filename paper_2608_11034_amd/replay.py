@@ -20,6 +20,7 @@ from __future__ import annotations
 import ctypes
 import math
 import operator
+import struct
 from typing import NamedTuple
 
 import torch
@@ -58,13 +59,20 @@ class ExpertRows(ctypes.Structure):
                 ("sorted_stride", ctypes.c_int64), ("slot", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
 
 
-_ready = False
+# The same fields in one step: setting them one by one costs a call several microseconds.
+_HEADS = struct.Struct("@2P7q")
+_POS = struct.Struct("@2q")
+_ATTENTION = struct.Struct("@6ifi2q2i2P")
+_ATTN_TENSOR = struct.Struct("@P3q")
+_EXPERT_ROWS = struct.Struct("@2i4q2P")
+
+_ready = None
 
 
 def _lib():
     global _ready
-    L = c3.lib()
-    if not _ready:
+    if _ready is None:
+        L = c3.lib()
         vp, i32, i64, sz, dbl = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t,
                                  ctypes.c_double)
         L.c3_rotary.restype = i32
@@ -86,8 +94,8 @@ def _lib():
         L.c3_expert_combine.argtypes = [vp] * 5
         L.c3_expert_combine_grad.restype = i32
         L.c3_expert_combine_grad.argtypes = [vp] * 7
-        _ready = True
-    return L
+        _ready = L
+    return _ready
 
 
 def _rows(t, name, dtype=None, device=None, dim=None):
@@ -100,16 +108,22 @@ def _rows(t, name, dtype=None, device=None, dim=None):
         raise C3Error(f"{name} must be {dtype}, got {t.dtype}")
     if device is not None and t.device != device:
         raise C3Error(f"{name} must be on {device}")
-    if dim is not None and t.dim() not in dim:
+    n = t.dim()
+    if dim is not None and n not in dim:
         raise C3Error(f"{name} must have {' or '.join(map(str, dim))} dimensions")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if n and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise C3Error(f"{name}: the last dimension must be contiguous")
     return t
 
 
-def _overlap(t):
-    """Whether an output's elements share memory."""
-    return any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride()))
+def _out(t, name, shape, dtype, device, stream):
+    """The caller's result tensor, checked, or a new one."""
+    if t is None:
+        return _new(shape, dtype, device, stream)
+    _rows(t, name, dtype, device)
+    if t.shape != shape or any(n > 1 and s == 0 for n, s in zip(shape, t.stride())):
+        raise C3Error(f"{name} must have the shape {tuple(shape)} and no repeated elements")
+    return t
 
 
 def _new(shape, dtype, device, stream):
@@ -183,30 +197,32 @@ def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
     ``inverse`` turns back, which is the gradient.  ``out`` (same structure as
     ``x``) may be ``x`` itself.  Returns what ``out`` is, or new tensors."""
     single = isinstance(x, torch.Tensor)
-    xs = [x] if single else list(x)
+    xs = (x,) if single else tuple(x)
     if len(xs) not in (1, 2):
         raise C3Error("rotary takes one tensor or two")
-    for i, t in enumerate(xs):
-        _rows(t, f"x[{i}]", xs[0].dtype if i else None, xs[0].device if i else None, (3, 4))
-        if t.dim() != xs[0].dim() or t.shape[:-2] != xs[0].shape[:-2] or t.shape[-1] != xs[0].shape[-1]:
-            raise C3Error("the tensors must agree in all but their heads")
-    first = xs[0]
-    B, S = (first.shape[0], first.shape[1]) if first.dim() == 4 else (1, first.shape[0])
-    D, dev = first.shape[-1], first.device
-    outs = [_new(t.shape, t.dtype, dev, stream) for t in xs] if out is None else [out] if single else list(out)
+    first = _rows(xs[0], "x[0]", dim=(3, 4))
+    shape, dtype, dev = first.shape, first.dtype, first.device
+    outs = (None,) * len(xs) if out is None else (out,) if single else tuple(out)
     if len(outs) != len(xs):
         raise C3Error("out must have one tensor for each of x")
-    for t, y in zip(xs, outs):
-        _rows(y, "out", t.dtype, dev)
-        if y.shape != t.shape or _overlap(y):
-            raise C3Error("out must have the shape of x and no repeated elements")
+    table, done = b"", []
+    for i, (t, y) in enumerate(zip(xs, outs)):
+        if i:
+            _rows(t, f"x[{i}]", dtype, dev, (len(shape),))
+            if t.shape[:-2] != shape[:-2] or t.shape[-1] != shape[-1]:
+                raise C3Error("the tensors must agree in all but their heads")
+        y = _out(y, "out", t.shape, dtype, dev, stream)
+        done.append(y)
+        table += _HEADS.pack(t.data_ptr(), y.data_ptr(), *_strides4(t), *_strides4(y), t.shape[-2])
+    B, S = shape[:2] if len(shape) == 4 else (1, shape[0])
     if not isinstance(positions, torch.Tensor) or positions.device != dev or positions.dtype not in (
             torch.int32, torch.int64):
         raise C3Error("positions must be int32 or int64 on the device of x")
-    if positions.dim() == 1 and positions.shape[0] == S:
-        pos = (0, positions.stride(0))
-    elif positions.dim() == 2 and tuple(positions.shape) == (B, S):
-        pos = (positions.stride(0), positions.stride(1))
+    where = positions.shape
+    if len(where) == 1 and where[0] == S:
+        pos = _POS.pack(0, positions.stride(0))
+    elif len(where) == 2 and where[0] == B and where[1] == S:
+        pos = _POS.pack(*positions.stride())
     else:
         raise C3Error("positions must be [S] or [B, S]")
     _dev_tensor(freqs, "freqs")
@@ -214,66 +230,52 @@ def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
         raise C3Error("freqs must be fp64 [rot / 2] on the device of x")
     if layout not in _LAYOUT:
         raise C3Error(f"unknown layout {layout}")
-    table = (Heads * len(xs))()
-    for h, t, y in zip(table, xs, outs):
-        h.in_, h.out, h.heads = t.data_ptr(), y.data_ptr(), t.shape[-2]
-        h.in_stride[:], h.out_stride[:] = _strides4(t), _strides4(y)
-    rc = _lib().c3_rotary(table, len(xs), _CODE[first.dtype], B, S, D, _ptr(positions),
-                          positions.element_size(), (ctypes.c_int64 * 2)(*pos), _ptr(freqs),
-                          2 * freqs.numel(), _LAYOUT[layout], int(bool(inverse)), float(amplitude),
-                          _stream(stream))
+    rc = _lib().c3_rotary(table, len(xs), _CODE[dtype], B, S, shape[-1], positions.data_ptr(),
+                          positions.element_size(), pos, freqs.data_ptr(), 2 * freqs.numel(),
+                          _LAYOUT[layout], int(bool(inverse)), float(amplitude), _stream(stream))
     _check(rc, "c3_rotary")
-    return outs[0] if single else tuple(outs)
+    return done[0] if single else tuple(done)
 
 
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
 def _attn_tensor(t):
-    a = AttnTensor()
-    a.ptr = t.data_ptr()
-    a.stride[:] = _strides4(t)
-    return a
+    return _ATTN_TENSOR.pack(t.data_ptr(), *_strides4(t))
 
 
 def _attention_args(q, k, v, causal, window, scale, q_lens, k_lens):
     _rows(q, "q", dim=(3, 4))
+    qs, ks = q.shape, k.shape if isinstance(k, torch.Tensor) else None
     for t, n in ((k, "k"), (v, "v")):
-        _rows(t, n, q.dtype, q.device, (q.dim(),))
-    if k.shape != v.shape:
+        _rows(t, n, q.dtype, q.device, (len(qs),))
+    if ks != v.shape:
         raise C3Error("k and v must have the same shape")
-    if q.shape[-1] != k.shape[-1]:
+    if qs[-1] != ks[-1]:
         raise C3Error("q and k must have the same head size")
-    packed = q.dim() == 3
+    packed = len(qs) == 3
     if (q_lens is None) != (k_lens is None):
         raise C3Error("q_lens and k_lens go together")
-    if not packed and q.shape[0] != k.shape[0]:
+    if not packed and qs[0] != ks[0]:
         raise C3Error("q and k must have the same batch")
     if packed and q_lens is None:
-        q_lens, k_lens = [q.shape[0]], [k.shape[0]]
-    batch = len(q_lens) if packed else q.shape[0]
-    a = Attention()
-    keep = ()
+        q_lens, k_lens = [qs[0]], [ks[0]]
+    batch = len(q_lens) if packed else qs[0]
+    keep, at = (), (0, 0)
     if q_lens is not None:
         if len(q_lens) != batch or len(k_lens) != batch:
             raise C3Error("q_lens and k_lens need one length for each sequence")
         keep = tuple((ctypes.c_int32 * max(batch, 1))(*[_int32(n, "a length") for n in x])
                      for x in (q_lens, k_lens))
-        a.q_lens, a.k_lens = (ctypes.cast(x, ctypes.c_void_p) for x in keep)
-    a.dtype, a.heads, a.kv_heads, a.dim = _CODE[q.dtype], q.shape[-2], k.shape[-2], q.shape[-1]
-    a.causal, a.window, a.batch, a.packed = int(bool(causal)), _int32(window, "window"), batch, int(packed)
-    a.scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
-    a.q_tokens, a.k_tokens = (q.shape[0], k.shape[0]) if packed else (q.shape[1], k.shape[1])
+        at = tuple(ctypes.addressof(x) for x in keep)
+    q_tokens, k_tokens = (qs[0], ks[0]) if packed else (qs[1], ks[1])
+    try:
+        a = _ATTENTION.pack(_CODE[q.dtype], qs[-2], ks[-2], qs[-1], int(bool(causal)),
+                            _int32(window, "window"), (qs[-1] or 1) ** -0.5 if scale is None else scale, batch,
+                            q_tokens, k_tokens, int(packed), 0, *at)
+    except (struct.error, OverflowError):
+        raise C3Error("scale must be a number, and sizes below 2^31") from None
     return a, keep
-
-
-def _attn_out(t, like, name, stream):
-    if t is None:
-        return _new(like.shape, like.dtype, like.device, stream)
-    _rows(t, name, like.dtype, like.device)
-    if t.shape != like.shape or _overlap(t):
-        raise C3Error(f"{name} must have the shape {tuple(like.shape)} and no repeated elements")
-    return t
 
 
 def _workspace(need, workspace, device, what, stream):
@@ -306,12 +308,11 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: float = 
     each query that many keys.  ``scale`` defaults to D ** -0.5.  lse is fp32
     [.., H]; a row that sees no key has out 0 and lse -inf."""
     a, keep = _attention_args(q, k, v, causal, window, scale, q_lens, k_lens)
-    out = _attn_out(out, q, "out", stream)
+    out = _out(out, "out", q.shape, q.dtype, q.device, stream)
     lse = _new(q.shape[:-1], torch.float32, q.device, stream) if lse is None else _lse(lse, q)
-    ws = _workspace(_lib().c3_attention_workspace_size(ctypes.byref(a)), workspace, q.device,
+    ws = _workspace(_lib().c3_attention_workspace_size(a), workspace, q.device,
                     "attention", stream)
-    t = [_attn_tensor(x) for x in (q, k, v, out)]
-    rc = _lib().c3_attention(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse), _ptr(ws),
+    rc = _lib().c3_attention(a, *map(_attn_tensor, (q, k, v, out)), _ptr(lse), _ptr(ws),
                              ws.numel() * ws.element_size(), _stream(stream))
     _check(rc, "c3_attention")
     return out, lse
@@ -328,13 +329,12 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
         if t.shape != q.shape:
             raise C3Error(f"{n} must have the shape of q")
     _lse(lse, q)
-    dq, dk, dv = (_attn_out(t, x, n, stream) for t, x, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
-    ws = _workspace(_lib().c3_attention_grad_workspace_size(ctypes.byref(a)), workspace, q.device,
+    dq, dk, dv = (_out(t, n, x.shape, q.dtype, q.device, stream)
+                  for t, x, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
+    ws = _workspace(_lib().c3_attention_grad_workspace_size(a), workspace, q.device,
                     "attention_grad", stream)
-    t = [_attn_tensor(x) for x in (dout, q, k, v, out)]
-    d = [_attn_tensor(x) for x in (dq, dk, dv)]
-    rc = _lib().c3_attention_grad(ctypes.byref(a), *map(ctypes.byref, t), _ptr(lse),
-                                  *map(ctypes.byref, d), _ptr(ws), ws.numel() * ws.element_size(),
+    rc = _lib().c3_attention_grad(a, *map(_attn_tensor, (dout, q, k, v, out)), _ptr(lse),
+                                  *map(_attn_tensor, (dq, dk, dv)), _ptr(ws), ws.numel() * ws.element_size(),
                                   _stream(stream))
     _check(rc, "c3_attention_grad")
     return dq, dk, dv
@@ -377,36 +377,27 @@ def expert_sort(ids: torch.Tensor, num_experts: int, *, workspace=None, stream=N
 
 
 def _expert_rows(order, token_rows, sorted_rows, dtype):
-    """c3_expert_rows_t from tensors or None for either side."""
+    """c3_expert_rows_t of both sides' tensors."""
     for t, n in zip(order, ("offsets", "source", "slot")):
         _dev_tensor(t, n)
         if t.dtype != torch.int32:
             raise C3Error(f"{n} must be int32")
-    T, top = order.slot.shape
-    r = ExpertRows()
+    slot, dev = order.slot, order.slot.device
+    T, top = slot.shape
+    stride = []
     for t, n, rows in ((token_rows, "tokens' rows", T), (sorted_rows, "sorted rows", T * top)):
         if t.dim() != 2 or t.shape[0] != rows:
             raise C3Error(f"the {n} must be [{rows}, hidden]")
-        if t.dtype != dtype or t.device != order.slot.device:
+        if t.dtype != dtype or t.device != dev:
             raise C3Error("the rows must have one dtype and the order's device")
-    if token_rows.shape[1] != sorted_rows.shape[1]:
-        raise C3Error("the rows must have one hidden size")
+        # the stride of a single row says nothing
+        stride.append(t.stride(0) if rows > 1 else max(t.shape[1], t.stride(0)))
     H = token_rows.shape[1]
-    r.dtype, r.top, r.tokens, r.hidden = _CODE[dtype], top, T, H
-    # the stride of a single row says nothing
-    r.token_stride = token_rows.stride(0) if T > 1 else max(H, token_rows.stride(0))
-    r.sorted_stride = sorted_rows.stride(0) if T * top > 1 else max(H, sorted_rows.stride(0))
-    r.slot, r.kept = order.slot.data_ptr(), order.offsets.data_ptr() + 4 * (order.offsets.numel() - 1)
-    return r
-
-
-def _expert_out(t, shape, like, stream):
-    if t is None:
-        return _new(shape, like.dtype, like.device, stream)
-    _rows(t, "out", like.dtype, like.device)
-    if tuple(t.shape) != tuple(shape) or _overlap(t):
-        raise C3Error(f"out must be {tuple(shape)} without repeated elements")
-    return t
+    if H != sorted_rows.shape[1]:
+        raise C3Error("the rows must have one hidden size")
+    offsets = order.offsets
+    return stride[1], _EXPERT_ROWS.pack(_CODE[dtype], top, T, H, *stride, slot.data_ptr(),
+                                        offsets.data_ptr() + 4 * (offsets.numel() - 1))
 
 
 def _weights(weights, order):
@@ -423,9 +414,9 @@ def expert_dispatch(x, order: ExpertOrder, *, out=None, stream=None):
     """Rows [T * top, hidden] sorted by expert from tokens x [T, hidden]; the
     rows behind the last kept choice are zeros."""
     _rows(x, "x", dim=(2,))
-    out = _expert_out(out, (order.slot.numel(), x.shape[1]), x, stream)
-    r = _expert_rows(order, x, out, x.dtype)
-    _check(_lib().c3_expert_dispatch(ctypes.byref(r), _ptr(x), _ptr(out), _stream(stream)),
+    out = _out(out, "out", (order.slot.numel(), x.shape[1]), x.dtype, x.device, stream)
+    r = _expert_rows(order, x, out, x.dtype)[1]
+    _check(_lib().c3_expert_dispatch(r, _ptr(x), _ptr(out), _stream(stream)),
            "c3_expert_dispatch")
     return out
 
@@ -434,10 +425,10 @@ def expert_combine(y, order: ExpertOrder, weights=None, *, out=None, stream=None
     """out[t] = sum over t's choices of weight * y[their place]; y [T * top,
     hidden], weights fp32 [T, top] or None (ones)."""
     _rows(y, "y", dim=(2,))
-    out = _expert_out(out, (order.slot.shape[0], y.shape[1]), y, stream)
+    out = _out(out, "out", (order.slot.shape[0], y.shape[1]), y.dtype, y.device, stream)
     weights = _weights(weights, order)
-    r = _expert_rows(order, out, y, y.dtype)
-    _check(_lib().c3_expert_combine(ctypes.byref(r), _ptr(y), _ptr(weights), _ptr(out),
+    r = _expert_rows(order, out, y, y.dtype)[1]
+    _check(_lib().c3_expert_combine(r, _ptr(y), _ptr(weights), _ptr(out),
                                     _stream(stream)), "c3_expert_combine")
     return out
 
@@ -447,17 +438,17 @@ def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, s
     without weights dweights is None (and y may be)."""
     _rows(dout, "dout", dim=(2,))
     weights = _weights(weights, order)
-    dy = _expert_out(dy, (order.slot.numel(), dout.shape[1]), dout, stream)
-    r = _expert_rows(order, dout, dy, dout.dtype)
+    dy = _out(dy, "dy", (order.slot.numel(), dout.shape[1]), dout.dtype, dout.device, stream)
+    sorted_stride, r = _expert_rows(order, dout, dy, dout.dtype)
     dw = None
     if weights is not None:
         _rows(y, "y", dout.dtype, dout.device, (2,))
         if y.shape != dy.shape:
             raise C3Error(f"y must be {tuple(dy.shape)}")
-        if y.shape[0] > 1 and y.stride(0) != r.sorted_stride:
+        if y.shape[0] > 1 and y.stride(0) != sorted_stride:
             raise C3Error("y and dy must have the same row stride")
         dw = _new(order.slot.shape, torch.float32, dout.device, stream)
-    _check(_lib().c3_expert_combine_grad(ctypes.byref(r), _ptr(dout), _ptr(y if dw is not None else None),
+    _check(_lib().c3_expert_combine_grad(r, _ptr(dout), _ptr(y if dw is not None else None),
                                          _ptr(weights), _ptr(dy), _ptr(dw), _stream(stream)),
            "c3_expert_combine_grad")
     return dy, dw
