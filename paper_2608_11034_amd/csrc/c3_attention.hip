@@ -16,6 +16,10 @@ namespace c3 {
 namespace {
 
 constexpr int kKeys = 64;           // keys of a tile
+// Parts of a walk: at most, and those that one wave joins for a row.
+constexpr int kMostParts = 256, kFewParts = 16;
+// Workgroups of the kernel for few rows that run at a time: its LDS fills a compute unit.
+constexpr int64_t kTokenSlots = 256;
 
 // Parts that a walk over k_len keys is divided into.
 __device__ __forceinline__ int key_parts(const AttnArgs& a, int k_len) {
@@ -447,7 +451,7 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
 }
 
 // Joins the parts of divided walks.  A wave takes a row: lane p the maximum and sum
-// of part p (64 parts at most), then each lane two elements of the row.
+// of part p (kFewParts at most), then each lane two elements of the row.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_t rows, int parts, FastDiv tokens) {
     const int lane = threadIdx.x & 63;
@@ -474,12 +478,85 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
     if (2 * lane >= a.dim) return;
     float x = 0.0f, y = 0.0f;
     const uint64_t full = __ballot(l != 0.0f);
-    for (int p = 0; p < parts; ++p) {
-        if (!((full >> p) & 1)) continue;
-        const float2 v = *reinterpret_cast<const float2*>(a.side[0].part + (p * rows + row) * a.dim + 2 * lane);
-        const float g = __shfl(f, p);
-        x = fmaf(v.x, g, x);
-        y = fmaf(v.y, g, y);
+    const float* from = a.side[0].part + row * a.dim + 2 * lane;
+    for (int p0 = 0; p0 < parts; p0 += 8) {         // eight parts' loads together
+        float2 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = *reinterpret_cast<const float2*>(from + min(p0 + j, parts - 1) * rows * a.dim);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (p0 + j >= parts || !((full >> (p0 + j)) & 1)) continue;      // not written
+            const float g = __shfl(f, p0 + j);
+            x = fmaf(v[j].x, g, x);
+            y = fmaf(v[j].y, g, y);
+        }
+    }
+    const float inv = none ? 0.0f : 1.0f / total;
+    T e[2] = {(T)(none ? 0.0f : x * inv), (T)(none ? 0.0f : y * inv)};
+    uint32_t two;
+    __builtin_memcpy(&two, e, 4);
+    *reinterpret_cast<uint32_t*>(a.o.ptr + b * a.o.sb + (token - b * tokens.d) * a.o.st + head * a.o.sh + lane * 4) = two;
+}
+
+// The same with a workgroup a row, for many parts (256 at most): thread p the maximum
+// and sum of part p, then each wave a quarter of the parts, joined in the waves' order.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_many_kernel(AttnArgs a, int64_t rows, int parts, FastDiv tokens) {
+    __shared__ float factor[256], tops[4], sums[4];
+    __shared__ float2 partial[4][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    float m = -__builtin_inff(), l = 0.0f;
+    if (tid < parts) {
+        const float2 x = reinterpret_cast<const float2*>(a.part_ml)[tid * rows + row];
+        m = x.x;
+        l = x.y;
+    }
+    if (l == 0.0f) m = -__builtin_inff();
+    float top = m;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) tops[wave] = top;
+    const bool none = !__syncthreads_or(l != 0.0f);
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const float f = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    factor[tid] = l == 0.0f ? -1.0f : f;            // -1: not written
+    float total = f * l;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+    if (lane == 0) sums[wave] = total;
+    __syncthreads();
+    total = sums[0] + sums[1] + sums[2] + sums[3];
+    float x = 0.0f, y = 0.0f;
+    const int each = (parts + 3) / 4, end = min(wave * each + each, parts);
+    if (2 * lane < a.dim) {
+        const float* from = a.side[0].part + row * a.dim + 2 * lane;
+        for (int p0 = wave * each; p0 < end; p0 += 8) {
+            float2 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = *reinterpret_cast<const float2*>(from + min(p0 + j, end - 1) * rows * a.dim);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float g = p0 + j < end ? factor[p0 + j] : -1.0f;
+                if (g < 0.0f) continue;
+                x = fmaf(v[j].x, g, x);
+                y = fmaf(v[j].y, g, y);
+            }
+        }
+    }
+    partial[wave][lane] = make_float2(x, y);
+    __syncthreads();
+    if (wave != 0) return;
+    const int64_t token = row / a.heads, b = token / tokens.d;
+    const int head = (int)(row - token * a.heads);
+    if (lane == 0) a.lse[row] = none ? -__builtin_inff() : (top + __log2f(total)) * kLn2;
+    if (2 * lane >= a.dim) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        x += partial[w][lane].x;
+        y += partial[w][lane].y;
     }
     const float inv = none ? 0.0f : 1.0f / total;
     T e[2] = {(T)(none ? 0.0f : x * inv), (T)(none ? 0.0f : y * inv)};
@@ -497,9 +574,15 @@ hipError_t launch_forward(const AttnPlan& p, bool tokens, hipStream_t s) {
         attn_forward_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
     if (!tokens && (p.args.causal || p.args.window) && p.key_rows > 0)
         attn_forward_careful_kernel<T, DP><<<dim3(32), block, 0, s>>>(p.args, p.table, grid.x);
-    if (p.args.split_keys)
-        attn_join_parts_kernel<T><<<dim3((unsigned)((p.rows + 3) / 4)), dim3(256), 0, s>>>(
-            p.args, p.rows, (int)p.args.side[0].splits.d, FastDiv((uint32_t)p.args.q_tokens));
+    if (p.args.split_keys) {
+        const int parts = (int)p.args.side[0].splits.d;
+        const FastDiv q_tokens((uint32_t)p.args.q_tokens);
+        if (parts > kFewParts)
+            attn_join_many_kernel<T><<<dim3((unsigned)p.rows), dim3(256), 0, s>>>(p.args, p.rows, parts, q_tokens);
+        else
+            attn_join_parts_kernel<T><<<dim3((unsigned)((p.rows + 3) / 4)), dim3(256), 0, s>>>(p.args, p.rows, parts,
+                                                                                            q_tokens);
+    }
     return hipGetLastError();
 }
 
@@ -525,16 +608,37 @@ struct ForwardShape {
         };
         split_keys = 0;
         parts = 1;
-        const int64_t want = tokens ? 768 : 512, least = tokens ? 256 : 512;
-        const int64_t n = units(0);
-        if (n > 0 && n < want && p.max_k > least) {
-            // as many keys to each of `want` workgroups, in whole tiles
-            const int64_t all = std::max<int64_t>(units(1), 1);        // keys times tiles of rows
-            split_keys = std::max(least, (all / want + 127) / 128 * 128);
-            split_keys = std::max(split_keys, ((p.max_k + 63) / 64 + 127) / 128 * 128);
-            parts = (p.max_k + split_keys - 1) / split_keys;
-            if (parts < 2) split_keys = 0, parts = 1;
+        const int64_t n = units(0), all = std::max<int64_t>(units(1), 1);       // all: keys times tiles of rows
+        const int64_t least = tokens ? 256 : 512;
+        auto whole = [&](int64_t keys) {        // in whole tiles, and no more parts than can be joined
+            keys = std::max({keys, least, (p.max_k + kMostParts - 1) / kMostParts});
+            return (keys + 127) / 128 * 128;
+        };
+        if (n > 0 && p.max_k > least && tokens && n < 4 * kTokenSlots) {
+            // The cheapest of a few divisions, in keys' time.  A workgroup costs kFixed
+            // beside its keys and joining costs kJoin; one round of workgroups lasts as long
+            // as its longest, more of them as long as the mean and half of the longest.
+            // us at one, two and three rounds of workgroups: 8 caches of 8,192 tokens and 8
+            // heads of 128 52, 56, 62; one of 32,768 tokens 31, 35, 41; 16 of 1 to 32,768
+            // tokens 152, 134, 118.
+            constexpr int64_t kFixed = 200, kJoin = 250;
+            auto cost = [&](int64_t split) {
+                const int64_t u = units(split), longest = split ? std::min(split, p.max_k) : p.max_k;
+                if (u < 0) return INT64_MAX;
+                const int64_t join = split ? kJoin : 0;
+                return u <= kTokenSlots ? longest + kFixed + join
+                                        : (all + kFixed * u) / kTokenSlots + longest / 2 + join;
+            };
+            int64_t best = cost(0);
+            for (const int64_t twelfths : {3, 4, 6, 8, 12, 18, 24}) {
+                const int64_t split = whole(all * twelfths / 12 / kTokenSlots), c = cost(split);
+                if (split < p.max_k && c < best) best = c, split_keys = split;
+            }
+        } else if (n > 0 && n < 512 && p.max_k > least && !tokens) {
+            split_keys = whole(all / 512);              // as many keys to each of 512 workgroups
         }
+        if (split_keys) parts = (p.max_k + split_keys - 1) / split_keys;
+        if (parts < 2) split_keys = 0, parts = 1;
         const int64_t blocks = units(split_keys);
         fits = blocks >= 0;
         uint64_t at = 0;

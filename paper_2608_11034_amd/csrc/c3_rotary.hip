@@ -3,10 +3,14 @@
 // Pair i of every head of a token is turned by position * freqs[i].  One pass:
 // each element is read and written once, so HBM bounds it.  The cosines and
 // sines of a token are shared by all its heads: a workgroup takes as many
-// tokens as give its 256 threads about four items each, puts the tokens'
+// tokens as give its 256 threads about two items each, puts the tokens'
 // rot / 2 pairs of (cos, sin) into LDS once, and turns the heads of both tensors
 // with them.  An item is one 16-byte piece of a head (both halves of it where
-// the pair's elements are half a head apart).
+// the pair's elements are half a head apart).  The first items are loaded before the
+// cosines and sines are formed, and few of them a thread keep many waves on a compute
+// unit.  4 x 4,096 tokens of 64 heads of 128 in bf16: 103 us, 5.2 TB/s, what a large copy
+// reaches (four items a thread 112); 16,383 tokens of 36 heads of 64 in fp32, a quarter
+// turned: 53 us, 5.7 TB/s (60; trigonometry before any load 81).
 //
 // The angle is formed in fp64 in whole turns and only its fraction is rounded
 // to fp32: at position 131,072 an fp32 angle is off by up to 0.004 radians.
@@ -17,7 +21,7 @@ namespace c3 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItems = 4;
+constexpr int kItems = 2;
 
 struct RotaryArgs {
     c3_heads_t t[2];
@@ -52,25 +56,14 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     const int half = a.rot / 2;
     const int64_t tok0 = (int64_t)blockIdx.x * a.block_tokens;
     const int nt = (int)min((int64_t)a.block_tokens, a.tokens - tok0);
-    for (int i = threadIdx.x; i < nt * half; i += kThreads) {
-        const int t = i / half, p = i - t * half;
-        const uint32_t tok = (uint32_t)(tok0 + t), b = a.length.quot(tok);
-        const int64_t at = (int64_t)b * a.pos_stride[0] + (int64_t)(tok - b * a.length.d) * a.pos_stride[1];
-        const double pos = a.pos_bytes == 8 ? (double)((const int64_t*)a.pos)[at]
-                                            : (double)((const int32_t*)a.pos)[at];
-        const double turns = pos * a.freqs[p] * 0.15915494309189533577;
-        float s, c;
-        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
-    }
-    __syncthreads();
     const bool pairs_apart = V == 1 || !a.interleaved;
     const int turned = pairs_apart ? half / V : a.rot / V;
     const uint32_t n = (uint32_t)nt * a.token_items.d;
-    for (uint32_t base = threadIdx.x; base < n; base += kThreads * kItems) {
-        AlignedPack<T, V> x[kItems], y[kItems];
-        T* out[kItems];
-        int first[kItems], second[kItems], cs[kItems];
+
+    AlignedPack<T, V> x[kItems], y[kItems];
+    T* out[kItems];
+    int first[kItems], second[kItems], cs[kItems];
+    auto load = [&](uint32_t base) {
 #pragma unroll
         for (int u = 0; u < kItems; ++u) {
             const uint32_t i = base + u * kThreads;
@@ -106,6 +99,24 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
             }
             x[u] = load_piece<T, V>(in + first[u]);
         }
+    };
+
+    // the first items are on their way while the cosines and sines are formed
+    load(threadIdx.x);
+    for (int i = threadIdx.x; i < nt * half; i += kThreads) {
+        const int t = i / half, p = i - t * half;
+        const uint32_t tok = (uint32_t)(tok0 + t), b = a.length.quot(tok);
+        const int64_t at = (int64_t)b * a.pos_stride[0] + (int64_t)(tok - b * a.length.d) * a.pos_stride[1];
+        const double pos = a.pos_bytes == 8 ? (double)((const int64_t*)a.pos)[at]
+                                            : (double)((const int32_t*)a.pos)[at];
+        const double turns = pos * a.freqs[p] * 0.15915494309189533577;
+        float s, c;
+        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+        turn[i] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
+    }
+    __syncthreads();
+    for (uint32_t base = threadIdx.x; base < n; base += kThreads * kItems) {
+        if (base >= kThreads * kItems) load(base);
 #pragma unroll
         for (int u = 0; u < kItems; ++u) {
             if (out[u] == nullptr) continue;
