@@ -6,7 +6,12 @@
 // maximum and sum of a row are lane values (one exchange with the other half), and
 // the probabilities are the next product's operand where they are.  Scores are
 // kept in units of the raw product; exp is exp2 of (s - m) scale log2 e, one fma
-// and one v_exp_f32 an element.
+// and one v_exp_f32 an element.  2 x 4,096 causal tokens of 32 heads of 128: 310 us,
+// 888 TFLOP/s (a large library product 1,290).  Matrix units are busy 43% of the time, at
+// a clock near 2 GHz; reading operands further ahead of their products
+// (scheduling barriers) or raising the waves' priority there changed nothing once the
+// clock has settled.  Heads of 64 have half the products for the same exponentials:
+// packed documents of 8,693 tokens, 32 heads, window 1,024: 82 us, 565 TFLOP/s.
 #include <algorithm>
 #include <new>
 
@@ -18,8 +23,8 @@ namespace {
 constexpr int kKeys = 64;           // keys of a tile
 // Parts of a walk: at most, and those that one wave joins for a row.
 constexpr int kMostParts = 256, kFewParts = 16;
-// Workgroups of the kernel for few rows that run at a time: its LDS fills a compute unit.
-constexpr int64_t kTokenSlots = 256;
+// Workgroups of the kernel for few rows that run at a time: two a compute unit.
+constexpr int64_t kTokenSlots = 512;
 
 // Parts that a walk over k_len keys is divided into.
 __device__ __forceinline__ int key_parts(const AttnArgs& a, int k_len) {
@@ -251,14 +256,16 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_forward_careful_kernel(A
 // once and bound it.  The 32 rows of a workgroup stand in every one of its four
 // waves, which share out the keys 32 at a time, each through buffers of its own, so
 // that no wave waits for another before the end; there their maxima and sums are
-// joined in LDS.  Long caches are divided among workgroups as well.
+// joined in LDS.  Long caches are divided among workgroups as well.  One buffer each
+// for keys and values, refilled as soon as its product has read it, lets two
+// workgroups share a compute unit: one starts or ends while the other streams
+// (16 caches of 1 to 32,768 tokens, 8 key heads of 128: 115 us with the joining, 4.9
+// TB/s; two buffers each and one workgroup 124).
 template <typename T, int DP>
-__global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_kernel(AttnArgs a, AttnTable tab) {
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a, AttnTable tab) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
     __shared__ __attribute__((aligned(1024))) char k0[kAttnWaves * kSub];
     __shared__ __attribute__((aligned(1024))) char v0[kAttnWaves * kSub];
-    __shared__ __attribute__((aligned(1024))) char k1[kAttnWaves * kSub];
-    __shared__ __attribute__((aligned(1024))) char v1[kAttnWaves * kSub];
     __shared__ T words[kAttnWaves][32 * 32];      // for the masked product
     __shared__ float stats[2][kAttnWaves][64];
 
@@ -308,25 +315,35 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
     f32x16 acc[NDB] = {};
     float m = -__builtin_inff(), l = 0.0f;
 
-    auto load = [&](int t, char* kt, char* vt) {
+    // 32 rows of keys or values to the wave's buffer
+    auto load = [&](int t, const char* from, int64_t st, const uint32_t (&off)[kLoads], char* to) {
         const int rows = min(w.k_len - t * 32, 32);
-        const uint32_t k_bytes = (uint32_t)((rows - 1) * (int)a.k.st) + a.dim * 2;
-        const uint32_t v_bytes = (uint32_t)((rows - 1) * (int)a.v.st) + a.dim * 2;
-        const char* kr = kb + (int64_t)t * 32 * a.k.st;
-        const char* vr = vb + (int64_t)t * 32 * a.v.st;
+        const uint32_t bytes = (uint32_t)((rows - 1) * (int)st) + a.dim * 2;
+        const char* first_row = from + (int64_t)t * 32 * st;
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) load_piece_lds(kr, k_bytes, k_off[n], kt + wave * kSub + n * 1024);
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) load_piece_lds(vr, v_bytes, v_off[n], vt + wave * kSub + n * 1024);
+        for (int n = 0; n < kLoads; ++n) load_piece_lds(first_row, bytes, off[n], to + wave * kSub + n * 1024);
     };
-    auto step = [&](int t, const char* kt, const char* vt) {
-        kt += wave * kSub;
-        vt += wave * kSub;
+    // The wave's own loads, in order: all but the latest kLoads have landed.
+    auto landed = [&](bool more) {
+        if (more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    // reads of the buffer that is filled next have ended: their values are used
+    auto read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    const char *kt = k0 + wave * kSub, *vt = v0 + wave * kSub;
+    // One block of keys; the next block's keys are on their way during the softmax and
+    // the second product, its values during the first.
+    auto step = [&](int t, bool more) {
         const int key0 = t * 32;
+        landed(true);
         const bool masked = __any(key0 + 32 > see_hi || key0 < see_lo);
         f32x16 s = {};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) s = mfma<T>(rd.along(kt, ks), qf[ks], s);
+        read();
+        if (more) load(t + kAttnWaves, kb, a.k.st, k_off, k0);
         uint32_t seen = 0;
         if (masked) {
 #pragma unroll
@@ -357,6 +374,7 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
             s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -mc));
             l += s[i];
         }
+        landed(more);
         if (masked && __any(tile_not_finite<T>(KS, [&](int ks) { return rd.along(vt, ks); }) != 0)) {
             masked_product<T, NDB>(acc, s, seen, words[wave], [&](int k, int d) { return rd.four(vt, k, d); });
             return;
@@ -368,27 +386,15 @@ __global__ __launch_bounds__(kAttnThreads, DP > 64 ? 1 : 2) void attn_tokens_ker
             for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(rd.across(vt + j * 16 * DP * 2, db), p, acc[db]);
         }
     };
-    // The wave's own loads, in order: all but the latest 2 kLoads have landed.
-    auto landed = [&](bool more) {
-        if (more)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    };
-
-    if (t0 < t1) load(t0, k0, v0);
-    for (int t = t0; t < t1; t += 2 * kAttnWaves) {
-        const int next = t + kAttnWaves, after = t + 2 * kAttnWaves;
-        if (next < t1) load(next, k1, v1);
-        landed(next < t1);
-        step(t, k0, v0);
-        if (next >= t1) break;
-        // reads of the buffer that is filled next have ended: their values are used
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (after < t1) load(after, k0, v0);
-        landed(after < t1);
-        step(next, k1, v1);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (t0 < t1) {
+        load(t0, kb, a.k.st, k_off, k0);
+        load(t0, vb, a.v.st, v_off, v0);
+    }
+    for (int t = t0; t < t1; t += kAttnWaves) {
+        const bool more = t + kAttnWaves < t1;
+        step(t, more);
+        read();
+        if (more) load(t + kAttnWaves, vb, a.v.st, v_off, v0);
     }
     l += __shfl_xor(l, 32);
 
@@ -618,10 +624,10 @@ struct ForwardShape {
             // The cheapest of a few divisions, in keys' time.  A workgroup costs kFixed
             // beside its keys and joining costs kJoin; one round of workgroups lasts as long
             // as its longest, more of them as long as the mean and half of the longest.
-            // us at one, two and three rounds of workgroups: 8 caches of 8,192 tokens and 8
-            // heads of 128 52, 56, 62; one of 32,768 tokens 31, 35, 41; 16 of 1 to 32,768
-            // tokens 152, 134, 118.
-            constexpr int64_t kFixed = 200, kJoin = 250;
+            // With one workgroup a compute unit, us at 256, 512 and 768 of them: 8 caches of
+            // 8,192 tokens and 8 heads of 128 52, 56, 62; one of 32,768 tokens 31, 35, 41;
+            // 16 of 1 to 32,768 tokens 152, 134, 118.  By this rule: 53, 31 and 115.
+            constexpr int64_t kFixed = 100, kJoin = 250;
             auto cost = [&](int64_t split) {
                 const int64_t u = units(split), longest = split ? std::min(split, p.max_k) : p.max_k;
                 if (u < 0) return INT64_MAX;

@@ -1,7 +1,10 @@
 // A unit of the second pass of attention's gradient: dk and dv of a block of keys.
 //
 // A wave holds 32 NT keys and values and walks the rows of the query heads that
-// share them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+// share them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  2 x 4,096 causal
+// tokens of 32 heads of 128: 667 us, 825 TFLOP/s; 16,384 tokens of 16 heads on 2 key
+// heads 2,270 us, 970.  With 64 keys a wave (NT 2) half of the LDS reads go, but one wave
+// a SIMD has nothing to run beside its exponentials: 890 us.
 #pragma once
 
 #include "c3_attention.h"
@@ -232,11 +235,11 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     if (t0 < t1) load(t0, q0, g0, s0);
     for (int t = t0; t < t1; t += 2) {
         tiles_ready();
-            if (t + 1 < t1) load(t + 1, q1, g1, s1);
+        if (t + 1 < t1) load(t + 1, q1, g1, s1);
         step(t, q0, g0, s0);
         if (t + 1 >= t1) break;
         tiles_ready();
-            if (t + 2 < t1) load(t + 2, q0, g0, s0);
+        if (t + 2 < t1) load(t + 2, q0, g0, s0);
         step(t + 1, q1, g1, s1);
     }
 

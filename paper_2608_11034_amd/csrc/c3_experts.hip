@@ -12,6 +12,8 @@
 // (four times as many where there are enough rows) of one token's row to or
 // from the rows of all its choices, so a token's row stays in registers for all
 // of them, and sums run in fp32 in the order of the choices.
+#include <type_traits>
+
 #include "c3_internal.h"
 #include "c3_replay_types.h"
 
@@ -158,32 +160,34 @@ using Piece = AlignedPack<T, V>;
 // Zeros in the sorted rows that hold no token: wave w of `waves` takes every
 // waves-th of them.
 template <typename T, int V>
-__device__ void zero_tail(const RowArgs& a, T* sorted, int64_t w, int64_t waves) {
+__device__ void zero_tail(const RowArgs& a, T* sorted, int64_t kept, int64_t w, int64_t waves) {
     const int lane = threadIdx.x & 63;
     const int64_t rows = a.tokens * a.top;
     Piece<T, V> zero;
 #pragma unroll
     for (int j = 0; j < V; ++j) zero.v[j] = (T)0.0f;
-    for (int64_t r = max(*a.kept, 0) + w; r < rows; r += waves)
+    for (int64_t r = kept + w; r < rows; r += waves)
         for (int64_t c = lane; c < a.pieces; c += 64)
             *reinterpret_cast<Piece<T, V>*>(sorted + r * a.sorted_stride + c * V) = zero;
 }
 
 template <typename T, int V, int U>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const T* x, T* sorted) {
+    // a piece that is only moved: kept as one word, or the compiler holds it in LDS
+    using Word = std::conditional_t<sizeof(Piece<T, V>) == 16, u32x4, T>;
     const int lane = threadIdx.x & 63;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int64_t waves = (int64_t)gridDim.x * 4;
     const int64_t token = w / a.parts, c0 = (w - token * a.parts) * 64 * U + lane;
+    const int64_t kept = max(*a.kept, 0);
     if (token < a.tokens) {
         const uint32_t rows = (uint32_t)(a.tokens * a.top);     // a slot outside is a dropped choice
-    const int32_t my_slot = lane < a.top ? a.slot[token * a.top + lane] : -1;
+        const int32_t my_slot = lane < a.top ? a.slot[token * a.top + lane] : -1;
         const T* row = x + token * a.token_stride;
-        Piece<T, V> p[U] = {};
+        Word p[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c0 + u * 64 < a.pieces)
-                p[u] = *reinterpret_cast<const Piece<T, V>*>(row + (c0 + u * 64) * V);
+        for (int u = 0; u < U; ++u)             // behind the row's end the last piece again
+            p[u] = *reinterpret_cast<const Word*>(row + min(c0 + u * 64, a.pieces - 1) * V);
         for (int k = 0; k < a.top; ++k) {
             const int32_t s = __builtin_amdgcn_readlane(my_slot, k);
             if ((uint32_t)s >= rows) continue;
@@ -191,10 +195,10 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const T
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (c0 + u * 64 < a.pieces)
-                    *reinterpret_cast<Piece<T, V>*>(to + (c0 + u * 64) * V) = p[u];
+                    *reinterpret_cast<Word*>(to + (c0 + u * 64) * V) = p[u];
         }
     }
-    zero_tail<T, V>(a, sorted, w, waves);
+    zero_tail<T, V>(a, sorted, kept, w, waves);
 }
 
 template <typename T, int V, int U>
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(256) void expert_combine_grad_kernel(RowArgs a, con
                                                                   const T* sorted, T* dsorted) {
     __shared__ float part[4][C3_MAX_EXPERT_TOP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = blockIdx.x;
+    const int64_t token = blockIdx.x, kept = max(*a.kept, 0);
     const uint32_t rows = (uint32_t)(a.tokens * a.top);     // a slot outside is a dropped choice
     const int32_t my_slot = lane < a.top ? a.slot[token * a.top + lane] : -1;
     float my_weight = 1.0f;
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(256) void expert_combine_grad_kernel(RowArgs a, con
             a.dweights[token * a.top + threadIdx.x] =
                 part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
     }
-    zero_tail<T, V>(a, dsorted, token * 4 + wave, (int64_t)gridDim.x * 4);
+    zero_tail<T, V>(a, dsorted, kept, token * 4 + wave, (int64_t)gridDim.x * 4);
 }
 
 enum class Move { kDispatch, kCombine, kGrad };

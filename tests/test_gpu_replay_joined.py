@@ -85,3 +85,40 @@ def test_argument_ranges():
     for n in (2 ** 32 + 4, 0, -1, replay.MAX_EXPERTS + 1, 4.0, "4"):
         with bad:
             replay.expert_sort(ids, n)
+
+
+@pytest.mark.parametrize("window", [0, 5000])
+@pytest.mark.parametrize("k_len,heads,dim", [(70001, 2, 64), (33000, 1, 128), (3100, 3, 72), (257, 1, 8)])
+def test_many_parts(k_len, heads, dim, window):
+    """One token against caches that are divided into few and into many parts, some of
+    which a window leaves empty; the same bits every time."""
+    print("CASE", k_len, heads, dim, window, flush=True)
+    gen = torch.Generator().manual_seed(33)
+    q = torch.randn((1, heads, dim), generator=gen).to(BF)
+    k, v = (torch.randn((k_len, 1, dim), generator=gen).to(BF) for _ in range(2))
+    k[k_len // 3] *= 4                      # one part's maximum stands out
+    how = dict(causal=True, window=window, q_lens=[1], k_lens=[k_len])
+    x = [t.to(DEV) for t in (q, k, v)]
+    out, lse = replay.attention(*x, **how)
+    want = plain.attention(q, k, v, [1], [k_len], True, window, dim ** -0.5, None, BF)
+    plain.within(out, want["out"], want["out_bound"], "out")
+    plain.within(lse, want["lse"], want["lse_bound"], "lse")
+    again = replay.attention(*x, **how)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_workgroups_of_every_length_and_head():
+    """Key heads and sequences that are no multiple of the eight dies, of very different
+    lengths: every unit is done once."""
+    q_lens, k_lens = [260, 1, 130, 0, 515], [260, 77, 600, 9, 515]
+    gen = torch.Generator().manual_seed(34)
+    H, Hk, D = 9, 3, 64
+    q, g = (torch.randn((sum(q_lens), H, D), generator=gen).to(BF) for _ in range(2))
+    k, v = (torch.randn((sum(k_lens), Hk, D), generator=gen).to(BF) for _ in range(2))
+    how = dict(causal=True, q_lens=q_lens, k_lens=k_lens)
+    Q, K, V, Gd = (t.to(DEV) for t in (q, k, v, g))
+    out, lse = replay.attention(Q, K, V, **how)
+    dq, dk, dv = replay.attention_grad(Gd, Q, K, V, out, lse, **how)
+    want = plain.attention(q, k, v, q_lens, k_lens, True, 0, D ** -0.5, g, BF)
+    for n, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        plain.within(t, want[n], want[n + "_bound"], n)
