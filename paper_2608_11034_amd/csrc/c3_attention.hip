@@ -11,7 +11,7 @@
 // a clock near 2 GHz; reading operands further ahead of their products
 // (scheduling barriers) or raising the waves' priority there changed nothing once the
 // clock has settled.  Heads of 64 have half the products for the same exponentials:
-// packed documents of 8,693 tokens, 32 heads, window 1,024: 82 us, 565 TFLOP/s.
+// packed documents of 8,192 tokens, 32 heads, window 1,024: 82 us, 565 TFLOP/s.
 #include <algorithm>
 #include <new>
 
@@ -161,7 +161,7 @@ __device__ __forceinline__ bool forward_unit(const AttnArgs& a, const AttnTable&
         // 2^8 of it: sums and products keep their relative precision, and the
         // accumulators are rescaled in few steps.
         if (__any((top - m) * cs > 8.0f)) {
-            const float next = fmaxf(m, top);
+            const float next = (top - m) * cs > 8.0f ? top : m;     // each row by itself
             const float f = next == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - next) * cs);
             m = next;
             l *= f;
@@ -189,7 +189,10 @@ __device__ __forceinline__ bool forward_unit(const AttnArgs& a, const AttnTable&
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
                         masked_product<T, NDB>(acc, s[n], seen[n], words[wave],
-                                               [&](int k, int d) { return rd.four(vt + n * kSub, k, d); });
+                                               [&](int k, int d) { return rd.four(vt + n * kSub, k, d); },
+                                               [&](int j, int db) {
+                                                   return rd.across(vt + n * kSub + j * 16 * DP * 2, db);
+                                               });
                     return;
                 }
             }
@@ -250,6 +253,11 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_forward_careful_kernel(A
                                                                                uint32_t blocks) {
     repeat_marked(a.side[0].marks, blocks, blockIdx.x, gridDim.x,
                   [&](uint32_t unit) { forward_unit<T, DP, true>(a, tab, unit); });
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 1) void attn_forward_direct_kernel(AttnArgs a, AttnTable tab) {
+    forward_unit<T, DP, true>(a, tab, blockIdx.x);
 }
 
 // Few rows against many keys, as new tokens against a cache: the keys are read
@@ -359,7 +367,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = fmaxf(top, __shfl_xor(top, 32));
         if (__any((top - m) * cs > 8.0f)) {         // as in the kernel above
-            const float next = fmaxf(m, top);
+            const float next = (top - m) * cs > 8.0f ? top : m;     // each row by itself
             const float f = next == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - next) * cs);
             m = next;
             l *= f;
@@ -376,7 +384,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_tokens_kernel(AttnArgs a
         }
         landed(more);
         if (masked && __any(tile_not_finite<T>(KS, [&](int ks) { return rd.along(vt, ks); }) != 0)) {
-            masked_product<T, NDB>(acc, s, seen, words[wave], [&](int k, int d) { return rd.four(vt, k, d); });
+            masked_product<T, NDB>(acc, s, seen, words[wave], [&](int k, int d) { return rd.four(vt, k, d); },
+                                   [&](int j, int db) { return rd.across(vt + j * 16 * DP * 2, db); });
             return;
         }
 #pragma unroll
@@ -573,13 +582,16 @@ __global__ __launch_bounds__(256) void attn_join_many_kernel(AttnArgs a, int64_t
 
 template <typename T, int DP>
 hipError_t launch_forward(const AttnPlan& p, bool tokens, hipStream_t s) {
-    const dim3 grid(p.args.side[0].units * (uint32_t)p.args.kv_heads), block(kAttnThreads);
-    if (tokens)
+    const dim3 grid(attn_blocks(p, 0)), block(kAttnThreads);
+    if (tokens) {
         attn_tokens_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
-    else
+    } else if (attn_direct(p, 0)) {
+        attn_forward_direct_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    } else {
         attn_forward_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
-    if (!tokens && (p.args.causal || p.args.window) && p.key_rows > 0)
-        attn_forward_careful_kernel<T, DP><<<dim3(32), block, 0, s>>>(p.args, p.table, grid.x);
+        if ((p.args.causal || p.args.window) && p.key_rows > 0)
+            attn_forward_careful_kernel<T, DP><<<dim3(32), block, 0, s>>>(p.args, p.table, grid.x);
+    }
     if (p.args.split_keys) {
         const int parts = (int)p.args.side[0].splits.d;
         const FastDiv q_tokens((uint32_t)p.args.q_tokens);

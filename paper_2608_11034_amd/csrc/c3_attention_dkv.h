@@ -220,9 +220,11 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
 #pragma unroll
                         for (int m = 0; m < NT; ++m) {
                             masked_product<T, NDB>(dv[m], s[m], seen[m], words[wave],
-                                                   [&](int k, int d) { return rd.four(g_sub, k, d); });
+                                                   [&](int k, int d) { return rd.four(g_sub, k, d); },
+                                                   [&](int j, int db) { return rd.across(g_sub, j, db); });
                             masked_product<T, NDB>(dk[m], dp[m], seen[m], words[wave],
-                                                   [&](int k, int d) { return rd.four(q_sub, k, d); });
+                                                   [&](int k, int d) { return rd.four(q_sub, k, d); },
+                                                   [&](int j, int db) { return rd.across(q_sub, j, db); });
                         }
                         continue;
                     }

@@ -14,9 +14,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, A
 }
 
 template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 1) void attn_dkv_direct_kernel(AttnArgs a, AttnTable tab) {
+    dkv_unit<T, DP, kDkvTiles, true>(a, tab, blockIdx.x);
+}
+
+template <typename T, int DP>
 hipError_t launch(const AttnPlan& p, hipStream_t s) {
-    const uint32_t blocks = p.args.side[1].units * (uint32_t)p.args.kv_heads;
-    attn_dkv_kernel<T, DP><<<dim3(blocks), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
+    const dim3 grid(attn_blocks(p, 1)), block(kAttnThreads);
+    if (attn_direct(p, 1))
+        attn_dkv_direct_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    else
+        attn_dkv_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
     return hipGetLastError();
 }
 

@@ -12,6 +12,7 @@
 namespace c3 {
 
 constexpr int kDqKeys = 64;         // keys of a tile
+constexpr int kShortWalk = 2;       // tiles
 
 // Returns whether a tile that the mask cuts held an infinity or NaN, which only
 // CAREFUL keeps from rows that do not see it.
@@ -44,6 +45,7 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
     if (a.window) lo = max(lo, first + off - a.window + 1);
     if (first >= w.q_len) hi = 0;
     int t0 = lo / kDqKeys, t1 = hi > lo ? (hi + kDqKeys - 1) / kDqKeys : t0;
+    const int all0 = t0, all1 = t1;
     if (side.splits.d > 1) {       // this workgroup's part of the walk
         const int64_t n = t1 - t0;
         t1 = t0 + (int)side.splits.quot((uint32_t)(n * (part + 1)));
@@ -76,10 +78,7 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
             const float lse = a.lse[at];
             if (lse != -__builtin_inff()) lse2 = lse * kLog2e;
         }
-        if (there && h == 0 && part == 0) {
-            a.lse2[at] = lse2;
-            a.delta[at] = delta;
-        }
+        if (there && h == 0 && part == 0) a.lse2[at] = lse2;
     }
 
     TileReads<DP> rd;
@@ -96,6 +95,36 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
         load_tile<DP, kDqKeys>(kb + (int64_t)key * a.k.st, a.k.st, a.dim, w.k_len - key, k_off, kt);
         load_tile<DP, kDqKeys>(vb + (int64_t)key * a.v.st, a.v.st, a.dim, w.k_len - key, v_off, vt);
     };
+    // Rows that see few keys have an output near the values' size, and its rounding to 16
+    // bits would enter delta as much as that of dS enters the product: for them delta is
+    // the sum of P dP, which needs no output.  Over 128 keys it is a fiftieth of it.
+    if (all1 - all0 <= kShortWalk) {
+        float sum = 0.0f;
+        for (int t = all0; t < all1; ++t) {
+            load(t, k0, v0);
+            tiles_ready();
+#pragma unroll 1
+            for (int n = 0; n < 2; ++n) {
+                const int key0 = t * kDqKeys + n * 32;
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    s = mfma<T>(rd.along(k0 + n * kSub, ks), qf[ks], s);
+                    dp = mfma<T>(rd.along(v0 + n * kSub, ks), gf[ks], dp);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = key0 + (i >> 2) * 8 + h * 4 + (i & 3);
+                    const bool see = valid && key < see_hi && key >= see_lo;
+                    sum += see ? __builtin_amdgcn_exp2f(fmaf(s[i], cs, -lse2)) * dp[i] : 0.0f;
+                }
+            }
+            __syncthreads();        // before the tile is loaded anew
+        }
+        delta = sum + __shfl_xor(sum, 32);
+    }
+    if (there && h == 0 && part == 0) a.delta[seq_row(a, w) + (int64_t)pos * a.heads + head] = delta;
+
     auto step = [&](int t, const char* kt, const char* vt) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
@@ -126,7 +155,8 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
                 if constexpr (CAREFUL) {
                     if (__any(here != 0)) {
                         masked_product<T, NDB>(acc, s, seen, words[wave],
-                                               [&](int k, int d) { return rd.four(sub, k, d); });
+                                               [&](int k, int d) { return rd.four(sub, k, d); },
+                                               [&](int j, int db) { return rd.across(sub + j * 16 * DP * 2, db); });
                         continue;
                     }
                 }

@@ -14,8 +14,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_kernel(AttnArgs a, At
 }
 
 template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, 1) void attn_dq_direct_kernel(AttnArgs a, AttnTable tab) {
+    dq_unit<T, DP, true>(a, tab, blockIdx.x);
+}
+
+template <typename T, int DP>
 hipError_t launch(const AttnPlan& p, hipStream_t s) {
-    attn_dq_kernel<T, DP><<<dim3(p.args.side[0].units * p.args.kv_heads), dim3(kAttnThreads), 0, s>>>(p.args, p.table);
+    const dim3 grid(attn_blocks(p, 0)), block(kAttnThreads);
+    if (attn_direct(p, 0))
+        attn_dq_direct_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
+    else
+        attn_dq_kernel<T, DP><<<grid, block, 0, s>>>(p.args, p.table);
     return hipGetLastError();
 }
 

@@ -97,8 +97,9 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_grad_careful_kernel(Attn
 
 template <typename T, int DP>
 hipError_t launch_careful(const AttnPlan& p, hipStream_t s) {
-    const uint32_t q = p.rows > 0 ? p.args.side[0].units * (uint32_t)p.args.kv_heads : 0;
-    const uint32_t k = p.key_rows > 0 ? p.args.side[1].units * (uint32_t)p.args.kv_heads : 0;
+    const uint32_t q = attn_direct(p, 0) ? 0 : attn_blocks(p, 0);
+    const uint32_t k = attn_direct(p, 1) ? 0 : attn_blocks(p, 1);
+    if (q + k == 0) return hipSuccess;
     attn_grad_careful_kernel<T, DP><<<dim3(64), dim3(kAttnThreads), 0, s>>>(p.args, p.table, q, k);
     return hipGetLastError();
 }

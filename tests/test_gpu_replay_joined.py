@@ -122,3 +122,43 @@ def test_workgroups_of_every_length_and_head():
     want = plain.attention(q, k, v, q_lens, k_lens, True, 0, D ** -0.5, g, BF)
     for n, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
         plain.within(t, want[n], want[n + "_bound"], n)
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("window", [0, 90])
+def test_hidden_values_in_large_grids(value, dim, window):
+    """More workgroups than compute units: units that met a hidden value which is not
+    finite are marked and repeated with care, and rows that do not see it keep their bits."""
+    n, H, bad = 600, 64, 301
+    gen = torch.Generator().manual_seed(35)
+    x = {c: torch.randn((n, H, dim), generator=gen).to(BF).to(DEV) for c in "qkvg"}
+    how = dict(causal=True, window=window)
+
+    def run(t):
+        out, lse = replay.attention(t["q"], t["k"], t["v"], **how)
+        return dict(zip(("out", "lse", "dq", "dk", "dv"),
+                        (out, lse) + replay.attention_grad(t["g"], t["q"], t["k"], t["v"], out, lse, **how)))
+    clean = run(x)
+    see = plain.seen(n, n, True, window)
+    for which in "vkgq":
+        print("CASE", which, value, dim, window, flush=True)
+        y = dict(x)
+        y[which] = x[which].clone()
+        y[which][bad, 5::7, 3] = value
+        got = run(y)
+        torch.cuda.synchronize()
+        if which in "vk":
+            away_q = ~see[:, bad]
+            away_k = ~(see[~away_q].any(0))
+        else:
+            away_q = torch.arange(n) != bad
+            away_k = ~see[bad]
+        touched = torch.zeros(H, dtype=torch.bool)
+        touched[5::7] = True
+        for name, rows in (("out", away_q), ("lse", away_q), ("dq", away_q), ("dk", away_k), ("dv", away_k)):
+            a, b = got[name].cpu(), clean[name].cpu()
+            assert torch.equal(a[rows], b[rows]), (which, name)
+            assert torch.equal(a[:, ~touched], b[:, ~touched]), (which, name)
+        if which == "v":
+            assert not bool(torch.isfinite(got["out"].cpu()[~away_q][:, touched, 3]).any())
