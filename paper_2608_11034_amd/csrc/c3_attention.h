@@ -414,7 +414,10 @@ __device__ __forceinline__ void masked_product(f32x16 (&acc)[NDB], const f32x16&
     for (int j = 0; j < 2; ++j) {
         const u32x4 p = operand<T>(x, j);
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) acc[db] = mfma<T>(finite_part<T>(across(j, db)), p, acc[db]);
+        for (int db = 0; db < NDB; ++db) {
+            acc[db] = mfma<T>(finite_part<T>(across(j, db)), p, acc[db]);
+            __builtin_amdgcn_sched_barrier(0);      // no operands ahead: registers are short here
+        }
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i)        // -0 stands for a hidden pair
