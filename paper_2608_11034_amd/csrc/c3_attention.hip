@@ -490,10 +490,11 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
     const int64_t token = row / a.heads, b = token / tokens.d;
     const int head = (int)(row - token * a.heads);
     if (lane == 0) a.lse[row] = none ? -__builtin_inff() : (top + __log2f(total)) * kLn2;
-    if (2 * lane >= a.dim) return;
+    // Every lane stays to the end, whatever the head's size: lane p has part p's factor.
+    // Those behind the head take its last elements again.
     float x = 0.0f, y = 0.0f;
     const uint64_t full = __ballot(l != 0.0f);
-    const float* from = a.side[0].part + row * a.dim + 2 * lane;
+    const float* from = a.side[0].part + row * a.dim + min(2 * lane, a.dim - 2);
     for (int p0 = 0; p0 < parts; p0 += 8) {         // eight parts' loads together
         float2 v[8];
 #pragma unroll
@@ -507,6 +508,7 @@ __global__ __launch_bounds__(256) void attn_join_parts_kernel(AttnArgs a, int64_
             y = fmaf(v[j].y, g, y);
         }
     }
+    if (2 * lane >= a.dim) return;
     const float inv = none ? 0.0f : 1.0f / total;
     T e[2] = {(T)(none ? 0.0f : x * inv), (T)(none ? 0.0f : y * inv)};
     uint32_t two;
