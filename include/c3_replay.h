@@ -94,6 +94,11 @@ typedef struct {
     int64_t stride[3];      /* batch, token, head */
 } c3_attn_tensor_t;
 
+/* Sequences whose lengths go along with a kernel's arguments.  Longer lists are
+ * staged through host memory that later calls use again, so a stream under graph
+ * capture refuses them (C3_E_UNSUPPORTED): a replay would read another call's list. */
+#define C3_ATTENTION_CAPTURE_SEQUENCES 112
+
 /* Device workspace bytes of c3_attention and of c3_attention_grad (256 at
  * least; 0 on invalid arguments). */
 size_t c3_attention_workspace_size(const c3_attention_t *a);
@@ -111,10 +116,9 @@ size_t c3_attention_grad_workspace_size(const c3_attention_t *a);
  *   [batch][q_tokens][heads] (packed: [q_tokens][heads]).
  *   ws  256-byte aligned, c3_attention_workspace_size(a) bytes, not used by
  *       another call at the same time.
- * With lengths of more than 128 sequences the table of sequences is staged
- * through the workspace; such a call cannot be captured.
- * Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, dim), C3_E_WORKSPACE,
- * C3_E_HIP.
+ * Can be captured, with lengths of C3_ATTENTION_CAPTURE_SEQUENCES sequences at most.
+ * Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, dim, capture with more
+ * sequences), C3_E_WORKSPACE, C3_E_HIP.
  */
 int c3_attention(const c3_attention_t *a, const c3_attn_tensor_t *q, const c3_attn_tensor_t *k,
                  const c3_attn_tensor_t *v, const c3_attn_tensor_t *out, float *lse, void *ws,

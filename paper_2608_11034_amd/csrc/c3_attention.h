@@ -52,8 +52,8 @@ struct AttnSeq {
 };
 
 // Sequences that go along as a kernel's argument (4,096 bytes at most in all);
-// longer lists are staged.
-constexpr int kAttnArgSeqs = 112;
+// longer lists are staged, which a capture cannot record.
+constexpr int kAttnArgSeqs = C3_ATTENTION_CAPTURE_SEQUENCES;
 
 struct AttnTable {
     int32_t n;              // 0: every sequence has q_tokens and k_tokens
@@ -487,6 +487,9 @@ int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
     return n;
 }
 size_t attn_table_bytes(const c3_attention_t* a);
+// Stages a list of sequences that does not go along as an argument at `to`; refuses
+// a stream under capture.
+int attn_stage(const c3_attention_t* a, AttnPlan& p, char* to, hipStream_t s);
 
 // The passes of the gradient; the plan's units are numbered.
 hipError_t launch_attn_dq(const AttnPlan& p, bool bf16, hipStream_t s);

@@ -677,6 +677,18 @@ size_t attn_table_bytes(const c3_attention_t* a) {
     return a->q_lens != nullptr && a->batch > kAttnArgSeqs ? align256(sizeof(AttnSeq) * (size_t)a->batch) : 0;
 }
 
+int attn_stage(const c3_attention_t* a, AttnPlan& p, char* to, hipStream_t s) {
+    if (p.seqs == nullptr) return C3_OK;
+    // A captured fetch would read its pinned slot again at every replay, when the slot
+    // holds what a later call staged there.
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &status) != hipSuccess) return C3_E_HIP;
+    if (status != hipStreamCaptureStatusNone) return C3_E_UNSUPPORTED;
+    if (stage_bytes(to, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;
+    p.table.staged = reinterpret_cast<const AttnSeq*>(to);
+    return C3_OK;
+}
+
 int attn_plan(const c3_attention_t* a, AttnPlan& p) {
     if (a == nullptr || a->batch < 0 || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads != 0 ||
         a->heads > 65536 || a->dim < 1 || a->q_tokens < 0 || a->k_tokens < 0 || a->window < 0 ||
@@ -805,10 +817,7 @@ int c3_attention(const c3_attention_t* a, const c3_attn_tensor_t* q, const c3_at
         p.args.split_keys = (int32_t)f.split_keys;
         p.args.part_ml = reinterpret_cast<float*>(base + f.part_ml);
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        if (p.seqs != nullptr) {
-            if (stage_bytes(base + f.table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess) return C3_E_HIP;
-            p.table.staged = reinterpret_cast<const AttnSeq*>(base + f.table);
-        }
+        if ((rc = attn_stage(a, p, base + f.table, s)) != C3_OK) return rc;
         hipError_t e;
         if (a->dtype == C3_BF16)
             e = a->dim > 64 ? launch_forward<__bf16, 128>(p, f.tokens, s) : launch_forward<__bf16, 64>(p, f.tokens, s);

@@ -201,11 +201,7 @@ int c3_attention_grad(const c3_attention_t* a, const c3_attn_tensor_t* dout,
         }
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
         const bool bf16 = a->dtype == C3_BF16, wide = a->dim > 64;
-        if (p.seqs != nullptr && p.rows + p.key_rows > 0) {
-            if (stage_bytes(base + sp.table, p.seqs, sizeof(AttnSeq) * (size_t)a->batch, s) != hipSuccess)
-                return C3_E_HIP;
-            p.table.staged = reinterpret_cast<const AttnSeq*>(base + sp.table);
-        }
+        if (p.rows + p.key_rows > 0 && (rc = attn_stage(a, p, base + sp.table, s)) != C3_OK) return rc;
         if (p.rows > 0 && launch_attn_dq(p, bf16, s) != hipSuccess) return C3_E_HIP;
         if (p.key_rows > 0 && launch_attn_dkv(p, bf16, s) != hipSuccess) return C3_E_HIP;
         if ((g.causal || g.window) && p.rows > 0 && p.key_rows > 0) {

@@ -31,6 +31,7 @@ from .c3 import BF16, F16, F32, C3Error, _check, _dev_tensor, _empty, _ptr, _str
 HALF, INTERLEAVED = 0, 1
 MAX_HEAD_DIM = 128
 MAX_EXPERTS, MAX_TOP = 512, 64
+MAX_CAPTURED_SEQUENCES = 112
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _LAYOUT = {"half": HALF, "interleaved": INTERLEAVED}
@@ -306,7 +307,9 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: float = 
     D a multiple of 8 up to 128, H a multiple of Hk.  Lengths are host integers.
     ``causal`` lines the last query up with the last key; ``window`` > 0 leaves
     each query that many keys.  ``scale`` defaults to D ** -0.5.  lse is fp32
-    [.., H]; a row that sees no key has out 0 and lse -inf."""
+    [.., H]; a row that sees no key has out 0 and lse -inf.  A graph can capture the
+    call and its gradient with the lengths of up to 112 sequences (more are refused
+    there); the lengths are those of the capture at every replay."""
     a, keep = _attention_args(q, k, v, causal, window, scale, q_lens, k_lens)
     out = _out(out, "out", q.shape, q.dtype, q.device, stream)
     lse = _new(q.shape[:-1], torch.float32, q.device, stream) if lse is None else _lse(lse, q)
