@@ -66,6 +66,9 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
 
     f32x16 dk[NT][NDB] = {}, dv[NT][NDB] = {};
     uint32_t bad = 0;
+    float factor[NT];       // of dS
+#pragma unroll
+    for (int m = 0; m < NT; ++m) factor[m] = kDsScaled<T> ? kDsFactor : 1.0f;
 
     auto load = [&](int t, char* qt, char* gt, float* st) {
         const int row0 = t * kTileRows, rows = min(kTileRows, n_rows - row0);
@@ -155,6 +158,7 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
                 for (int i = 0; i < 4; ++i) {
                     s[m][4 * q + i] = __builtin_amdgcn_exp2f(fmaf(s[m][4 * q + i], cs, -l2[i]));
                     dp[m][4 * q + i] = s[m][4 * q + i] * (dp[m][4 * q + i] - de[i]);
+                    if constexpr (kDsScaled<T>) dp[m][4 * q + i] *= factor[m];
                 }
         }
     };
@@ -211,6 +215,11 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
                         dp[m][i] = see ? dp[m][i] : 0.0f;
                     }
                 }
+            }
+            if constexpr (kDsScaled<T>)
+#pragma unroll
+                for (int m = 0; m < NT; ++m) fit_ds<NDB>(dp[m], dk[m], factor[m]);
+            if (masked) {
                 const char *q_sub = qt + n * kSub, *g_sub = gt + n * kSub;
                 const uint32_t here = tile_not_finite<T>(KS, [&](int ks) { return rd.along(q_sub, ks); }) |
                                       tile_not_finite<T>(KS, [&](int ks) { return rd.along(g_sub, ks); });
@@ -250,6 +259,13 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
         const int k = key + 32 * m;
         if (k >= k_pad) continue;
         const bool valid = k < w.k_len;
+        if constexpr (kDsScaled<T>) {
+            const float back = 1.0f / factor[m];
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dk[m][db][i] *= back;
+        }
         if (side.splits.d > 1) {
             // dk and dv of this part, in fp32 and not yet scaled
             const int64_t keys = (int64_t)(a.packed ? 0 : w.b) * a.k_tokens + w.k_start + k;

@@ -89,6 +89,8 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
 
     f32x16 acc[NDB] = {};
     uint32_t bad = 0;
+    float factor = kDsScaled<T> ? kDsFactor : 1.0f;     // of dS: it comes with the probabilities
+    float shift = kDsScaled<T> ? 64.0f - lse2 : -lse2;
 
     auto load = [&](int t, char* kt, char* vt) {
         const int key = t * kDqKeys;
@@ -139,7 +141,7 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -lse2)) * (dp[i] - delta);
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, shift)) * (dp[i] - delta);
             uint32_t seen = 0;
             if (masked) {
 #pragma unroll
@@ -149,6 +151,9 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
                     seen |= see ? 1u << i : 0u;
                     s[i] = see ? s[i] : 0.0f;
                 }
+            }
+            if constexpr (kDsScaled<T>) shift -= fit_ds<NDB>(s, acc, factor);
+            if (masked) {
                 const char* sub = kt + n * kSub;
                 const uint32_t here = tile_not_finite<T>(KS, [&](int ks) { return rd.along(sub, ks); });
                 bad |= here;
@@ -183,6 +188,13 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
     }
 
     if (!there) return bad != 0;
+    if constexpr (kDsScaled<T>) {
+        const float back = 1.0f / factor;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] *= back;
+    }
     if (side.splits.d > 1) {
         // this part's sum, in fp32 and not yet scaled
         float* to = side.part + (part * side.part_rows + seq_row(a, w) + (int64_t)pos * a.heads + head) * a.dim;
