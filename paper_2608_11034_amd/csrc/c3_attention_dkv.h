@@ -191,7 +191,9 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
             const int pb = (int)a.group.quot(min(row0 + 31, n_rows - 1)) + off;
             if (a.causal && wkey > pb) continue;
             if (a.window && wkey + kWaveKeys - 1 <= pa - a.window) continue;
-            const bool masked = (a.causal && wkey + kWaveKeys - 1 > pa) || (a.window && wkey <= pb - a.window);
+            // rows behind the last hold zeros, which times an infinite key is NaN: hidden too
+            const bool masked = (a.causal && wkey + kWaveKeys - 1 > pa) || (a.window && wkey <= pb - a.window) ||
+                                row0 + 32 > n_rows;
             f32x16 s[NT] = {}, dp[NT] = {};
             uint32_t seen[NT] = {};
             scores(n, qt, gt, s, dp);
@@ -205,7 +207,8 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
                     // rows from r_lo to below r_hi of these 32 see the lane's key
                     const int64_t at = (int64_t)(k_ + 32 * m - off) * G - row0, all = (int64_t)a.window * G;
                     const int r_lo = a.causal ? (int)min(max(at, (int64_t)0), (int64_t)32) : 0;
-                    const int r_hi = a.window ? (int)min(max(at + all, (int64_t)0), (int64_t)32) : 32;
+                    const int r_hi = min(a.window ? (int)min(max(at + all, (int64_t)0), (int64_t)32) : 32,
+                                         n_rows - row0);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int r = (i >> 2) * 8 + h_ + (i & 3);
