@@ -15,8 +15,9 @@ constexpr int kDqKeys = 64;         // keys of a tile
 constexpr int kShortWalk = 2;       // tiles
 
 // Returns whether a tile that the mask cuts held an infinity or NaN, which only
-// CAREFUL keeps from rows that do not see it.
-template <typename T, int DP, bool CAREFUL>
+// CAREFUL keeps from rows that do not see it.  REPEATED: lse2 and delta are there, and
+// workgroups beside this one read them.
+template <typename T, int DP, bool CAREFUL, bool REPEATED = false>
 __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
     constexpr int kRows = 32 * kAttnWaves;
@@ -78,7 +79,7 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
             const float lse = a.lse[at];
             if (lse != -__builtin_inff()) lse2 = lse * kLog2e;
         }
-        if (there && h == 0 && part == 0) a.lse2[at] = lse2;
+        if (!REPEATED && there && h == 0 && part == 0) a.lse2[at] = lse2;
     }
 
     TileReads<DP> rd;
@@ -125,7 +126,7 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
         }
         delta = sum + __shfl_xor(sum, 32);
     }
-    if (there && h == 0 && part == 0) a.delta[seq_row(a, w) + (int64_t)pos * a.heads + head] = delta;
+    if (!REPEATED && there && h == 0 && part == 0) a.delta[seq_row(a, w) + (int64_t)pos * a.heads + head] = delta;
 
     auto step = [&](int t, const char* kt, const char* vt) {
 #pragma unroll

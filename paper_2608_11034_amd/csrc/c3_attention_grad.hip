@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_grad_careful_kernel(Attn
     const uint32_t half = gridDim.x / 2;
     if (blockIdx.x < half)
         repeat_marked(a.side[0].marks, q_blocks, blockIdx.x, half,
-                      [&](uint32_t unit) { dq_unit<T, DP, true>(a, tab, unit); });
+                      [&](uint32_t unit) { dq_unit<T, DP, true, true>(a, tab, unit); });
     else
         repeat_marked(a.side[1].marks, k_blocks, blockIdx.x - half, half,
                       [&](uint32_t unit) { dkv_unit<T, DP, kDkvTiles, true>(a, tab, unit); });
