@@ -130,9 +130,9 @@ int c3_attention(const c3_attention_t *a, const c3_attn_tensor_t *q, const c3_at
  * dout * out over a head,
  *     dv = P^T dout,  dS = P (dout v^T - delta),
  *     dq = scale dS k,  dk = scale dS^T q,
- * key heads summing over the query heads that share them.  Where a tile of queries
- * sees at most 128 keys delta is the sum of P * dout v^T, which the output's rounding
- * does not enter.  out and lse are those of c3_attention for the same arguments.
+ * key heads summing over the query heads that share them.  Where a query of a tile sees
+ * 16 keys or fewer, or the tile spans at most two blocks of 64 keys, its delta is the sum
+ * of P * dout v^T, which the output's rounding does not enter.  out and lse are those of c3_attention for the same arguments.
  * Padding rows get zeros.  Results are deterministic.  Workspace and errors as c3_attention.
  */
 int c3_attention_grad(const c3_attention_t *a, const c3_attn_tensor_t *dout,

@@ -13,6 +13,7 @@ namespace c3 {
 
 constexpr int kDqKeys = 64;         // keys of a tile
 constexpr int kShortWalk = 2;       // tiles
+constexpr int kFewKeys = 16;
 
 // Returns whether a tile that the mask cuts held an infinity or NaN, which only
 // CAREFUL keeps from rows that do not see it.  REPEATED: lse2 and delta are there, and
@@ -99,9 +100,15 @@ __device__ __forceinline__ bool dq_unit(const AttnArgs& a, const AttnTable& tab,
         load_tile<DP, kDqKeys>(vb + (int64_t)key * a.v.st, a.v.st, a.dim, w.k_len - key, v_off, vt);
     };
     // Rows that see few keys have an output near the values' size, and its rounding to 16
-    // bits would enter delta as much as that of dS enters the product: for them delta is
-    // the sum of P dP, which needs no output.  Over 128 keys it is a fiftieth of it.
-    if (all1 - all0 <= kShortWalk) {
+    // bits would enter delta as much as that of dS enters the product (bf16, two keys: dq
+    // off by 0.0036 in the norm, not 0.0023): for them delta is the sum of P dP, which
+    // needs no output.  From 16 keys on it shows no more; the walk over a tile with a row
+    // of so few is of 16 and a tile's rows at most.  Two tiles of keys cost little, so
+    // they go this way too.
+    int fewest = INT32_MAX;
+    if (a.causal) fewest = first + off + 1;
+    if (a.window) fewest = min(fewest, a.causal ? a.window : w.q_len - 1 - last + a.window);
+    if (all1 - all0 <= kShortWalk || fewest <= kFewKeys) {
         float sum = 0.0f;
         for (int t = all0; t < all1; ++t) {
             load(t, k0, v0);
