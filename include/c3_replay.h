@@ -117,8 +117,9 @@ size_t c3_attention_grad_workspace_size(const c3_attention_t *a);
  *   ws  256-byte aligned, c3_attention_workspace_size(a) bytes, not used by
  *       another call at the same time.
  * Can be captured, with lengths of C3_ATTENTION_CAPTURE_SEQUENCES sequences at most.
- * Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, dim, capture with more
- * sequences), C3_E_WORKSPACE, C3_E_HIP.
+ * Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, dim, 2^24 tiles of rows or
+ * blocks of keys over all key heads or more, capture with more sequences),
+ * C3_E_WORKSPACE, C3_E_HIP.
  */
 int c3_attention(const c3_attention_t *a, const c3_attn_tensor_t *q, const c3_attn_tensor_t *k,
                  const c3_attn_tensor_t *v, const c3_attn_tensor_t *out, float *lse, void *ws,

@@ -500,9 +500,11 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p);
 int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTensor& to);
 // Numbers the units of each sequence on one side, of which `units_of(queries, k_len,
 // keys)` (queries and keys with the padding of a dense batch) gives the count, and
-// returns those of one key head, or -1 where there are too many.
+// returns those of one key head, or -1 where a launch of kAttnThreads threads a unit and
+// key head would pass the 2^32 that its dimension holds.  Not to be launched: the number
+// alone, whatever it is.
 template <typename F>
-int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
+int64_t attn_number(AttnPlan& p, int batch, int side, F units_of, bool launched = true) {
     AttnSide& d = p.args.side[side];
     int64_t n = 0;
     if (p.table.n == 0) {
@@ -514,10 +516,11 @@ int64_t attn_number(AttnPlan& p, int batch, int side, F units_of) {
             s[i].unit0[side] = (int32_t)n;
             n += units_of(p.args.packed ? s[i].q_len : p.args.q_tokens, s[i].k_len,
                           p.args.packed ? s[i].k_len : p.args.k_tokens);
-            if (n >= (1ll << 31)) return -1;
+            if (launched && n >= (1ll << 31)) return -1;
         }
     }
-    if (n * p.args.kv_heads >= (1ll << 31)) return -1;
+    if (!launched) return n;
+    if (n >= (1ll << 31) || n * p.args.kv_heads >= (1ll << 32) / kAttnThreads) return -1;
     d.units = (uint32_t)(n < 1 ? 1 : n);
     return n;
 }

@@ -624,7 +624,7 @@ struct ForwardShape {
             return kv * attn_number(p, a->batch, 0, [&](int64_t nq, int64_t nk, int64_t) {
                 const int64_t t = (nq * group + rows - 1) / rows;
                 return split ? t * std::max<int64_t>(1, (nk + split - 1) / split) : t;
-            });
+            }, split != 1);
         };
         split_keys = 0;
         parts = 1;

@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const T
     // a piece that is only moved: kept as one word, or the compiler holds it in LDS
     using Word = std::conditional_t<sizeof(Piece<T, V>) == 16, u32x4, T>;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t waves = (int64_t)gridDim.x * 4;
+    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
+    const int64_t waves = wide_blocks() * 4;
     const int64_t token = w / a.parts, c0 = (w - token * a.parts) * 64 * U + lane;
     const int64_t kept = max(*a.kept, 0);
     if (token < a.tokens) {
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const T
 template <typename T, int V, int U>
 __global__ __launch_bounds__(256) void expert_combine_kernel(RowArgs a, const T* sorted, T* out) {
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
     const int64_t token = w / a.parts, c0 = (w - token * a.parts) * 64 * U + lane;
     if (token >= a.tokens) return;
     const uint32_t rows = (uint32_t)(a.tokens * a.top);     // a slot outside is a dropped choice
@@ -257,7 +257,8 @@ __global__ __launch_bounds__(256) void expert_combine_grad_kernel(RowArgs a, con
                                                                   const T* sorted, T* dsorted) {
     __shared__ float part[4][C3_MAX_EXPERT_TOP];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = blockIdx.x, kept = max(*a.kept, 0);
+    const int64_t token = wide_block(), kept = max(*a.kept, 0);
+    if (token >= a.tokens) return;          // zero_tail's waves are those of tokens
     const uint32_t rows = (uint32_t)(a.tokens * a.top);     // a slot outside is a dropped choice
     const int32_t my_slot = lane < a.top ? a.slot[token * a.top + lane] : -1;
     float my_weight = 1.0f;
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(256) void expert_combine_grad_kernel(RowArgs a, con
             a.dweights[token * a.top + threadIdx.x] =
                 part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
     }
-    zero_tail<T, V>(a, dsorted, kept, token * 4 + wave, (int64_t)gridDim.x * 4);
+    zero_tail<T, V>(a, dsorted, kept, token * 4 + wave, a.tokens * 4);
 }
 
 enum class Move { kDispatch, kCombine, kGrad };
@@ -317,7 +318,7 @@ hipError_t launch_rows(Move m, RowArgs a, int64_t hidden, const void* in, const 
                        hipStream_t s) {
     a.pieces = hidden / V;
     if (m == Move::kGrad) {
-        const dim3 grid((unsigned)a.tokens), block(256);
+        const dim3 grid = wide_grid((uint64_t)a.tokens), block(256);
         if (a.pieces > 512)
             expert_combine_grad_kernel<T, V, 4><<<grid, block, 0, s>>>(a, (const T*)in, (const T*)sorted, (T*)to);
         else if (a.pieces > 256)
@@ -329,7 +330,7 @@ hipError_t launch_rows(Move m, RowArgs a, int64_t hidden, const void* in, const 
     const int64_t parts4 = (a.pieces + 255) / 256;
     const bool few = a.tokens * parts4 < kFewWaves;
     a.parts = (uint32_t)(few ? (a.pieces + 63) / 64 : parts4);
-    const dim3 grid((unsigned)((a.tokens * a.parts + 3) / 4)), block(256);
+    const dim3 grid = wide_grid((uint64_t)(a.tokens * a.parts + 3) / 4), block(256);
     if (m == Move::kDispatch) {
         if (few)
             expert_dispatch_kernel<T, V, 1><<<grid, block, 0, s>>>(a, (const T*)in, (T*)to);

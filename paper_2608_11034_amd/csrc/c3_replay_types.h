@@ -40,6 +40,16 @@ struct FastDiv {
     }
 };
 
+// A launch dimension holds fewer than 2^32 threads, and one with more is cut off without
+// an error.  So grids that may pass that have two dimensions; the last workgroups of
+// the second may have nothing to do.
+inline dim3 wide_grid(uint64_t blocks) {
+    constexpr uint64_t kRow = 1u << 22;         // workgroups of 256 threads
+    return blocks <= kRow ? dim3((unsigned)blocks) : dim3((unsigned)kRow, (unsigned)((blocks + kRow - 1) / kRow));
+}
+__device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+__device__ __forceinline__ int64_t wide_blocks() { return (int64_t)gridDim.y * gridDim.x; }
+
 inline int replay_elem_size(int dtype) {
     return dtype == C3_F32 ? 4 : dtype == C3_BF16 || dtype == C3_F16 ? 2 : 0;
 }

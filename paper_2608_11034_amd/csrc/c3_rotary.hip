@@ -54,7 +54,8 @@ template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     extern __shared__ float2 turn[];        // [block_tokens][rot / 2]
     const int half = a.rot / 2;
-    const int64_t tok0 = (int64_t)blockIdx.x * a.block_tokens;
+    const int64_t tok0 = wide_block() * a.block_tokens;
+    if (tok0 >= a.tokens) return;
     const int nt = (int)min((int64_t)a.block_tokens, a.tokens - tok0);
     const bool pairs_apart = V == 1 || !a.interleaved;
     const int turned = pairs_apart ? half / V : a.rot / V;
@@ -151,7 +152,7 @@ template <typename T, int V>
 hipError_t launch(const RotaryArgs& a, hipStream_t s) {
     const int64_t blocks = (a.tokens + a.block_tokens - 1) / a.block_tokens;
     const size_t lds = sizeof(float2) * (size_t)a.block_tokens * (size_t)(a.rot / 2);
-    rotary_kernel<T, V><<<dim3((unsigned)blocks), dim3(kThreads), lds, s>>>(a);
+    rotary_kernel<T, V><<<wide_grid((uint64_t)blocks), dim3(kThreads), lds, s>>>(a);
     return hipGetLastError();
 }
 

@@ -1,4 +1,5 @@
 """Limits of the replay operators that stand in more than one place, without a GPU."""
+import ctypes
 import os
 import re
 
@@ -32,3 +33,19 @@ def test_nothing_is_staged_unasked():
     body = _read("paper_2608_11034_amd", "csrc", "c3_attention.hip")
     at = body.index("int attn_stage(")
     assert at < body.index("hipStreamIsCapturing", at) < body.index("stage_bytes(", at) < body.index("\n}", at)
+
+
+def _attention(batch, kv_heads, grad=False):
+    """Workspace bytes of one token a sequence on one key (0: refused)."""
+    a = replay.Attention(dtype=replay.BF16, heads=kv_heads, kv_heads=kv_heads, dim=8, causal=1, window=0, scale=1.0,
+                         batch=batch, q_tokens=1, k_tokens=1)
+    f = replay._lib().c3_attention_grad_workspace_size if grad else replay._lib().c3_attention_workspace_size
+    return f(ctypes.byref(a))
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_workgroups_of_attention(grad):
+    """A launch holds fewer than 2^32 threads, 256 to a workgroup: more are refused
+    before anything is launched."""
+    assert _attention(2 ** 14 - 1, 2 ** 10, grad) > 0
+    assert _attention(2 ** 14, 2 ** 10, grad) == 0 and _attention(2 ** 16, 2 ** 12, grad) == 0
