@@ -379,13 +379,28 @@ def expert_sort(ids: torch.Tensor, num_experts: int, *, workspace=None, stream=N
     return order
 
 
+def _check_order(order):
+    """An order that the kernels can follow: ``ExpertOrder`` is a plain tuple, and they
+    read the number of kept rows behind the last expert's first."""
+    offsets, source, slot = order
+    i32 = torch.int32
+    try:
+        dev = slot.device
+        fine = (slot.is_cuda and slot.dtype == i32 and slot.dim() == 2 and slot.is_contiguous() and
+                offsets.dtype == i32 and offsets.device == dev and offsets.dim() == 1 and
+                offsets.numel() > 1 and offsets.is_contiguous() and
+                source.dtype == i32 and source.device == dev and source.numel() == slot.numel() and
+                source.dim() == 1 and source.is_contiguous())
+    except AttributeError:
+        fine = False
+    if not fine:
+        raise C3Error("the order must be that of expert_sort: int32 offsets [experts + 1], source "
+                      "[tokens * top] and slot [tokens, top], contiguous and on one device")
+
+
 def _expert_rows(order, token_rows, sorted_rows, dtype):
     """c3_expert_rows_t of both sides' tensors."""
-    for t, n in zip(order, ("offsets", "source", "slot")):
-        _dev_tensor(t, n)
-        if t.dtype != torch.int32:
-            raise C3Error(f"{n} must be int32")
-    slot, dev = order.slot, order.slot.device
+    slot, offsets, dev = order.slot, order.offsets, order.slot.device
     T, top = slot.shape
     stride = []
     for t, n, rows in ((token_rows, "tokens' rows", T), (sorted_rows, "sorted rows", T * top)):
@@ -398,7 +413,6 @@ def _expert_rows(order, token_rows, sorted_rows, dtype):
     H = token_rows.shape[1]
     if H != sorted_rows.shape[1]:
         raise C3Error("the rows must have one hidden size")
-    offsets = order.offsets
     return stride[1], _EXPERT_ROWS.pack(_CODE[dtype], top, T, H, *stride, slot.data_ptr(),
                                         offsets.data_ptr() + 4 * (offsets.numel() - 1))
 
@@ -417,6 +431,7 @@ def expert_dispatch(x, order: ExpertOrder, *, out=None, stream=None):
     """Rows [T * top, hidden] sorted by expert from tokens x [T, hidden]; the
     rows behind the last kept choice are zeros."""
     _rows(x, "x", dim=(2,))
+    _check_order(order)
     out = _out(out, "out", (order.slot.numel(), x.shape[1]), x.dtype, x.device, stream)
     r = _expert_rows(order, x, out, x.dtype)[1]
     _check(_lib().c3_expert_dispatch(r, _ptr(x), _ptr(out), _stream(stream)),
@@ -428,6 +443,7 @@ def expert_combine(y, order: ExpertOrder, weights=None, *, out=None, stream=None
     """out[t] = sum over t's choices of weight * y[their place]; y [T * top,
     hidden], weights fp32 [T, top] or None (ones)."""
     _rows(y, "y", dim=(2,))
+    _check_order(order)
     out = _out(out, "out", (order.slot.shape[0], y.shape[1]), y.dtype, y.device, stream)
     weights = _weights(weights, order)
     r = _expert_rows(order, out, y, y.dtype)[1]
@@ -440,6 +456,7 @@ def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, s
     """(dy [T * top, hidden], dweights fp32 [T, top]) of ``expert_combine``;
     without weights dweights is None (and y may be)."""
     _rows(dout, "dout", dim=(2,))
+    _check_order(order)
     weights = _weights(weights, order)
     dy = _out(dy, "dy", (order.slot.numel(), dout.shape[1]), dout.dtype, dout.device, stream)
     sorted_stride, r = _expert_rows(order, dout, dy, dout.dtype)
