@@ -88,7 +88,7 @@ typedef struct {
 
 /* A tensor [batch][tokens][heads][dim] (packed: [tokens][heads][dim], stride[0]
  * unused), last dimension contiguous; pointers 16-byte aligned and strides
- * multiples of 8 elements. */
+ * multiples of 8 elements (that of a dimension with one entry is not looked at). */
 typedef struct {
     void *ptr;
     int64_t stride[3];      /* batch, token, head */

@@ -761,14 +761,21 @@ int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTen
     }
     if (t->ptr == nullptr) return C3_E_INVAL;
     if ((uintptr_t)t->ptr % 16 != 0) return C3_E_ALIGN;
-    for (int i = g.packed ? 1 : 0; i < 3; ++i) {
+    // The stride of a dimension with one entry says nothing.  A row's length stands for
+    // the tokens', so that rows behind a tile's only one lie behind its end.
+    const int64_t entries[3] = {g.packed ? 1 : (int64_t)g.batch.d, keys ? g.k_tokens : g.q_tokens,
+                                keys ? g.kv_heads : g.heads};
+    int64_t stride[3] = {0, g.dim, 0};
+    for (int i = 0; i < 3; ++i) {
+        if (entries[i] == 1) continue;
         if (t->stride[i] < 0 || t->stride[i] >= (1ll << 40)) return C3_E_INVAL;
         if (t->stride[i] % 8 != 0) return C3_E_ALIGN;
+        stride[i] = t->stride[i];
     }
     to.ptr = static_cast<char*>(t->ptr);
-    to.sb = g.packed ? 0 : t->stride[0] * 2;
-    to.st = t->stride[1] * 2;
-    to.sh = t->stride[2] * 2;
+    to.sb = stride[0] * 2;
+    to.st = stride[1] * 2;
+    to.sh = stride[2] * 2;
     // a tile is addressed with 31 bits from its first row
     if (to.st * 64 + to.sh * (int64_t)g.group.d >= (1ll << 31) - 4096) return C3_E_UNSUPPORTED;
     return C3_OK;
