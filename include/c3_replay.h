@@ -88,7 +88,9 @@ typedef struct {
 
 /* A tensor [batch][tokens][heads][dim] (packed: [tokens][heads][dim], stride[0]
  * unused), last dimension contiguous; pointers 16-byte aligned and strides
- * multiples of 8 elements (that of a dimension with one entry is not looked at). */
+ * multiples of 8 elements (that of a dimension with one entry is not looked at).  Of k
+ * and v 64 tokens span less than 2^31 bytes; of the gradient's q and dout 64 tokens
+ * together with the heads that share a key head (C3_E_UNSUPPORTED). */
 typedef struct {
     void *ptr;
     int64_t stride[3];      /* batch, token, head */

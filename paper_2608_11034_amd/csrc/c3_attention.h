@@ -496,8 +496,12 @@ struct AttnPlan {
     AttnSeq* list() { return seqs != nullptr ? seqs : table.seq; }
 };
 
+// How a tensor's tiles are addressed: row by row with 64 bits, or with 31 from the first
+// of 64 tokens of a head, or of all heads that share a key head.
+enum class Tiles { kNone, kHead, kGroup };
+
 int attn_plan(const c3_attention_t* a, AttnPlan& p);
-int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTensor& to);
+int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, Tiles tiles, AttnTensor& to);
 // Numbers the units of each sequence on one side, of which `units_of(queries, k_len,
 // keys)` (queries and keys with the padding of a dense batch) gives the count, and
 // returns those of one key head, or -1 where a launch of kAttnThreads threads a unit and

@@ -751,7 +751,7 @@ int attn_plan(const c3_attention_t* a, AttnPlan& p) {
     return C3_OK;
 }
 
-int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTensor& to) {
+int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, Tiles tiles, AttnTensor& to) {
     if (t == nullptr) return C3_E_INVAL;
     const AttnArgs& g = p.args;
     const bool none = (keys ? p.key_rows : p.rows) == 0;
@@ -776,8 +776,8 @@ int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, AttnTen
     to.sb = stride[0] * 2;
     to.st = stride[1] * 2;
     to.sh = stride[2] * 2;
-    // a tile is addressed with 31 bits from its first row
-    if (to.st * 64 + to.sh * (int64_t)g.group.d >= (1ll << 31) - 4096) return C3_E_UNSUPPORTED;
+    const int64_t span = tiles == Tiles::kNone ? 0 : to.st * 64 + (tiles == Tiles::kGroup ? to.sh * (g.group.d - 1) : 0);
+    if (span >= (1ll << 31) - 4096) return C3_E_UNSUPPORTED;
     return C3_OK;
 }
 
@@ -804,10 +804,10 @@ int c3_attention(const c3_attention_t* a, const c3_attn_tensor_t* q, const c3_at
         AttnPlan p;
         int rc = attn_plan(a, p);
         if (rc != C3_OK) return rc;
-        if ((rc = attn_tensor(q, p, false, p.args.q)) != C3_OK) return rc;
-        if ((rc = attn_tensor(k, p, true, p.args.k)) != C3_OK) return rc;
-        if ((rc = attn_tensor(v, p, true, p.args.v)) != C3_OK) return rc;
-        if ((rc = attn_tensor(out, p, false, p.args.o)) != C3_OK) return rc;
+        if ((rc = attn_tensor(q, p, false, Tiles::kNone, p.args.q)) != C3_OK) return rc;
+        if ((rc = attn_tensor(k, p, true, Tiles::kHead, p.args.k)) != C3_OK) return rc;
+        if ((rc = attn_tensor(v, p, true, Tiles::kHead, p.args.v)) != C3_OK) return rc;
+        if ((rc = attn_tensor(out, p, false, Tiles::kNone, p.args.o)) != C3_OK) return rc;
         if (p.rows > 0 && lse == nullptr) return C3_E_INVAL;
         if ((uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
         const ForwardShape f(a, p);

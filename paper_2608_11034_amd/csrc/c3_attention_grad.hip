@@ -178,14 +178,14 @@ int c3_attention_grad(const c3_attention_t* a, const c3_attn_tensor_t* dout,
         int rc = attn_plan(a, p);
         if (rc != C3_OK) return rc;
         AttnArgs& g = p.args;
-        if ((rc = attn_tensor(dout, p, false, g.d_o)) != C3_OK) return rc;
-        if ((rc = attn_tensor(q, p, false, g.q)) != C3_OK) return rc;
-        if ((rc = attn_tensor(k, p, true, g.k)) != C3_OK) return rc;
-        if ((rc = attn_tensor(v, p, true, g.v)) != C3_OK) return rc;
-        if ((rc = attn_tensor(out, p, false, g.o)) != C3_OK) return rc;
-        if ((rc = attn_tensor(dq, p, false, g.dq)) != C3_OK) return rc;
-        if ((rc = attn_tensor(dk, p, true, g.dk)) != C3_OK) return rc;
-        if ((rc = attn_tensor(dv, p, true, g.dv)) != C3_OK) return rc;
+        if ((rc = attn_tensor(dout, p, false, Tiles::kGroup, g.d_o)) != C3_OK) return rc;
+        if ((rc = attn_tensor(q, p, false, Tiles::kGroup, g.q)) != C3_OK) return rc;
+        if ((rc = attn_tensor(k, p, true, Tiles::kHead, g.k)) != C3_OK) return rc;
+        if ((rc = attn_tensor(v, p, true, Tiles::kHead, g.v)) != C3_OK) return rc;
+        if ((rc = attn_tensor(out, p, false, Tiles::kNone, g.o)) != C3_OK) return rc;
+        if ((rc = attn_tensor(dq, p, false, Tiles::kNone, g.dq)) != C3_OK) return rc;
+        if ((rc = attn_tensor(dk, p, true, Tiles::kNone, g.dk)) != C3_OK) return rc;
+        if ((rc = attn_tensor(dv, p, true, Tiles::kNone, g.dv)) != C3_OK) return rc;
         if (p.rows > 0 && lse == nullptr) return C3_E_INVAL;
         if ((uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
         const GradSpace sp(a, p);
