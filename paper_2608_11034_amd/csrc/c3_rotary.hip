@@ -193,12 +193,13 @@ extern "C" int c3_rotary(const c3_heads_t* tensors, int n, int dtype, int64_t ba
         if (t.heads == 0) continue;
         if (t.in == nullptr || t.out == nullptr) return C3_E_INVAL;
         if ((uintptr_t)t.in % es != 0 || (uintptr_t)t.out % es != 0) return C3_E_ALIGN;
-        if (t.in == t.out)
-            for (int j = 0; j < 3; ++j)
-                if (t.in_stride[j] != t.out_stride[j]) return C3_E_INVAL;
         wide = wide && (uintptr_t)t.in % 16 == 0 && (uintptr_t)t.out % 16 == 0;
-        for (int j = 0; j < 3; ++j)
+        const int64_t entries[3] = {batch, length, t.heads};
+        for (int j = 0; j < 3; ++j) {
+            if (entries[j] == 1) continue;          // its stride says nothing
+            if (t.in == t.out && t.in_stride[j] != t.out_stride[j]) return C3_E_INVAL;
             wide = wide && multiple(t.in_stride[j], v) && multiple(t.out_stride[j], v);
+        }
     }
     a.t[0] = tensors[0];
     a.t[1] = tensors[n - 1];
