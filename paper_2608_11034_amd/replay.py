@@ -14,6 +14,10 @@ every step runs in the HIP kernels of libc3.so and there is no CPU fallback.
 * ``expert_dispatch(x, order)``           tokens to their experts' rows
 * ``expert_combine(y, order, weights)``   and back, weighted
 * ``expert_combine_grad``, ``expert_dispatch_grad``  their gradients
+
+The calls record no graph.  Where torch would record one, tensors that require a
+gradient are refused; under ``torch.no_grad()`` and inside the forward and backward of a
+``torch.autograd.Function`` they are taken.
 """
 from __future__ import annotations
 
@@ -99,10 +103,18 @@ def _lib():
     return _ready
 
 
+def _no_graph(t, name):
+    """Refuses a tensor whose gradient would stop here without a word."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise C3Error(f"{name} requires a gradient, which this call does not record: call it under "
+                      "torch.no_grad() or in a torch.autograd.Function")
+
+
 def _rows(t, name, dtype=None, device=None, dim=None):
     """A device tensor whose last dimension is contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise C3Error(f"{name} must be a tensor on a ROCm GPU device")
+    _no_graph(t, name)
     if t.dtype not in _CODE:
         raise C3Error(f"{name}: unsupported dtype {t.dtype}")
     if dtype is not None and t.dtype != dtype:
@@ -227,6 +239,7 @@ def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
     else:
         raise C3Error("positions must be [S] or [B, S]")
     _dev_tensor(freqs, "freqs")
+    _no_graph(freqs, "freqs")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or freqs.device != dev:
         raise C3Error("freqs must be fp64 [rot / 2] on the device of x")
     if layout not in _LAYOUT:
@@ -292,6 +305,7 @@ def _workspace(need, workspace, device, what, stream):
 
 def _lse(t, q, name="lse"):
     _dev_tensor(t, name)
+    _no_graph(t, name)
     if t.dtype != torch.float32 or t.shape != q.shape[:-1] or t.device != q.device:
         raise C3Error(f"{name} must be fp32 {tuple(q.shape[:-1])}")
     return t
@@ -421,6 +435,7 @@ def _weights(weights, order):
     if weights is None:
         return None
     _dev_tensor(weights, "weights")
+    _no_graph(weights, "weights")
     if weights.dtype != torch.float32 or (
             weights.shape != order.slot.shape or weights.device != order.slot.device):
         raise C3Error("weights must be fp32 [tokens, top] on the order's device")
