@@ -90,7 +90,9 @@ typedef struct {
  * unused), last dimension contiguous; pointers 16-byte aligned and strides
  * multiples of 8 elements (that of a dimension with one entry is not looked at).  Of k
  * and v 64 tokens span less than 2^31 bytes; of the gradient's q and dout 64 tokens
- * together with the heads that share a key head (C3_E_UNSUPPORTED). */
+ * together with the heads that share a key head (C3_E_UNSUPPORTED).  Results overlap
+ * neither inputs nor each other; one that starts where another tensor does is
+ * C3_E_INVAL. */
 typedef struct {
     void *ptr;
     int64_t stride[3];      /* batch, token, head */

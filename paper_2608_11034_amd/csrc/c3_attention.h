@@ -26,6 +26,7 @@
 #pragma once
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "c3_internal.h"
 #include "c3_replay_types.h"
@@ -528,6 +529,9 @@ int64_t attn_number(AttnPlan& p, int batch, int side, F units_of, bool launched 
     d.units = (uint32_t)(n < 1 ? 1 : n);
     return n;
 }
+// Whether one of `results` starts where another or one of `inputs` does: units that are
+// repeated read their rows again after others were written.
+bool attn_overlap(std::initializer_list<const AttnTensor*> results, std::initializer_list<const AttnTensor*> inputs);
 size_t attn_table_bytes(const c3_attention_t* a);
 // Stages a list of sequences that does not go along as an argument at `to`; refuses
 // a stream under capture.

@@ -781,6 +781,17 @@ int attn_tensor(const c3_attn_tensor_t* t, const AttnPlan& p, bool keys, Tiles t
     return C3_OK;
 }
 
+bool attn_overlap(std::initializer_list<const AttnTensor*> results, std::initializer_list<const AttnTensor*> inputs) {
+    for (const AttnTensor* r : results) {
+        if (r->ptr == nullptr) continue;
+        for (const AttnTensor* t : results)
+            if (t != r && t->ptr == r->ptr) return true;
+        for (const AttnTensor* t : inputs)
+            if (t->ptr == r->ptr) return true;
+    }
+    return false;
+}
+
 }  // namespace c3
 
 extern "C" {
@@ -814,6 +825,7 @@ int c3_attention(const c3_attention_t* a, const c3_attn_tensor_t* q, const c3_at
         if (!f.fits) return C3_E_UNSUPPORTED;
         if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)f.total) return C3_E_WORKSPACE;
         if (p.rows == 0) return C3_OK;
+        if (attn_overlap({&p.args.o}, {&p.args.q, &p.args.k, &p.args.v})) return C3_E_INVAL;
         p.args.lse = lse;
         char* base = static_cast<char*>(ws);
         AttnSide& side = p.args.side[0];

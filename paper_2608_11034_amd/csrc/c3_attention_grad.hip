@@ -191,6 +191,7 @@ int c3_attention_grad(const c3_attention_t* a, const c3_attn_tensor_t* dout,
         const GradSpace sp(a, p);
         if (!sp.fits) return C3_E_UNSUPPORTED;
         if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < sp.total) return C3_E_WORKSPACE;
+        if (attn_overlap({&g.dq, &g.dk, &g.dv}, {&g.d_o, &g.q, &g.k, &g.v, &g.o})) return C3_E_INVAL;
         char* base = static_cast<char*>(ws);
         g.lse = const_cast<float*>(lse);
         g.lse2 = reinterpret_cast<float*>(base + sp.lse2);
