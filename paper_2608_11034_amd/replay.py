@@ -30,7 +30,7 @@ from typing import NamedTuple
 import torch
 
 from . import c3
-from .c3 import BF16, F16, F32, C3Error, _check, _dev_tensor, _empty, _ptr, _stream
+from .c3 import BF16, F16, F32, C3Error, _check, _dev_tensor, _empty, _ptr, _raw_stream, _stream
 
 HALF, INTERLEAVED = 0, 1
 MAX_HEAD_DIM = 128
@@ -103,9 +103,9 @@ def _lib():
     return _ready
 
 
-def _no_graph(t, name):
-    """Refuses a tensor whose gradient would stop here without a word."""
-    if t.requires_grad and torch.is_grad_enabled():
+def _no_graph(name):
+    """Refuses a tensor that requires a gradient, which would stop here without a word."""
+    if torch.is_grad_enabled():
         raise C3Error(f"{name} requires a gradient, which this call does not record: call it under "
                       "torch.no_grad() or in a torch.autograd.Function")
 
@@ -114,7 +114,8 @@ def _rows(t, name, dtype=None, device=None, dim=None):
     """A device tensor whose last dimension is contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise C3Error(f"{name} must be a tensor on a ROCm GPU device")
-    _no_graph(t, name)
+    if t.requires_grad:
+        _no_graph(name)
     if t.dtype not in _CODE:
         raise C3Error(f"{name}: unsupported dtype {t.dtype}")
     if dtype is not None and t.dtype != dtype:
@@ -146,6 +147,16 @@ def _new(shape, dtype, device, stream):
         return _empty(shape, dtype, device)
     with torch.cuda.stream(stream):
         return _empty(shape, dtype, device)
+
+
+def _handle(stream, device):
+    """The stream's handle.  Kernels run on the current device, and the memory of another
+    one is not theirs to reach."""
+    at = torch.cuda.current_device()
+    if device.index != at or (stream is not None and stream.device != device):
+        raise C3Error(f"the tensors are on {device}: make it the current device, and pass a stream of it")
+    # c3._stream would ask for the device once more, a microsecond a call
+    return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _int32(x, name):
@@ -239,14 +250,15 @@ def rotary(x, positions, freqs, *, layout: str = "half", inverse: bool = False,
     else:
         raise C3Error("positions must be [S] or [B, S]")
     _dev_tensor(freqs, "freqs")
-    _no_graph(freqs, "freqs")
+    if freqs.requires_grad:
+        _no_graph("freqs")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or freqs.device != dev:
         raise C3Error("freqs must be fp64 [rot / 2] on the device of x")
     if layout not in _LAYOUT:
         raise C3Error(f"unknown layout {layout}")
     rc = _lib().c3_rotary(table, len(xs), _CODE[dtype], B, S, shape[-1], positions.data_ptr(),
                           positions.element_size(), pos, freqs.data_ptr(), 2 * freqs.numel(),
-                          _LAYOUT[layout], int(bool(inverse)), float(amplitude), _stream(stream))
+                          _LAYOUT[layout], int(bool(inverse)), float(amplitude), _handle(stream, dev))
     _check(rc, "c3_rotary")
     return done[0] if single else tuple(done)
 
@@ -298,6 +310,8 @@ def _workspace(need, workspace, device, what, stream):
     if workspace is None:
         return _new((need,), torch.uint8, device, stream)
     _dev_tensor(workspace, "workspace")
+    if workspace.device != device:
+        raise C3Error(f"{what} workspace must be on {device}")
     if workspace.numel() * workspace.element_size() < need:
         raise C3Error(f"{what} workspace too small")
     return workspace
@@ -305,7 +319,8 @@ def _workspace(need, workspace, device, what, stream):
 
 def _lse(t, q, name="lse"):
     _dev_tensor(t, name)
-    _no_graph(t, name)
+    if t.requires_grad:
+        _no_graph(name)
     if t.dtype != torch.float32 or t.shape != q.shape[:-1] or t.device != q.device:
         raise C3Error(f"{name} must be fp32 {tuple(q.shape[:-1])}")
     return t
@@ -330,7 +345,7 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: float = 
     ws = _workspace(_lib().c3_attention_workspace_size(a), workspace, q.device,
                     "attention", stream)
     rc = _lib().c3_attention(a, *map(_attn_tensor, (q, k, v, out)), _ptr(lse), _ptr(ws),
-                             ws.numel() * ws.element_size(), _stream(stream))
+                             ws.numel() * ws.element_size(), _handle(stream, q.device))
     _check(rc, "c3_attention")
     return out, lse
 
@@ -352,7 +367,7 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
                     "attention_grad", stream)
     rc = _lib().c3_attention_grad(a, *map(_attn_tensor, (dout, q, k, v, out)), _ptr(lse),
                                   *map(_attn_tensor, (dq, dk, dv)), _ptr(ws), ws.numel() * ws.element_size(),
-                                  _stream(stream))
+                                  _handle(stream, q.device))
     _check(rc, "c3_attention_grad")
     return dq, dk, dv
 
@@ -388,7 +403,7 @@ def expert_sort(ids: torch.Tensor, num_experts: int, *, workspace=None, stream=N
                     "expert_sort", stream)
     rc = _lib().c3_expert_sort(_ptr(ids), n, num_experts, _ptr(order.offsets), _ptr(order.source),
                                _ptr(order.slot), _ptr(ws), ws.numel() * ws.element_size(),
-                               _stream(stream))
+                               _handle(stream, dev))
     _check(rc, "c3_expert_sort")
     return order
 
@@ -435,7 +450,8 @@ def _weights(weights, order):
     if weights is None:
         return None
     _dev_tensor(weights, "weights")
-    _no_graph(weights, "weights")
+    if weights.requires_grad:
+        _no_graph("weights")
     if weights.dtype != torch.float32 or (
             weights.shape != order.slot.shape or weights.device != order.slot.device):
         raise C3Error("weights must be fp32 [tokens, top] on the order's device")
@@ -449,7 +465,7 @@ def expert_dispatch(x, order: ExpertOrder, *, out=None, stream=None):
     _check_order(order)
     out = _out(out, "out", (order.slot.numel(), x.shape[1]), x.dtype, x.device, stream)
     r = _expert_rows(order, x, out, x.dtype)[1]
-    _check(_lib().c3_expert_dispatch(r, _ptr(x), _ptr(out), _stream(stream)),
+    _check(_lib().c3_expert_dispatch(r, _ptr(x), _ptr(out), _handle(stream, x.device)),
            "c3_expert_dispatch")
     return out
 
@@ -463,7 +479,7 @@ def expert_combine(y, order: ExpertOrder, weights=None, *, out=None, stream=None
     weights = _weights(weights, order)
     r = _expert_rows(order, out, y, y.dtype)[1]
     _check(_lib().c3_expert_combine(r, _ptr(y), _ptr(weights), _ptr(out),
-                                    _stream(stream)), "c3_expert_combine")
+                                    _handle(stream, y.device)), "c3_expert_combine")
     return out
 
 
@@ -484,7 +500,7 @@ def expert_combine_grad(dout, y, order: ExpertOrder, weights=None, *, dy=None, s
             raise C3Error("y and dy must have the same row stride")
         dw = _new(order.slot.shape, torch.float32, dout.device, stream)
     _check(_lib().c3_expert_combine_grad(r, _ptr(dout), _ptr(y if dw is not None else None),
-                                         _ptr(weights), _ptr(dy), _ptr(dw), _stream(stream)),
+                                         _ptr(weights), _ptr(dy), _ptr(dw), _handle(stream, dout.device)),
            "c3_expert_combine_grad")
     return dy, dw
 
