@@ -203,8 +203,7 @@ __host__ __device__ constexpr int swizzle(int row) {
 
 // A lane's reads in a tile.  The piece of a row that is read enters the address
 // only through the exclusive or, so each read is one of two base offsets with
-// constant bits flipped; fresh() keeps the compiler from holding every one of
-// them in a register for the whole walk.
+// constant bits flipped.
 template <int DP>
 struct TileReads {
     int row;            // A operand along rows: lane's row, piece h
@@ -215,7 +214,6 @@ struct TileReads {
         const int r = h * 4 + (i >> 2);
         col = r * DP * 2 + (((g * 2 + ((i & 3) >> 1)) ^ swizzle<DP>(r)) << 4) + (i & 1) * 8;
     }
-    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(col)); }
     // Rows 0..31 of `tile`, inner step ks.
     __device__ __forceinline__ u32x4 along(const char* tile, int ks) const {
         return *reinterpret_cast<const u32x4*>(tile + (row ^ (ks << 5)));
@@ -540,7 +538,6 @@ int attn_stage(const c3_attention_t* a, AttnPlan& p, char* to, hipStream_t s);
 // The passes of the gradient; the plan's units are numbered.
 hipError_t launch_attn_dq(const AttnPlan& p, bool bf16, hipStream_t s);
 hipError_t launch_attn_dkv(const AttnPlan& p, bool bf16, hipStream_t s);
-int attn_dkv_keys(int dim);         // keys of a unit of the second
 // Workgroups of a pass, and whether it takes care of hidden infinities itself.
 inline uint32_t attn_blocks(const AttnPlan& p, int side) {
     return p.args.side[side].units * (uint32_t)p.args.kv_heads;

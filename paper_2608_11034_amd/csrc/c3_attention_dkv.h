@@ -1,24 +1,23 @@
 // A unit of the second pass of attention's gradient: dk and dv of a block of keys.
 //
-// A wave holds 32 NT keys and values and walks the rows of the query heads that
-// share them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  2 x 4,096 causal
-// tokens of 32 heads of 128: 667 us, 825 TFLOP/s; 16,384 tokens of 16 heads on 2 key
-// heads 2,270 us, 970.  With 64 keys a wave (NT 2) half of the LDS reads go, but one wave
-// a SIMD has nothing to run beside its exponentials: 890 us.
+// A wave holds 32 keys and values and walks the rows of the query heads that share
+// them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  2 x 4,096 causal tokens of
+// 32 heads of 128: 667 us, 825 TFLOP/s; 16,384 tokens of 16 heads on 2 key heads 2,270 us,
+// 970.  With 64 keys a wave half of the LDS reads go, but one wave a SIMD has nothing to
+// run beside its exponentials: 890 us.
 #pragma once
 
 #include "c3_attention.h"
 
 namespace c3 {
 
-constexpr int kDkvTiles = 1;        // blocks of 32 keys of a wave
+constexpr int kDkvKeys = 32 * kAttnWaves;       // of a unit
 
 // Returns whether a tile that the mask cuts held an infinity or NaN, which only
 // CAREFUL keeps from keys that its row does not see.
-template <typename T, int DP, int NT, bool CAREFUL>
+template <typename T, int DP, bool CAREFUL>
 __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab, uint32_t block) {
     constexpr int KS = DP / 16, NDB = DP / 32, kSub = 32 * DP * 2;
-    constexpr int kWaveKeys = 32 * NT, kBlockKeys = kWaveKeys * kAttnWaves;
     // Heads over 64: the values lie in LDS and tiles have 32 rows, so that two
     // workgroups fit a compute unit's registers (256 a lane) and LDS (160 KiB).
     constexpr bool kValuesLds = DP > 64;
@@ -31,7 +30,7 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     __shared__ __attribute__((aligned(1024))) char q1[kTileBytes];
     __shared__ __attribute__((aligned(1024))) char g1[kTileBytes];
     __shared__ __attribute__((aligned(1024))) float s1[2 * 64];
-    __shared__ __attribute__((aligned(1024))) char v_tile[kValuesLds ? kBlockKeys * DP * 2 : 16];
+    __shared__ __attribute__((aligned(1024))) char v_tile[kValuesLds ? kDkvKeys * DP * 2 : 16];
     __shared__ T words[CAREFUL ? kAttnWaves : 1][32 * 32];        // for the masked product
 
     const AttnUnit w = attn_unit(a, tab, 1, block);
@@ -40,15 +39,15 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     const int n_rows = w.q_len * G, off = w.k_len - w.q_len;
     const int k_pad = a.packed ? w.k_len : a.k_tokens;
     const int tile = (int)side.splits.quot(w.unit), part = (int)w.unit - tile * (int)side.splits.d;
-    const int key_block = tile * kBlockKeys;
+    const int key_block = tile * kDkvKeys;
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wkey = key_block + wave * kWaveKeys, key = wkey + c;      // and every 32nd from it
+    const int wkey = key_block + wave * 32, key = wkey + c;
 
     // queries that see any of the block's keys
     int p_lo = 0, p_hi = w.q_len;
     if (a.causal) p_lo = max(0, key_block - off);
-    if (a.window) p_hi = min(p_hi, key_block + kBlockKeys - 1 - off + a.window);
+    if (a.window) p_hi = min(p_hi, key_block + kDkvKeys - 1 - off + a.window);
     if (key_block >= w.k_len) p_hi = 0;
     int t0 = p_lo * G / kTileRows;
     int t1 = p_hi > p_lo ? (p_hi * G + kTileRows - 1) / kTileRows : t0;
@@ -64,11 +63,9 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
     const int64_t stat_row = seq_row(a, w) + w.hk * G;
     const float cs = a.scale * kLog2e;
 
-    f32x16 dk[NT][NDB] = {}, dv[NT][NDB] = {};
+    f32x16 dk[NDB] = {}, dv[NDB] = {};
     uint32_t bad = 0;
-    float factor[NT];       // of dS
-#pragma unroll
-    for (int m = 0; m < NT; ++m) factor[m] = kDsScaled<T> ? kDsFactor : 1.0f;
+    float factor = kDsScaled<T> ? kDsFactor : 1.0f;     // of dS
 
     auto load = [&](int t, char* qt, char* gt, float* st) {
         const int row0 = t * kTileRows, rows = min(kTileRows, n_rows - row0);
@@ -101,85 +98,64 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
                 rs, (__attribute__((address_space(3))) void*)(st + wave * 64), 4, (int)at, 0, 0, 0);
         }
     };
-    u32x4 kf[NT][KS], vf[kValuesLds ? 1 : NT][KS];
+    u32x4 kf[KS], vf[KS];
     {
         const char* kb = seq_base(a.k, a.packed, w.b, w.k_start, w.hk);
         const char* vb = seq_base(a.v, a.packed, w.b, w.k_start, w.hk);
-#pragma unroll
-        for (int m = 0; m < NT; ++m) {
-            load_row<DP>(kf[m], kb + (int64_t)(key + 32 * m) * a.k.st, key + 32 * m < w.k_len, a.dim);
-            if constexpr (!kValuesLds)
-                load_row<DP>(vf[m], vb + (int64_t)(key + 32 * m) * a.v.st, key + 32 * m < w.k_len, a.dim);
-        }
+        load_row<DP>(kf, kb + (int64_t)key * a.k.st, key < w.k_len, a.dim);
+        if constexpr (!kValuesLds) load_row<DP>(vf, vb + (int64_t)key * a.v.st, key < w.k_len, a.dim);
         if constexpr (kValuesLds) {
             // each wave its own keys'
-            const int rows = min(w.k_len - wkey, kWaveKeys);
+            const int rows = min(w.k_len - wkey, 32);
             const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * a.v.st) + a.dim * 2 : 0;
 #pragma unroll
-            for (int n = 0; n < NT * KS; ++n) {
-                const int i = n / KS * 32 + rd.load_row(lane, n), piece = 2 * (n % KS) + rd.load_half(lane);
+            for (int n = 0; n < KS; ++n) {
+                const int i = rd.load_row(lane, n), piece = 2 * n + rd.load_half(lane);
                 const bool ok = i < rows && piece * 8 < a.dim;
                 load_piece_lds(vb + (int64_t)wkey * a.v.st, bytes,
                                ok ? (uint32_t)(i * (int)a.v.st + piece * 16) : 0xFFFFFF00u,
-                               v_tile + (wave * NT * KS + n) * 1024);
+                               v_tile + (wave * KS + n) * 1024);
             }
         }
     }
 
     // The four parts of 32 rows' work: scores and dP; P and dS; what they add to
     // dv and dk.
-    auto scores = [&](int n, const char* qt, const char* gt, f32x16 (&s)[NT], f32x16 (&dp)[NT]) {
+    auto scores = [&](int n, const char* qt, const char* gt, f32x16& s, f32x16& dp) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 x = rd.along(qt + n * kSub, ks);
-#pragma unroll
-            for (int m = 0; m < NT; ++m) s[m] = mfma<T>(x, kf[m][ks], s[m]);
+            s = mfma<T>(rd.along(qt + n * kSub, ks), kf[ks], s);
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const u32x4 x = rd.along(gt + n * kSub, ks);
-#pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                if constexpr (kValuesLds)
-                    dp[m] = mfma<T>(x, rd.along(v_tile + (wave * NT + m) * kSub, ks), dp[m]);
-                else
-                    dp[m] = mfma<T>(x, vf[m][ks], dp[m]);
-            }
+            if constexpr (kValuesLds)
+                dp = mfma<T>(x, rd.along(v_tile + wave * kSub, ks), dp);
+            else
+                dp = mfma<T>(x, vf[ks], dp);
         }
     };
-    auto probabilities = [&](int n, const float* st, f32x16 (&s)[NT], f32x16 (&dp)[NT]) {
+    auto probabilities = [&](int n, const float* st, f32x16& s, f32x16& dp) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const f32x4 l2 = *reinterpret_cast<const f32x4*>(st + n * 32 + q * 8 + h * 4);
             const f32x4 de = *reinterpret_cast<const f32x4*>(st + 64 + n * 32 + q * 8 + h * 4);
 #pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[m][4 * q + i] = __builtin_amdgcn_exp2f(fmaf(s[m][4 * q + i], cs, -l2[i]));
-                    dp[m][4 * q + i] = s[m][4 * q + i] * (dp[m][4 * q + i] - de[i]);
-                    if constexpr (kDsScaled<T>) dp[m][4 * q + i] *= factor[m];
-                }
+            for (int i = 0; i < 4; ++i) {
+                s[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + i], cs, -l2[i]));
+                dp[4 * q + i] = s[4 * q + i] * (dp[4 * q + i] - de[i]);
+                if constexpr (kDsScaled<T>) dp[4 * q + i] *= factor;
+            }
         }
     };
-    auto gradients = [&](int n, const char* qt, const char* gt, const f32x16 (&s)[NT], const f32x16 (&dp)[NT]) {
+    auto gradients = [&](int n, const char* qt, const char* gt, const f32x16& s, const f32x16& dp) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            u32x4 p[NT], ds[NT];
+            const u32x4 p = operand<T>(s, j), ds = operand<T>(dp, j);
 #pragma unroll
-            for (int m = 0; m < NT; ++m) p[m] = operand<T>(s[m], j), ds[m] = operand<T>(dp[m], j);
+            for (int db = 0; db < NDB; ++db) dv[db] = mfma<T>(rd.across(gt + n * kSub, j, db), p, dv[db]);
 #pragma unroll
-            for (int db = 0; db < NDB; ++db) {
-                const u32x4 x = rd.across(gt + n * kSub, j, db);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) dv[m][db] = mfma<T>(x, p[m], dv[m][db]);
-            }
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) {
-                const u32x4 x = rd.across(qt + n * kSub, j, db);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) dk[m][db] = mfma<T>(x, ds[m], dk[m][db]);
-            }
+            for (int db = 0; db < NDB; ++db) dk[db] = mfma<T>(rd.across(qt + n * kSub, j, db), ds, dk[db]);
         }
     };
     auto step = [&](int t, const char* qt, const char* gt, const float* st) {
@@ -190,38 +166,33 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
             const int pa = (int)a.group.quot(row0) + off;
             const int pb = (int)a.group.quot(min(row0 + 31, n_rows - 1)) + off;
             if (a.causal && wkey > pb) continue;
-            if (a.window && wkey + kWaveKeys - 1 <= pa - a.window) continue;
+            if (a.window && wkey + 31 <= pa - a.window) continue;
             // rows behind the last hold zeros, which times an infinite key is NaN: hidden too
-            const bool masked = (a.causal && wkey + kWaveKeys - 1 > pa) || (a.window && wkey <= pb - a.window) ||
+            const bool masked = (a.causal && wkey + 31 > pa) || (a.window && wkey <= pb - a.window) ||
                                 row0 + 32 > n_rows;
-            f32x16 s[NT] = {}, dp[NT] = {};
-            uint32_t seen[NT] = {};
+            f32x16 s = {}, dp = {};
+            uint32_t seen = 0;
             scores(n, qt, gt, s, dp);
             probabilities(n, st, s, dp);
             if (masked) {
                 // formed here, not held in registers through the walk
                 int k_ = key, h_ = h * 4;
                 asm volatile("" : "+v"(k_), "+v"(h_));
+                // rows from r_lo to below r_hi of these 32 see the lane's key
+                const int64_t at = (int64_t)(k_ - off) * G - row0, all = (int64_t)a.window * G;
+                const int r_lo = a.causal ? (int)min(max(at, (int64_t)0), (int64_t)32) : 0;
+                const int r_hi = min(a.window ? (int)min(max(at + all, (int64_t)0), (int64_t)32) : 32,
+                                     n_rows - row0);
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    // rows from r_lo to below r_hi of these 32 see the lane's key
-                    const int64_t at = (int64_t)(k_ + 32 * m - off) * G - row0, all = (int64_t)a.window * G;
-                    const int r_lo = a.causal ? (int)min(max(at, (int64_t)0), (int64_t)32) : 0;
-                    const int r_hi = min(a.window ? (int)min(max(at + all, (int64_t)0), (int64_t)32) : 32,
-                                         n_rows - row0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = (i >> 2) * 8 + h_ + (i & 3);
-                        const bool see = r >= r_lo && r < r_hi;
-                        seen[m] |= see ? 1u << i : 0u;
-                        s[m][i] = see ? s[m][i] : 0.0f;
-                        dp[m][i] = see ? dp[m][i] : 0.0f;
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const int r = (i >> 2) * 8 + h_ + (i & 3);
+                    const bool see = r >= r_lo && r < r_hi;
+                    seen |= see ? 1u << i : 0u;
+                    s[i] = see ? s[i] : 0.0f;
+                    dp[i] = see ? dp[i] : 0.0f;
                 }
             }
-            if constexpr (kDsScaled<T>)
-#pragma unroll
-                for (int m = 0; m < NT; ++m) fit_ds<NDB>(dp[m], dk[m], factor[m]);
+            if constexpr (kDsScaled<T>) fit_ds<NDB>(dp, dk, factor);
             if (masked) {
                 const char *q_sub = qt + n * kSub, *g_sub = gt + n * kSub;
                 const uint32_t here = tile_not_finite<T>(KS, [&](int ks) { return rd.along(q_sub, ks); }) |
@@ -229,15 +200,12 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
                 bad |= here;
                 if constexpr (CAREFUL) {
                     if (__any(here != 0)) {
-#pragma unroll
-                        for (int m = 0; m < NT; ++m) {
-                            masked_product<T, NDB>(dv[m], s[m], seen[m], words[wave],
-                                                   [&](int k, int d) { return rd.four(g_sub, k, d); },
-                                                   [&](int j, int db) { return rd.across(g_sub, j, db); });
-                            masked_product<T, NDB>(dk[m], dp[m], seen[m], words[wave],
-                                                   [&](int k, int d) { return rd.four(q_sub, k, d); },
-                                                   [&](int j, int db) { return rd.across(q_sub, j, db); });
-                        }
+                        masked_product<T, NDB>(dv, s, seen, words[wave],
+                                               [&](int k, int d) { return rd.four(g_sub, k, d); },
+                                               [&](int j, int db) { return rd.across(g_sub, j, db); });
+                        masked_product<T, NDB>(dk, dp, seen, words[wave],
+                                               [&](int k, int d) { return rd.four(q_sub, k, d); },
+                                               [&](int j, int db) { return rd.across(q_sub, j, db); });
                         continue;
                     }
                 }
@@ -257,60 +225,56 @@ __device__ __forceinline__ bool dkv_unit(const AttnArgs& a, const AttnTable& tab
         step(t + 1, q1, g1, s1);
     }
 
+    if (key >= k_pad) return bad != 0;
+    const bool valid = key < w.k_len;
+    if constexpr (kDsScaled<T>) {
+        const float back = 1.0f / factor;
 #pragma unroll
-    for (int m = 0; m < NT; ++m) {
-        const int k = key + 32 * m;
-        if (k >= k_pad) continue;
-        const bool valid = k < w.k_len;
-        if constexpr (kDsScaled<T>) {
-            const float back = 1.0f / factor[m];
+        for (int db = 0; db < NDB; ++db)
 #pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) dk[m][db][i] *= back;
-        }
-        if (side.splits.d > 1) {
-            // dk and dv of this part, in fp32 and not yet scaled
-            const int64_t keys = (int64_t)(a.packed ? 0 : w.b) * a.k_tokens + w.k_start + k;
-            float* to = side.part + (part * 2 * side.part_rows + keys * a.kv_heads + w.hk) * a.dim;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int d = db * 32 + q * 8 + h * 4;
-                    if (d >= a.dim) continue;
-                    f32x4 x, y;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[i] = valid ? dk[m][db][4 * q + i] : 0.0f;
-                        y[i] = valid ? dv[m][db][4 * q + i] : 0.0f;
-                    }
-                    *reinterpret_cast<f32x4*>(to + d) = x;
-                    *reinterpret_cast<f32x4*>(to + side.part_rows * a.dim + d) = y;
-                }
-            continue;
-        }
-        char* ok = seq_base(a.dk, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dk.st;
-        char* ov = seq_base(a.dv, a.packed, w.b, w.k_start, w.hk) + (int64_t)k * a.dv.st;
+            for (int i = 0; i < 16; ++i) dk[db][i] *= back;
+    }
+    if (side.splits.d > 1) {
+        // dk and dv of this part, in fp32 and not yet scaled
+        const int64_t keys = (int64_t)(a.packed ? 0 : w.b) * a.k_tokens + w.k_start + key;
+        float* to = side.part + (part * 2 * side.part_rows + keys * a.kv_heads + w.hk) * a.dim;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int d = db * 32 + q * 8 + h * 4;
                 if (d >= a.dim) continue;
-                T e[4], f[4];
+                f32x4 x, y;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    e[i] = valid ? (T)(dk[m][db][4 * q + i] * a.scale) : (T)0.0f;
-                    f[i] = valid ? (T)dv[m][db][4 * q + i] : (T)0.0f;
+                    x[i] = valid ? dk[db][4 * q + i] : 0.0f;
+                    y[i] = valid ? dv[db][4 * q + i] : 0.0f;
                 }
-                u32x2 x, y;
-                __builtin_memcpy(&x, e, 8);
-                __builtin_memcpy(&y, f, 8);
-                *reinterpret_cast<u32x2*>(ok + d * 2) = x;
-                *reinterpret_cast<u32x2*>(ov + d * 2) = y;
+                *reinterpret_cast<f32x4*>(to + d) = x;
+                *reinterpret_cast<f32x4*>(to + side.part_rows * a.dim + d) = y;
             }
+        return bad != 0;
     }
+    char* ok = seq_base(a.dk, a.packed, w.b, w.k_start, w.hk) + (int64_t)key * a.dk.st;
+    char* ov = seq_base(a.dv, a.packed, w.b, w.k_start, w.hk) + (int64_t)key * a.dv.st;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = db * 32 + q * 8 + h * 4;
+            if (d >= a.dim) continue;
+            T e[4], f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[i] = valid ? (T)(dk[db][4 * q + i] * a.scale) : (T)0.0f;
+                f[i] = valid ? (T)dv[db][4 * q + i] : (T)0.0f;
+            }
+            u32x2 x, y;
+            __builtin_memcpy(&x, e, 8);
+            __builtin_memcpy(&y, f, 8);
+            *reinterpret_cast<u32x2*>(ok + d * 2) = x;
+            *reinterpret_cast<u32x2*>(ov + d * 2) = y;
+        }
     return bad != 0;
 }
 

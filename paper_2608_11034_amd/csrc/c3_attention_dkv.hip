@@ -6,7 +6,7 @@ namespace {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, AttnTable tab) {
-    const bool bad = dkv_unit<T, DP, kDkvTiles, false>(a, tab, blockIdx.x);
+    const bool bad = dkv_unit<T, DP, false>(a, tab, blockIdx.x);
     if (a.causal || a.window) {
         const int any = __syncthreads_or(bad);
         if (threadIdx.x == 0) a.side[1].marks[blockIdx.x] = any;
@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_kernel(AttnArgs a, A
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, 1) void attn_dkv_direct_kernel(AttnArgs a, AttnTable tab) {
-    dkv_unit<T, DP, kDkvTiles, true>(a, tab, blockIdx.x);
+    dkv_unit<T, DP, true>(a, tab, blockIdx.x);
 }
 
 template <typename T, int DP>
@@ -29,8 +29,6 @@ hipError_t launch(const AttnPlan& p, hipStream_t s) {
 }
 
 }  // namespace
-
-int attn_dkv_keys(int dim) { return 32 * kDkvTiles * kAttnWaves; }
 
 hipError_t launch_attn_dkv(const AttnPlan& p, bool bf16, hipStream_t s) {
     if (bf16) return p.args.dim > 64 ? launch<__bf16, 128>(p, s) : launch<__bf16, 64>(p, s);

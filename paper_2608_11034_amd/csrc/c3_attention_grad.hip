@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_grad_careful_kernel(Attn
                       [&](uint32_t unit) { dq_unit<T, DP, true, true>(a, tab, unit); });
     else
         repeat_marked(a.side[1].marks, k_blocks, blockIdx.x - half, half,
-                      [&](uint32_t unit) { dkv_unit<T, DP, kDkvTiles, true>(a, tab, unit); });
+                      [&](uint32_t unit) { dkv_unit<T, DP, true>(a, tab, unit); });
 }
 
 template <typename T, int DP>
@@ -124,7 +124,7 @@ struct GradSpace {
     int64_t parts[2];
     bool fits;
     GradSpace(const c3_attention_t* a, AttnPlan& p) {
-        const int64_t group = p.args.group.d, kv = p.args.kv_heads, block_keys = attn_dkv_keys(a->dim);
+        const int64_t group = p.args.group.d, kv = p.args.kv_heads, block_keys = kDkvKeys;
         auto number = [&](int side, int64_t times) {
             return kv * attn_number(p, a->batch, side, [&](int64_t nq, int64_t, int64_t nk) {
                 return times * (side ? (nk + block_keys - 1) / block_keys : (nq * group + kDqRows - 1) / kDqRows);

@@ -13,10 +13,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // V elements of one load: 16 bytes on the wide paths, one element otherwise.
 template <typename T, int V>
-struct Pack {
-    T v[V];
-};
-template <typename T, int V>
 struct alignas(sizeof(T) * V) AlignedPack {
     T v[V];
 };
