@@ -2,8 +2,8 @@
 //
 // A wave holds 32 keys and values and walks the rows of the query heads that share
 // them: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  2 x 4,096 causal tokens of
-// 32 heads of 128: 667 us, 825 TFLOP/s; 16,384 tokens of 16 heads on 2 key heads 2,270 us,
-// 970.  With 64 keys a wave half of the LDS reads go, but one wave a SIMD has nothing to
+// 32 heads of 128: 606 us, 907 TFLOP/s; 16,384 tokens of 16 heads on 2 key heads 2,279 us,
+// 965.  With 64 keys a wave half of the LDS reads go, but one wave a SIMD has nothing to
 // run beside its exponentials: 890 us.
 #pragma once
 

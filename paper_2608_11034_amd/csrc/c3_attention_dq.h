@@ -3,8 +3,8 @@
 //
 // A wave holds 32 rows' queries and output gradients and walks the keys, as the
 // forward does: S^T = K Q^T, dP^T = V dO^T, dS = P (dP - delta), dQ^T += K^T dS.
-// 2 x 4,096 causal tokens of 32 heads of 128: 444 us, 928 TFLOP/s; 16,384 tokens of 16
-// heads on 2 key heads 1,480 us, 1,110.
+// 2 x 4,096 causal tokens of 32 heads of 128: 408 us, 1,010 TFLOP/s; 16,384 tokens of 16
+// heads on 2 key heads 1,508 us, 1,094.
 #pragma once
 
 #include "c3_attention.h"
