@@ -207,6 +207,117 @@ int c3_expert_combine_grad(const c3_expert_rows_t *r, const void *dout, const vo
                            const float *weights, void *dsorted, float *dweights,
                            c3_stream_t stream);
 
+/* ---------------------------------------------------------------------- */
+/* Embedding                                                               */
+/* ---------------------------------------------------------------------- */
+
+/* Sizes of a lookup of `tokens` rows out of a table of `rows`, and of its
+ * gradient.  Strides count elements and are not looked at where there is one row. */
+typedef struct {
+    int32_t dtype;          /* C3_F32, C3_BF16 or C3_F16                       */
+    int32_t id_bytes;       /* 4 or 8: signed integers                         */
+    int64_t tokens;
+    int64_t rows;           /* of the table, 1 .. 2^31 - 1                     */
+    int64_t hidden;         /* elements of a row                               */
+    int64_t row_stride;     /* of the tokens' side: out, dout                  */
+    int64_t table_stride;
+    float scale;            /* finite                                          */
+    int32_t reserved;
+} c3_embedding_t;
+
+/* c3_embedding -- out[t] = scale * table[ids[t]], rounded once; zeros for an id
+ * outside [0, rows).  ids device [tokens].  `out` does not overlap the table. */
+int c3_embedding(const c3_embedding_t *a, const void *ids, const void *table, void *out,
+                 c3_stream_t stream);
+
+/* Device workspace bytes of c3_embedding_grad (256 at least; 0 if invalid). */
+size_t c3_embedding_grad_workspace_size(const c3_embedding_t *a);
+
+/*
+ * c3_embedding_grad -- dtable[v] = scale * the sum of dout[t] over the tokens
+ * with ids[t] = v, rounded once; ids outside [0, rows) add nothing.  Tokens are
+ * sorted by row; a row's sum runs in the order of its tokens, in parts that its
+ * place in the sorted list fixes.
+ *
+ *   dtable       [rows][hidden] of dtype or of C3_F32 (table_dtype), table_stride
+ *                apart; all rows are written, those without a token as zeros.
+ *   accumulate   not 0: rows with tokens get their sum added, others are left as
+ *                they are (a table that is also the output's weights).
+ *   ws           256-byte aligned, not used by another call at the same time.
+ * Can be captured.  dtable overlaps no input.
+ */
+int c3_embedding_grad(const c3_embedding_t *a, const void *dout, const void *ids, void *dtable,
+                      int table_dtype, int accumulate, void *ws, size_t ws_bytes,
+                      c3_stream_t stream);
+
+/* ---------------------------------------------------------------------- */
+/* Residual sum and norms around a block                                   */
+/* ---------------------------------------------------------------------- */
+
+#define C3_MAX_NORM_HIDDEN 16384
+
+typedef enum {
+    C3_GATE_NONE = 0,
+    C3_GATE_CHANNELS = 1,   /* [hidden], the same for every token */
+    C3_GATE_TOKENS = 2      /* [tokens][hidden]                   */
+} c3_gate_t;
+
+/* Sizes and types of c3_residual_norm.  Strides as in c3_embedding_t. */
+typedef struct {
+    int32_t dtype;          /* of y, gate, weight, post, n and their gradients  */
+    int32_t residual;       /* of x, h, dh and dx: dtype or C3_F32              */
+    int64_t tokens;
+    int64_t hidden;         /* 1 .. C3_MAX_NORM_HIDDEN                          */
+    float scale;            /* of the block's output, finite                    */
+    float eps;              /* added to the mean of squares, >= 0               */
+    int32_t gate;           /* c3_gate_t                                        */
+    int32_t reserved;
+} c3_residual_norm_t;
+
+/* Rows [tokens][hidden], last dimension contiguous; ptr NULL: not there. */
+typedef struct {
+    void *ptr;
+    int64_t stride;
+} c3_rows_t;
+
+/*
+ * c3_residual_norm -- joins a block's output y to the residual stream x and
+ * norms the sum for the next block:
+ *     z = post * y / rms(y)      (without post: z = y)
+ *     h = x + scale * gate * z   (without y: h = x, not written)
+ *     n = weight * h / rms(h)    with rms(a) = sqrt(mean of a^2 + eps),
+ * in 32 bits, n from h before it is rounded.
+ *
+ *   y      may be missing, and then has neither gate nor post.
+ *   gate   [hidden] (stride unused) or rows, by a->gate.
+ *   weight, post  device [hidden], post may be NULL.
+ *   h      may be x with the same stride; no other overlaps.
+ *   stats  device fp32 [tokens][2]: 1 / rms(h), and 1 / rms(y) (1 without post).
+ * Can be captured.
+ */
+int c3_residual_norm(const c3_residual_norm_t *a, const c3_rows_t *x, const c3_rows_t *y,
+                     const c3_rows_t *gate, const void *weight, const void *post,
+                     const c3_rows_t *h, const c3_rows_t *n, float *stats, c3_stream_t stream);
+
+/* Device workspace bytes of c3_residual_norm_grad (256 at least; 0 if invalid). */
+size_t c3_residual_norm_grad_workspace_size(const c3_residual_norm_t *a);
+
+/*
+ * c3_residual_norm_grad -- gradients for dn, that of n, and dh, that of h from
+ * what else reads it (ptr NULL: zeros).  stats are those of c3_residual_norm.
+ * dx is the gradient of x (and of h as a whole); dy, and dgate as rows, are there
+ * where y and such a gate are.  Sums over the tokens go to sums, device fp32
+ * [3][hidden]: of weight, of post (left alone without post) and of a gate of
+ * channels (left alone without one).  They run in an order that the sizes fix.
+ *   dx may be dh with the same stride, dy may be dn with the same stride; results
+ *   overlap nothing else.  ws as c3_embedding_grad.  Can be captured.
+ */
+int c3_residual_norm_grad(const c3_residual_norm_t *a, const c3_rows_t *dn, const c3_rows_t *dh,
+                          const c3_rows_t *x, const c3_rows_t *y, const c3_rows_t *gate,
+                          const void *weight, const void *post, const float *stats,
+                          const c3_rows_t *dx, const c3_rows_t *dy, const c3_rows_t *dgate,
+                          float *sums, void *ws, size_t ws_bytes, c3_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

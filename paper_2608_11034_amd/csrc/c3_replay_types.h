@@ -21,6 +21,15 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
 
+// An fp32 result rounded to T.  In fp16 the compiler may join a last product or sum with
+// the rounding, which then rounds once instead of twice; where it does goes by how the
+// stores are laid out, and the bits must not: what is rounded is an fp32 value in a register.
+template <typename T>
+__device__ __forceinline__ T from_f32(float x) {
+    if constexpr (sizeof(T) == 2) asm("" : "+v"(x));
+    return (T)x;
+}
+
 // Division by a run-time constant d of numbers below 2^31: q = (mulhi(n, m) +
 // n) >> s, with s = ceil(log2 d) and m = ceil(2^32 (2^s - d) / d) (Granlund and
 // Montgomery, division by invariant integers, 1994).

@@ -14,6 +14,9 @@ every step runs in the HIP kernels of libc3.so and there is no CPU fallback.
 * ``expert_dispatch(x, order)``           tokens to their experts' rows
 * ``expert_combine(y, order, weights)``   and back, weighted
 * ``expert_combine_grad``, ``expert_dispatch_grad``  their gradients
+* ``embedding(ids, table)``               rows of a table; ``embedding_grad`` its gradient
+* ``residual_norm(x, y, weight)``         residual sum and the norms around a block
+* ``residual_norm_grad``                  its gradient
 
 The calls record no graph.  Where torch would record one, tensors that require a
 gradient are refused; under ``torch.no_grad()`` and inside the forward and backward of a
@@ -36,6 +39,8 @@ HALF, INTERLEAVED = 0, 1
 MAX_HEAD_DIM = 128
 MAX_EXPERTS, MAX_TOP = 512, 64
 MAX_CAPTURED_SEQUENCES = 112
+MAX_NORM_HIDDEN = 16384
+GATE_NONE, GATE_CHANNELS, GATE_TOKENS = 0, 1, 2
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _LAYOUT = {"half": HALF, "interleaved": INTERLEAVED}
@@ -64,12 +69,31 @@ class ExpertRows(ctypes.Structure):
                 ("sorted_stride", ctypes.c_int64), ("slot", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
 
 
+class Embedding(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("hidden", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("table_stride", ctypes.c_int64), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ResidualNorm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("residual", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("hidden", ctypes.c_int64), ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("gate", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class RowsOf(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
 # The same fields in one step: setting them one by one costs a call several microseconds.
 _HEADS = struct.Struct("@2P7q")
 _POS = struct.Struct("@2q")
 _ATTENTION = struct.Struct("@6ifi2q2i2P")
 _ATTN_TENSOR = struct.Struct("@P3q")
 _EXPERT_ROWS = struct.Struct("@2i4q2P")
+_EMBEDDING = struct.Struct("@2i5qfi")
+_RESIDUAL_NORM = struct.Struct("@2i2q2f2i")
+_ROWS = struct.Struct("@Pq")
 
 _ready = None
 
@@ -99,6 +123,18 @@ def _lib():
         L.c3_expert_combine.argtypes = [vp] * 5
         L.c3_expert_combine_grad.restype = i32
         L.c3_expert_combine_grad.argtypes = [vp] * 7
+        L.c3_embedding.restype = i32
+        L.c3_embedding.argtypes = [vp] * 5
+        L.c3_embedding_grad_workspace_size.restype = sz
+        L.c3_embedding_grad_workspace_size.argtypes = [vp]
+        L.c3_embedding_grad.restype = i32
+        L.c3_embedding_grad.argtypes = [vp] * 4 + [i32, i32, vp, sz, vp]
+        L.c3_residual_norm.restype = i32
+        L.c3_residual_norm.argtypes = [vp] * 10
+        L.c3_residual_norm_grad_workspace_size.restype = sz
+        L.c3_residual_norm_grad_workspace_size.argtypes = [vp]
+        L.c3_residual_norm_grad.restype = i32
+        L.c3_residual_norm_grad.argtypes = [vp] * 14 + [sz, vp]
         _ready = L
     return _ready
 
@@ -509,3 +545,186 @@ def expert_dispatch_grad(dsorted, order: ExpertOrder, *, out=None, stream=None):
     """Gradient [T, hidden] of ``expert_dispatch``: each token's sum over its
     choices' rows of dsorted [T * top, hidden]."""
     return expert_combine(dsorted, order, None, out=out, stream=stream)
+
+
+# ---------------------------------------------------------------------------
+# embedding
+# ---------------------------------------------------------------------------
+def _ids(t, name, device=None):
+    _dev_tensor(t, name)
+    if t.dtype not in (torch.int32, torch.int64) or t.dim() != 1:
+        raise C3Error(f"{name} must be int32 or int64 [tokens]")
+    if device is not None and t.device != device:
+        raise C3Error(f"{name} must be on {device}")
+    return t
+
+
+def _pack(form, *values):
+    try:
+        return form.pack(*values)
+    except (struct.error, OverflowError):
+        raise C3Error("scale and eps must be numbers that fp32 holds") from None
+
+
+def _embedding_args(ids, dtype, rows, hidden, side, table, scale):
+    return _pack(_EMBEDDING, _CODE[dtype], ids.element_size(), ids.numel(), rows, hidden, side.stride(0),
+                 table.stride(0), scale, 0)
+
+
+def embedding(ids, table, *, scale: float = 1.0, out=None, stream=None):
+    """Rows [T, hidden] with scale * table[ids[t]]; zeros for an id outside
+    [0, rows).  ids int32 or int64 [T], table [rows, hidden]."""
+    _rows(table, "table", dim=(2,))
+    _ids(ids, "ids", table.device)
+    rows, hidden = table.shape
+    out = _out(out, "out", torch.Size((ids.numel(), hidden)), table.dtype, table.device, stream)
+    a = _embedding_args(ids, table.dtype, rows, hidden, out, table, scale)
+    _check(_lib().c3_embedding(a, _ptr(ids), _ptr(table), _ptr(out), _handle(stream, table.device)),
+           "c3_embedding")
+    return out
+
+
+def embedding_grad(dout, ids, rows: int, *, scale: float = 1.0, dtype=None, dtable=None,
+                   accumulate: bool = False, workspace=None, stream=None):
+    """Gradient [rows, hidden] of ``embedding``'s table for dout [T, hidden]: each row's
+    sum over the tokens that read it.  ``dtype`` is that of dout (default) or
+    torch.float32.  ``accumulate`` adds to the rows of ``dtable`` that have tokens and
+    leaves the others, as for a table that is also the output's weights."""
+    _rows(dout, "dout", dim=(2,))
+    _ids(ids, "ids", dout.device)
+    if dout.shape[0] != ids.numel():
+        raise C3Error("dout must have one row for each id")
+    rows = _int32(rows, "rows")
+    if dtype is None:
+        dtype = dout.dtype if dtable is None else dtable.dtype
+    if dtype not in (dout.dtype, torch.float32):
+        raise C3Error("dtable must have the dtype of dout or be fp32")
+    if accumulate and dtable is None:
+        raise C3Error("accumulate needs a dtable to add to")
+    dtable = _out(dtable, "dtable", torch.Size((rows, dout.shape[1])), dtype, dout.device, stream)
+    a = _embedding_args(ids, dout.dtype, rows, dout.shape[1], dout, dtable, scale)
+    ws = _workspace(_lib().c3_embedding_grad_workspace_size(a), workspace, dout.device, "embedding_grad", stream)
+    _check(_lib().c3_embedding_grad(a, _ptr(dout), _ptr(ids), _ptr(dtable), _CODE[dtype], int(bool(accumulate)),
+                                    _ptr(ws), ws.numel() * ws.element_size(), _handle(stream, dout.device)),
+           "c3_embedding_grad")
+    return dtable
+
+
+# ---------------------------------------------------------------------------
+# residual sum and the norms around a block
+# ---------------------------------------------------------------------------
+class ResidualNormGrad(NamedTuple):
+    """Gradients of ``residual_norm``; None where there is no such input.  dweight,
+    dpost and the gradient of a gate [hidden] are fp32, sums over the tokens."""
+    dx: torch.Tensor
+    dy: torch.Tensor
+    dweight: torch.Tensor
+    dpost: torch.Tensor
+    dgate: torch.Tensor
+
+
+def _at(t):
+    return None if t is None else _ROWS.pack(t.data_ptr(), t.stride(0))
+
+
+def _norm_args(x, y, weight, post, gate, scale, eps):
+    _rows(x, "x", dim=(2,))
+    _rows(weight, "weight", device=x.device, dim=(1,))
+    dtype, (T, H) = weight.dtype, x.shape
+    if x.dtype not in (dtype, torch.float32):
+        raise C3Error("x must have the dtype of weight or be fp32")
+    if weight.shape[0] != H:
+        raise C3Error(f"weight must be [{H}]")
+    kind = GATE_NONE
+    if y is not None:
+        _rows(y, "y", dtype, x.device, (2,))
+        if y.shape != x.shape:
+            raise C3Error("x and y must have the same shape")
+    elif post is not None or gate is not None:
+        raise C3Error("post and gate need y")
+    if post is not None:
+        _rows(post, "post", dtype, x.device, (1,))
+        if post.shape[0] != H:
+            raise C3Error(f"post must be [{H}]")
+    if gate is not None:
+        _rows(gate, "gate", dtype, x.device, (1, 2))
+        if gate.shape != x.shape and gate.shape != weight.shape:
+            raise C3Error("gate must be [hidden] or [tokens, hidden]")
+        kind = GATE_CHANNELS if gate.dim() == 1 else GATE_TOKENS
+    return _pack(_RESIDUAL_NORM, _CODE[dtype], _CODE[x.dtype], T, H, scale, eps, kind, 0), kind
+
+
+def residual_norm(x, y, weight, *, post=None, gate=None, scale: float = 1.0, eps: float = 1e-6, h=None,
+                  n=None, stats=None, stream=None):
+    """(n, h, stats) of a block's output y [T, hidden] joined to the residual stream x
+    and normed for the next block:
+
+        z = post * y / rms(y), or y without ``post``
+        h = x + scale * gate * z, or x itself where y is None
+        n = weight * h / rms(h),    rms(a) = sqrt(mean of a^2 + eps)
+
+    ``gate`` is [hidden] or [T, hidden].  x may be fp32 beside a 16-bit weight, and h is
+    of x's dtype; all else has weight's.  ``h`` may be x.  stats fp32 [T, 2] goes to
+    ``residual_norm_grad``.  hidden up to 16,384."""
+    a, _ = _norm_args(x, y, weight, post, gate, scale, eps)
+    n = _out(n, "n", x.shape, weight.dtype, x.device, stream)
+    if y is None:
+        if h is not None and h is not x:
+            raise C3Error("without y, h is x")
+        h = x
+    else:
+        h = _out(h, "h", x.shape, x.dtype, x.device, stream)
+    stats = _new((x.shape[0], 2), torch.float32, x.device, stream) if stats is None else _stats(stats, x)
+    rc = _lib().c3_residual_norm(a, _at(x), _at(y), None if gate is None else _gate(gate), _ptr(weight), _ptr(post),
+                                 _at(h), _at(n), _ptr(stats), _handle(stream, x.device))
+    _check(rc, "c3_residual_norm")
+    return n, h, stats
+
+
+def _gate(t):
+    return _ROWS.pack(t.data_ptr(), t.stride(0) if t.dim() == 2 else 0)
+
+
+def _stats(t, x):
+    _dev_tensor(t, "stats")
+    if t.requires_grad:
+        _no_graph("stats")
+    if t.dtype != torch.float32 or t.shape != (x.shape[0], 2) or t.device != x.device:
+        raise C3Error(f"stats must be fp32 [{x.shape[0]}, 2] on the device of x")
+    return t
+
+
+def residual_norm_grad(dn, dh, x, y, weight, stats, *, post=None, gate=None, scale: float = 1.0,
+                       eps: float = 1e-6, dx=None, dy=None, dgate=None, workspace=None,
+                       stream=None) -> ResidualNormGrad:
+    """Gradients of ``residual_norm`` with the same arguments, for dn, that of n, and
+    dh, that of h from what else reads it (None: nothing does).  ``dx`` may be dh,
+    ``dy`` may be dn."""
+    a, kind = _norm_args(x, y, weight, post, gate, scale, eps)
+    _stats(stats, x)
+    for t, name, like in ((dn, "dn", weight), (dh, "dh", x)):
+        if t is None and name == "dh":
+            continue
+        _rows(t, name, like.dtype, x.device, (2,))
+        if t.shape != x.shape:
+            raise C3Error(f"{name} must have the shape of x")
+    dx = _out(dx, "dx", x.shape, x.dtype, x.device, stream)
+    if y is None:
+        if dy is not None:
+            raise C3Error("dy needs y")
+    else:
+        dy = _out(dy, "dy", x.shape, weight.dtype, x.device, stream)
+    if kind == GATE_TOKENS:
+        dgate = _out(dgate, "dgate", x.shape, weight.dtype, x.device, stream)
+    elif dgate is not None:
+        raise C3Error("dgate as rows needs such a gate")
+    sums = _new((3, x.shape[1]), torch.float32, x.device, stream)
+    ws = _workspace(_lib().c3_residual_norm_grad_workspace_size(a), workspace, x.device, "residual_norm_grad",
+                    stream)
+    rc = _lib().c3_residual_norm_grad(a, _at(dn), _at(dh), _at(x), _at(y), None if gate is None else _gate(gate),
+                                      _ptr(weight), _ptr(post), _ptr(stats), _at(dx), _at(dy), _at(dgate),
+                                      _ptr(sums), _ptr(ws), ws.numel() * ws.element_size(),
+                                      _handle(stream, x.device))
+    _check(rc, "c3_residual_norm_grad")
+    return ResidualNormGrad(dx, dy, sums[0], None if post is None else sums[1],
+                            sums[2] if kind == GATE_CHANNELS else dgate)
