@@ -318,6 +318,59 @@ int c3_residual_norm_grad(const c3_residual_norm_t *a, const c3_rows_t *dn, cons
                           const c3_rows_t *dx, const c3_rows_t *dy, const c3_rows_t *dgate,
                           float *sums, void *ws, size_t ws_bytes, c3_stream_t stream);
 
+/* ---------------------------------------------------------------------- */
+/* Loss over a vocabulary                                                  */
+/* ---------------------------------------------------------------------- */
+
+/* Sizes and types of a softmax cross entropy of hidden states x [tokens][hidden] over
+ * the rows of weight [rows][hidden].  Pointers of x, weight, dx and dweight are 16-byte
+ * aligned, their last dimension contiguous and their strides (elements; not looked at
+ * where there is one row) multiples of 8 below 2^22. */
+typedef struct {
+    int32_t dtype;          /* C3_BF16 or C3_F16                               */
+    int32_t target_bytes;   /* 4 or 8: signed integers                         */
+    int64_t tokens;
+    int64_t hidden;         /* a multiple of 8 below 2^20                      */
+    int64_t rows;           /* of the vocabulary                               */
+    int64_t x_stride;
+    int64_t weight_stride;
+    float scale;            /* of the logits, finite                           */
+    int32_t reserved;
+} c3_vocab_loss_t;
+
+/* Device workspace bytes of c3_vocab_loss and of c3_vocab_loss_grad (256 at least; 0 if
+ * invalid). */
+size_t c3_vocab_loss_workspace_size(const c3_vocab_loss_t *a);
+size_t c3_vocab_loss_grad_workspace_size(const c3_vocab_loss_t *a);
+
+/*
+ * c3_vocab_loss -- with the logits l = scale * x[t] . weight[v], which are not kept,
+ *     lse[t] = log of the sum over v of exp(l[t][v]),  loss[t] = lse[t] - l[t][targets[t]].
+ * A token whose target is outside [0, rows) takes no part: its loss and lse are 0 and
+ * what its row of x holds is not looked at.
+ *   targets device [tokens]; loss, lse device fp32 [tokens].
+ *   ws      256-byte aligned, not used by another call at the same time.
+ * Can be captured.  Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, hidden,
+ * stride, 2^24 tiles of 256 rows by 256 tokens or more), C3_E_WORKSPACE, C3_E_HIP.
+ */
+int c3_vocab_loss(const c3_vocab_loss_t *a, const void *x, const void *weight, const void *targets,
+                  float *loss, float *lse, void *ws, size_t ws_bytes, c3_stream_t stream);
+
+/*
+ * c3_vocab_loss_grad -- gradients of c3_vocab_loss for dloss fp32 [tokens], dloss_stride
+ * elements apart (0: one number for all): with d = scale * dloss[t] * (exp(l - lse[t]) -
+ * onehot(targets[t])), dx = d weight and dweight = d^T x.  d is rounded to 16 bits on its
+ * way into the products (in fp16 times a power of two that follows the largest dloss);
+ * all sums are fp32, in an order that the sizes and the number of tokens that take part
+ * fix.  lse is that of c3_vocab_loss.  dx and dweight are of a->dtype; rows of dx whose
+ * token takes no part are zeros.  Results overlap neither inputs nor each other.
+ * Workspace and errors as c3_vocab_loss.  Can be captured.
+ */
+int c3_vocab_loss_grad(const c3_vocab_loss_t *a, const float *dloss, int64_t dloss_stride,
+                       const void *x, const void *weight, const void *targets, const float *lse,
+                       void *dx, int64_t dx_stride, void *dweight, int64_t dweight_stride, void *ws,
+                       size_t ws_bytes, c3_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,601 @@
+// Softmax cross entropy over a vocabulary and its gradient (include/c3_replay.h).
+//
+// Three products bound both: logits x W^T in the forward pass, and again in the gradient
+// together with d W and d^T x, where d = (softmax - onehot) * dloss.  The logits are never
+// kept: the forward pass reduces each tile to a maximum and a sum a token, and the
+// gradient makes d for a piece of the vocabulary at a time, rounded to the inputs' 16
+// bits as the matrix units take it, and adds its part of dx in fp32.
+//
+// Tokens whose target is no row of the vocabulary take no part: the others are copied
+// together first, so that neither their time nor what they hold enters anything.
+#include <algorithm>
+#include <type_traits>
+
+#include "c3_internal.h"
+#include "c3_product.h"
+
+namespace c3 {
+namespace {
+
+// What the first launch finds out, at the workspace's start.
+struct Found {
+    int32_t count;          // tokens that take part
+    float raise, lower;     // d is kept times `raise`; lower = 1 / raise
+    int32_t pad;
+};
+
+struct LossArgs {
+    const char* x;
+    const char* weight;
+    const void* targets;
+    const float* dloss;         // null in the forward pass
+    const float* lse_in;
+    float* loss;
+    float* lse;
+    int64_t x_stride, weight_stride, dloss_stride;      // bytes, bytes, elements
+    int64_t tokens, rows;
+    int32_t hidden, wide_targets, half;
+    float scale;
+    // workspace
+    Found* found;
+    int32_t* token;             // [tokens] of each place
+    int32_t* place;             // [tokens] of each token, -1
+    int32_t* target;            // [tokens] by place
+    float* grad;                // [tokens] by place: dloss * scale * raise
+    float* lse_at;              // [tokens] by place
+    char* xc;                   // [tokens][pitch] the rows that take part
+    float2* parts;              // [row tiles][tokens] maximum and sum
+    float* picked;              // [tokens] the target's logit
+    char* d;                    // [tokens][d_pitch]
+    float* dx_parts;            // [splits][tokens][pitch] fp32
+    int32_t pitch;              // elements, hidden rounded up to 8
+    int32_t d_pitch;
+    // this piece of the vocabulary
+    int64_t row0;
+    int32_t piece, first;
+    int32_t splits, split_len;  // of the inner index
+    char* out;                  // dweight
+    int64_t out_stride;
+    float* w_parts;             // [splits][piece][pitch] fp32
+};
+
+__device__ __forceinline__ int32_t target_of(const LossArgs& a, int64_t t) {
+    const int64_t v = a.wide_targets ? static_cast<const int64_t*>(a.targets)[t]
+                                     : (int64_t)static_cast<const int32_t*>(a.targets)[t];
+    return (uint64_t)v < (uint64_t)a.rows ? (int32_t)v : -1;
+}
+
+// ---------------------------------------------------------------------------
+// which tokens take part
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
+    __shared__ int32_t wave_count[16];
+    __shared__ float wave_most[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // a wave's tokens: whole steps of 64 in a row
+    const int64_t each = (a.tokens + 1023) / 1024 * 64;
+    const int64_t begin = wave * each, end = min(a.tokens, begin + each);
+    int32_t count = 0;
+    float most = 0.0f;
+    for (int64_t t = begin + lane; t < end; t += 64) {
+        if (target_of(a, t) < 0) continue;
+        ++count;
+        if (a.dloss != nullptr) most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        count += __shfl_xor(count, m);
+        most = fmaxf(most, __shfl_xor(most, m));
+    }
+    if (lane == 0) {
+        wave_count[wave] = count;
+        wave_most[wave] = most;
+    }
+    __syncthreads();
+    int32_t at = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) at += wave_count[w];
+        all += wave_count[w];
+        most = fmaxf(most, wave_most[w]);
+    }
+    // fp16 holds 6e-8 to 65,504, and d is about dloss over the size of the vocabulary: it
+    // is raised by a power of two that brings the largest dloss to 2^13 .. 2^14
+    int raise = 0;
+    if (a.half && most > 0.0f && most < __builtin_inff())
+        raise = min(max(13 - ilogbf(most), -100), 100);
+    const float up = ldexpf(1.0f, raise);
+    for (int64_t t0 = begin; t0 < end; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const int32_t target = t < end ? target_of(a, t) : -1;
+        const uint64_t some = __ballot(target >= 0);
+        const int32_t p = at + __popcll(some & ((1ull << lane) - 1));
+        at += __popcll(some);
+        if (t >= end) continue;
+        if (target >= 0) {
+            a.token[p] = (int32_t)t;
+            a.target[p] = target;
+            if (a.dloss != nullptr) {
+                a.grad[p] = a.dloss[t * a.dloss_stride] * a.scale * up;
+                a.lse_at[p] = a.lse_in[t];
+                a.place[t] = p;
+            }
+        } else if (a.dloss != nullptr) {
+            a.place[t] = -1;
+        } else {
+            a.loss[t] = 0.0f;
+            a.lse[t] = 0.0f;
+        }
+    }
+    if (tid == 0) *a.found = Found{all, up, ldexpf(1.0f, -raise), 0};
+}
+
+// Their rows, one a wave.
+__global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
+    const int64_t p = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (p >= a.found->count) return;
+    const u32x4* from = reinterpret_cast<const u32x4*>(a.x + (int64_t)a.token[p] * a.x_stride);
+    u32x4* to = reinterpret_cast<u32x4*>(a.xc + p * a.pitch * 2);
+    for (int c = threadIdx.x & 63; c < a.hidden / 8; c += 64) to[c] = from[c];
+}
+
+// ---------------------------------------------------------------------------
+// logits
+// ---------------------------------------------------------------------------
+template <typename T, bool GRAD, int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
+    using P = Product<T, WM, WN, MB, NB, true, true>;
+    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
+    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    uint32_t tm, tn;
+    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), tm, tn)) return;
+    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    const int n0 = tn * P::TN, m0 = tm * P::TM;
+    if (n0 >= count) return;
+    const int64_t row0 = a.row0 + m0;
+    const int rows = (int)min((int64_t)P::TM, a.rows - row0);       // of the vocabulary, left in the tile
+    f32x16 acc[MB][NB] = {};
+    const Operand wa{a.weight + row0 * a.weight_stride, a.weight_stride, rows, a.hidden};
+    const Operand xb{a.xc + (int64_t)n0 * a.pitch * 2, (int64_t)a.pitch * 2, count - n0, a.hidden};
+    P::run(acc, wa, xb, a0, b0, a1, b1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if constexpr (!GRAD) {
+        // maximum and sum a token: in the lane, with the other half's rows, then over the waves
+        float2(*stat)[P::TN] = reinterpret_cast<float2(*)[P::TN]>(a0);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int n = P::n_of(j);
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i][j] *= a.scale;
+            if (rows < P::TM)
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (P::m_of(i, r) >= rows) acc[i][j][r] = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][j][r]);
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - from);
+            sum += __shfl_xor(sum, 32);
+            const int32_t target = n0 + n < count ? a.target[n0 + n] - (int32_t)row0 : -1;
+            if (__ballot(target >= 0 && target < P::TM) != 0) {
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (P::m_of(i, r) == target) a.picked[n0 + n] = acc[i][j][r];
+            }
+            if (lane < 32) stat[wave % WM][n] = make_float2(most, sum);
+        }
+        __syncthreads();
+        for (int n = threadIdx.x; n < P::TN; n += P::kThreads) {
+            if (n0 + n >= count) continue;
+            float most = stat[0][n].x;
+#pragma unroll
+            for (int w = 1; w < WM; ++w) most = fmaxf(most, stat[w][n].x);
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WM; ++w) sum += stat[w][n].y * __expf(stat[w][n].x - from);
+            a.parts[(int64_t)tm * a.tokens + n0 + n] = make_float2(most, sum);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int n = P::n_of(j);
+            if (n0 + n >= count) continue;
+            const float lse = a.lse_at[n0 + n], g = a.grad[n0 + n];
+            const int32_t target = a.target[n0 + n] - (int32_t)row0;
+            T* to = reinterpret_cast<T*>(a.d) + (int64_t)(n0 + n) * a.d_pitch + m0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int m = P::m_of(i, 4 * q);
+                    if (m0 + m >= a.d_pitch) continue;      // zeros up to the pitch
+                    AlignedPack<T, 4> v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float p = __expf(fmaf(acc[i][j][4 * q + r], a.scale, -lse));
+                        if (m + r == target) p -= 1.0f;
+                        v.v[r] = from_f32<T>(m + r < rows ? p * g : 0.0f);
+                    }
+                    *reinterpret_cast<AlignedPack<T, 4>*>(to + m) = v;
+                }
+        }
+    }
+}
+
+// lse and loss of 64 places a workgroup: each of its sixteen waves a run of the tiles.
+__global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int tiles) {
+    __shared__ float2 stat[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t p = (int64_t)blockIdx.x * 64 + lane, count = a.found->count;
+    if ((int64_t)blockIdx.x * 64 >= count) return;
+    const int64_t at = min(p, count - 1);
+    const int each = (tiles + 15) / 16, begin = wave * each, end = min(tiles, begin + each);
+    float most = -__builtin_inff(), sum = 0.0f;
+    for (int t0 = begin; t0 < end; t0 += 8) {
+        float2 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = a.parts[(int64_t)min(t0 + i, end - 1) * a.tokens + at];
+        float next = most;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) next = fmaxf(next, v[i].x);
+        const float from = next == -__builtin_inff() ? 0.0f : next;
+        sum *= __expf(most - from);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += t0 + i < end ? v[i].y * __expf(v[i].x - from) : 0.0f;
+        most = next;
+    }
+    stat[wave][lane] = make_float2(most, sum);
+    __syncthreads();
+    if (wave != 0 || p >= count) return;
+    for (int w = 1; w < 16; ++w) most = fmaxf(most, stat[w][lane].x);
+    const float from = most == -__builtin_inff() ? 0.0f : most;
+    sum = 0.0f;
+    for (int w = 0; w < 16; ++w) sum += stat[w][lane].y * __expf(stat[w][lane].x - from);
+    const float lse = logf(sum) + from;
+    const int32_t token = a.token[p];
+    a.lse[token] = lse;
+    a.loss[token] = lse - a.picked[p];
+}
+
+// ---------------------------------------------------------------------------
+// dx and dweight
+// ---------------------------------------------------------------------------
+// A split's sums in fp32: rows n of `pitch`, added to what earlier pieces left.
+template <typename P, int MB, int NB>
+__device__ __forceinline__ void store_parts(const f32x16 (&acc)[MB][NB], float* to, int64_t pitch, int n_left, int m_left,
+                                            bool add) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int n = P::n_of(j);
+        if (n >= n_left) continue;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int m = P::m_of(i, 4 * q);
+                if (m >= m_left) continue;
+                f32x4* at = reinterpret_cast<f32x4*>(to + n * pitch + m);
+                f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (add) v += *at;
+                *at = v;
+            }
+    }
+}
+
+// dx_parts[split] += d W over the split's share of the piece.
+template <typename T, int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
+    using P = Product<T, WM, WN, MB, NB, false, true>;
+    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
+    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    uint32_t tm, tn;
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), tm, tn)) return;
+    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = blockIdx.y * a.split_len;
+    if (n0 >= count) return;
+    const int inner = min(a.split_len, a.piece - k0);
+    f32x16 acc[MB][NB] = {};
+    const Operand w{a.weight + (a.row0 + k0) * a.weight_stride + (int64_t)m0 * 2, a.weight_stride, a.hidden - m0, inner};
+    const Operand d{a.d + ((int64_t)n0 * a.d_pitch + k0) * 2, (int64_t)a.d_pitch * 2, count - n0, inner};
+    P::run(acc, w, d, a0, b0, a1, b1);
+    float* to = a.dx_parts + ((int64_t)blockIdx.y * a.tokens + n0) * a.pitch + m0;
+    store_parts<P>(acc, to, a.pitch, count - n0, a.hidden - m0, a.first == 0);
+}
+
+// dweight's rows of the piece, or with SPLIT a share of their sums.
+template <typename T, bool SPLIT, int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) {
+    using P = Product<T, WM, WN, MB, NB, false, false>;
+    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
+    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
+    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    uint32_t tm, tn;
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.piece + P::TN - 1) / P::TN), tm, tn)) return;
+    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = SPLIT ? blockIdx.y * a.split_len : 0;
+    const int inner = SPLIT ? min(a.split_len, count - k0) : count;
+    f32x16 acc[MB][NB] = {};
+    const Operand x{a.xc + ((int64_t)k0 * a.pitch + m0) * 2, (int64_t)a.pitch * 2, a.hidden - m0, inner};
+    const Operand d{a.d + ((int64_t)k0 * a.d_pitch + n0) * 2, (int64_t)a.d_pitch * 2, a.d_pitch - n0, inner};
+    P::run(acc, x, d, a0, b0, a1, b1);
+    const int n_left = a.piece - n0;
+    if constexpr (SPLIT) {
+        float* to = a.w_parts + ((int64_t)blockIdx.y * a.piece + n0) * a.pitch + m0;
+        store_parts<P>(acc, to, a.pitch, n_left, a.hidden - m0, false);
+    } else {
+        const float lower = a.found->lower;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int n = P::n_of(j);
+            if (n >= n_left) continue;
+            T* to = reinterpret_cast<T*>(a.out + (a.row0 + n0 + n) * a.out_stride) + m0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int m = P::m_of(i, 4 * q);
+                    if (m0 + m >= a.hidden) continue;
+                    AlignedPack<T, 4> v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v.v[r] = from_f32<T>(acc[i][j][4 * q + r] * lower);
+                    *reinterpret_cast<AlignedPack<T, 4>*>(to + m) = v;
+                }
+        }
+    }
+}
+
+// Rows of results from the splits' sums, in order; one wave a row.  place: which row of
+// the sums a row is (-1: zeros), or null.
+template <typename T>
+__global__ __launch_bounds__(256) void loss_finish_kernel(const Found* found, const float* parts, int splits,
+                                                          int64_t split_rows, int64_t pitch, const int32_t* place,
+                                                          int64_t rows, int hidden, char* out, int64_t out_stride) {
+    const int64_t r = wide_block() * 4 + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    const int64_t p = place != nullptr ? place[r] : r;
+    const float lower = found->lower;
+    for (int c = (threadIdx.x & 63) * 4; c < hidden; c += 256) {
+        f32x4 sum = {};
+        if (p >= 0)
+            for (int s = 0; s < splits; ++s)
+                sum += *reinterpret_cast<const f32x4*>(parts + (s * split_rows + p) * pitch + c);
+        AlignedPack<T, 4> v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.v[i] = from_f32<T>(sum[i] * lower);
+        *reinterpret_cast<AlignedPack<T, 4>*>(out + r * out_stride + c * 2) = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+constexpr int kTile = 256;
+constexpr int64_t kPieceBytes = 512ll << 20;        // of d
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct LossPlan {
+    int64_t found, token, place, target, grad, lse_at, xc, parts, picked, d, dx_parts, w_parts, bytes;
+    int64_t pitch, piece, tiles, splits, split_len, w_splits, w_split_len;
+};
+
+LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
+    LossPlan p{};
+    auto take = [&](int64_t bytes) {
+        const int64_t at = p.bytes;
+        p.bytes += up(bytes, 256);
+        return at;
+    };
+    const int64_t T = a->tokens;
+    p.pitch = up(a->hidden, 8);
+    p.tiles = (a->rows + kTile - 1) / kTile;
+    p.found = take(sizeof(Found));
+    p.token = take(4 * T);
+    p.target = take(4 * T);
+    p.xc = take(2 * T * p.pitch);
+    if (!grad) {
+        p.parts = take(8 * T * p.tiles);
+        p.picked = take(4 * T);
+        return p;
+    }
+    p.place = take(4 * T);
+    p.grad = take(4 * T);
+    p.lse_at = take(4 * T);
+    p.piece = std::min(up(a->rows, kTile), std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kTile * kTile));
+    p.d = take(2 * T * p.piece);
+    // a split of 512 inner indices at least, two workgroups a compute unit
+    const int64_t m_tiles = (a->hidden + kTile - 1) / kTile;
+    const int64_t dx_tiles = std::max<int64_t>(1, m_tiles * ((T + kTile - 1) / kTile));
+    p.splits = std::max<int64_t>(1, std::min(512 / dx_tiles, p.piece / 512));
+    p.split_len = up((p.piece + p.splits - 1) / p.splits, kInner);
+    p.splits = (p.piece + p.split_len - 1) / p.split_len;
+    p.dx_parts = take(4 * p.splits * T * p.pitch);
+    const int64_t w_tiles = m_tiles * (p.piece / kTile);
+    p.w_splits = std::max<int64_t>(1, std::min(512 / w_tiles, T / 512));
+    p.w_split_len = up((T + p.w_splits - 1) / p.w_splits, kInner);
+    p.w_splits = T == 0 ? 1 : (T + p.w_split_len - 1) / p.w_split_len;
+    if (p.w_splits > 1) p.w_parts = take(4 * p.w_splits * p.piece * p.pitch);
+    return p;
+}
+
+int check_sizes(const c3_vocab_loss_t* a) {
+    if (a == nullptr || a->tokens < 0 || a->tokens >= (1ll << 31) || a->rows < 1 || a->rows >= (1ll << 31) ||
+        a->hidden < 1 || (a->target_bytes != 4 && a->target_bytes != 8) || !(a->scale - a->scale == 0.0f) ||
+        a->x_stride < 0 || a->weight_stride < 0)
+        return C3_E_INVAL;
+    if ((a->dtype != C3_BF16 && a->dtype != C3_F16) || a->hidden % 8 != 0 || a->hidden >= (1 << 20) ||
+        a->rows > (1ll << 31) - 2 * kTile ||
+        ((a->rows + kTile - 1) / kTile) * ((a->tokens + kTile - 1) / kTile) >= (1ll << 24))
+        return C3_E_UNSUPPORTED;
+    return C3_OK;
+}
+
+// Rows of 16-byte pieces, `rows` of them.
+int check_rows(const void* p, int64_t stride, int64_t rows, int64_t hidden) {
+    if (p == nullptr || (rows > 1 && stride < hidden)) return C3_E_INVAL;
+    if ((uintptr_t)p % 16 != 0 || (rows > 1 && stride % 8 != 0)) return C3_E_ALIGN;
+    if (rows > 1 && stride >= (1ll << 22)) return C3_E_UNSUPPORTED;    // 256 rows in 31 bits of bytes
+    return C3_OK;
+}
+
+LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, const void* weight, const void* targets,
+                   char* ws) {
+    LossArgs a{};
+    a.x = static_cast<const char*>(x);
+    a.weight = static_cast<const char*>(weight);
+    a.targets = targets;
+    a.x_stride = c->x_stride * 2;
+    a.weight_stride = c->weight_stride * 2;
+    a.tokens = c->tokens;
+    a.rows = c->rows;
+    a.hidden = (int32_t)c->hidden;
+    a.wide_targets = c->target_bytes == 8;
+    a.half = c->dtype == C3_F16;
+    a.scale = c->scale;
+    a.found = reinterpret_cast<Found*>(ws + p.found);
+    a.token = reinterpret_cast<int32_t*>(ws + p.token);
+    a.target = reinterpret_cast<int32_t*>(ws + p.target);
+    a.place = reinterpret_cast<int32_t*>(ws + p.place);
+    a.grad = reinterpret_cast<float*>(ws + p.grad);
+    a.lse_at = reinterpret_cast<float*>(ws + p.lse_at);
+    a.xc = ws + p.xc;
+    a.parts = reinterpret_cast<float2*>(ws + p.parts);
+    a.picked = reinterpret_cast<float*>(ws + p.picked);
+    a.d = ws + p.d;
+    a.dx_parts = reinterpret_cast<float*>(ws + p.dx_parts);
+    a.w_parts = reinterpret_cast<float*>(ws + p.w_parts);
+    a.pitch = (int32_t)p.pitch;
+    a.d_pitch = (int32_t)p.piece;
+    return a;
+}
+
+template <typename T>
+hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
+    loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
+    loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
+    a.row0 = 0;
+    a.piece = (int32_t)up(a.rows, kTile);
+    loss_logits_kernel<T, false, 2, 4, 4, 2><<<dim3(tile_blocks(p.tiles, (a.tokens + kTile - 1) / kTile)), dim3(512), 0,
+                                               s>>>(a);
+    loss_join_kernel<<<dim3((unsigned)((a.tokens + 63) / 64)), dim3(1024), 0, s>>>(a, (int)p.tiles);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_stride, hipStream_t s) {
+    if (a.tokens > 0) {
+        loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
+        loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
+    } else {
+        loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
+    }
+    const int64_t m_tiles = (a.hidden + kTile - 1) / kTile, t_tiles = (a.tokens + kTile - 1) / kTile;
+    for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
+        a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
+        a.first = a.row0 == 0;
+        const int64_t v_tiles = (a.piece + kTile - 1) / kTile;
+        if (a.tokens > 0) {
+            loss_logits_kernel<T, true, 2, 4, 4, 2><<<dim3(tile_blocks(v_tiles, t_tiles)), dim3(512), 0, s>>>(a);
+            a.split_len = (int32_t)p.split_len;
+            loss_dx_kernel<T, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, t_tiles), (unsigned)p.splits), dim3(512), 0, s>>>(a);
+        }
+        a.split_len = (int32_t)p.w_split_len;
+        if (p.w_splits > 1) {
+            loss_dweight_kernel<T, true, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, v_tiles), (unsigned)p.w_splits),
+                                                      dim3(512), 0, s>>>(a);
+            loss_finish_kernel<T><<<wide_grid((uint64_t)(a.piece + 3) / 4), dim3(256), 0, s>>>(
+                a.found, a.w_parts, (int)p.w_splits, a.piece, a.pitch, nullptr, a.piece, a.hidden,
+                a.out + a.row0 * a.out_stride, a.out_stride);
+        } else {
+            loss_dweight_kernel<T, false, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, v_tiles)), dim3(512), 0, s>>>(a);
+        }
+    }
+    if (a.tokens > 0)
+        loss_finish_kernel<T><<<wide_grid((uint64_t)(a.tokens + 3) / 4), dim3(256), 0, s>>>(
+            a.found, a.dx_parts, (int)p.splits, a.tokens, a.pitch, a.place, a.tokens, a.hidden, dx, dx_stride);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace c3
+
+extern "C" {
+
+size_t c3_vocab_loss_workspace_size(const c3_vocab_loss_t* a) {
+    return c3::check_sizes(a) == C3_OK ? (size_t)c3::loss_plan(a, false).bytes : 0;
+}
+
+size_t c3_vocab_loss_grad_workspace_size(const c3_vocab_loss_t* a) {
+    return c3::check_sizes(a) == C3_OK ? (size_t)c3::loss_plan(a, true).bytes : 0;
+}
+
+int c3_vocab_loss(const c3_vocab_loss_t* a, const void* x, const void* weight, const void* targets, float* loss,
+                  float* lse, void* ws, size_t ws_bytes, c3_stream_t stream) {
+    using namespace c3;
+    int rc = check_sizes(a);
+    if (rc != C3_OK || a->tokens == 0) return rc;
+    if (targets == nullptr || loss == nullptr || lse == nullptr || loss == lse) return C3_E_INVAL;
+    if ((rc = check_rows(x, a->x_stride, a->tokens, a->hidden)) != C3_OK ||
+        (rc = check_rows(weight, a->weight_stride, a->rows, a->hidden)) != C3_OK)
+        return rc;
+    if ((uintptr_t)targets % a->target_bytes != 0 || (uintptr_t)loss % 4 != 0 || (uintptr_t)lse % 4 != 0) return C3_E_ALIGN;
+    const LossPlan p = loss_plan(a, false);
+    if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)p.bytes) return C3_E_WORKSPACE;
+    LossArgs k = loss_args(a, p, x, weight, targets, static_cast<char*>(ws));
+    k.loss = loss;
+    k.lse = lse;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const hipError_t e = a->dtype == C3_BF16 ? launch_loss<__bf16>(k, p, s) : launch_loss<_Float16>(k, p, s);
+    return e == hipSuccess ? C3_OK : C3_E_HIP;
+}
+
+int c3_vocab_loss_grad(const c3_vocab_loss_t* a, const float* dloss, int64_t dloss_stride, const void* x,
+                       const void* weight, const void* targets, const float* lse, void* dx, int64_t dx_stride,
+                       void* dweight, int64_t dweight_stride, void* ws, size_t ws_bytes, c3_stream_t stream) {
+    using namespace c3;
+    int rc = check_sizes(a);
+    if (rc != C3_OK) return rc;
+    if ((rc = check_rows(dweight, dweight_stride, a->rows, a->hidden)) != C3_OK) return rc;
+    if (a->tokens > 0) {
+        if (targets == nullptr || dloss == nullptr || lse == nullptr || dloss_stride < 0) return C3_E_INVAL;
+        if ((rc = check_rows(x, a->x_stride, a->tokens, a->hidden)) != C3_OK ||
+            (rc = check_rows(weight, a->weight_stride, a->rows, a->hidden)) != C3_OK ||
+            (rc = check_rows(dx, dx_stride, a->tokens, a->hidden)) != C3_OK)
+            return rc;
+        if (dx == x || dx == weight || dx == dweight || dweight == x || dweight == weight) return C3_E_INVAL;
+        if ((uintptr_t)targets % a->target_bytes != 0 || (uintptr_t)dloss % 4 != 0 || (uintptr_t)lse % 4 != 0)
+            return C3_E_ALIGN;
+    }
+    const LossPlan p = loss_plan(a, true);
+    if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)p.bytes) return C3_E_WORKSPACE;
+    LossArgs k = loss_args(a, p, x, weight, targets, static_cast<char*>(ws));
+    k.dloss = dloss != nullptr ? dloss : reinterpret_cast<const float*>(ws);       // not read without tokens
+    k.dloss_stride = dloss_stride;
+    k.lse_in = lse;
+    k.out = static_cast<char*>(dweight);
+    k.out_stride = dweight_stride * 2;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const hipError_t e = a->dtype == C3_BF16 ? launch_grad<__bf16>(k, p, static_cast<char*>(dx), dx_stride * 2, s)
+                                             : launch_grad<_Float16>(k, p, static_cast<char*>(dx), dx_stride * 2, s);
+    return e == hipSuccess ? C3_OK : C3_E_HIP;
+}
+
+}  // extern "C"

@@ -17,6 +17,7 @@ every step runs in the HIP kernels of libc3.so and there is no CPU fallback.
 * ``embedding(ids, table)``               rows of a table; ``embedding_grad`` its gradient
 * ``residual_norm(x, y, weight)``         residual sum and the norms around a block
 * ``residual_norm_grad``                  its gradient
+* ``vocab_loss(x, weight, targets)``      cross entropy without the logits; ``vocab_loss_grad``
 
 The calls record no graph.  Where torch would record one, tensors that require a
 gradient are refused; under ``torch.no_grad()`` and inside the forward and backward of a
@@ -81,6 +82,12 @@ class ResidualNorm(ctypes.Structure):
                 ("gate", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class VocabLoss(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("target_bytes", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("hidden", ctypes.c_int64), ("rows", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("weight_stride", ctypes.c_int64), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 class RowsOf(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("stride", ctypes.c_int64)]
 
@@ -94,6 +101,7 @@ _EXPERT_ROWS = struct.Struct("@2i4q2P")
 _EMBEDDING = struct.Struct("@2i5qfi")
 _RESIDUAL_NORM = struct.Struct("@2i2q2f2i")
 _ROWS = struct.Struct("@Pq")
+_VOCAB_LOSS = struct.Struct("@2i5qfi")
 
 _ready = None
 
@@ -135,6 +143,13 @@ def _lib():
         L.c3_residual_norm_grad_workspace_size.argtypes = [vp]
         L.c3_residual_norm_grad.restype = i32
         L.c3_residual_norm_grad.argtypes = [vp] * 14 + [sz, vp]
+        for n in ("c3_vocab_loss_workspace_size", "c3_vocab_loss_grad_workspace_size"):
+            getattr(L, n).restype = sz
+            getattr(L, n).argtypes = [vp]
+        L.c3_vocab_loss.restype = i32
+        L.c3_vocab_loss.argtypes = [vp] * 7 + [sz, vp]
+        L.c3_vocab_loss_grad.restype = i32
+        L.c3_vocab_loss_grad.argtypes = [vp, vp, i64] + [vp] * 5 + [i64, vp, i64, vp, sz, vp]
         _ready = L
     return _ready
 
@@ -728,3 +743,72 @@ def residual_norm_grad(dn, dh, x, y, weight, stats, *, post=None, gate=None, sca
     _check(rc, "c3_residual_norm_grad")
     return ResidualNormGrad(dx, dy, sums[0], None if post is None else sums[1],
                             sums[2] if kind == GATE_CHANNELS else dgate)
+
+
+# ---------------------------------------------------------------------------
+# loss over a vocabulary
+# ---------------------------------------------------------------------------
+def _loss_args(x, weight, targets, scale):
+    _rows(x, "x", dim=(2,))
+    _rows(weight, "weight", x.dtype, x.device, (2,))
+    _ids(targets, "targets", x.device)
+    if weight.shape[1] != x.shape[1]:
+        raise C3Error("x and weight must have the same hidden size")
+    if targets.numel() != x.shape[0]:
+        raise C3Error("targets must have one number for each row of x")
+    return _pack(_VOCAB_LOSS, _CODE[x.dtype], targets.element_size(), *x.shape, weight.shape[0], x.stride(0),
+                 weight.stride(0), scale, 0)
+
+
+def _tokens(t, name, x, stream):
+    """fp32 [tokens], the caller's or new."""
+    if t is None:
+        return _new((x.shape[0],), torch.float32, x.device, stream)
+    _dev_tensor(t, name)
+    if t.requires_grad:
+        _no_graph(name)
+    if t.dtype != torch.float32 or t.shape != (x.shape[0],) or t.device != x.device:
+        raise C3Error(f"{name} must be fp32 [{x.shape[0]}] on the device of x")
+    return t
+
+
+def vocab_loss(x, weight, targets, *, scale: float = 1.0, loss=None, lse=None, workspace=None, stream=None):
+    """(loss, lse) fp32 [T] of the softmax cross entropy of the logits scale * x weight^T,
+    which are not kept: lse is their log-sum-exp, loss lse less the target's logit.
+
+    x [T, hidden], weight [rows, hidden], bf16 or fp16, hidden a multiple of 8; targets
+    int32 or int64 [T].  A token whose target is outside [0, rows) takes no part: loss and
+    lse 0, and what its row of x holds is not looked at."""
+    a = _loss_args(x, weight, targets, scale)
+    loss, lse = _tokens(loss, "loss", x, stream), _tokens(lse, "lse", x, stream)
+    ws = _workspace(_lib().c3_vocab_loss_workspace_size(a), workspace, x.device, "vocab_loss", stream)
+    rc = _lib().c3_vocab_loss(a, _ptr(x), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(ws),
+                              ws.numel() * ws.element_size(), _handle(stream, x.device))
+    _check(rc, "c3_vocab_loss")
+    return loss, lse
+
+
+def vocab_loss_grad(dloss, x, weight, targets, lse, *, scale: float = 1.0, dx=None, dweight=None,
+                    workspace=None, stream=None):
+    """(dx, dweight) of ``vocab_loss`` with the same arguments, from its ``lse`` and the
+    gradient dloss fp32 [T] of its losses, which may be one number expanded to [T].  Rows
+    of dx whose token takes no part are zeros.  The workspace holds the softmax of up to
+    512 MiB of tokens by vocabulary at a time."""
+    a = _loss_args(x, weight, targets, scale)
+    if not isinstance(dloss, torch.Tensor) or not dloss.is_cuda:
+        raise C3Error("dloss must be a tensor on a ROCm GPU device")
+    if dloss.requires_grad:
+        _no_graph("dloss")
+    if dloss.dtype != torch.float32 or dloss.shape != (x.shape[0],) or dloss.device != x.device:
+        raise C3Error(f"dloss must be fp32 [{x.shape[0]}] on the device of x")
+    if lse is None:
+        raise C3Error("lse must be that of vocab_loss")
+    lse = _tokens(lse, "lse", x, stream)
+    dx = _out(dx, "dx", x.shape, x.dtype, x.device, stream)
+    dweight = _out(dweight, "dweight", weight.shape, x.dtype, x.device, stream)
+    ws = _workspace(_lib().c3_vocab_loss_grad_workspace_size(a), workspace, x.device, "vocab_loss_grad", stream)
+    rc = _lib().c3_vocab_loss_grad(a, _ptr(dloss), dloss.stride(0), _ptr(x), _ptr(weight), _ptr(targets), _ptr(lse),
+                                   _ptr(dx), dx.stride(0), _ptr(dweight), dweight.stride(0), _ptr(ws),
+                                   ws.numel() * ws.element_size(), _handle(stream, x.device))
+    _check(rc, "c3_vocab_loss_grad")
+    return dx, dweight

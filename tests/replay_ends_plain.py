@@ -113,3 +113,50 @@ def residual_norm(x, y, weight, post, gate, scale, eps, dn=None, dh=None):
     e = ry * (e_a + yhat.abs() * e_c + e_y * c.abs()) + (ROW + 5 * U32) * ry * (a.abs() + (yhat * c).abs())
     out["dy"] = (dy, 1.01 * (U[dt] * dy.abs() + e) + TINY[dt])
     return out
+
+
+# ---------------------------------------------------------------------------
+# loss over a vocabulary
+# ---------------------------------------------------------------------------
+def vocab_loss(x, weight, targets, scale, dloss=None):
+    """{name: (value, bound)} of loss and lse and, with dloss, dx and dweight.
+
+    A logit is a sum of hidden exact products in fp32, off by (hidden + 2) U32 of the sum
+    of their magnitudes at most; exp of an argument a is off by (|a| + 4) U32 of itself,
+    and the sum over the vocabulary, of positive terms, by as much as its terms and 512
+    U32 (2 x 128 in a lane, then tiles: far fewer than that one after the other).  d is
+    rounded once to the inputs' type, and the results once."""
+    T, (V, H) = x.shape[0], weight.shape
+    dt = x.dtype
+    kept = (targets >= 0) & (targets < V)
+    X = torch.where(kept[:, None], d(x), 0.0)
+    W = d(weight)
+    z = scale * (X @ W.T)
+    e_z = ((H + 2) * U32 * abs(scale) * (X.abs() @ W.abs().T) + 2 * U32 * z.abs()).amax(1)
+    lse = torch.logsumexp(z, 1)
+    at = targets.clamp(0, V - 1).long()[:, None]
+    picked = z.gather(1, at)[:, 0]
+    spread = (z.amax(1) - z.amin(1)).clamp(max=90.0)
+    e_lse = e_z + (spread + 4 + 512) * U32 + 2 * U32 * lse.abs()
+    out = {"lse": (torch.where(kept, lse, 0.0), torch.where(kept, e_lse, 0.0)),
+           "loss": (torch.where(kept, lse - picked, 0.0),
+                    torch.where(kept, e_lse + e_z + U32 * (lse - picked).abs(), 0.0))}
+    if dloss is None:
+        return out
+    g = torch.where(kept, d(dloss), 0.0)[:, None] * scale
+    p = (z - lse[:, None]).exp()
+    D = p.clone()
+    D.scatter_add_(1, at, torch.full((T, 1), -1.0, dtype=torch.float64))
+    e_p = p * (e_z + e_lse + (spread + 4) * U32)[:, None] + U32 * D.abs()
+    u = U[dt]
+    # in fp16 the largest d is raised to 2^13 at least, so the smallest step, 2^-24, is
+    # 2^-37 of it; in bf16 nothing is below its numbers
+    small = 2.0 ** -37 * g.abs().max() if dt == torch.float16 else 0.0
+    e_d = (u * D.abs() + e_p) * 1.01 * g.abs() + small
+    D = D * g
+    dx, dw = D @ W, D.T @ X
+    # sums in fp32: hidden or tokens or vocabulary terms, at most (n + 8) U32 of their size
+    out["dx"] = (dx, 1.01 * (u * dx.abs() + e_d @ W.abs() + (V + 8) * U32 * (D.abs() @ W.abs())) + TINY[dt])
+    out["dx"] = (out["dx"][0], torch.where(kept[:, None], out["dx"][1], 0.0))
+    out["dweight"] = (dw, 1.01 * (u * dw.abs() + e_d.T @ X.abs() + (T + 8) * U32 * (D.abs().T @ X.abs())) + TINY[dt])
+    return out

@@ -1,0 +1,177 @@
+"""The loss over a vocabulary and its gradient against plain 64-bit forms: one token to
+many, odd vocabularies, widths that end inside a tile, ignored tokens and what they hold."""
+import pytest
+import torch
+
+import replay_ends_plain as plain
+from replay_plain import within
+
+pytestmark = pytest.mark.gpu
+
+replay = pytest.importorskip("paper_2608_11034_amd.replay")
+DEV = "cuda"
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def _inputs(T, H, V, dtype, ignored=0.0, seed=1, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    weight = (torch.randn((V, H), generator=g) * H ** -0.5).to(dtype)
+    targets = torch.randint(0, V, (T,), generator=g)
+    x = torch.randn((T, H), generator=g) + 5 * torch.rand((T, 1), generator=g) * weight[targets].float()
+    targets[torch.rand((T,), generator=g) < ignored] = -100
+    targets[torch.rand((T,), generator=g) < ignored / 4] = V
+    dloss = (0.5 + torch.rand((T,), generator=g)) * ((64.0 if dtype == F16 else 1.0) / max(T, 1))
+    return x.to(dtype), weight, targets, dloss
+
+
+def _both(x, weight, targets, dloss, scale=1.0, **how):
+    x, weight, targets, dloss = (t.to(DEV) for t in (x, weight, targets, dloss))
+    loss, lse = replay.vocab_loss(x, weight, targets, scale=scale)
+    dx, dweight = replay.vocab_loss_grad(dloss, x, weight, targets, lse, scale=scale, **how)
+    return dict(loss=loss, lse=lse, dx=dx, dweight=dweight)
+
+
+def _compare(got, want, what=""):
+    for name, (value, bound) in want.items():
+        within(got[name], value, bound, f"{what} {name}")
+
+
+SIZES = [(1, 8, 1), (1, 64, 300), (2, 8, 3), (5, 72, 17), (31, 128, 255), (32, 200, 256), (33, 64, 257),
+         (64, 136, 513), (65, 1000, 700), (255, 64, 100), (256, 128, 64), (257, 520, 1000), (600, 264, 1031),
+         (7, 2048, 2500), (16, 64, 5003), (1500, 64, 40), (2100, 136, 300), (3, 4104, 9)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("T,H,V", SIZES)
+def test_sizes(dtype, T, H, V):
+    for ignored, scale in ((0.0, 1.0), (0.4, 0.7)):
+        print("CASE", dtype, T, H, V, ignored, flush=True)
+        v = _inputs(T, H, V, dtype, ignored)
+        _compare(_both(*v, scale=scale), plain.vocab_loss(*v[:3], scale, v[3]), f"{T} {H} {V}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_pieces(dtype):
+    """More of the vocabulary than the softmax of one piece holds."""
+    T, H, V = 33000, 16, 9000
+    print("CASE", dtype, T, H, V, flush=True)
+    v = _inputs(T, H, V, dtype, 0.2, seed=2)
+    _compare(_both(*v), plain.vocab_loss(*v[:3], 1.0, v[3]))
+
+
+def test_ignored_tokens():
+    """What an ignored token holds enters nothing, and the others' bits do not go by it."""
+    T, H, V = 300, 136, 500
+    x, weight, targets, dloss = _inputs(T, H, V, BF16, 0.3, seed=3)
+    gone = (targets < 0) | (targets >= V)
+    clean = _both(x, weight, targets, dloss)
+    x, dloss = x.clone(), dloss.clone()
+    x[gone] = float("nan")
+    dloss[gone] = float("inf")
+    got = _both(x, weight, targets, dloss)
+    for name, t in clean.items():
+        assert torch.equal(got[name], t), name
+    for name in ("loss", "lse", "dx"):
+        assert bool((got[name].cpu()[gone] == 0).all()), name
+    # alone, the others give the same rows
+    alone = _both(x[~gone], weight, targets[~gone], dloss[~gone])
+    for name in ("loss", "lse"):
+        assert torch.equal(alone[name].cpu(), got[name].cpu()[~gone])
+
+
+def test_all_ignored_and_none():
+    x, weight, targets, dloss = _inputs(40, 64, 300, BF16, seed=4)
+    got = _both(torch.full_like(x, float("nan")), weight, torch.full_like(targets, -1), dloss)
+    for t in got.values():
+        assert bool((t == 0).all())
+    got = _both(x[:0], weight, targets[:0], dloss[:0])
+    assert got["dx"].shape == (0, 64) and bool((got["dweight"] == 0).all())
+
+
+def test_strides_and_types_of_targets():
+    T, H, V = 70, 136, 400
+    v = _inputs(T, H, V, BF16, 0.2, seed=5)
+    want = _both(*v)
+    kept = []
+
+    def moved(t):
+        big = torch.full((t.shape[0], H + 24), 77.0, dtype=t.dtype, device=DEV)
+        y = big[:, 8:8 + H]
+        y.copy_(t)
+        kept.append((y, big))
+        return y
+    x, weight = moved(v[0]), moved(v[1])
+    dx, dweight = moved(torch.zeros((T, H), dtype=BF16)), moved(torch.zeros((V, H), dtype=BF16))
+    targets, dloss = v[2].to(torch.int32).to(DEV), v[3].to(DEV)
+    loss, lse = replay.vocab_loss(x, weight, targets)
+    replay.vocab_loss_grad(dloss, x, weight, targets, lse, dx=dx, dweight=dweight)
+    for name, t in dict(loss=loss, lse=lse, dx=dx, dweight=dweight).items():
+        assert torch.equal(t, want[name]), name
+    for y, big in kept:
+        y.fill_(77.0)
+        assert bool((big == 77.0).all())
+    # one number for all tokens, not laid out
+    one = torch.full((1,), 0.25, device=DEV)
+    a = replay.vocab_loss_grad(one.expand(T), x, weight, targets, lse)
+    b = replay.vocab_loss_grad(one.expand(T).contiguous(), x, weight, targets, lse)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -20, 2.0 ** 12])
+def test_gradients_of_any_size_in_fp16(factor):
+    """dx and dweight scale with dloss: a power of two on it is one on them, as long as
+    fp16 holds the results (normal numbers: compared where they are)."""
+    x, weight, targets, dloss = _inputs(200, 64, 3000, F16, seed=6)
+    one = _both(x, weight, targets, dloss)
+    other = _both(x, weight, targets, dloss * factor)
+    for name in ("dx", "dweight"):
+        a, b = one[name].double() * factor, other[name].double()
+        fine = (a.abs() > 2.0 ** -14) & (a.abs() < 60000) & (one[name].double().abs() > 2.0 ** -14)
+        assert factor < 1 or bool(fine.any())
+        assert torch.equal(a[fine], b[fine]), name
+
+
+def test_sure_and_far_logits():
+    """Logits of a few hundred: one row takes all of the sum, or the target has none."""
+    T, H, V = 64, 64, 1000
+    g = torch.Generator().manual_seed(7)
+    weight = torch.randn((V, H), generator=g).to(BF16)
+    targets = torch.randint(0, V, (T,), generator=g)
+    x = (6 * weight[targets].float()).to(BF16)
+    targets[::2] = (targets[::2] + 1) % V
+    dloss = torch.ones((T,))
+    _compare(_both(x, weight, targets, dloss), plain.vocab_loss(x, weight, targets, 1.0, dloss))
+
+
+def test_against_differences():
+    """Differences of the mean loss along the gradient; bf16 steps that the inputs hold
+    exactly (multiples of 2^-4 added to multiples of 2^-4)."""
+    T, H, V = 48, 64, 120
+    g = torch.Generator().manual_seed(8)
+    x = torch.randint(-16, 17, (T, H), generator=g).double() / 16
+    weight = torch.randint(-16, 17, (V, H), generator=g).double() / 16
+    targets = torch.randint(0, V, (T,), generator=g)
+    dloss = torch.ones((T,))
+    got = _both(x.to(BF16), weight.to(BF16), targets, dloss)
+
+    def f(a, b):
+        loss, _ = replay.vocab_loss(a.to(BF16).to(DEV), b.to(BF16).to(DEV), targets.to(DEV))
+        return float(loss.double().sum())
+    for name, (da, db) in dict(dx=(1, 0), dweight=(0, 1)).items():
+        grad = got[name].cpu().double()
+        step = torch.zeros_like(grad)
+        # one entry a row, so that the step is short: the largest of each
+        at = grad.abs().argmax(1, keepdim=True)
+        step.scatter_(1, at, grad.gather(1, at).sign() / 16)
+        quotient = (f(x + da * (step if da else 0), weight + db * (step if db else 0)) -
+                    f(x - da * (step if da else 0), weight - db * (step if db else 0))) / 2
+        want = float((grad * step).sum())
+        assert abs(quotient - want) <= 0.02 * abs(want), (name, quotient, want)
+
+
+def test_same_bits_every_time():
+    v = _inputs(700, 264, 1500, BF16, 0.2, seed=9)
+    first = _both(*v)
+    for _ in range(3):
+        again = _both(*v)
+        assert all(torch.equal(again[n], t) for n, t in first.items())
