@@ -351,7 +351,8 @@ size_t c3_vocab_loss_grad_workspace_size(const c3_vocab_loss_t *a);
  *   targets device [tokens]; loss, lse device fp32 [tokens].
  *   ws      256-byte aligned, not used by another call at the same time.
  * Can be captured.  Errors: C3_E_INVAL, C3_E_ALIGN, C3_E_UNSUPPORTED (type, hidden,
- * stride, 2^24 tiles of 256 rows by 256 tokens or more), C3_E_WORKSPACE, C3_E_HIP.
+ * stride, 2^26 tokens, 2^28 rows or 2^22 tiles of 256 by 256 between any two of tokens,
+ * rows and hidden, or more), C3_E_WORKSPACE, C3_E_HIP.
  */
 int c3_vocab_loss(const c3_vocab_loss_t *a, const void *x, const void *weight, const void *targets,
                   float *loss, float *lse, void *ws, size_t ws_bytes, c3_stream_t stream);

@@ -12,7 +12,7 @@
 // many waves, and every sum is a function of the list alone.
 //
 // Writing a whole table of zeros is most of the gradient's bytes.  It needs no sorted
-// list, so it runs on the other compute units while one workgroup sorts.
+// list, so it runs beside the sort, on compute units that have no part in that.
 #include <algorithm>
 
 #include "c3_internal.h"
@@ -23,12 +23,14 @@ namespace {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kOneSort = 16384;             // tokens that one workgroup sorts in LDS
+constexpr int kOneSort = 4096;              // tokens that one workgroup sorts in LDS
 constexpr int kPerThread = kOneSort / kSortThreads;
-constexpr int kMostBits = 11;               // of a digit
-constexpr int kOneBits = 9;                 // of a digit where one workgroup sorts
+constexpr int kMostBits = 10;               // of a digit
+constexpr int kMostPasses = 4;              // keys have 32 bits at most
 constexpr int kMostRuns = 64;
+constexpr int kNextCounts = 16384;          // runs times digits at most: they are counted in LDS
 constexpr int kMostChunk = 64;
+constexpr int kSumRows = 16;                // rows that a wave has in flight
 
 struct Ids {
     const void* p;
@@ -94,41 +96,29 @@ __device__ __forceinline__ int32_t place_of(uint32_t digit, bool there, int bits
 }
 
 // lds[w][digit] holds wave w's number of keys with the digit: turns it into the wave's
-// first place of the digit.  A thread takes 1 << kPerDigit digits in a row.
-// `extra`: keys of earlier workgroups with the digit, `total`: of all workgroups.
-template <typename Total, typename Before>
-__device__ __forceinline__ void first_places(int32_t* lds, int32_t* wave_sum, int digits, Total total,
-                                             Before before) {
+// first place of the digit, of which a thread has one.  total, before: keys with the
+// digit in all workgroups, and in those before this one.
+template <typename Counted>
+__device__ __forceinline__ void first_places(int32_t* lds, int32_t* wave_sum, int digits, Counted counted) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    constexpr int kEach = (1 << kMostBits) / kSortThreads;
-    int32_t t[kEach], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int d = tid * kEach + j;
-        t[j] = d < digits ? total(d) : 0;
-        sum += t[j];
-    }
-    const int32_t own = sum;
+    int32_t total = 0, before = 0;
+    if (tid < digits) counted(tid, total, before);
+    int32_t sum = total;
     for (int d = 1; d < 64; d <<= 1) {
         const int32_t up = __shfl_up(sum, d);
         if (lane >= d) sum += up;
     }
     if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
-    int32_t first = sum - own;
-    for (int w = 0; w < wave; ++w) first += wave_sum[w];
+    int32_t at = sum - total + before;
+    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+    if (tid < digits) {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int d = tid * kEach + j;
-        if (d < digits) {
-            int32_t at = first + before(d);
-            for (int w = 0; w < kSortWaves; ++w) {
-                const int32_t c = lds[w * digits + d];
-                lds[w * digits + d] = at;
-                at += c;
-            }
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int32_t c = lds[w * digits + tid];
+            lds[w * digits + tid] = at;
+            at += c;
         }
-        first += t[j];
     }
     __syncthreads();
 }
@@ -136,9 +126,9 @@ __device__ __forceinline__ void first_places(int32_t* lds, int32_t* wave_sum, in
 // Up to kOneSort tokens: the keys stay in registers between the passes and change
 // places through LDS.
 __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uint32_t* keys, int32_t* source,
-                         int32_t* lds) {
+                         uint8_t* present, int32_t* lds) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t* wave_sum = lds + (kSortWaves << kOneBits);
+    int32_t* wave_sum = lds + (kSortWaves << kMostBits);
     uint32_t* key_at = reinterpret_cast<uint32_t*>(wave_sum + kSortWaves);
     uint16_t* token_at = reinterpret_cast<uint16_t*>(key_at + kOneSort);
     const int steps = (n + kSortThreads - 1) / kSortThreads;       // of 64 keys, for each wave
@@ -150,7 +140,11 @@ __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uin
         t[s] = base + s * 64;
         k[s] = s < steps && t[s] < n ? ids.key(t[s], rows) : 0;
     }
-    const int passes = (key_bits + kOneBits - 1) / kOneBits;
+    for (uint32_t i = tid; i <= rows / 4; i += kSortThreads) reinterpret_cast<uint32_t*>(present)[i] = 0;
+    // written before the first mark, barriers later; a fence for the whole device would
+    // write back what the zeros' workgroups leave in the cache (30 us)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const int passes = (key_bits + kMostBits - 1) / kMostBits;
     for (int pass = 0; pass < passes; ++pass) {
         const int lo = key_bits * pass / passes, bits = key_bits * (pass + 1) / passes - lo, digits = 1 << bits;
         for (int i = tid; i < kSortWaves * digits; i += kSortThreads) lds[i] = 0;
@@ -160,13 +154,10 @@ __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uin
         for (int s = 0; s < kPerThread; ++s)
             if (s < steps && base + s * 64 < n) atomicAdd(&mine[(k[s] >> lo) & (digits - 1)], 1);
         __syncthreads();
-        first_places(lds, wave_sum, digits,
-                     [&](int d) {
-                         int32_t c = 0;
-                         for (int w = 0; w < kSortWaves; ++w) c += lds[w * digits + d];
-                         return c;
-                     },
-                     [](int) { return 0; });
+        first_places(lds, wave_sum, digits, [&](int d, int32_t& total, int32_t&) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) total += lds[w * digits + d];
+        });
         const bool last = pass == passes - 1;
 #pragma unroll
         for (int s = 0; s < kPerThread; ++s) {
@@ -176,6 +167,7 @@ __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uin
             if (last) {
                 keys[at] = k[s];
                 source[at] = t[s];
+                if (k[s] < rows) present[k[s]] = 1;
             } else {
                 key_at[at] = k[s];
                 token_at[at] = (uint16_t)t[s];
@@ -192,100 +184,144 @@ __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uin
         __syncthreads();
     }
 }
-constexpr int kOneSortWords = (kSortWaves << kOneBits) + kSortWaves + kOneSort + kOneSort / 2;
+constexpr int kOneSortWords = (kSortWaves << kMostBits) + kSortWaves + kOneSort + kOneSort / 2;
 
-// Zeros in the whole table, workgroup b of `blocks`.
+// Rows row0 .. row1 - 1 as zeros, each by one of the workgroups from `first` on, but for
+// those that `present` (null: none) marks.
 template <typename D, int V>
-__device__ void zero_table(D* table, int64_t stride, int64_t rows, int64_t pieces, int64_t b, int64_t blocks) {
-    AlignedPack<D, V> zero;
+struct Zeros {
+    D* table;
+    int64_t stride, row0, row1;
+    const uint8_t* present;
+    FastDiv pieces;
+    uint32_t each;                          // rows of a workgroup: 64 KiB or one
+    int first;
+    static uint32_t rows_of(int64_t pieces) { return (uint32_t)std::max<int64_t>(1, 65536 / V / (int64_t)sizeof(D) / pieces); }
+    int64_t blocks() const { return (row1 - row0 + each - 1) / each; }
+    __device__ __forceinline__ void write() const {
+        const int64_t at = row0 + (wide_block() - first) * each;
+        const uint32_t all = (uint32_t)max((int64_t)0, min((int64_t)each, row1 - at)) * pieces.d;
+        for (uint32_t i = threadIdx.x; i < all; i += blockDim.x) {
+            const uint32_t r = pieces.quot(i), c = i - r * pieces.d;
+            const int64_t row = at + r;
+            if (present != nullptr && present[row] != 0) continue;
+            D* to = table + row * stride + (int64_t)c * V;
+            if constexpr (V == 1) {
+                *to = (D)0.0f;
+            } else {                        // whole words, or they are written piecemeal
 #pragma unroll
-    for (int j = 0; j < V; ++j) zero.v[j] = (D)0.0f;
-    if (stride == pieces * V) {             // one long row
-        pieces *= rows;
-        rows = 1;
-        const int64_t part = (pieces + blocks - 1) / blocks, end = min(pieces, (b + 1) * part);
-        for (int64_t c = b * part + threadIdx.x; c < end; c += kSortThreads)
-            *reinterpret_cast<AlignedPack<D, V>*>(table + c * V) = zero;
-        return;
-    }
-    for (int64_t r = b; r < rows; r += blocks)
-        for (int64_t c = threadIdx.x; c < pieces; c += kSortThreads)
-            *reinterpret_cast<AlignedPack<D, V>*>(table + r * stride + c * V) = zero;
-}
-
-// Workgroup 0 sorts, the others write zeros; or, not SORTS, all write zeros.
-template <typename D, int V, bool SORTS>
-__global__ __launch_bounds__(kSortThreads) void sort_and_zero_kernel(Ids ids, int n, uint32_t rows, int key_bits,
-                                                                     uint32_t* keys, int32_t* source, D* table,
-                                                                     int64_t stride, int64_t pieces) {
-    if constexpr (SORTS) {
-        __shared__ int32_t lds[kOneSortWords];
-        if (blockIdx.x == 0) {
-            sort_one(ids, n, rows, key_bits, keys, source, lds);
-            return;
+                for (int j = 0; j < (int)sizeof(D) * V / 16; ++j) reinterpret_cast<u32x4*>(to)[j] = u32x4{};
+            }
         }
     }
-    zero_table<D, V>(table, stride, rows, pieces, (int64_t)blockIdx.x - SORTS, (int64_t)gridDim.x - SORTS);
+};
+
+// Workgroup 0 sorts, the others write zeros.
+template <typename D, int V>
+__global__ __launch_bounds__(kSortThreads) void sort_one_kernel(Ids ids, int n, uint32_t rows, int key_bits,
+                                                                uint32_t* keys, int32_t* source, uint8_t* present,
+                                                                Zeros<D, V> z) {
+    __shared__ int32_t lds[kOneSortWords];
+    if (wide_block() < z.first)
+        sort_one(ids, n, rows, key_bits, keys, source, present, lds);
+    else
+        z.write();
 }
 
-// More tokens: a counting and a placing launch for every digit.
+// More tokens: a launch counts the lowest digits of every run of tokens, and one for each
+// digit places them.  A placed key counts its next digit for the run that it comes to;
+// these are integers, so their order does not matter.  A workgroup counts in LDS first:
+// one by one a frequent digit's counts would wait for each other in memory (10 us of 18
+// with 16,384 tokens of which half have one high digit).
 struct SortPass {
     Ids ids;                // of the first pass, whose keys and tokens are not written down
     const uint32_t* in_keys;
     const int32_t* in_source;
     uint32_t* keys;
     int32_t* source;
-    int32_t* counts;        // [runs][digits]
-    int64_t n, run;
+    int32_t* counts;        // [passes][runs][1 << kMostBits]
+    uint8_t* present;       // 1 for each row of the table that has a token: stores of one
+                            // value, where bits would be atomics on few words
+    int64_t n;
     uint32_t rows;
-    int lo, bits, first;
-    __device__ __forceinline__ uint32_t key(int64_t i) const { return first ? ids.key(i, rows) : in_keys[i]; }
+    int run_shift;          // log2 of a run's length
+    int runs, pass, passes, key_bits;
+    __device__ __forceinline__ uint32_t key(int64_t i) const { return pass == 0 ? ids.key(i, rows) : in_keys[i]; }
+    __device__ __forceinline__ int lo(int p) const { return key_bits * p / passes; }
+    __device__ __forceinline__ int bits(int p) const { return lo(p + 1) - lo(p); }
+    __device__ __forceinline__ int32_t* count(int p, int64_t r) const {
+        return counts + (((int64_t)p * runs + r) << kMostBits);
+    }
 };
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p) {
+template <typename D, int V>
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Zeros<D, V> z) {
     __shared__ int32_t lds[1 << kMostBits];
-    const int digits = 1 << p.bits;
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) lds[d] = 0;
+    if (wide_block() >= z.first) {
+        z.write();
+        return;
+    }
+    const int digits = 1 << p.bits(0);
+    lds[threadIdx.x] = 0;
+    for (int q = 1; q < p.passes; ++q) p.count(q, blockIdx.x)[threadIdx.x] = 0;
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i <= p.rows / 4; i += (int64_t)p.runs * kSortThreads)
+        reinterpret_cast<uint32_t*>(p.present)[i] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * p.run, end = min(begin + p.run, p.n);
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads)
-        atomicAdd(&lds[(p.key(i) >> p.lo) & (digits - 1)], 1);
+    const int64_t begin = (int64_t)blockIdx.x << p.run_shift, end = min(begin + (1ll << p.run_shift), p.n);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&lds[p.key(i) & (digits - 1)], 1);
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) p.counts[(int64_t)blockIdx.x * digits + d] = lds[d];
+    p.count(0, blockIdx.x)[threadIdx.x] = lds[threadIdx.x];
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p) {
+template <typename D, int V>
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Zeros<D, V> z) {
     __shared__ int32_t lds[(kSortWaves << kMostBits) + kSortWaves];
-    const int digits = 1 << p.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ int32_t next[kNextCounts];
+    if (wide_block() >= z.first) {
+        z.write();
+        return;
+    }
+    const int lo = p.lo(p.pass), bits = p.bits(p.pass), digits = 1 << bits;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t* wave_sum = lds + kSortWaves * digits;
-    const int64_t begin = (int64_t)blockIdx.x * p.run, end = min(begin + p.run, p.n);
-    const int64_t part = p.run / kSortWaves, wb = begin + wave * part, we = min(wb + part, end);
+    const int64_t begin = (int64_t)blockIdx.x << p.run_shift, end = min(begin + (1ll << p.run_shift), p.n);
+    const int64_t part = (1ll << p.run_shift) / kSortWaves, wb = begin + wave * part, we = min(wb + part, end);
+    const bool last = p.pass == p.passes - 1;
+    const int next_lo = p.lo(p.pass + 1), next_bits = last ? 0 : p.bits(p.pass + 1);
     for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortThreads) lds[i] = 0;
+    if (!last)
+        for (int i = threadIdx.x; i < p.runs << next_bits; i += kSortThreads) next[i] = 0;
     __syncthreads();
     int32_t* mine = lds + wave * digits;
-    for (int64_t i = wb + lane; i < we; i += 64) atomicAdd(&mine[(p.key(i) >> p.lo) & (digits - 1)], 1);
+    for (int64_t i = wb + lane; i < we; i += 64) atomicAdd(&mine[(p.key(i) >> lo) & (digits - 1)], 1);
     __syncthreads();
-    const int runs = gridDim.x;
-    auto counted = [&](int d, int before) {
-        int32_t c[16], sum = 0;             // sixteen loads in flight
-        for (int b = 0; b < before; b += 16) {
+    first_places(lds, wave_sum, digits, [&](int d, int32_t& total, int32_t& before) {
+        for (int b = 0; b < p.runs; b += 16) {          // sixteen loads in flight
+            int32_t c[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) c[j] = p.counts[(int64_t)min(b + j, runs - 1) * digits + d];
+            for (int j = 0; j < 16; ++j) c[j] = p.count(p.pass, min(b + j, p.runs - 1))[d];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum += b + j < before ? c[j] : 0;
+            for (int j = 0; j < 16; ++j) {
+                before += b + j < (int)blockIdx.x ? c[j] : 0;
+                total += b + j < p.runs ? c[j] : 0;
+            }
         }
-        return sum;
-    };
-    first_places(lds, wave_sum, digits, [&](int d) { return counted(d, runs); },
-                 [&](int d) { return counted(d, (int)blockIdx.x); });
+    });
     for (int64_t i0 = wb; i0 < we; i0 += 64) {
         const int64_t i = i0 + lane;
         const uint32_t k = i < we ? p.key(i) : 0;
-        const int32_t at = place_of((k >> p.lo) & (digits - 1), i < we, p.bits, mine);
+        const bool repeats = lane > 0 && __shfl_up(k, 1) == k;     // a mark for each lane would crowd a frequent row's
+        const int32_t at = place_of((k >> lo) & (digits - 1), i < we, bits, mine);
         if (at < 0) continue;
         p.keys[at] = k;
-        p.source[at] = p.first ? (int32_t)i : p.in_source[i];
+        p.source[at] = p.pass == 0 ? (int32_t)i : p.in_source[i];
+        if (last && k < p.rows && !repeats) p.present[k] = 1;
+        if (!last) atomicAdd(&next[((at >> p.run_shift) << next_bits) + ((k >> next_lo) & ((1 << next_bits) - 1))], 1);
     }
+    if (last) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.runs << next_bits; i += kSortThreads)
+        if (next[i] != 0) atomicAdd(&p.count(p.pass + 1, i >> next_bits)[i & ((1 << next_bits) - 1)], next[i]);
 }
 
 // ---------------------------------------------------------------------------
@@ -315,10 +351,15 @@ __device__ __forceinline__ void write_row(const SumArgs& a, D* table, uint32_t r
 
 // A wave: the places of one chunk, 64 pieces of the width.
 template <typename S, typename D, int V>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* dout, D* table) {
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* dout, D* table, Zeros<D, V> z) {
+    if (wide_block() >= z.first) {
+        z.write();
+        return;
+    }
     const int lane = threadIdx.x & 63;
-    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
-    const int64_t chunk = w / a.slabs, c = (w - chunk * a.slabs) * 64 + lane;
+    // the same for every lane, in scalar registers; chunks are fewer than 2^31
+    const int64_t w = wide_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t chunk = __builtin_amdgcn_readfirstlane((int)(w / a.slabs)), c = (w - chunk * a.slabs) * 64 + lane;
     if (chunk >= a.chunks) return;
     const int64_t begin = chunk * a.chunk;
     const int count = (int)min((int64_t)a.chunk, a.n - begin);
@@ -331,14 +372,14 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* 
     const int64_t col = (in ? c : 0) * V;
     float sum[V] = {};
     bool whole = (uint32_t)__builtin_amdgcn_readlane(my_key, 0) != before;      // the run began here
-    for (int i0 = 0; i0 < count; i0 += 8) {
-        AlignedPack<S, V> p[8];
+    for (int i0 = 0; i0 < count; i0 += kSumRows) {
+        AlignedPack<S, V> p[kSumRows];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)         // the rows stand without a branch between the loads
+        for (int i = 0; i < kSumRows; ++i)  // the rows stand without a branch between the loads
             p[i] = *reinterpret_cast<const AlignedPack<S, V>*>(
                 dout + (int64_t)__builtin_amdgcn_readlane(my_token, min(i0 + i, count - 1)) * a.dout_stride + col);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kSumRows; ++i) {
             const int at = i0 + i;
             if (at >= count) break;
             const uint32_t key = __builtin_amdgcn_readlane(my_key, at);
@@ -372,14 +413,17 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, D* table
     const int64_t b = wide_block(), chunk = b / a.slabs, c = (b - chunk * a.slabs) * 64 + lane;
     if (chunk + 1 >= a.chunks) return;
     const int64_t begin = chunk * a.chunk, next = begin + a.chunk;
-    const uint32_t key = a.keys[next - 1];
-    if (key >= a.rows || a.keys[next] != key) return;
-    if (a.keys[begin] == key && begin > 0 && a.keys[begin - 1] == key) return;      // began before
-    // the run's last place
-    int64_t lo = next, hi = a.n - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (a.keys[mid] == key) lo = mid; else hi = mid - 1;
+    const uint32_t key = a.keys[next - 1], behind = a.keys[next], at_begin = a.keys[begin];
+    const uint32_t before = begin > 0 ? a.keys[begin - 1] : a.rows;
+    if (key >= a.rows || behind != key || (at_begin == key && before == key)) return;   // no run, or it began before
+    // the run's last place: 64 places are looked at in a step, not one
+    int64_t lo = next, hi = a.n;            // keys[lo] == key, and from hi on it is another
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, probe = lo + lane * step;
+        const uint64_t same = __ballot(probe < hi && a.keys[min(probe, hi - 1)] == key);
+        const int last = 63 - __clzll(same);            // lane 0 looks at lo
+        hi = min(hi, lo + (last + 1) * step);
+        lo += last * step;
     }
     const int64_t last = lo / a.chunk, count = last - chunk + 1, each = (count + 3) / 4;
     const bool in = c < a.pieces;
@@ -421,19 +465,20 @@ int key_bits_of(int64_t rows) {             // keys are 0 .. rows
     return bits;
 }
 
-// Places of a wave.  Sixteen, and with enough of them to fill the device 64, which
-// writes and reads a quarter of the parts.  The sizes alone decide, not the alignment:
-// the order of the sums goes by it.
+// Places of a wave: 16 to 64, as many as leave 4,096 waves.  The sizes alone decide, not
+// the alignment: the order of the sums goes by it.
 int chunk_of(int64_t n, int64_t hidden) {
-    return n * ((hidden + 511) / 512) >= ((int64_t)1 << 19) ? kMostChunk : 16;
+    int chunk = 16;
+    while (chunk < kMostChunk && n / (2 * chunk) * ((hidden + 511) / 512) >= 4096) chunk *= 2;
+    return chunk;
 }
 
 // What stands where in the workspace.
 struct GradPlan {
-    int64_t keys, source, keys2, source2, counts, parts, bytes;
+    int64_t keys, source, keys2, source2, counts, present, parts, bytes;
     bool one;
 };
-GradPlan grad_plan(int64_t n, int64_t hidden) {
+GradPlan grad_plan(int64_t n, int64_t rows, int64_t hidden) {
     GradPlan p{};
     auto take = [&](int64_t bytes) {
         const int64_t at = p.bytes;
@@ -443,10 +488,11 @@ GradPlan grad_plan(int64_t n, int64_t hidden) {
     p.one = n <= kOneSort;
     p.keys = take(4 * n);
     p.source = take(4 * n);
+    p.present = take(rows + 4);
     if (!p.one) {
         p.keys2 = take(4 * n);
         p.source2 = take(4 * n);
-        p.counts = take(4 * (int64_t)kMostRuns << kMostBits);
+        p.counts = take(4 * (int64_t)kMostPasses * kMostRuns << kMostBits);
     }
     const int chunk = chunk_of(n, hidden);
     p.parts = take(4 * 2 * ((n + chunk - 1) / chunk) * hidden);
@@ -467,7 +513,7 @@ struct GradCall {
 
 template <typename S, typename D, int V>
 hipError_t launch_grad(const GradCall& g) {
-    const GradPlan p = grad_plan(g.n, g.hidden);
+    const GradPlan p = grad_plan(g.n, g.rows, g.hidden);
     SumArgs a{};
     a.keys = reinterpret_cast<uint32_t*>(g.ws + p.keys);
     a.source = reinterpret_cast<int32_t*>(g.ws + p.source);
@@ -486,46 +532,68 @@ hipError_t launch_grad(const GradCall& g) {
     const int key_bits = key_bits_of(g.rows);
     uint32_t* keys = reinterpret_cast<uint32_t*>(g.ws + p.keys);
     int32_t* source = reinterpret_cast<int32_t*>(g.ws + p.source);
-    // 1,024 threads write 64 KiB of zeros at least, two workgroups a compute unit
-    const int64_t bytes = g.rows * g.hidden * (int64_t)sizeof(D);
-    const int64_t most = std::min<int64_t>(512, (bytes + 65535) / 65536);
-    const unsigned zeros = g.accumulate ? 0u : (unsigned)most;
-    if (p.one && g.n > 0)
-        sort_and_zero_kernel<D, V, true><<<dim3(1 + zeros), dim3(kSortThreads), 0, g.s>>>(
-            g.ids, (int)g.n, a.rows, key_bits, keys, source, static_cast<D*>(g.table), g.table_stride, a.pieces);
-    else if (zeros > 0)
-        sort_and_zero_kernel<D, V, false><<<dim3(zeros), dim3(kSortThreads), 0, g.s>>>(
-            g.ids, 0, a.rows, key_bits, keys, source, static_cast<D*>(g.table), g.table_stride, a.pieces);
-    if (g.n == 0) return hipGetLastError();
-    if (!p.one) {
-        const int passes = (key_bits + kMostBits - 1) / kMostBits;
-        int64_t run = (g.n + kMostRuns - 1) / kMostRuns;
-        run = (run + kSortThreads - 1) / kSortThreads * kSortThreads;
-        const unsigned runs = (unsigned)((g.n + run - 1) / run);
-        for (int pass = 0; pass < passes; ++pass) {
+    uint8_t* present = reinterpret_cast<uint8_t*>(g.ws + p.present);
+    // The sort's launches leave most of the device idle for some microseconds, in which
+    // kBeside bytes of zeros are written; the rest comes beside the sums, without the rows
+    // that have one.
+    constexpr int64_t kBeside = 24 << 20;
+    const int passes = (key_bits + kMostBits - 1) / kMostBits;
+    Zeros<D, V> z{};
+    z.table = static_cast<D*>(g.table);
+    z.stride = g.table_stride;
+    z.pieces = FastDiv((uint32_t)a.pieces);
+    z.each = Zeros<D, V>::rows_of(a.pieces);
+    z.row1 = g.accumulate ? g.rows : 0;
+    // the grid of a launch with `blocks` workgroups of its own that takes `bytes` of the zeros
+    const auto with_zeros = [&](int64_t blocks, int64_t bytes) {
+        z.first = (int)blocks;
+        z.row0 = z.row1;
+        z.row1 = std::min(g.rows, z.row0 + bytes / (g.hidden * (int64_t)sizeof(D)) / z.each * z.each);
+        return wide_grid((uint64_t)(blocks + z.blocks()));
+    };
+    constexpr int64_t kAll = (int64_t)1 << 62;
+    if (g.n == 0) {
+        const dim3 grid = with_zeros(0, kAll);
+        embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
+                                                                  static_cast<D*>(g.table), z);
+        return hipGetLastError();
+    }
+    if (p.one) {
+        const dim3 grid = with_zeros(1, 2 * kBeside);
+        sort_one_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits, keys, source,
+                                                                   present, z);
+    } else {
+        SortPass q{};
+        q.ids = g.ids;
+        q.counts = reinterpret_cast<int32_t*>(g.ws + p.counts);
+        q.present = present;
+        q.n = g.n;
+        q.rows = a.rows;
+        q.run_shift = 10;
+        const int most_runs = std::min(kMostRuns, kNextCounts >> ((key_bits + passes - 1) / passes));
+        while (((g.n - 1) >> q.run_shift) >= most_runs) ++q.run_shift;
+        q.runs = (int)((g.n - 1) >> q.run_shift) + 1;
+        q.passes = passes;
+        q.key_bits = key_bits;
+        dim3 grid = with_zeros(q.runs, kBeside);
+        sort_count_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
+        for (q.pass = 0; q.pass < passes; ++q.pass) {
             // the last pass writes to the first pair of lists
-            const bool to_first = (passes - 1 - pass) % 2 == 0;
+            const bool to_first = (passes - 1 - q.pass) % 2 == 0;
             uint32_t* k2 = reinterpret_cast<uint32_t*>(g.ws + p.keys2);
             int32_t* s2 = reinterpret_cast<int32_t*>(g.ws + p.source2);
-            SortPass q{};
-            q.ids = g.ids;
             q.in_keys = to_first ? k2 : keys;
             q.in_source = to_first ? s2 : source;
             q.keys = to_first ? keys : k2;
             q.source = to_first ? source : s2;
-            q.counts = reinterpret_cast<int32_t*>(g.ws + p.counts);
-            q.n = g.n;
-            q.run = run;
-            q.rows = a.rows;
-            q.lo = key_bits * pass / passes;
-            q.bits = key_bits * (pass + 1) / passes - q.lo;
-            q.first = pass == 0;
-            sort_count_kernel<<<dim3(runs), dim3(kSortThreads), 0, g.s>>>(q);
-            sort_place_kernel<<<dim3(runs), dim3(kSortThreads), 0, g.s>>>(q);
+            grid = with_zeros(q.runs, kBeside);
+            sort_place_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         }
     }
-    embedding_sum_kernel<S, D, V><<<wide_grid((uint64_t)(a.chunks * a.slabs + 3) / 4), dim3(256), 0, g.s>>>(
-        a, static_cast<const S*>(g.dout), static_cast<D*>(g.table));
+    const dim3 grid = with_zeros((a.chunks * a.slabs + 3) / 4, kAll);
+    z.present = present;
+    embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
+                                                              static_cast<D*>(g.table), z);
     if (a.chunks > 1)
         embedding_join_kernel<D, V><<<wide_grid((uint64_t)(a.chunks - 1) * a.slabs), dim3(256), 0, g.s>>>(
             a, static_cast<D*>(g.table));
@@ -612,7 +680,7 @@ int c3_embedding(const c3_embedding_t* a, const void* ids, const void* table, vo
 size_t c3_embedding_grad_workspace_size(const c3_embedding_t* a) {
     using namespace c3;
     if (check_sizes(a) != C3_OK) return 0;
-    return (size_t)grad_plan(a->tokens, a->hidden).bytes;
+    return (size_t)grad_plan(a->tokens, a->rows, a->hidden).bytes;
 }
 
 int c3_embedding_grad(const c3_embedding_t* a, const void* dout, const void* ids, void* dtable, int table_dtype,
@@ -628,10 +696,12 @@ int c3_embedding_grad(const c3_embedding_t* a, const void* dout, const void* ids
     if ((uintptr_t)ids % a->id_bytes != 0 || (uintptr_t)dout % replay_elem_size(a->dtype) != 0 ||
         (uintptr_t)dtable % replay_elem_size(table_dtype) != 0)
         return C3_E_ALIGN;
-    if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)grad_plan(a->tokens, a->hidden).bytes)
+    if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)grad_plan(a->tokens, a->rows, a->hidden).bytes)
         return C3_E_WORKSPACE;
-    // workgroups are counted in 32 bits
-    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34)) return C3_E_UNSUPPORTED;
+    // the sums' workgroups are counted in 31 bits, the zeros' in a grid's 2^22 by 2^16
+    const int64_t row_bytes = a->hidden * replay_elem_size(table_dtype);
+    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34) || a->rows / std::max<int64_t>(1, 65536 / row_bytes) >= (1ll << 37))
+        return C3_E_UNSUPPORTED;
     const GradCall g{{ids, a->id_bytes == 8}, a->tokens, a->rows, a->hidden, a->row_stride, a->table_stride, dout,
                      dtable, a->scale, accumulate != 0, static_cast<char*>(ws), reinterpret_cast<hipStream_t>(stream)};
     hipError_t e;

@@ -48,7 +48,7 @@ struct LossArgs {
     float* picked;              // [tokens] the target's logit
     char* d;                    // [tokens][d_pitch]
     float* dx_parts;            // [splits][tokens][pitch] fp32
-    int32_t pitch;              // elements, hidden rounded up to 8
+    int32_t pitch;              // elements: hidden
     int32_t d_pitch;
     // this piece of the vocabulary
     int64_t row0;
@@ -211,30 +211,154 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
             a.parts[(int64_t)tm * a.tokens + n0 + n] = make_float2(most, sum);
         }
     } else {
+        float lse[NB], g[NB];
+        int32_t target[NB];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const int n = P::n_of(j);
-            if (n0 + n >= count) continue;
-            const float lse = a.lse_at[n0 + n], g = a.grad[n0 + n];
-            const int32_t target = a.target[n0 + n] - (int32_t)row0;
-            T* to = reinterpret_cast<T*>(a.d) + (int64_t)(n0 + n) * a.d_pitch + m0;
+            const int n = min(n0 + P::n_of(j), count - 1);
+            lse[j] = a.lse_at[n];
+            g[j] = a.grad[n];
+            target[j] = a.target[n] - (int32_t)row0;
+        }
+        __syncthreads();
+        store_rows<P, T, MB, NB>(
+            a0, b0, a1, b1, a.d_pitch - m0,         // zeros up to the pitch
+            [&](int j, int i, int r) {
+                const int m = P::m_of(i, r);
+                float p = __expf(fmaf(acc[i][j][r], a.scale, -lse[j]));
+                if (m == target[j]) p -= 1.0f;
+                return from_f32<T>(m < rows ? p * g[j] : 0.0f);
+            },
+            [&](int n) {
+                return n0 + n < count ? reinterpret_cast<T*>(a.d) + (int64_t)(n0 + n) * a.d_pitch + m0 : nullptr;
+            });
+    }
+}
+
+// The forward pass of few tokens is bound by reading the weights once.  A workgroup has
+// 32 MB rows of them, and its two waves take every other tile of the inner index: each
+// loads tiles to LDS of its own, two ahead of the one that it multiplies, and waits for
+// no other wave.  The sums come together at the end, in the order of the waves.
+constexpr int kFewWaves = 2;
+
+template <typename T, int MB, int NB>
+__global__ __launch_bounds__(kFewWaves * 64) void loss_few_kernel(LossArgs a) {
+    // each wave's tiles as those of a workgroup of one wave
+    using TileW = Tile<MB * 32, true, 1>;
+    using TileX = Tile<NB * 32, true, 1>;
+    constexpr int kPart = TileW::kBytes + TileX::kBytes, kLoads = TileW::kLoads + TileX::kLoads;
+    // a stage each its own object, or the compiler would wait for all loads before a read
+    __shared__ __attribute__((aligned(1024))) char s0[kFewWaves * kPart];
+    __shared__ __attribute__((aligned(1024))) char s1[kFewWaves * kPart];
+    __shared__ __attribute__((aligned(1024))) char s2[kFewWaves * kPart];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tokens = (int)a.tokens;
+    const int64_t row0 = (int64_t)blockIdx.x * MB * 32;
+    const int rows = (int)min((int64_t)MB * 32, a.rows - row0);
+    const Operand ow{a.weight + row0 * a.weight_stride, a.weight_stride, rows, a.hidden};
+    const Operand ox{a.x, a.x_stride, tokens, a.hidden};
+    const TileW tw(ow, 0);
+    const TileX tx(ox, 0);
+    f32x16 acc[MB][NB] = {};
+    const int steps = (a.hidden + kInner - 1) / kInner;     // of all waves
+    const auto load = [&](int s, char* stage) {             // zeros behind the last step
+        char* p = stage + wave * kPart;
+        tw.load(ow, min(s, steps) * kInner, p, 0);
+        tx.load(ox, min(s, steps) * kInner, p + TileW::kBytes, 0);
+    };
+    const auto step = [&](int s, const char* stage, char* ahead) {
+        // the reads of the tile that was in `ahead` are through
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load(s + 2 * kFewWaves, ahead);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        const char* p = stage + wave * kPart;
+#pragma unroll
+        for (int ks = 0; ks < kInner / 16; ++ks) {
+            u32x4 fw[MB], fx[NB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) fw[i] = tw.operand(p, i, ks);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) fx[j] = tx.operand(p + TileW::kBytes, j, ks);
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int m = P::m_of(i, 4 * q);
-                    if (m0 + m >= a.d_pitch) continue;      // zeros up to the pitch
-                    AlignedPack<T, 4> v;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float p = __expf(fmaf(acc[i][j][4 * q + r], a.scale, -lse));
-                        if (m + r == target) p -= 1.0f;
-                        v.v[r] = from_f32<T>(m + r < rows ? p * g : 0.0f);
-                    }
-                    *reinterpret_cast<AlignedPack<T, 4>*>(to + m) = v;
-                }
+                for (int j = 0; j < NB; ++j) acc[i][j] = mfma_32x32x16<T>(fw[i], fx[j], acc[i][j]);
         }
+    };
+    load(wave, s0);
+    load(wave + kFewWaves, s1);
+    for (int s = wave; s < steps; s += 3 * kFewWaves) {
+        step(s, s0, s2);
+        step(s + kFewWaves, s1, s0);
+        step(s + 2 * kFewWaves, s2, s1);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    // block i, j, register r of wave w: [(w - 1)][i][j][r][lane]
+    float* sums = reinterpret_cast<float*>(s0);
+    static_assert((kFewWaves - 1) * MB * NB * 4096 <= sizeof(s0), "room for the sums");
+    if (wave > 0)
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sums[((((wave - 1) * MB + i) * NB + j) * 16 + r) * 64 + lane] = acc[i][j][r];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int n = j * 32 + (lane & 31);
+        const int32_t target = n < tokens ? target_of(a, n) : -1;
+        const int64_t at = target >= 0 ? target - row0 : -1;
+        float most = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float v = acc[i][j][r];
+#pragma unroll
+                for (int w = 0; w < kFewWaves - 1; ++w) v += sums[(((w * MB + i) * NB + j) * 16 + r) * 64 + lane];
+                const int m = i * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+                v = m < rows ? v * a.scale : -__builtin_inff();
+                if (m == at) a.picked[n] = v;
+                acc[i][j][r] = v;
+                most = fmaxf(most, v);
+            }
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float from = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - from);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 32 && n < tokens) a.parts[(int64_t)n * gridDim.x + blockIdx.x] = make_float2(most, sum);
+    }
+}
+
+// lse and loss of one of few tokens a workgroup.
+__global__ __launch_bounds__(1024) void loss_few_join_kernel(LossArgs a, int tiles) {
+    __shared__ float2 stat[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t = blockIdx.x;
+    float most = -__builtin_inff(), sum = 0.0f;
+    const auto join = [&](float2 v) {
+        const float next = fmaxf(most, v.x), from = next == -__builtin_inff() ? 0.0f : next;
+        sum = sum * __expf(most - from) + v.y * __expf(v.x - from);
+        most = next;
+    };
+    for (int i = threadIdx.x; i < tiles; i += 1024) join(a.parts[t * tiles + i]);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) join(make_float2(__shfl_xor(most, m), __shfl_xor(sum, m)));
+    if (lane == 0) stat[wave] = make_float2(most, sum);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 16; ++w) join(stat[w]);
+    const bool kept = target_of(a, t) >= 0;
+    const float lse = logf(sum) + (most == -__builtin_inff() ? 0.0f : most);
+    a.lse[t] = kept ? lse : 0.0f;
+    a.loss[t] = kept ? lse - a.picked[t] : 0.0f;
 }
 
 // lse and loss of 64 places a workgroup: each of its sixteen waves a run of the tiles.
@@ -342,60 +466,77 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) 
         store_parts<P>(acc, to, a.pitch, n_left, a.hidden - m0, false);
     } else {
         const float lower = a.found->lower;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int n = P::n_of(j);
-            if (n >= n_left) continue;
-            T* to = reinterpret_cast<T*>(a.out + (a.row0 + n0 + n) * a.out_stride) + m0;
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int m = P::m_of(i, 4 * q);
-                    if (m0 + m >= a.hidden) continue;
-                    AlignedPack<T, 4> v;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v.v[r] = from_f32<T>(acc[i][j][4 * q + r] * lower);
-                    *reinterpret_cast<AlignedPack<T, 4>*>(to + m) = v;
-                }
-        }
+        __syncthreads();
+        store_rows<P, T, MB, NB>(
+            a0, b0, a1, b1, a.hidden - m0, [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] * lower); },
+            [&](int n) {
+                return n < n_left ? reinterpret_cast<T*>(a.out + (a.row0 + n0 + n) * a.out_stride) + m0 : nullptr;
+            });
     }
 }
 
-// Rows of results from the splits' sums, in order; one wave a row.  place: which row of
-// the sums a row is (-1: zeros), or null.
+// Rows of results from the splits' sums, in order; a wave has 256 columns of a row.
+// place: which row of the sums a row is (-1: zeros), or null.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_finish_kernel(const Found* found, const float* parts, int splits,
                                                           int64_t split_rows, int64_t pitch, const int32_t* place,
                                                           int64_t rows, int hidden, char* out, int64_t out_stride) {
-    const int64_t r = wide_block() * 4 + (threadIdx.x >> 6);
-    if (r >= rows) return;
+    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
+    const uint32_t slabs = (hidden + 255) / 256;
+    const int64_t r = w / slabs;
+    const int c = (int)(w - r * slabs) * 256 + (threadIdx.x & 63) * 4;
+    if (r >= rows || c >= hidden) return;
     const int64_t p = place != nullptr ? place[r] : r;
-    const float lower = found->lower;
-    for (int c = (threadIdx.x & 63) * 4; c < hidden; c += 256) {
-        f32x4 sum = {};
-        if (p >= 0)
-            for (int s = 0; s < splits; ++s)
-                sum += *reinterpret_cast<const f32x4*>(parts + (s * split_rows + p) * pitch + c);
-        AlignedPack<T, 4> v;
+    f32x4 sum = {};
+    if (p >= 0) {
+        const float* from = parts + p * pitch + c;
+        for (int s0 = 0; s0 < splits; s0 += 8) {
+            f32x4 v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.v[i] = from_f32<T>(sum[i] * lower);
-        *reinterpret_cast<AlignedPack<T, 4>*>(out + r * out_stride + c * 2) = v;
+            for (int i = 0; i < 8; ++i)
+                v[i] = *reinterpret_cast<const f32x4*>(from + min(s0 + i, splits - 1) * split_rows * pitch);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (s0 + i < splits) sum += v[i];
+        }
     }
+    const float lower = found->lower;
+    AlignedPack<T, 4> v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.v[i] = from_f32<T>(sum[i] * lower);
+    *reinterpret_cast<AlignedPack<T, 4>*>(out + r * out_stride + c * 2) = v;
 }
 
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-constexpr int kTile = 256;
 constexpr int64_t kPieceBytes = 512ll << 20;        // of d
+constexpr int kPieceRows = 256;                     // a piece is a multiple of
+constexpr int kFewTokens = 64;
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+int64_t tiles(int64_t x, int64_t size) { return (x + size - 1) / size; }
+
+// Tiles of 256 by 256 sums a workgroup of eight waves, or, where there are too few of them
+// for two on every compute unit, of 128 by 128 and four waves.
+int tile_size(int64_t first, int64_t second) { return tiles(first, 256) * tiles(second, 256) >= 512 ? 256 : 128; }
+// The few tokens' rows of the weights in a workgroup: the more tokens, the more of LDS is theirs.
+int few_rows(int64_t tokens) { return tokens <= 32 ? 64 : 32; }
 
 struct LossPlan {
     int64_t found, token, place, target, grad, lse_at, xc, parts, picked, d, dx_parts, w_parts, bytes;
-    int64_t pitch, piece, tiles, splits, split_len, w_splits, w_split_len;
+    int64_t pitch, piece, row_tiles, splits, split_len, w_splits, w_split_len;
+    int tile, dx_tile, w_tile;
+    bool few;
 };
+
+// How often an inner index of `length` is split: two workgroups a compute unit, with 512
+// indices or more each.
+void split(int64_t sums, int64_t length, int64_t* splits, int64_t* split_len) {
+    *splits = std::max<int64_t>(1, std::min(512 / std::max<int64_t>(sums, 1), length / 512));
+    *split_len = std::max<int64_t>(kInner, up((length + *splits - 1) / *splits, kInner));
+    *splits = std::max<int64_t>(1, tiles(length, *split_len));
+}
 
 LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     LossPlan p{};
@@ -404,35 +545,34 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
         p.bytes += up(bytes, 256);
         return at;
     };
-    const int64_t T = a->tokens;
-    p.pitch = up(a->hidden, 8);
-    p.tiles = (a->rows + kTile - 1) / kTile;
+    const int64_t T = a->tokens, H = a->hidden;
+    p.pitch = H;
     p.found = take(sizeof(Found));
+    if (!grad) {
+        p.few = T <= kFewTokens;
+        p.tile = tile_size(a->rows, T);
+        p.row_tiles = tiles(a->rows, p.few ? few_rows(T) : p.tile);
+        p.parts = take(8 * T * p.row_tiles);
+        p.picked = take(4 * T);
+        if (p.few) return p;
+    }
     p.token = take(4 * T);
     p.target = take(4 * T);
-    p.xc = take(2 * T * p.pitch);
-    if (!grad) {
-        p.parts = take(8 * T * p.tiles);
-        p.picked = take(4 * T);
-        return p;
-    }
+    p.xc = take(2 * T * H);
+    if (!grad) return p;
     p.place = take(4 * T);
     p.grad = take(4 * T);
     p.lse_at = take(4 * T);
-    p.piece = std::min(up(a->rows, kTile), std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kTile * kTile));
+    p.piece = std::min(up(a->rows, kPieceRows),
+                       std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows));
     p.d = take(2 * T * p.piece);
-    // a split of 512 inner indices at least, two workgroups a compute unit
-    const int64_t m_tiles = (a->hidden + kTile - 1) / kTile;
-    const int64_t dx_tiles = std::max<int64_t>(1, m_tiles * ((T + kTile - 1) / kTile));
-    p.splits = std::max<int64_t>(1, std::min(512 / dx_tiles, p.piece / 512));
-    p.split_len = up((p.piece + p.splits - 1) / p.splits, kInner);
-    p.splits = (p.piece + p.split_len - 1) / p.split_len;
-    p.dx_parts = take(4 * p.splits * T * p.pitch);
-    const int64_t w_tiles = m_tiles * (p.piece / kTile);
-    p.w_splits = std::max<int64_t>(1, std::min(512 / w_tiles, T / 512));
-    p.w_split_len = up((T + p.w_splits - 1) / p.w_splits, kInner);
-    p.w_splits = T == 0 ? 1 : (T + p.w_split_len - 1) / p.w_split_len;
-    if (p.w_splits > 1) p.w_parts = take(4 * p.w_splits * p.piece * p.pitch);
+    p.tile = tile_size(p.piece, T);
+    p.dx_tile = tile_size(H, T);
+    split(tiles(H, p.dx_tile) * tiles(T, p.dx_tile), p.piece, &p.splits, &p.split_len);
+    p.dx_parts = take(4 * p.splits * T * H);
+    p.w_tile = tile_size(H, p.piece);
+    split(tiles(H, p.w_tile) * tiles(p.piece, p.w_tile), T, &p.w_splits, &p.w_split_len);
+    if (p.w_splits > 1) p.w_parts = take(4 * p.w_splits * p.piece * H);
     return p;
 }
 
@@ -441,9 +581,10 @@ int check_sizes(const c3_vocab_loss_t* a) {
         a->hidden < 1 || (a->target_bytes != 4 && a->target_bytes != 8) || !(a->scale - a->scale == 0.0f) ||
         a->x_stride < 0 || a->weight_stride < 0)
         return C3_E_INVAL;
-    if ((a->dtype != C3_BF16 && a->dtype != C3_F16) || a->hidden % 8 != 0 || a->hidden >= (1 << 20) ||
-        a->rows > (1ll << 31) - 2 * kTile ||
-        ((a->rows + kTile - 1) / kTile) * ((a->tokens + kTile - 1) / kTile) >= (1ll << 24))
+    if ((a->dtype != C3_BF16 && a->dtype != C3_F16) || a->hidden % 8 != 0 || a->hidden >= (1 << 20)) return C3_E_UNSUPPORTED;
+    // a launch holds fewer than 2^32 threads
+    const int64_t t = tiles(a->tokens, 256), v = tiles(a->rows, 256), h = tiles(a->hidden, 256), most = 1 << 22;
+    if (a->tokens >= (1 << 26) || a->rows >= (1 << 28) || v * t >= most || h * t >= most || h * v >= most)
         return C3_E_UNSUPPORTED;
     return C3_OK;
 }
@@ -487,50 +628,78 @@ LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, c
     return a;
 }
 
+// Calls f with the waves and blocks of a tile: f(Shape<WM, WN, MB, NB>).
+template <int WM_, int WN_, int MB_, int NB_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, kThreads = WM * WN * 64;
+};
+template <typename F>
+void by_tile(int size, F f) {
+    if (size == 256) f(Shape<2, 4, 4, 2>{});
+    else f(Shape<2, 2, 2, 2>{});
+}
+
+template <typename T, bool GRAD>
+void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
+    by_tile(tile, [&](auto shape) {
+        using S = decltype(shape);
+        loss_logits_kernel<T, GRAD, S::WM, S::WN, S::MB, S::NB>
+            <<<dim3(tile_blocks(tiles(rows, tile), tiles(a.tokens, tile))), dim3(S::kThreads), 0, s>>>(a);
+    });
+}
+
 template <typename T>
 hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
+    if (p.few) {
+        const dim3 grid((unsigned)p.row_tiles), block(kFewWaves * 64);
+        if (few_rows(a.tokens) == 64) loss_few_kernel<T, 2, 1><<<grid, block, 0, s>>>(a);
+        else loss_few_kernel<T, 1, 2><<<grid, block, 0, s>>>(a);
+        loss_few_join_kernel<<<dim3((unsigned)a.tokens), dim3(1024), 0, s>>>(a, (int)p.row_tiles);
+        return hipGetLastError();
+    }
     loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
     loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
     a.row0 = 0;
-    a.piece = (int32_t)up(a.rows, kTile);
-    loss_logits_kernel<T, false, 2, 4, 4, 2><<<dim3(tile_blocks(p.tiles, (a.tokens + kTile - 1) / kTile)), dim3(512), 0,
-                                               s>>>(a);
-    loss_join_kernel<<<dim3((unsigned)((a.tokens + 63) / 64)), dim3(1024), 0, s>>>(a, (int)p.tiles);
+    a.piece = (int32_t)a.rows;
+    launch_logits<T, false>(a, a.rows, p.tile, s);
+    loss_join_kernel<<<dim3((unsigned)((a.tokens + 63) / 64)), dim3(1024), 0, s>>>(a, (int)p.row_tiles);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_stride, hipStream_t s) {
-    if (a.tokens > 0) {
-        loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
-        loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
-    } else {
-        loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
-    }
-    const int64_t m_tiles = (a.hidden + kTile - 1) / kTile, t_tiles = (a.tokens + kTile - 1) / kTile;
+    const auto finish = [&](const float* parts, int64_t splits, const int32_t* place, int64_t rows, char* out, int64_t stride) {
+        loss_finish_kernel<T><<<wide_grid((uint64_t)(rows * ((a.hidden + 255) / 256) + 3) / 4), dim3(256), 0, s>>>(
+            a.found, parts, (int)splits, rows, a.pitch, place, rows, a.hidden, out, stride);
+    };
+    loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
+    if (a.tokens > 0) loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
     for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
         a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
         a.first = a.row0 == 0;
-        const int64_t v_tiles = (a.piece + kTile - 1) / kTile;
         if (a.tokens > 0) {
-            loss_logits_kernel<T, true, 2, 4, 4, 2><<<dim3(tile_blocks(v_tiles, t_tiles)), dim3(512), 0, s>>>(a);
+            launch_logits<T, true>(a, a.piece, p.tile, s);
             a.split_len = (int32_t)p.split_len;
-            loss_dx_kernel<T, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, t_tiles), (unsigned)p.splits), dim3(512), 0, s>>>(a);
+            by_tile(p.dx_tile, [&](auto shape) {
+                using S = decltype(shape);
+                loss_dx_kernel<T, S::WM, S::WN, S::MB, S::NB>
+                    <<<dim3(tile_blocks(tiles(a.hidden, p.dx_tile), tiles(a.tokens, p.dx_tile)), (unsigned)p.splits),
+                       dim3(S::kThreads), 0, s>>>(a);
+            });
         }
         a.split_len = (int32_t)p.w_split_len;
-        if (p.w_splits > 1) {
-            loss_dweight_kernel<T, true, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, v_tiles), (unsigned)p.w_splits),
-                                                      dim3(512), 0, s>>>(a);
-            loss_finish_kernel<T><<<wide_grid((uint64_t)(a.piece + 3) / 4), dim3(256), 0, s>>>(
-                a.found, a.w_parts, (int)p.w_splits, a.piece, a.pitch, nullptr, a.piece, a.hidden,
-                a.out + a.row0 * a.out_stride, a.out_stride);
-        } else {
-            loss_dweight_kernel<T, false, 2, 4, 4, 2><<<dim3(tile_blocks(m_tiles, v_tiles)), dim3(512), 0, s>>>(a);
-        }
+        by_tile(p.w_tile, [&](auto shape) {
+            using S = decltype(shape);
+            const dim3 grid(tile_blocks(tiles(a.hidden, p.w_tile), tiles(a.piece, p.w_tile)), (unsigned)p.w_splits);
+            if (p.w_splits > 1)
+                loss_dweight_kernel<T, true, S::WM, S::WN, S::MB, S::NB><<<grid, dim3(S::kThreads), 0, s>>>(a);
+            else
+                loss_dweight_kernel<T, false, S::WM, S::WN, S::MB, S::NB><<<grid, dim3(S::kThreads), 0, s>>>(a);
+        });
+        if (p.w_splits > 1)
+            finish(a.w_parts, p.w_splits, nullptr, a.piece, a.out + a.row0 * a.out_stride, a.out_stride);
     }
-    if (a.tokens > 0)
-        loss_finish_kernel<T><<<wide_grid((uint64_t)(a.tokens + 3) / 4), dim3(256), 0, s>>>(
-            a.found, a.dx_parts, (int)p.splits, a.tokens, a.pitch, a.place, a.tokens, a.hidden, dx, dx_stride);
+    if (a.tokens > 0) finish(a.dx_parts, p.splits, a.place, a.tokens, dx, dx_stride);
     return hipGetLastError();
 }
 

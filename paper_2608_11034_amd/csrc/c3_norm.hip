@@ -8,101 +8,12 @@
 // are loaded, not which thread has them, so the bits do not go by it.
 //
 // The gradient's sums over tokens stay in a thread's registers while a workgroup walks
-// every kBlocks-th group of rows; a second launch adds up the workgroups' parts in
+// every so many-th group of rows; a second launch adds up the workgroups' parts in
 // order.
-#include <algorithm>
-#include <type_traits>
-
-#include "c3_internal.h"
-#include "c3_replay_types.h"
+#include "c3_norm.h"
 
 namespace c3 {
 namespace {
-
-constexpr int E = 8;                // elements of a thread's piece
-constexpr int kGradBlocks = 512;    // workgroups of the gradient: two a compute unit
-
-struct Rows {
-    char* p;
-    int64_t stride;                 // in elements
-};
-
-// 8 elements of a row from `at` on as fp32; zeros behind `hidden`.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const Rows& r, int64_t row, int at, int hidden, float (&x)[E]) {
-    const T* p = reinterpret_cast<const T*>(r.p) + row * r.stride;
-    if constexpr (WIDE) {
-        constexpr int V = 16 / sizeof(T);
-        if (at < hidden) {
-#pragma unroll
-            for (int i = 0; i < E; i += V) {
-                const AlignedPack<T, V> v = *reinterpret_cast<const AlignedPack<T, V>*>(p + at + i);
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[i + j] = to_f32(v.v[j]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = at + i < hidden ? to_f32(p[at + i]) : 0.0f;
-    }
-}
-
-template <typename T, bool WIDE>
-__device__ __forceinline__ void store8(const Rows& r, int64_t row, int at, int hidden, const float (&x)[E]) {
-    T* p = reinterpret_cast<T*>(r.p) + row * r.stride;
-    if constexpr (WIDE) {
-        constexpr int V = 16 / sizeof(T);
-        if (at >= hidden) return;
-#pragma unroll
-        for (int i = 0; i < E; i += V) {
-            AlignedPack<T, V> v;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v.v[j] = from_f32<T>(x[i + j]);
-            *reinterpret_cast<AlignedPack<T, V>*>(p + at + i) = v;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (at + i < hidden) p[at + i] = from_f32<T>(x[i]);
-    }
-}
-
-// The sum over the TPR threads of a row, the same in each of them.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float x, float* lds) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    if constexpr (TPR > 64) {
-        constexpr int kWaves = TPR / 64;
-        const int wave = threadIdx.x >> 6, first = wave / kWaves * kWaves;
-        __syncthreads();                    // the last sum's readers are through
-        if ((threadIdx.x & 63) == 0) lds[wave] = x;
-        __syncthreads();
-        x = lds[first];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) x += lds[first + w];
-    }
-    return x;
-}
-
-struct NormArgs {
-    Rows x, y, gate, h, n;                      // forward
-    Rows dn, dh, dx, dy, dgate;                 // gradient
-    Rows weight, post;                          // one row each
-    float* stats;
-    float* parts;                               // [kinds][groups][hidden]
-    float* sums;                                // [3][hidden]
-    int64_t tokens;
-    int64_t groups;                             // of rows walked together, for the parts
-    int hidden, gate_kind;
-    float scale, eps;
-};
-
-template <int TPR>
-constexpr int rows_of_block() { return TPR < 256 ? 256 / TPR : 1; }
 
 template <typename R, typename B, bool WIDE, int TPR, int PK>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(NormArgs a) {
@@ -169,135 +80,6 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(No
     if (tid == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(rh, ry);
 }
 
-// BLOCK, POST: whether y and post are there; GATE: a c3_gate_t.  Their code and sums
-// cost registers, so each form is a kernel of its own.
-template <typename R, typename B, bool WIDE, int TPR, int PK, bool BLOCK, bool POST, int GATE>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kernel(NormArgs a) {
-    constexpr int RPB = rows_of_block<TPR>();
-    __shared__ float lds[16];
-    const int tid = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    const float inv = 1.0f / (float)a.hidden;
-    float s_weight[PK][E] = {}, s_post[POST ? PK : 1][E] = {}, s_gate[GATE == C3_GATE_CHANNELS ? PK : 1][E] = {};
-    const int64_t walk = (int64_t)gridDim.x * RPB;
-    for (int64_t first = (int64_t)blockIdx.x * RPB; first < a.tokens; first += walk) {
-        const bool there = first + sub < a.tokens;
-        const int64_t row = there ? first + sub : a.tokens - 1;     // every thread takes part in the sums
-        const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * row);
-        const float rh = st.x, ry = st.y;
-        float d[PK][E], h[PK][E], y[BLOCK ? PK : 1][E], w[E];
-        // h as in the forward pass
-#pragma unroll
-        for (int k = 0; k < PK; ++k) load8<R, WIDE>(a.x, row, (k * TPR + tid) * E, a.hidden, h[k]);
-#pragma unroll
-        for (int k = 0; k < PK; ++k) load8<B, WIDE>(a.dn, row, (k * TPR + tid) * E, a.hidden, d[k]);
-        if constexpr (BLOCK) {
-#pragma unroll
-            for (int k = 0; k < PK; ++k) load8<B, WIDE>(a.y, row, (k * TPR + tid) * E, a.hidden, y[k]);
-#pragma unroll
-            for (int k = 0; k < PK; ++k) {
-                float z[E];
-                if constexpr (POST) load8<B, WIDE>(a.post, 0, (k * TPR + tid) * E, a.hidden, w);
-#pragma unroll
-                for (int i = 0; i < E; ++i) z[i] = POST ? y[k][i] * ry * w[i] : y[k][i];
-                if constexpr (GATE != C3_GATE_NONE) {
-                    load8<B, WIDE>(a.gate, GATE == C3_GATE_TOKENS ? row : 0, (k * TPR + tid) * E, a.hidden, w);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) z[i] *= w[i];
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) h[k][i] = fmaf(a.scale, z[i], h[k][i]);
-            }
-        }
-        // d becomes the gradient of h
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < PK; ++k) {
-            load8<B, WIDE>(a.weight, 0, (k * TPR + tid) * E, a.hidden, w);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                h[k][i] *= rh;
-                if (there) s_weight[k][i] = fmaf(d[k][i], h[k][i], s_weight[k][i]);
-                d[k][i] *= w[i];
-                sum = fmaf(d[k][i], h[k][i], sum);
-            }
-        }
-        const float mean = row_sum<TPR>(sum, lds) * inv;
-#pragma unroll
-        for (int k = 0; k < PK; ++k) {
-            if (a.dh.p != nullptr)
-                load8<R, WIDE>(a.dh, row, (k * TPR + tid) * E, a.hidden, w);
-            else
-#pragma unroll
-                for (int i = 0; i < E; ++i) w[i] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[k][i] = fmaf(rh, fmaf(-h[k][i], mean, d[k][i]), w[i]);
-            if (there) store8<R, WIDE>(a.dx, row, (k * TPR + tid) * E, a.hidden, d[k]);
-        }
-        if constexpr (BLOCK) {
-            // d becomes the gradient of z, then of y
-            sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < PK; ++k) {
-                const int at = (k * TPR + tid) * E;
-                float p[E];
-                if constexpr (POST) {
-                    load8<B, WIDE>(a.post, 0, at, a.hidden, p);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) y[k][i] *= ry;
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) d[k][i] *= a.scale;
-                if constexpr (GATE != C3_GATE_NONE) {
-                    float dg[E];
-#pragma unroll
-                    for (int i = 0; i < E; ++i) dg[i] = d[k][i] * (POST ? y[k][i] * p[i] : y[k][i]);
-                    if constexpr (GATE == C3_GATE_CHANNELS) {
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            if (there) s_gate[k][i] += dg[i];
-                    } else if (there) {
-                        store8<B, WIDE>(a.dgate, row, at, a.hidden, dg);
-                    }
-                    load8<B, WIDE>(a.gate, GATE == C3_GATE_TOKENS ? row : 0, at, a.hidden, w);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) d[k][i] *= w[i];
-                }
-                if constexpr (POST) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        if (there) s_post[k][i] = fmaf(d[k][i], y[k][i], s_post[k][i]);
-                        d[k][i] *= p[i];
-                        sum = fmaf(d[k][i], y[k][i], sum);
-                    }
-                }
-            }
-            if constexpr (POST) {
-                const float mean_y = row_sum<TPR>(sum, lds) * inv;
-#pragma unroll
-                for (int k = 0; k < PK; ++k)
-#pragma unroll
-                    for (int i = 0; i < E; ++i) d[k][i] = ry * fmaf(-y[k][i], mean_y, d[k][i]);
-            }
-            if (there)
-#pragma unroll
-                for (int k = 0; k < PK; ++k) store8<B, WIDE>(a.dy, row, (k * TPR + tid) * E, a.hidden, d[k]);
-        }
-    }
-    // the workgroup's parts
-    const int64_t group = (int64_t)blockIdx.x * RPB + sub;
-    auto part = [&](int kind, const float (*s)[E]) {
-        float* to = a.parts + (kind * a.groups + group) * a.hidden;
-#pragma unroll
-        for (int k = 0; k < PK; ++k)
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if ((k * TPR + tid) * E + i < a.hidden) to[(k * TPR + tid) * E + i] = s[k][i];
-    };
-    part(0, s_weight);
-    if constexpr (POST) part(1, s_post);
-    if constexpr (GATE == C3_GATE_CHANNELS) part(2, s_gate);
-}
-
 // sums[kind][c] = the groups' parts of column c: 64 columns a workgroup, each of its
 // sixteen waves a run of the groups.
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* parts, int64_t groups, int hidden,
@@ -325,54 +107,42 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* parts, in
     sums[(int64_t)kind * hidden + c] = sum;
 }
 
-// Threads that share a row: as few as hold it in two pieces each.
-int threads_of(int64_t hidden) {
-    int t = 64;
-    while (t < 1024 && t * 2 * E < hidden) t *= 2;
-    return t;
-}
-
+// Workgroups of the gradient: sixteen waves a compute unit.
 int64_t grad_blocks(int64_t tokens, int64_t hidden) {
-    const int rpb = std::max(1, 256 / threads_of(hidden));
-    return std::min<int64_t>((tokens + rpb - 1) / rpb, kGradBlocks);
+    const int t = norm_grad_threads(hidden), rpb = std::max(1, 256 / t);
+    return std::min<int64_t>((tokens + rpb - 1) / rpb, 262144 / std::max(256, t));
 }
 int64_t grad_groups(int64_t tokens, int64_t hidden) {
-    return grad_blocks(tokens, hidden) * std::max(1, 256 / threads_of(hidden));
+    return grad_blocks(tokens, hidden) * std::max(1, 256 / norm_grad_threads(hidden));
 }
 
 template <typename R, typename B, bool WIDE, int TPR, int PK>
-hipError_t launch(const NormArgs& a, bool grad, hipStream_t s) {
+hipError_t launch(const NormArgs& a, hipStream_t s) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR, RPB = rows_of_block<TPR>();
-    if (!grad) {
-        residual_norm_kernel<R, B, WIDE, TPR, PK><<<wide_grid((uint64_t)(a.tokens + RPB - 1) / RPB), dim3(kBlock), 0,
-                                                    s>>>(a);
-        return hipGetLastError();
-    }
-    const dim3 grid((unsigned)grad_blocks(a.tokens, a.hidden));
-#define C3_FORM(BLOCK, POST, GATE) residual_norm_grad_kernel<R, B, WIDE, TPR, PK, BLOCK, POST, GATE><<<grid, dim3(kBlock), 0, s>>>(a)
-    if (a.y.p == nullptr) C3_FORM(false, false, 0);
-    else if (a.post.p == nullptr && a.gate_kind == 0) C3_FORM(true, false, 0);
-    else if (a.post.p == nullptr && a.gate_kind == 1) C3_FORM(true, false, 1);
-    else if (a.post.p == nullptr) C3_FORM(true, false, 2);
-    else if (a.gate_kind == 0) C3_FORM(true, true, 0);
-    else if (a.gate_kind == 1) C3_FORM(true, true, 1);
-    else C3_FORM(true, true, 2);
-#undef C3_FORM
-    const int kinds = 1 | (a.post.p != nullptr ? 2 : 0) | (a.gate_kind == C3_GATE_CHANNELS ? 4 : 0);
-    norm_parts_kernel<<<dim3((unsigned)((a.hidden + 63) / 64), 3), dim3(1024), 0, s>>>(a.parts, a.groups, a.hidden,
-                                                                                      kinds, a.sums);
+    residual_norm_kernel<R, B, WIDE, TPR, PK><<<wide_grid((uint64_t)(a.tokens + RPB - 1) / RPB), dim3(kBlock), 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <typename R, typename B, bool WIDE>
-hipError_t by_width(const NormArgs& a, bool grad, hipStream_t s) {
-    switch (threads_of(a.hidden)) {
-        case 64: return a.hidden <= 64 * E ? launch<R, B, WIDE, 64, 1>(a, grad, s) : launch<R, B, WIDE, 64, 2>(a, grad, s);
-        case 128: return launch<R, B, WIDE, 128, 2>(a, grad, s);
-        case 256: return launch<R, B, WIDE, 256, 2>(a, grad, s);
-        case 512: return launch<R, B, WIDE, 512, 2>(a, grad, s);
-        default: return launch<R, B, WIDE, 1024, 2>(a, grad, s);
+hipError_t by_width(const NormArgs& a, hipStream_t s) {
+    switch (norm_threads(a.hidden)) {
+        case 64: return a.hidden <= 64 * E ? launch<R, B, WIDE, 64, 1>(a, s) : launch<R, B, WIDE, 64, 2>(a, s);
+        case 128: return launch<R, B, WIDE, 128, 2>(a, s);
+        case 256: return launch<R, B, WIDE, 256, 2>(a, s);
+        case 512: return launch<R, B, WIDE, 512, 2>(a, s);
+        default: return launch<R, B, WIDE, 1024, 2>(a, s);
     }
+}
+
+template <typename R, typename B>
+hipError_t by_kind(const NormArgs& a, bool grad, bool wide, hipStream_t s) {
+    if (!grad) return wide ? by_width<R, B, true>(a, s) : by_width<R, B, false>(a, s);
+    const hipError_t e = launch_norm_grad<R, B>(a, wide, (unsigned)grad_blocks(a.tokens, a.hidden), s);
+    if (e != hipSuccess) return e;
+    const int kinds = 1 | (a.post.p != nullptr ? 2 : 0) | (a.gate_kind == C3_GATE_CHANNELS ? 4 : 0);
+    norm_parts_kernel<<<dim3((unsigned)((a.hidden + 63) / 64), 3), dim3(1024), 0, s>>>(a.parts, a.groups, a.hidden,
+                                                                                      kinds, a.sums);
+    return hipGetLastError();
 }
 
 int by_type(const c3_residual_norm_t* c, NormArgs& a, bool grad, hipStream_t s) {
@@ -391,15 +161,12 @@ int by_type(const c3_residual_norm_t* c, NormArgs& a, bool grad, hipStream_t s) 
     }
     hipError_t e;
     if (c->dtype == C3_F32)
-        e = wide ? by_width<float, float, true>(a, grad, s) : by_width<float, float, false>(a, grad, s);
-    else if (c->dtype == C3_BF16 && c->residual == C3_F32)
-        e = wide ? by_width<float, __bf16, true>(a, grad, s) : by_width<float, __bf16, false>(a, grad, s);
+        e = by_kind<float, float>(a, grad, wide, s);
     else if (c->dtype == C3_BF16)
-        e = wide ? by_width<__bf16, __bf16, true>(a, grad, s) : by_width<__bf16, __bf16, false>(a, grad, s);
-    else if (c->residual == C3_F32)
-        e = wide ? by_width<float, _Float16, true>(a, grad, s) : by_width<float, _Float16, false>(a, grad, s);
+        e = c->residual == C3_F32 ? by_kind<float, __bf16>(a, grad, wide, s) : by_kind<__bf16, __bf16>(a, grad, wide, s);
     else
-        e = wide ? by_width<_Float16, _Float16, true>(a, grad, s) : by_width<_Float16, _Float16, false>(a, grad, s);
+        e = c->residual == C3_F32 ? by_kind<float, _Float16>(a, grad, wide, s)
+                                  : by_kind<_Float16, _Float16>(a, grad, wide, s);
     return e == hipSuccess ? C3_OK : C3_E_HIP;
 }
 

@@ -1,0 +1,9 @@
+// The gradient of the residual norm, blocks in fp16 (one source a type: they compile side by side).
+#include "c3_norm_grad.h"
+
+namespace c3 {
+
+template hipError_t launch_norm_grad<_Float16, _Float16>(const NormArgs&, bool, unsigned, hipStream_t);
+template hipError_t launch_norm_grad<float, _Float16>(const NormArgs&, bool, unsigned, hipStream_t);
+
+}  // namespace c3

@@ -74,8 +74,9 @@ struct Tile {
     }
     static __device__ __forceinline__ int swap_across(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
 
-    __device__ __forceinline__ explicit Tile(const Operand& x) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // wave: which of the WAVES that load the tile
+    __device__ __forceinline__ Tile(const Operand& x, int wave) {
+        const int lane = threadIdx.x & 63;
         const int h = lane >> 5, c = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
@@ -101,8 +102,7 @@ struct Tile {
     }
 
     // Loads the tile that begins at inner index k; zeros behind the last one.
-    __device__ __forceinline__ void load(const Operand& x, int k, char* lds) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __device__ __forceinline__ void load(const Operand& x, int k, char* lds, int wave) const {
         const int left = max(min(x.inner - k, kInner), 0);
         if constexpr (ALONG) {
             const char* base = x.p + (int64_t)k * 2;
@@ -139,7 +139,7 @@ __device__ __forceinline__ void loads_ready() {
 
 template <typename T, int WM, int WN, int MB, int NB, bool A_ALONG, bool B_ALONG>
 struct Product {
-    static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
+    static constexpr int kWM = WM, kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TM = WM * MB * 32, TN = WN * NB * 32;
     using TileA = Tile<TM, A_ALONG, kWaves>;
     using TileB = Tile<TN, B_ALONG, kWaves>;
@@ -183,27 +183,64 @@ struct Product {
     // before it reads another.  LDS is free to use behind the next barrier.
     static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b, char* a0,
                                                char* b0, char* a1, char* b1) {
-        const TileA ta(a);
-        const TileB tb(b);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const TileA ta(a, wave);
+        const TileB tb(b, wave);
         const int inner = a.inner;
         if (inner <= 0) return;
-        ta.load(a, 0, a0);
-        tb.load(b, 0, b0);
+        ta.load(a, 0, a0, wave);
+        tb.load(b, 0, b0, wave);
         // two tiles a turn; a last one of zeros where their number is odd
         for (int k = 0; k < inner; k += 2 * kInner) {
             loads_ready();
-            ta.load(a, k + kInner, a1);
-            tb.load(b, k + kInner, b1);
+            ta.load(a, k + kInner, a1, wave);
+            tb.load(b, k + kInner, b1, wave);
             step(acc, ta, tb, a0, b0);
             loads_ready();
             if (k + 2 * kInner < inner) {
-                ta.load(a, k + 2 * kInner, a0);
-                tb.load(b, k + 2 * kInner, b0);
+                ta.load(a, k + 2 * kInner, a0, wave);
+                tb.load(b, k + 2 * kInner, b0, wave);
             }
             step(acc, ta, tb, a1, b1);
         }
     }
 };
+
+// Writes a wave's sums as rows n of 16-bit elements m: each lane has four neighbours in m
+// of one row, so the wave turns its part in LDS, which it has to itself, and stores whole
+// rows of MB * 64 bytes.  value(j, i, r): element of block i, j, register r as T; row(n):
+// where m = 0 of the tile's row n is, or null; elements from m_left on (a multiple of 8)
+// are not there.  The buffers are those of Product::run, behind a barrier.
+template <typename P, typename T, int MB, int NB, typename Value, typename Row>
+__device__ __forceinline__ void store_rows(char* a0, char* b0, char* a1, char* b1, int m_left, Value value, Row row) {
+    constexpr int kPieces = MB * 4, kPart = NB * 32 * kPieces * 16, kShare = P::kWaves / 4;
+    static_assert(kShare * kPart <= P::TileA::kBytes && kShare * kPart <= P::TileB::kBytes, "room for the turn");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int which = wave / kShare;
+    char* lds = (which == 0 ? a0 : which == 1 ? b0 : which == 2 ? a1 : b1) + wave % kShare * kPart;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int n = j * 32 + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                AlignedPack<T, 4> v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v.v[r] = value(j, i, 4 * q + r);
+                *reinterpret_cast<AlignedPack<T, 4>*>(lds + (n * kPieces + ((i * 4 + q) ^ (n & (kPieces - 1)))) * 16 + h * 8) = v;
+            }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int m0 = wave % P::kWM * MB * 32, n0 = wave / P::kWM * NB * 32;
+#pragma unroll
+    for (int t = 0; t < NB * 32 * kPieces / 64; ++t) {
+        const int at = t * 64 + lane, n = at / kPieces, piece = at % kPieces;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (n * kPieces + (piece ^ (n & (kPieces - 1)))) * 16);
+        T* to = row(n0 + n);
+        if (to != nullptr && m0 + piece * 8 < m_left) *reinterpret_cast<u32x4*>(to + m0 + piece * 8) = v;
+    }
+}
 
 // Which tile a workgroup takes: the eight dies take workgroups in turn, and each gets a
 // run of the tiles of its own, in which kGroup tiles of the first index run fastest, so
