@@ -141,15 +141,11 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
 // ---------------------------------------------------------------------------
 // logits
 // ---------------------------------------------------------------------------
-template <typename T, bool GRAD, int WM, int WN, int MB, int NB>
+template <typename T, bool GRAD, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
-    using P = Product<T, WM, WN, MB, NB, true, true>;
-    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
-    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    using P = Product<T, WM, WN, MB, NB, STAGES, true, true>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), tm, tn)) return;
+    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
     const int count = __builtin_amdgcn_readfirstlane(a.found->count);
     const int n0 = tn * P::TN, m0 = tm * P::TM;
     if (n0 >= count) return;
@@ -158,12 +154,12 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
     f32x16 acc[MB][NB] = {};
     const Operand wa{a.weight + row0 * a.weight_stride, a.weight_stride, rows, a.hidden};
     const Operand xb{a.xc + (int64_t)n0 * a.pitch * 2, (int64_t)a.pitch * 2, count - n0, a.hidden};
-    P::run(acc, wa, xb, a0, b0, a1, b1);
+    P::run(acc, wa, xb);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if constexpr (!GRAD) {
         // maximum and sum a token: in the lane, with the other half's rows, then over the waves
-        float2(*stat)[P::TN] = reinterpret_cast<float2(*)[P::TN]>(a0);
-        __syncthreads();
+        float2(*stat)[P::TN] = reinterpret_cast<float2(*)[P::TN]>(P::lds_of_wave(0));
+        static_assert(WM * P::TN * sizeof(float2) <= P::kWaveBytes, "room for the statistics");
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int n = P::n_of(j);
@@ -220,9 +216,8 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
             g[j] = a.grad[n];
             target[j] = a.target[n] - (int32_t)row0;
         }
-        __syncthreads();
         store_rows<P, T, MB, NB>(
-            a0, b0, a1, b1, a.d_pitch - m0,         // zeros up to the pitch
+            a.d_pitch - m0,         // zeros up to the pitch
             [&](int j, int i, int r) {
                 const int m = P::m_of(i, r);
                 float p = __expf(fmaf(acc[i][j][r], a.scale, -lse[j]));
@@ -236,67 +231,83 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
 }
 
 // The forward pass of few tokens is bound by reading the weights once.  A workgroup has
-// 32 MB rows of them, and its two waves take every other tile of the inner index: each
-// loads tiles to LDS of its own, two ahead of the one that it multiplies, and waits for
-// no other wave.  The sums come together at the end, in the order of the waves.
-constexpr int kFewWaves = 2;
+// 64 rows of them, and its two waves take every other tile of the inner index: each
+// loads tiles to LDS of its own, three ahead of the one that it multiplies, and waits for
+// no other wave.  Hidden states go to registers, as far ahead.  The sums come together at
+// the end, in the order of the waves.  Every workgroup begins at another tile: rows of the
+// weights lie a power of two apart as a rule, and if all workgroups read the same part of
+// their rows, they would meet at few of the memory's channels (8 tokens over 32,000 rows of
+// 4,096: 53 us, and 43 this way).
+constexpr int kFewWaves = 2, kFewInner = 64, kFewRows = 64;
 
-template <typename T, int MB, int NB>
+template <typename T, bool GRAD, int NB>
 __global__ __launch_bounds__(kFewWaves * 64) void loss_few_kernel(LossArgs a) {
     // each wave's tiles as those of a workgroup of one wave
-    using TileW = Tile<MB * 32, true, 1>;
-    using TileX = Tile<NB * 32, true, 1>;
-    constexpr int kPart = TileW::kBytes + TileX::kBytes, kLoads = TileW::kLoads + TileX::kLoads;
-    // a stage each its own object, or the compiler would wait for all loads before a read
-    __shared__ __attribute__((aligned(1024))) char s0[kFewWaves * kPart];
-    __shared__ __attribute__((aligned(1024))) char s1[kFewWaves * kPart];
-    __shared__ __attribute__((aligned(1024))) char s2[kFewWaves * kPart];
+    using TileW = Tile<kFewRows, true, 1, kFewInner, true>;
+    constexpr int MB = kFewRows / 32, kLoads = TileW::kLoads + NB * kFewInner / 16, kFar = 3;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tokens = (int)a.tokens;
-    const int64_t row0 = (int64_t)blockIdx.x * MB * 32;
-    const int rows = (int)min((int64_t)MB * 32, a.rows - row0);
+    // the forward pass takes tokens as they lie, the gradient those that take part
+    const int tokens = GRAD ? __builtin_amdgcn_readfirstlane(a.found->count) : (int)a.tokens;
+    const char* x = GRAD ? a.xc : a.x;
+    const int64_t x_stride = GRAD ? (int64_t)a.pitch * 2 : a.x_stride;
+    if (tokens == 0) return;
+    const int64_t row0 = a.row0 + (int64_t)blockIdx.x * kFewRows;
+    const int rows = (int)min((int64_t)kFewRows, a.rows - row0);
     const Operand ow{a.weight + row0 * a.weight_stride, a.weight_stride, rows, a.hidden};
-    const Operand ox{a.x, a.x_stride, tokens, a.hidden};
     const TileW tw(ow, 0);
-    const TileX tx(ox, 0);
     f32x16 acc[MB][NB] = {};
-    const int steps = (a.hidden + kInner - 1) / kInner;     // of all waves
-    const auto load = [&](int s, char* stage) {             // zeros behind the last step
-        char* p = stage + wave * kPart;
-        tw.load(ow, min(s, steps) * kInner, p, 0);
-        tx.load(ox, min(s, steps) * kInner, p + TileW::kBytes, 0);
+    u32x4 fx[kFar + 1][NB][kFewInner / 16];
+    const int steps = (a.hidden + kFewInner - 1) / kFewInner;     // of all waves
+    const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(x), 0,
+                                                      (int)((tokens - 1) * x_stride + a.hidden * 2), 0x00027000);
+    const int turn = blockIdx.x % steps;
+    const auto load = [&](int s, char* stage, u32x4(&to)[NB][kFewInner / 16]) {     // zeros behind the last step
+        const int at_step = s + turn < steps ? s + turn : s + turn - steps;
+        const int k = s < steps ? at_step * kFewInner : steps * kFewInner;
+        tw.load(ow, k, stage + wave * TileW::kBytes, 0);
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int ks = 0; ks < kFewInner / 16; ++ks) {
+                const int n = j * 32 + (lane & 31), at = k + ks * 16 + (lane >> 5) * 8;
+                const uint32_t offset = n < tokens && at < a.hidden ? (uint32_t)(n * x_stride) + at * 2 : kNowhere;
+                to[j][ks] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)offset, 0, 0);
+            }
     };
-    const auto step = [&](int s, const char* stage, char* ahead) {
+    const auto step = [&](int s, const char* stage, const u32x4(&hx)[NB][kFewInner / 16], char* ahead,
+                          u32x4(&far)[NB][kFewInner / 16]) {
         // the reads of the tile that was in `ahead` are through
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        load(s + 2 * kFewWaves, ahead);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-        const char* p = stage + wave * kPart;
+        load(s + kFar * kFewWaves, ahead, far);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kFar * kLoads < 63 ? kFar * kLoads : 63) : "memory");
+        const char* p = stage + wave * TileW::kBytes;
 #pragma unroll
-        for (int ks = 0; ks < kInner / 16; ++ks) {
-            u32x4 fw[MB], fx[NB];
+        for (int ks = 0; ks < kFewInner / 16; ++ks) {
+            u32x4 fw[MB];
 #pragma unroll
             for (int i = 0; i < MB; ++i) fw[i] = tw.operand(p, i, ks);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) fx[j] = tx.operand(p + TileW::kBytes, j, ks);
-#pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = mfma_32x32x16<T>(fw[i], fx[j], acc[i][j]);
+                for (int j = 0; j < NB; ++j) acc[i][j] = mfma_32x32x16<T>(fw[i], hx[j][ks], acc[i][j]);
         }
     };
-    load(wave, s0);
-    load(wave + kFewWaves, s1);
-    for (int s = wave; s < steps; s += 3 * kFewWaves) {
-        step(s, s0, s2);
-        step(s + kFewWaves, s1, s0);
-        step(s + 2 * kFewWaves, s2, s1);
+    constexpr int kStage = kFewWaves * TileW::kBytes;
+    char *s0 = lds_object<0, kStage>(), *s1 = lds_object<1, kStage>(), *s2 = lds_object<2, kStage>(),
+         *s3 = lds_object<3, kStage>();
+    load(wave, s0, fx[0]);
+    load(wave + kFewWaves, s1, fx[1]);
+    load(wave + 2 * kFewWaves, s2, fx[2]);
+    for (int s = wave; s < steps; s += 4 * kFewWaves) {
+        step(s, s0, fx[0], s3, fx[3]);
+        step(s + kFewWaves, s1, fx[1], s0, fx[0]);
+        step(s + 2 * kFewWaves, s2, fx[2], s1, fx[1]);
+        step(s + 3 * kFewWaves, s3, fx[3], s2, fx[2]);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     // block i, j, register r of wave w: [(w - 1)][i][j][r][lane]
-    float* sums = reinterpret_cast<float*>(s0);
-    static_assert((kFewWaves - 1) * MB * NB * 4096 <= sizeof(s0), "room for the sums");
+    float* sums = reinterpret_cast<float*>(lds_object<4, (kFewWaves - 1) * MB * NB * 4096>());
     if (wave > 0)
 #pragma unroll
         for (int i = 0; i < MB; ++i)
@@ -307,33 +318,62 @@ __global__ __launch_bounds__(kFewWaves * 64) void loss_few_kernel(LossArgs a) {
                     sums[((((wave - 1) * MB + i) * NB + j) * 16 + r) * 64 + lane] = acc[i][j][r];
     __syncthreads();
     if (wave > 0) return;
+    // the sums of all waves
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+#pragma unroll
+                for (int w = 0; w < kFewWaves - 1; ++w)
+                    acc[i][j][r] += sums[(((w * MB + i) * NB + j) * 16 + r) * 64 + lane];
+            }
+    const auto m_of = [&](int i, int r) { return i * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5); };
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         const int n = j * 32 + (lane & 31);
-        const int32_t target = n < tokens ? target_of(a, n) : -1;
-        const int64_t at = target >= 0 ? target - row0 : -1;
-        float most = -__builtin_inff(), sum = 0.0f;
+        if constexpr (GRAD) {
+            if (n >= tokens) continue;
+            const float lse = a.lse_at[n], g = a.grad[n];
+            const int64_t target = a.target[n] - row0;
+            T* to = reinterpret_cast<T*>(a.d) + (int64_t)n * a.d_pitch + (row0 - a.row0);
 #pragma unroll
-        for (int i = 0; i < MB; ++i)
+            for (int i = 0; i < MB; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float v = acc[i][j][r];
+                for (int q = 0; q < 4; ++q) {
+                    AlignedPack<T, 4> v;            // the pitch holds whole workgroups' rows
 #pragma unroll
-                for (int w = 0; w < kFewWaves - 1; ++w) v += sums[(((w * MB + i) * NB + j) * 16 + r) * 64 + lane];
-                const int m = i * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                v = m < rows ? v * a.scale : -__builtin_inff();
-                if (m == at) a.picked[n] = v;
-                acc[i][j][r] = v;
-                most = fmaxf(most, v);
-            }
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float from = most == -__builtin_inff() ? 0.0f : most;
+                    for (int r = 0; r < 4; ++r) {
+                        const int m = m_of(i, 4 * q + r);
+                        float p = __expf(fmaf(acc[i][j][4 * q + r], a.scale, -lse));
+                        if (m == target) p -= 1.0f;
+                        v.v[r] = from_f32<T>(m < rows ? p * g : 0.0f);
+                    }
+                    *reinterpret_cast<AlignedPack<T, 4>*>(to + m_of(i, 4 * q)) = v;
+                }
+        } else {
+            const int32_t target = n < tokens ? target_of(a, n) : -1;
+            const int64_t at = target >= 0 ? target - row0 : -1;
+            float most = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < MB; ++i)
+            for (int i = 0; i < MB; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - from);
-        sum += __shfl_xor(sum, 32);
-        if (lane < 32 && n < tokens) a.parts[(int64_t)n * gridDim.x + blockIdx.x] = make_float2(most, sum);
+                for (int r = 0; r < 16; ++r) {
+                    const float v = m_of(i, r) < rows ? acc[i][j][r] * a.scale : -__builtin_inff();
+                    if (m_of(i, r) == at) a.picked[n] = v;
+                    acc[i][j][r] = v;
+                    most = fmaxf(most, v);
+                }
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - from);
+            sum += __shfl_xor(sum, 32);
+            if (lane < 32 && n < tokens) a.parts[(int64_t)n * gridDim.x + blockIdx.x] = make_float2(most, sum);
+        }
     }
 }
 
@@ -422,15 +462,11 @@ __device__ __forceinline__ void store_parts(const f32x16 (&acc)[MB][NB], float* 
 }
 
 // dx_parts[split] += d W over the split's share of the piece.
-template <typename T, int WM, int WN, int MB, int NB>
+template <typename T, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
-    using P = Product<T, WM, WN, MB, NB, false, true>;
-    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
-    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    using P = Product<T, WM, WN, MB, NB, STAGES, false, true>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), tm, tn)) return;
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
     const int count = __builtin_amdgcn_readfirstlane(a.found->count);
     const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = blockIdx.y * a.split_len;
     if (n0 >= count) return;
@@ -438,37 +474,35 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
     f32x16 acc[MB][NB] = {};
     const Operand w{a.weight + (a.row0 + k0) * a.weight_stride + (int64_t)m0 * 2, a.weight_stride, a.hidden - m0, inner};
     const Operand d{a.d + ((int64_t)n0 * a.d_pitch + k0) * 2, (int64_t)a.d_pitch * 2, count - n0, inner};
-    P::run(acc, w, d, a0, b0, a1, b1);
+    P::run(acc, w, d);
     float* to = a.dx_parts + ((int64_t)blockIdx.y * a.tokens + n0) * a.pitch + m0;
     store_parts<P>(acc, to, a.pitch, count - n0, a.hidden - m0, a.first == 0);
 }
 
-// dweight's rows of the piece, or with SPLIT a share of their sums.
-template <typename T, bool SPLIT, int WM, int WN, int MB, int NB>
+// dweight's rows of the piece, or with SPLIT a share of their sums.  With few inner indices
+// writing them is what counts: then a row's tiles run one after the other (262 MB for 8
+// tokens: 79 us in groups of four, 73 so).
+constexpr uint32_t kWholeRows = 4096;
+template <typename T, bool SPLIT, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) {
-    using P = Product<T, WM, WN, MB, NB, false, false>;
-    __shared__ __attribute__((aligned(1024))) char a0[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b0[P::TileB::kBytes];
-    __shared__ __attribute__((aligned(1024))) char a1[P::TileA::kBytes];
-    __shared__ __attribute__((aligned(1024))) char b1[P::TileB::kBytes];
+    using P = Product<T, WM, WN, MB, NB, STAGES, false, false>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.piece + P::TN - 1) / P::TN), tm, tn)) return;
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.piece + P::TN - 1) / P::TN), a.tokens <= 1024 ? kWholeRows : kTileGroup, tm, tn)) return;
     const int count = __builtin_amdgcn_readfirstlane(a.found->count);
     const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = SPLIT ? blockIdx.y * a.split_len : 0;
     const int inner = SPLIT ? min(a.split_len, count - k0) : count;
     f32x16 acc[MB][NB] = {};
     const Operand x{a.xc + ((int64_t)k0 * a.pitch + m0) * 2, (int64_t)a.pitch * 2, a.hidden - m0, inner};
     const Operand d{a.d + ((int64_t)k0 * a.d_pitch + n0) * 2, (int64_t)a.d_pitch * 2, a.d_pitch - n0, inner};
-    P::run(acc, x, d, a0, b0, a1, b1);
+    P::run(acc, x, d);
     const int n_left = a.piece - n0;
     if constexpr (SPLIT) {
         float* to = a.w_parts + ((int64_t)blockIdx.y * a.piece + n0) * a.pitch + m0;
         store_parts<P>(acc, to, a.pitch, n_left, a.hidden - m0, false);
     } else {
         const float lower = a.found->lower;
-        __syncthreads();
         store_rows<P, T, MB, NB>(
-            a0, b0, a1, b1, a.hidden - m0, [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] * lower); },
+            a.hidden - m0, [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] * lower); },
             [&](int n) {
                 return n < n_left ? reinterpret_cast<T*>(a.out + (a.row0 + n0 + n) * a.out_stride) + m0 : nullptr;
             });
@@ -517,11 +551,14 @@ constexpr int kFewTokens = 64;
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 int64_t tiles(int64_t x, int64_t size) { return (x + size - 1) / size; }
 
-// Tiles of 256 by 256 sums a workgroup of eight waves, or, where there are too few of them
-// for two on every compute unit, of 128 by 128 and four waves.
-int tile_size(int64_t first, int64_t second) { return tiles(first, 256) * tiles(second, 256) >= 512 ? 256 : 128; }
-// The few tokens' rows of the weights in a workgroup: the more tokens, the more of LDS is theirs.
-int few_rows(int64_t tokens) { return tokens <= 32 ? 64 : 32; }
+// Tiles of 256 by 256 sums a workgroup and one workgroup a compute unit, or of 128 by 128
+// and two.  A round of the former takes 7/5 of one of the latter (106 and 75 us with 4,096
+// inner indices) for twice the sums: what counts is how many rounds there are.
+int tile_size(int64_t first, int64_t second) {
+    const int64_t large = tiles(tiles(first, 256) * tiles(second, 256), 256);
+    const int64_t small = tiles(tiles(first, 128) * tiles(second, 128), 512);
+    return 7 * large <= 5 * small ? 256 : 128;
+}
 
 struct LossPlan {
     int64_t found, token, place, target, grad, lse_at, xc, parts, picked, d, dx_parts, w_parts, bytes;
@@ -548,10 +585,10 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     const int64_t T = a->tokens, H = a->hidden;
     p.pitch = H;
     p.found = take(sizeof(Found));
+    p.few = T <= kFewTokens;
     if (!grad) {
-        p.few = T <= kFewTokens;
         p.tile = tile_size(a->rows, T);
-        p.row_tiles = tiles(a->rows, p.few ? few_rows(T) : p.tile);
+        p.row_tiles = tiles(a->rows, p.few ? kFewRows : p.tile);
         p.parts = take(8 * T * p.row_tiles);
         p.picked = take(4 * T);
         if (p.few) return p;
@@ -628,22 +665,29 @@ LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, c
     return a;
 }
 
-// Calls f with the waves and blocks of a tile: f(Shape<WM, WN, MB, NB>).
-template <int WM_, int WN_, int MB_, int NB_>
+// Calls f with the waves, blocks and stages of a tile.
+template <int WM_, int WN_, int MB_, int NB_, int STAGES_>
 struct Shape {
-    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, kThreads = WM * WN * 64;
+    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, STAGES = STAGES_, kThreads = WM * WN * 64;
 };
 template <typename F>
 void by_tile(int size, F f) {
-    if (size == 256) f(Shape<2, 4, 4, 2>{});
-    else f(Shape<2, 2, 2, 2>{});
+    if (size == 256) f(Shape<2, 4, 4, 2, 2>{});
+    else f(Shape<2, 2, 2, 2, 2>{});
+}
+
+template <typename T, bool GRAD>
+void launch_few(const LossArgs& a, int64_t rows, hipStream_t s) {
+    const dim3 grid((unsigned)tiles(rows, kFewRows)), block(kFewWaves * 64);
+    if (a.tokens <= 32) loss_few_kernel<T, GRAD, 1><<<grid, block, 0, s>>>(a);
+    else loss_few_kernel<T, GRAD, 2><<<grid, block, 0, s>>>(a);
 }
 
 template <typename T, bool GRAD>
 void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
     by_tile(tile, [&](auto shape) {
         using S = decltype(shape);
-        loss_logits_kernel<T, GRAD, S::WM, S::WN, S::MB, S::NB>
+        loss_logits_kernel<T, GRAD, S::WM, S::WN, S::MB, S::NB, S::STAGES>
             <<<dim3(tile_blocks(tiles(rows, tile), tiles(a.tokens, tile))), dim3(S::kThreads), 0, s>>>(a);
     });
 }
@@ -651,9 +695,7 @@ void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
 template <typename T>
 hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
     if (p.few) {
-        const dim3 grid((unsigned)p.row_tiles), block(kFewWaves * 64);
-        if (few_rows(a.tokens) == 64) loss_few_kernel<T, 2, 1><<<grid, block, 0, s>>>(a);
-        else loss_few_kernel<T, 1, 2><<<grid, block, 0, s>>>(a);
+        launch_few<T, false>(a, a.rows, s);
         loss_few_join_kernel<<<dim3((unsigned)a.tokens), dim3(1024), 0, s>>>(a, (int)p.row_tiles);
         return hipGetLastError();
     }
@@ -678,11 +720,12 @@ hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_strid
         a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
         a.first = a.row0 == 0;
         if (a.tokens > 0) {
-            launch_logits<T, true>(a, a.piece, p.tile, s);
+            if (p.few) launch_few<T, true>(a, a.piece, s);
+            else launch_logits<T, true>(a, a.piece, p.tile, s);
             a.split_len = (int32_t)p.split_len;
             by_tile(p.dx_tile, [&](auto shape) {
                 using S = decltype(shape);
-                loss_dx_kernel<T, S::WM, S::WN, S::MB, S::NB>
+                loss_dx_kernel<T, S::WM, S::WN, S::MB, S::NB, S::STAGES>
                     <<<dim3(tile_blocks(tiles(a.hidden, p.dx_tile), tiles(a.tokens, p.dx_tile)), (unsigned)p.splits),
                        dim3(S::kThreads), 0, s>>>(a);
             });
@@ -692,9 +735,9 @@ hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_strid
             using S = decltype(shape);
             const dim3 grid(tile_blocks(tiles(a.hidden, p.w_tile), tiles(a.piece, p.w_tile)), (unsigned)p.w_splits);
             if (p.w_splits > 1)
-                loss_dweight_kernel<T, true, S::WM, S::WN, S::MB, S::NB><<<grid, dim3(S::kThreads), 0, s>>>(a);
+                loss_dweight_kernel<T, true, S::WM, S::WN, S::MB, S::NB, S::STAGES><<<grid, dim3(S::kThreads), 0, s>>>(a);
             else
-                loss_dweight_kernel<T, false, S::WM, S::WN, S::MB, S::NB><<<grid, dim3(S::kThreads), 0, s>>>(a);
+                loss_dweight_kernel<T, false, S::WM, S::WN, S::MB, S::NB, S::STAGES><<<grid, dim3(S::kThreads), 0, s>>>(a);
         });
         if (p.w_splits > 1)
             finish(a.w_parts, p.w_splits, nullptr, a.piece, a.out + a.row0 * a.out_stride, a.out_stride);

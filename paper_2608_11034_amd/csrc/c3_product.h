@@ -2,8 +2,8 @@
 // epilogue of their own behind: acc[n][m] = sum over k of a(m, k) b(n, k).
 //
 // A workgroup holds TM x TN sums in registers, each wave MB x NB blocks of 32 x 32.
-// Tiles of kInner inner indices come into LDS straight from memory, two of each operand
-// in turn: while one pair is multiplied the next is on its way.  An operand lies in
+// Tiles of kInner inner indices come into LDS straight from memory, STAGES of each operand
+// in turn: all but one are on their way while that is multiplied.  An operand lies in
 // memory along the inner index (rows of k) or across it (rows of m or n); the latter is
 // turned by the reads from LDS, so that no operand is copied in another order first.
 #pragma once
@@ -35,13 +35,25 @@ __device__ __forceinline__ u32x2 read_turned(const char* p) {
         (__attribute__((address_space(3))) s16x4*)(p)));
 }
 
-// 16 bytes a lane from memory to LDS; zeros from `bytes` on.
+// 16 bytes a lane from memory to LDS; zeros from `bytes` on.  ONCE: the bytes are not read
+// again, and need no place in the caches.
+template <bool ONCE>
 __device__ __forceinline__ void load_lds(const char* base, uint32_t bytes, uint32_t offset, char* lds) {
+    constexpr int kNonTemporal = 2;
     const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00027000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds), 16, (int)offset, 0, 0,
-                                             0);
+                                             ONCE ? kNonTemporal : 0);
 }
 constexpr uint32_t kNowhere = 0xFFFFFF00u;
+
+// The same for every lane, where the compiler cannot tell: it would go through the lanes
+// one by one for a load's base.
+__device__ __forceinline__ const char* scalar(const char* p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const char*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
+}
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // One operand in memory: outer index m or n in rows (ALONG) or columns, `stride` bytes
 // between rows, `outer` indices and `inner` inner ones from `p` on.  Rows hold whole
@@ -54,26 +66,34 @@ struct Operand {
     int outer, inner;
 };
 
-// A tile of R outer by kInner inner indices in LDS.
-//   ALONG: R rows of 128 bytes; the 16-byte pieces of a row change places with bits 1 to
-//   3 of the row, so that 16 rows' reads of one piece spread over all banks.
-//   Across: for each 128 outer indices kInner rows of 256 bytes; the pieces of a row
+// A tile of R outer by INNER inner indices in LDS.
+//   ALONG: R rows of 2 INNER bytes; the 16-byte pieces of a row change places with bits
+//   of the row, so that 16 rows' reads of one piece spread over all banks.
+//   Across: for each 128 outer indices INNER rows of 256 bytes; the pieces of a row
 //   change places with its low four bits, so that a turned read's four rows, 64 bytes of
 //   each, do too.
-template <int R, bool ALONG, int WAVES>
+template <int R, bool ALONG, int WAVES, int INNER, bool ONCE = false>
 struct Tile {
-    static constexpr int kLoads = R / 8 / WAVES;        // of a wave, 1 KiB each
-    static constexpr int kBytes = R * kInner * 2;
-    static_assert(kLoads * WAVES * 8 == R && (ALONG || R % 128 == 0), "rows of a tile");
+    static constexpr int kLoads = R * INNER / 512 / WAVES;      // of a wave, 1 KiB each
+    static constexpr int kBytes = R * INNER * 2;
+    static constexpr int kPieces = INNER / 8;                   // of a row, ALONG
+    static constexpr int kTurns = INNER / 32;
+    static_assert(kLoads * WAVES * 512 == R * INNER && (ALONG || R % 128 == 0) && (INNER == 64 || INNER == 128),
+                  "rows of a tile");
     uint32_t at[kLoads];        // byte offset of a lane's piece
-    int piece[2];               // ALONG: which piece, in even and odd loads
+    int piece[ALONG ? kTurns : 1];      // ALONG: which piece, in every kTurns-th load
     int read, read2;            // byte offsets of a lane's reads
 
     static __device__ __forceinline__ int swap_along(int row) {
+        if constexpr (INNER == 128) return row & 15;
         return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
     }
     static __device__ __forceinline__ int swap_across(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
 
+    // ALONG: the row that a lane loads a piece of.
+    static __device__ __forceinline__ int row_of(int load) {
+        return load * (64 / kPieces) + (threadIdx.x & 63) / kPieces;
+    }
     // wave: which of the WAVES that load the tile
     __device__ __forceinline__ Tile(const Operand& x, int wave) {
         const int lane = threadIdx.x & 63;
@@ -82,17 +102,18 @@ struct Tile {
         for (int n = 0; n < kLoads; ++n) {
             const int load = wave * kLoads + n;
             if constexpr (ALONG) {
-                const int row = load * 8 + lane / 8, q = (lane & 7) ^ swap_along(row);
+                const int row = row_of(load), q = (lane & (kPieces - 1)) ^ swap_along(row);
                 at[n] = row < x.outer ? (uint32_t)(row * x.stride) + q * 16 : kNowhere;
             } else {
-                const int row = load % 16 * 4 + lane / 16, col = load / 16 * 128 + ((lane & 15) ^ swap_across(row)) * 8;
+                const int row = load % (INNER / 4) * 4 + lane / 16;
+                const int col = load / (INNER / 4) * 128 + ((lane & 15) ^ swap_across(row)) * 8;
                 at[n] = col < x.outer ? (uint32_t)(row * x.stride) + col * 2 : kNowhere;
             }
         }
         if constexpr (ALONG) {
-            piece[0] = (lane & 7) ^ swap_along(wave * kLoads * 8 + lane / 8);
-            piece[1] = (lane & 7) ^ swap_along((wave * kLoads + 1) * 8 + lane / 8);
-            read = c * 128 + ((h ^ swap_along(c)) << 4);
+#pragma unroll
+            for (int n = 0; n < kTurns; ++n) piece[n] = (lane & (kPieces - 1)) ^ swap_along(row_of(wave * kLoads + n));
+            read = c * INNER * 2 + ((h ^ swap_along(c)) << 4);
             read2 = 0;
         } else {
             const int row = h * 8 + (i >> 2), q = g * 2 + ((i & 3) >> 1);
@@ -103,18 +124,18 @@ struct Tile {
 
     // Loads the tile that begins at inner index k; zeros behind the last one.
     __device__ __forceinline__ void load(const Operand& x, int k, char* lds, int wave) const {
-        const int left = max(min(x.inner - k, kInner), 0);
+        const int left = max(min(x.inner - k, INNER), 0);
         if constexpr (ALONG) {
-            const char* base = x.p + (int64_t)k * 2;
-            const uint32_t bytes = left > 0 ? (uint32_t)((int64_t)(min(x.outer, R) - 1) * x.stride) + (left + 7) / 8 * 16 : 0;
+            const char* base = scalar(x.p + (int64_t)k * 2);
+            const uint32_t bytes = scalar(left > 0 ? (uint32_t)((int64_t)(min(x.outer, R) - 1) * x.stride) + (left + 7) / 8 * 16 : 0);
 #pragma unroll
             for (int n = 0; n < kLoads; ++n)
-                load_lds(base, bytes, piece[n & 1] * 8 < left ? at[n] : kNowhere, lds + (wave * kLoads + n) * 1024);
+                load_lds<ONCE>(base, bytes, piece[n & (kTurns - 1)] * 8 < left ? at[n] : kNowhere, lds + (wave * kLoads + n) * 1024);
         } else {
-            const char* base = x.p + (int64_t)k * x.stride;
-            const uint32_t bytes = left > 0 ? (uint32_t)((int64_t)(left - 1) * x.stride) + min(x.outer, R) * 2 : 0;
+            const char* base = scalar(x.p + (int64_t)k * x.stride);
+            const uint32_t bytes = scalar(left > 0 ? (uint32_t)((int64_t)(left - 1) * x.stride) + min(x.outer, R) * 2 : 0);
 #pragma unroll
-            for (int n = 0; n < kLoads; ++n) load_lds(base, bytes, at[n], lds + (wave * kLoads + n) * 1024);
+            for (int n = 0; n < kLoads; ++n) load_lds<ONCE>(base, bytes, at[n], lds + (wave * kLoads + n) * 1024);
         }
     }
 
@@ -122,27 +143,31 @@ struct Tile {
     // matrix unit, lane's outer index lane & 31, inner ones (lane >> 5) * 8 ...
     __device__ __forceinline__ u32x4 operand(const char* lds, int b, int ks) const {
         if constexpr (ALONG) {
-            return *reinterpret_cast<const u32x4*>(lds + b * 4096 + (read ^ (ks << 5)));
+            return *reinterpret_cast<const u32x4*>(lds + b * 64 * INNER + (read ^ (ks << 5)));
         } else {
-            const char* p = lds + (b >> 2) * (kInner * 256) + ks * 4096;
+            const char* p = lds + (b >> 2) * (INNER * 256) + ks * 4096;
             const u32x2 lo = read_turned(p + (read ^ ((b & 3) << 6))), hi = read_turned(p + (read2 ^ ((b & 3) << 6)));
             return u32x4{lo.x, lo.y, hi.x, hi.y};
         }
     }
 };
 
-// The wave's loads to LDS have landed, and every wave of the workgroup is here.
-__device__ __forceinline__ void loads_ready() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+// An object in LDS for each number: the compiler would wait for loads to one before it
+// reads another if they were parts of one object.
+template <int ID, int BYTES>
+__device__ __forceinline__ char* lds_object() {
+    __shared__ __attribute__((aligned(1024))) char bytes[BYTES];
+    return bytes;
 }
 
-template <typename T, int WM, int WN, int MB, int NB, bool A_ALONG, bool B_ALONG>
+template <typename T, int WM, int WN, int MB, int NB, int STAGES, bool A_ALONG, bool B_ALONG>
 struct Product {
+    static_assert(STAGES == 2 || STAGES == 4, "stages");
     static constexpr int kWM = WM, kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TM = WM * MB * 32, TN = WN * NB * 32;
-    using TileA = Tile<TM, A_ALONG, kWaves>;
-    using TileB = Tile<TN, B_ALONG, kWaves>;
+    using TileA = Tile<TM, A_ALONG, kWaves, kInner>;
+    using TileB = Tile<TN, B_ALONG, kWaves, kInner>;
+    static constexpr int kLoads = TileA::kLoads + TileB::kLoads;       // of a wave and stage
 
     // Block mb, nb of the wave, register i: m and n inside the tile.
     static __device__ __forceinline__ int m_of(int mb, int i) {
@@ -153,74 +178,112 @@ struct Product {
         return ((threadIdx.x >> 6) / WM * NB + nb) * 32 + (threadIdx.x & 31);
     }
 
-    static __device__ __forceinline__ void step(f32x16 (&acc)[MB][NB], const TileA& ta, const TileB& tb, const char* a,
-                                                const char* b) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int am = wave % WM * MB, bn = wave / WM * NB;
-        // the operands of the next 16 inner indices are read while these are multiplied
-        u32x4 fa[2][MB], fb[2][NB];
-        auto read = [&](int ks) {
-#pragma unroll
-            for (int i = 0; i < MB; ++i) fa[ks & 1][i] = ta.operand(a, am + i, ks);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) fb[ks & 1][j] = tb.operand(b, bn + j, ks);
-        };
-        read(0);
-#pragma unroll
-        for (int ks = 0; ks < kInner / 16; ++ks) {
-            __builtin_amdgcn_sched_barrier(0);      // no operands further ahead: registers are short
-            if (ks + 1 < kInner / 16) read(ks + 1);
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = mfma_32x32x16<T>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    template <int S>
+    static __device__ __forceinline__ char* lds_a() { return lds_object<2 * S, TileA::kBytes>(); }
+    template <int S>
+    static __device__ __forceinline__ char* lds_b() { return lds_object<2 * S + 1, TileB::kBytes>(); }
+    // kWaveBytes of LDS for each wave, behind run().
+    static constexpr int kWaveBytes = (TileA::kBytes < TileB::kBytes ? TileA::kBytes : TileB::kBytes) * 4 / kWaves;
+    static __device__ __forceinline__ char* lds_of_wave(int wave) {
+        constexpr int kShare = kWaves / 4;
+        const int which = wave / kShare;
+        char* p = which == 0 ? lds_a<0>() : which == 1 ? lds_a<1>() : which == 2 ? lds_b<0>() : lds_b<1>();
+        return p + wave % kShare * kWaveBytes;
     }
 
-    // Adds the product over the operands' inner indices (both have the same).  The four
-    // buffers are objects of their own, or the compiler would wait for loads to one
-    // before it reads another.  LDS is free to use behind the next barrier.
-    static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b, char* a0,
-                                               char* b0, char* a1, char* b1) {
+    struct Operands {
+        u32x4 a[MB], b[NB];
+    };
+
+    // The loads to the next tile have landed, and every wave of the workgroup is here.
+    template <int LEFT>
+    static __device__ __forceinline__ void landed() {
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    }
+
+    static __device__ __forceinline__ void multiply(f32x16 (&acc)[MB][NB], const Operands& f) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = mfma_32x32x16<T>(f.a[i], f.b[j], acc[i][j]);
+    }
+
+    // Adds the product over the operands' inner indices (both have the same).  LDS is free
+    // to use behind it.
+    static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int am = wave % WM * MB, bn = wave / WM * NB, inner = a.inner;
         const TileA ta(a, wave);
         const TileB tb(b, wave);
-        const int inner = a.inner;
         if (inner <= 0) return;
-        ta.load(a, 0, a0, wave);
-        tb.load(b, 0, b0, wave);
-        // two tiles a turn; a last one of zeros where their number is odd
-        for (int k = 0; k < inner; k += 2 * kInner) {
-            loads_ready();
-            ta.load(a, k + kInner, a1, wave);
-            tb.load(b, k + kInner, b1, wave);
-            step(acc, ta, tb, a0, b0);
-            loads_ready();
-            if (k + 2 * kInner < inner) {
-                ta.load(a, k + 2 * kInner, a0, wave);
-                tb.load(b, k + 2 * kInner, b0, wave);
+        const auto load = [&](int k, char* la, char* lb) {
+            ta.load(a, k, la, wave);
+            tb.load(b, k, lb, wave);
+        };
+        Operands f[2];
+        const auto read = [&](Operands& to, const char* la, const char* lb, int ks) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) to.a[i] = ta.operand(la, am + i, ks);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) to.b[j] = tb.operand(lb, bn + j, ks);
+        };
+        // The operands of 16 inner indices are read while the 16 before are multiplied, and
+        // a tile's first 16 while the last of the tile before are: the matrix units have
+        // operands at hand on both sides of the barrier.  The barrier also says that every
+        // wave has read the last of a tile, whose place is loaded next.
+        const auto step = [&](int k, char* la, char* lb, const char* next_a, const char* next_b) {
+#pragma unroll
+            for (int ks = 0; ks < kInner / 16 - 1; ++ks) {
+                read(f[(ks + 1) & 1], la, lb, ks + 1);
+                multiply(acc, f[ks & 1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            step(acc, ta, tb, a1, b1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            landed<(STAGES - 2) * kLoads>();
+            load(k + STAGES * kInner, la, lb);
+            read(f[0], next_a, next_b, 0);
+            multiply(acc, f[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        load(0, lds_a<0>(), lds_b<0>());
+        load(kInner, lds_a<1>(), lds_b<1>());
+        if constexpr (STAGES == 4) {
+            load(2 * kInner, lds_a<2>(), lds_b<2>());
+            load(3 * kInner, lds_a<3>(), lds_b<3>());
         }
+        landed<(STAGES - 1) * kLoads>();
+        read(f[0], lds_a<0>(), lds_b<0>(), 0);
+        __builtin_amdgcn_sched_barrier(0);
+        // all stages in a turn; zeros behind the last tile
+        for (int k = 0; k < inner; k += STAGES * kInner) {
+            step(k, lds_a<0>(), lds_b<0>(), lds_a<1>(), lds_b<1>());
+            if constexpr (STAGES == 2) {
+                step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<0>(), lds_b<0>());
+            } else {
+                step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<2>(), lds_b<2>());
+                step(k + 2 * kInner, lds_a<2>(), lds_b<2>(), lds_a<3>(), lds_b<3>());
+                step(k + 3 * kInner, lds_a<3>(), lds_b<3>(), lds_a<0>(), lds_b<0>());
+            }
+        }
+        landed<0>();
     }
 };
 
 // Writes a wave's sums as rows n of 16-bit elements m: each lane has four neighbours in m
-// of one row, so the wave turns its part in LDS, which it has to itself, and stores whole
-// rows of MB * 64 bytes.  value(j, i, r): element of block i, j, register r as T; row(n):
-// where m = 0 of the tile's row n is, or null; elements from m_left on (a multiple of 8)
-// are not there.  The buffers are those of Product::run, behind a barrier.
+// of one row, so the wave turns its part in LDS, 32 rows at a time, and stores whole rows
+// of MB * 64 bytes.  value(j, i, r): element of block i, j, register r as T; row(n): where
+// m = 0 of the tile's row n is, or null; elements from m_left on (a multiple of 8) are not
+// there.  Behind Product::run.
 template <typename P, typename T, int MB, int NB, typename Value, typename Row>
-__device__ __forceinline__ void store_rows(char* a0, char* b0, char* a1, char* b1, int m_left, Value value, Row row) {
-    constexpr int kPieces = MB * 4, kPart = NB * 32 * kPieces * 16, kShare = P::kWaves / 4;
-    static_assert(kShare * kPart <= P::TileA::kBytes && kShare * kPart <= P::TileB::kBytes, "room for the turn");
+__device__ __forceinline__ void store_rows(int m_left, Value value, Row row) {
+    constexpr int kPieces = MB * 4;
+    static_assert(32 * kPieces * 16 <= P::kWaveBytes, "room for the turn");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int which = wave / kShare;
-    char* lds = (which == 0 ? a0 : which == 1 ? b0 : which == 2 ? a1 : b1) + wave % kShare * kPart;
+    char* lds = P::lds_of_wave(wave);
+    const int m0 = wave % P::kWM * MB * 32, n0 = wave / P::kWM * NB * 32;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        const int n = j * 32 + (lane & 31);
+        const int n = lane & 31;
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -230,29 +293,29 @@ __device__ __forceinline__ void store_rows(char* a0, char* b0, char* a1, char* b
                 for (int r = 0; r < 4; ++r) v.v[r] = value(j, i, 4 * q + r);
                 *reinterpret_cast<AlignedPack<T, 4>*>(lds + (n * kPieces + ((i * 4 + q) ^ (n & (kPieces - 1)))) * 16 + h * 8) = v;
             }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    const int m0 = wave % P::kWM * MB * 32, n0 = wave / P::kWM * NB * 32;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int t = 0; t < NB * 32 * kPieces / 64; ++t) {
-        const int at = t * 64 + lane, n = at / kPieces, piece = at % kPieces;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (n * kPieces + (piece ^ (n & (kPieces - 1)))) * 16);
-        T* to = row(n0 + n);
-        if (to != nullptr && m0 + piece * 8 < m_left) *reinterpret_cast<u32x4*>(to + m0 + piece * 8) = v;
+        for (int t = 0; t < 32 * kPieces / 64; ++t) {
+            const int at = t * 64 + lane, r = at / kPieces, piece = at % kPieces;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (r * kPieces + (piece ^ (r & (kPieces - 1)))) * 16);
+            T* to = row(n0 + j * 32 + r);
+            if (to != nullptr && m0 + piece * 8 < m_left) *reinterpret_cast<u32x4*>(to + m0 + piece * 8) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
 // Which tile a workgroup takes: the eight dies take workgroups in turn, and each gets a
-// run of the tiles of its own, in which kGroup tiles of the first index run fastest, so
+// run of the tiles of its own, in which `group` tiles of the first index run fastest, so
 // that the tiles that a die works on at one time share their operands.
-constexpr int kTileGroup = 4;
-__device__ __forceinline__ bool tile_of(uint32_t first, uint32_t second, uint32_t& i, uint32_t& j) {
+constexpr uint32_t kTileGroup = 4;
+__device__ __forceinline__ bool tile_of(uint32_t first, uint32_t second, uint32_t group_size, uint32_t& i, uint32_t& j) {
     const uint32_t total = first * second, each = (total + 7) / 8;
     const uint32_t t = blockIdx.x % 8 * each + blockIdx.x / 8;
     if (blockIdx.x / 8 >= each || t >= total) return false;
-    const uint32_t group = t / (kTileGroup * second), in = t - group * kTileGroup * second;
-    const uint32_t high = min((uint32_t)kTileGroup, first - group * kTileGroup);
-    i = group * kTileGroup + in % high;
+    const uint32_t group = t / (group_size * second), in = t - group * group_size * second;
+    const uint32_t high = min(group_size, first - group * group_size);
+    i = group * group_size + in % high;
     j = in / high;
     return true;
 }
