@@ -360,9 +360,10 @@ int c3_vocab_loss(const c3_vocab_loss_t *a, const void *x, const void *weight, c
 /*
  * c3_vocab_loss_grad -- gradients of c3_vocab_loss for dloss fp32 [tokens], dloss_stride
  * elements apart (0: one number for all): with d = scale * dloss[t] * (exp(l - lse[t]) -
- * onehot(targets[t])), dx = d weight and dweight = d^T x.  d is rounded to 16 bits on its
- * way into the products (in fp16 times a power of two that follows the largest dloss);
- * all sums are fp32, in an order that the sizes and the number of tokens that take part
+ * onehot(targets[t])), dx = d weight and dweight = d^T x.  d, relative to the largest
+ * dloss, is rounded to 16 bits on its way into the products (up to 128 tokens twice, with
+ * what rounding left as a second row; dx always has the target's entry in full); all sums
+ * are fp32, in an order that the sizes and the number of tokens that take part
  * fix.  lse is that of c3_vocab_loss.  dx and dweight are of a->dtype; rows of dx whose
  * token takes no part are zeros.  Results overlap neither inputs nor each other.
  * Workspace and errors as c3_vocab_loss.  Can be captured.

@@ -20,9 +20,18 @@ namespace {
 // What the first launch finds out, at the workspace's start.
 struct Found {
     int32_t count;          // tokens that take part
-    float raise, lower;     // d is kept times `raise`; lower = 1 / raise
-    int32_t pad;
+    float raise, lower;     // d is kept times `raise`; sums of it go out times `lower`
+    int32_t low;            // rows of d that hold what rounding left of as many others
 };
+
+// d is rounded to 16 bits, and where one entry outweighs a token's others, as its target's
+// does, so does that one's rounding: as large as rounding the result, but the same way in
+// all of a row.  Over many tokens it averages out to 1.4 times the result's; over few it
+// may be twice that.  So up to kLowTokens tokens have a second row of d each, with what
+// rounding left of the first, and their rows of x twice: dweight's sums run over both.  dx
+// takes both up to kLowDx tokens, which no tile is fuller for; of more it takes what was
+// left of the target's entry times its row of the weights, in fp32.
+constexpr int kLowTokens = 128, kLowDx = 64;
 
 struct LossArgs {
     const char* x;
@@ -43,13 +52,15 @@ struct LossArgs {
     int32_t* target;            // [tokens] by place
     float* grad;                // [tokens] by place: dloss * scale * raise
     float* lse_at;              // [tokens] by place
-    char* xc;                   // [tokens][pitch] the rows that take part
+    float* low_target;          // [tokens] by place: what rounding left of the target's d
+    char* xc;                   // [tokens and low][pitch] the rows that take part
     float2* parts;              // [row tiles][tokens] maximum and sum
     float* picked;              // [tokens] the target's logit
-    char* d;                    // [tokens][d_pitch]
-    float* dx_parts;            // [splits][tokens][pitch] fp32
+    char* d;                    // [tokens and low][d_pitch]
+    float* dx_parts;            // [splits][dx_rows][pitch] fp32
     int32_t pitch;              // elements: hidden
     int32_t d_pitch;
+    int64_t dx_rows;            // tokens, and again as many as kLowDx of them
     // this piece of the vocabulary
     int64_t row0;
     int32_t piece, first;
@@ -98,12 +109,14 @@ __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
         all += wave_count[w];
         most = fmaxf(most, wave_most[w]);
     }
-    // fp16 holds 6e-8 to 65,504, and d is about dloss over the size of the vocabulary: it
-    // is raised by a power of two that brings the largest dloss to 2^13 .. 2^14
-    int raise = 0;
-    if (a.half && most > 0.0f && most < __builtin_inff())
-        raise = min(max(13 - ilogbf(most), -100), 100);
-    const float up = ldexpf(1.0f, raise);
+    // d is kept relative to the largest dloss: with one dloss for all tokens, a mean's, the
+    // target's entry of an unlikely token then is -1 in 16 bits, and not wherever that dloss
+    // falls between two numbers, for all tokens on the same side.  In fp16 times 2^13, as
+    // that holds 6e-8 to 65,504 and most entries are about one over the vocabulary's size.
+    const float unit = a.half ? 8192.0f : 1.0f;
+    const bool fine = most > 0.0f && most < __builtin_inff();
+    const float largest = fine ? fminf(fmaxf(most, 0x1p-100f), 0x1p100f) : 1.0f;
+    const float up = unit / largest;
     for (int64_t t0 = begin; t0 < end; t0 += 64) {
         const int64_t t = t0 + lane;
         const int32_t target = t < end ? target_of(a, t) : -1;
@@ -126,14 +139,15 @@ __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
             a.lse[t] = 0.0f;
         }
     }
-    if (tid == 0) *a.found = Found{all, up, ldexpf(1.0f, -raise), 0};
+    if (tid == 0) *a.found = Found{all, up, largest / unit, a.dloss != nullptr && all <= kLowTokens ? all : 0};
 }
 
 // Their rows, one a wave.
 __global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
     const int64_t p = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (p >= a.found->count) return;
-    const u32x4* from = reinterpret_cast<const u32x4*>(a.x + (int64_t)a.token[p] * a.x_stride);
+    const int count = a.found->count;
+    if (p >= count + a.found->low) return;
+    const u32x4* from = reinterpret_cast<const u32x4*>(a.x + (int64_t)a.token[p < count ? p : p - count] * a.x_stride);
     u32x4* to = reinterpret_cast<u32x4*>(a.xc + p * a.pitch * 2);
     for (int c = threadIdx.x & 63; c < a.hidden / 8; c += 64) to[c] = from[c];
 }
@@ -145,10 +159,9 @@ template <typename T, bool GRAD, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
     using P = Product<T, WM, WN, MB, NB, STAGES, true, true>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
     const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((count + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
     const int n0 = tn * P::TN, m0 = tm * P::TM;
-    if (n0 >= count) return;
     const int64_t row0 = a.row0 + m0;
     const int rows = (int)min((int64_t)P::TM, a.rows - row0);       // of the vocabulary, left in the tile
     f32x16 acc[MB][NB] = {};
@@ -207,26 +220,41 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
             a.parts[(int64_t)tm * a.tokens + n0 + n] = make_float2(most, sum);
         }
     } else {
-        float lse[NB], g[NB];
-        int32_t target[NB];
+        // the sums become d, in place
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const int n = min(n0 + P::n_of(j), count - 1);
-            lse[j] = a.lse_at[n];
-            g[j] = a.grad[n];
-            target[j] = a.target[n] - (int32_t)row0;
+            const int n = n0 + P::n_of(j), at = min(n, count - 1);
+            const float lse = a.lse_at[at], g = a.grad[at];
+            const int32_t target = a.target[at] - (int32_t)row0;
+            const bool here = __ballot(n < count && target >= 0 && target < P::TM) != 0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = P::m_of(i, r);
+                    float p = __expf(fmaf(acc[i][j][r], a.scale, -lse));
+                    if (m == target) p -= 1.0f;
+                    acc[i][j][r] = m < rows ? p * g : 0.0f;
+                }
+            if (!here) continue;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (P::m_of(i, r) == target && n < count)
+                        a.low_target[n] = acc[i][j][r] - to_f32(from_f32<T>(acc[i][j][r]));
         }
-        store_rows<P, T, MB, NB>(
-            a.d_pitch - m0,         // zeros up to the pitch
-            [&](int j, int i, int r) {
-                const int m = P::m_of(i, r);
-                float p = __expf(fmaf(acc[i][j][r], a.scale, -lse[j]));
-                if (m == target[j]) p -= 1.0f;
-                return from_f32<T>(m < rows ? p * g[j] : 0.0f);
-            },
-            [&](int n) {
-                return n0 + n < count ? reinterpret_cast<T*>(a.d) + (int64_t)(n0 + n) * a.d_pitch + m0 : nullptr;
-            });
+        const auto row_of = [&](int n, int first) {
+            return n0 + n < count ? reinterpret_cast<T*>(a.d) + (int64_t)(first + n0 + n) * a.d_pitch + m0 : nullptr;
+        };
+        // zeros up to the pitch
+        store_rows<P, T, MB, NB>(a.d_pitch - m0, [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r]); },
+                                 [&](int n) { return row_of(n, 0); });
+        if (a.found->low > 0)
+            store_rows<P, T, MB, NB>(
+                a.d_pitch - m0,
+                [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] - to_f32(from_f32<T>(acc[i][j][r]))); },
+                [&](int n) { return row_of(n, count); });
     }
 }
 
@@ -342,15 +370,18 @@ __global__ __launch_bounds__(kFewWaves * 64) void loss_few_kernel(LossArgs a) {
             for (int i = 0; i < MB; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    AlignedPack<T, 4> v;            // the pitch holds whole workgroups' rows
+                    AlignedPack<T, 4> v, low;       // the pitch holds whole workgroups' rows
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int m = m_of(i, 4 * q + r);
                         float p = __expf(fmaf(acc[i][j][4 * q + r], a.scale, -lse));
                         if (m == target) p -= 1.0f;
-                        v.v[r] = from_f32<T>(m < rows ? p * g : 0.0f);
+                        const float d = m < rows ? p * g : 0.0f;
+                        v.v[r] = from_f32<T>(d);
+                        low.v[r] = from_f32<T>(d - to_f32(v.v[r]));
                     }
                     *reinterpret_cast<AlignedPack<T, 4>*>(to + m_of(i, 4 * q)) = v;
+                    *reinterpret_cast<AlignedPack<T, 4>*>(to + (int64_t)tokens * a.d_pitch + m_of(i, 4 * q)) = low;
                 }
         } else {
             const int32_t target = n < tokens ? target_of(a, n) : -1;
@@ -466,16 +497,15 @@ template <typename T, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
     using P = Product<T, WM, WN, MB, NB, STAGES, false, true>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.tokens + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
-    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    const int tokens = __builtin_amdgcn_readfirstlane(a.found->count), count = tokens <= kLowDx ? 2 * tokens : tokens;
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((count + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
     const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = blockIdx.y * a.split_len;
-    if (n0 >= count) return;
     const int inner = min(a.split_len, a.piece - k0);
     f32x16 acc[MB][NB] = {};
     const Operand w{a.weight + (a.row0 + k0) * a.weight_stride + (int64_t)m0 * 2, a.weight_stride, a.hidden - m0, inner};
     const Operand d{a.d + ((int64_t)n0 * a.d_pitch + k0) * 2, (int64_t)a.d_pitch * 2, count - n0, inner};
     P::run(acc, w, d);
-    float* to = a.dx_parts + ((int64_t)blockIdx.y * a.tokens + n0) * a.pitch + m0;
+    float* to = a.dx_parts + ((int64_t)blockIdx.y * a.dx_rows + n0) * a.pitch + m0;
     store_parts<P>(acc, to, a.pitch, count - n0, a.hidden - m0, a.first == 0);
 }
 
@@ -487,8 +517,10 @@ template <typename T, bool SPLIT, int WM, int WN, int MB, int NB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) {
     using P = Product<T, WM, WN, MB, NB, STAGES, false, false>;
     uint32_t tm, tn;
-    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.piece + P::TN - 1) / P::TN), a.tokens <= 1024 ? kWholeRows : kTileGroup, tm, tn)) return;
-    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    if (!tile_of((uint32_t)((a.hidden + P::TM - 1) / P::TM), (uint32_t)((a.piece + P::TN - 1) / P::TN),
+                 a.tokens <= 1024 ? kWholeRows : kTileGroup, tm, tn))
+        return;
+    const int count = __builtin_amdgcn_readfirstlane(a.found->count + a.found->low);
     const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = SPLIT ? blockIdx.y * a.split_len : 0;
     const int inner = SPLIT ? min(a.split_len, count - k0) : count;
     f32x16 acc[MB][NB] = {};
@@ -510,35 +542,62 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) 
 }
 
 // Rows of results from the splits' sums, in order; a wave has 256 columns of a row.
-// place: which row of the sums a row is (-1: zeros), or null.
-template <typename T>
-__global__ __launch_bounds__(256) void loss_finish_kernel(const Found* found, const float* parts, int splits,
-                                                          int64_t split_rows, int64_t pitch, const int32_t* place,
-                                                          int64_t rows, int hidden, char* out, int64_t out_stride) {
-    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
-    const uint32_t slabs = (hidden + 255) / 256;
-    const int64_t r = w / slabs;
-    const int c = (int)(w - r * slabs) * 256 + (threadIdx.x & 63) * 4;
-    if (r >= rows || c >= hidden) return;
-    const int64_t p = place != nullptr ? place[r] : r;
+__device__ __forceinline__ f32x4 split_sums(const float* from, int splits, int64_t stride) {
     f32x4 sum = {};
-    if (p >= 0) {
-        const float* from = parts + p * pitch + c;
-        for (int s0 = 0; s0 < splits; s0 += 8) {
-            f32x4 v[8];
+    for (int s0 = 0; s0 < splits; s0 += 8) {
+        f32x4 v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = *reinterpret_cast<const f32x4*>(from + min(s0 + i, splits - 1) * split_rows * pitch);
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x4*>(from + min(s0 + i, splits - 1) * stride);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (s0 + i < splits) sum += v[i];
-        }
+        for (int i = 0; i < 8; ++i)
+            if (s0 + i < splits) sum += v[i];
     }
-    const float lower = found->lower;
+    return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_four(char* to, f32x4 x) {
     AlignedPack<T, 4> v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.v[i] = from_f32<T>(sum[i] * lower);
-    *reinterpret_cast<AlignedPack<T, 4>*>(out + r * out_stride + c * 2) = v;
+    for (int i = 0; i < 4; ++i) v.v[i] = from_f32<T>(x[i]);
+    *reinterpret_cast<AlignedPack<T, 4>*>(to) = v;
+}
+
+// Rows of the piece of dweight.
+template <typename T>
+__global__ __launch_bounds__(256) void loss_dweight_finish_kernel(LossArgs a) {
+    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
+    const uint32_t slabs = (a.hidden + 255) / 256;
+    const int64_t r = w / slabs;
+    const int c = (int)(w - r * slabs) * 256 + (threadIdx.x & 63) * 4;
+    if (r >= a.piece || c >= a.hidden) return;
+    const f32x4 sum = split_sums(a.w_parts + r * a.pitch + c, a.splits, (int64_t)a.piece * a.pitch);
+    store_four<T>(a.out + (a.row0 + r) * a.out_stride + c * 2, sum * a.found->lower);
+}
+
+// Rows of dx: zeros for a token that takes no part.
+template <typename T>
+__global__ __launch_bounds__(256) void loss_dx_finish_kernel(LossArgs a, char* dx, int64_t dx_stride) {
+    const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
+    const uint32_t slabs = (a.hidden + 255) / 256;
+    const int64_t t = w / slabs;
+    const int c = (int)(w - t * slabs) * 256 + (threadIdx.x & 63) * 4;
+    if (t >= a.tokens || c >= a.hidden) return;
+    const int64_t p = a.place[t], count = a.found->count, stride = a.dx_rows * a.pitch;
+    f32x4 sum = {};
+    if (p >= 0) {
+        sum = split_sums(a.dx_parts + p * a.pitch + c, a.splits, stride);
+        if (count <= kLowDx) {
+            sum += split_sums(a.dx_parts + (count + p) * a.pitch + c, a.splits, stride);
+        } else {
+            const AlignedPack<T, 4> row = *reinterpret_cast<const AlignedPack<T, 4>*>(
+                a.weight + a.target[p] * a.weight_stride + c * 2);
+            const float low = a.low_target[p];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(low, to_f32(row.v[i]), sum[i]);
+        }
+    }
+    store_four<T>(dx + t * dx_stride + c * 2, sum * a.found->lower);
 }
 
 // ---------------------------------------------------------------------------
@@ -561,8 +620,8 @@ int tile_size(int64_t first, int64_t second) {
 }
 
 struct LossPlan {
-    int64_t found, token, place, target, grad, lse_at, xc, parts, picked, d, dx_parts, w_parts, bytes;
-    int64_t pitch, piece, row_tiles, splits, split_len, w_splits, w_split_len;
+    int64_t found, token, place, target, grad, lse_at, low_target, xc, parts, picked, d, dx_parts, w_parts, bytes;
+    int64_t dx_rows, pitch, piece, row_tiles, splits, split_len, w_splits, w_split_len;
     int tile, dx_tile, w_tile;
     bool few;
 };
@@ -595,20 +654,23 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     }
     p.token = take(4 * T);
     p.target = take(4 * T);
-    p.xc = take(2 * T * H);
+    const int64_t with_low = T + (grad ? std::min<int64_t>(T, kLowTokens) : 0);
+    p.xc = take(2 * with_low * H);
     if (!grad) return p;
     p.place = take(4 * T);
     p.grad = take(4 * T);
     p.lse_at = take(4 * T);
+    p.low_target = take(4 * T);
     p.piece = std::min(up(a->rows, kPieceRows),
                        std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows));
-    p.d = take(2 * T * p.piece);
+    p.d = take(2 * with_low * p.piece);
     p.tile = tile_size(p.piece, T);
-    p.dx_tile = tile_size(H, T);
-    split(tiles(H, p.dx_tile) * tiles(T, p.dx_tile), p.piece, &p.splits, &p.split_len);
-    p.dx_parts = take(4 * p.splits * T * H);
+    p.dx_rows = T + std::min<int64_t>(T, kLowDx);
+    p.dx_tile = tile_size(H, p.dx_rows);
+    split(tiles(H, p.dx_tile) * tiles(p.dx_rows, p.dx_tile), p.piece, &p.splits, &p.split_len);
+    p.dx_parts = take(4 * p.splits * p.dx_rows * H);
     p.w_tile = tile_size(H, p.piece);
-    split(tiles(H, p.w_tile) * tiles(p.piece, p.w_tile), T, &p.w_splits, &p.w_split_len);
+    split(tiles(H, p.w_tile) * tiles(p.piece, p.w_tile), with_low, &p.w_splits, &p.w_split_len);
     if (p.w_splits > 1) p.w_parts = take(4 * p.w_splits * p.piece * H);
     return p;
 }
@@ -654,6 +716,8 @@ LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, c
     a.place = reinterpret_cast<int32_t*>(ws + p.place);
     a.grad = reinterpret_cast<float*>(ws + p.grad);
     a.lse_at = reinterpret_cast<float*>(ws + p.lse_at);
+    a.low_target = reinterpret_cast<float*>(ws + p.low_target);
+    a.dx_rows = p.dx_rows;
     a.xc = ws + p.xc;
     a.parts = reinterpret_cast<float2*>(ws + p.parts);
     a.picked = reinterpret_cast<float*>(ws + p.picked);
@@ -710,12 +774,10 @@ hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_stride, hipStream_t s) {
-    const auto finish = [&](const float* parts, int64_t splits, const int32_t* place, int64_t rows, char* out, int64_t stride) {
-        loss_finish_kernel<T><<<wide_grid((uint64_t)(rows * ((a.hidden + 255) / 256) + 3) / 4), dim3(256), 0, s>>>(
-            a.found, parts, (int)splits, rows, a.pitch, place, rows, a.hidden, out, stride);
-    };
+    const uint64_t slabs = (a.hidden + 255) / 256;
     loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
-    if (a.tokens > 0) loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
+    if (a.tokens > 0)
+        loss_rows_kernel<<<dim3((unsigned)((a.tokens + std::min<int64_t>(a.tokens, kLowTokens) + 3) / 4)), dim3(256), 0, s>>>(a);
     for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
         a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
         a.first = a.row0 == 0;
@@ -726,7 +788,7 @@ hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_strid
             by_tile(p.dx_tile, [&](auto shape) {
                 using S = decltype(shape);
                 loss_dx_kernel<T, S::WM, S::WN, S::MB, S::NB, S::STAGES>
-                    <<<dim3(tile_blocks(tiles(a.hidden, p.dx_tile), tiles(a.tokens, p.dx_tile)), (unsigned)p.splits),
+                    <<<dim3(tile_blocks(tiles(a.hidden, p.dx_tile), tiles(a.dx_rows, p.dx_tile)), (unsigned)p.splits),
                        dim3(S::kThreads), 0, s>>>(a);
             });
         }
@@ -739,10 +801,13 @@ hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_strid
             else
                 loss_dweight_kernel<T, false, S::WM, S::WN, S::MB, S::NB, S::STAGES><<<grid, dim3(S::kThreads), 0, s>>>(a);
         });
+        a.splits = (int32_t)p.w_splits;
         if (p.w_splits > 1)
-            finish(a.w_parts, p.w_splits, nullptr, a.piece, a.out + a.row0 * a.out_stride, a.out_stride);
+            loss_dweight_finish_kernel<T><<<wide_grid((a.piece * slabs + 3) / 4), dim3(256), 0, s>>>(a);
     }
-    if (a.tokens > 0) finish(a.dx_parts, p.splits, a.place, a.tokens, dx, dx_stride);
+    a.splits = (int32_t)p.splits;
+    if (a.tokens > 0)
+        loss_dx_finish_kernel<T><<<wide_grid((a.tokens * slabs + 3) / 4), dim3(256), 0, s>>>(a, dx, dx_stride);
     return hipGetLastError();
 }
 
