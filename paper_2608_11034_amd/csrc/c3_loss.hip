@@ -60,7 +60,7 @@ struct LossArgs {
     float* dx_parts;            // [splits][dx_rows][pitch] fp32
     int32_t pitch;              // elements: hidden
     int32_t d_pitch;
-    int64_t dx_rows;            // tokens, and again as many as kLowDx of them
+    int64_t dx_rows;            // most rows of d that dx takes: the tokens', up to kLowDx twice
     // this piece of the vocabulary
     int64_t row0;
     int32_t piece, first;
@@ -626,10 +626,18 @@ struct LossPlan {
     bool few;
 };
 
-// How often an inner index of `length` is split: two workgroups a compute unit, with 512
-// indices or more each.
-void split(int64_t sums, int64_t length, int64_t* splits, int64_t* split_len) {
-    *splits = std::max<int64_t>(1, std::min(512 / std::max<int64_t>(sums, 1), length / 512));
+// How often an inner index of `length` is split, with 512 indices or more each: as makes
+// the rounds of workgroups shortest, each of which costs as much as 640 indices beside its
+// own (its launch, first loads and stores).
+void split(int64_t first, int64_t second, int tile, int64_t length, int64_t* splits, int64_t* split_len) {
+    const int64_t sums = std::max<int64_t>(1, tiles(first, tile) * tiles(second, tile)), slots = tile == 256 ? 256 : 512;
+    int64_t best = INT64_MAX;
+    for (int64_t s = 1; s <= 64 && (s == 1 || length / s >= 512); ++s) {
+        const int64_t cost = tiles(sums * s, slots) * (length / s + 640);
+        if (cost >= best) continue;
+        best = cost;
+        *splits = s;
+    }
     *split_len = std::max<int64_t>(kInner, up((length + *splits - 1) / *splits, kInner));
     *splits = std::max<int64_t>(1, tiles(length, *split_len));
 }
@@ -665,12 +673,12 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
                        std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows));
     p.d = take(2 * with_low * p.piece);
     p.tile = tile_size(p.piece, T);
-    p.dx_rows = T + std::min<int64_t>(T, kLowDx);
+    p.dx_rows = T <= kLowDx ? 2 * T : std::max<int64_t>(T, 2 * kLowDx);
     p.dx_tile = tile_size(H, p.dx_rows);
-    split(tiles(H, p.dx_tile) * tiles(p.dx_rows, p.dx_tile), p.piece, &p.splits, &p.split_len);
+    split(H, p.dx_rows, p.dx_tile, p.piece, &p.splits, &p.split_len);
     p.dx_parts = take(4 * p.splits * p.dx_rows * H);
     p.w_tile = tile_size(H, p.piece);
-    split(tiles(H, p.w_tile) * tiles(p.piece, p.w_tile), with_low, &p.w_splits, &p.w_split_len);
+    split(H, p.piece, p.w_tile, with_low, &p.w_splits, &p.w_split_len);
     if (p.w_splits > 1) p.w_parts = take(4 * p.w_splits * p.piece * H);
     return p;
 }
