@@ -79,6 +79,97 @@ __device__ __forceinline__ int32_t target_of(const LossArgs& a, int64_t t) {
 // ---------------------------------------------------------------------------
 // which tokens take part
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ Found found_of(const LossArgs& a, int count, float most) {
+    // d is kept relative to the largest dloss: with one dloss for all tokens, a mean's, the
+    // target's entry of an unlikely token then is -1 in 16 bits, and not wherever that dloss
+    // falls between two numbers, for all tokens on the same side.  In fp16 times 2^13, as
+    // that holds 6e-8 to 65,504 and most entries are about one over the vocabulary's size.
+    const float unit = a.half ? 8192.0f : 1.0f;
+    const bool fine = most > 0.0f && most < __builtin_inff();
+    const float largest = fine ? fminf(fmaxf(most, 0x1p-100f), 0x1p100f) : 1.0f;
+    const float up = unit / largest;
+    return Found{count, up, largest / unit, a.dloss != nullptr && count <= kLowTokens ? count : 0};
+}
+
+// Token t, which takes part at place p or, target < 0, does not.
+__device__ __forceinline__ void put_token(const LossArgs& a, const Found& found, int64_t t, int32_t target, int32_t p) {
+    if (target >= 0) {
+        a.token[p] = (int32_t)t;
+        a.target[p] = target;
+        if (a.dloss != nullptr) {
+            a.grad[p] = a.dloss[t * a.dloss_stride] * a.scale * found.raise;
+            a.lse_at[p] = a.lse_in[t];
+            a.place[t] = p;
+        }
+    } else if (a.dloss != nullptr) {
+        a.place[t] = -1;
+    } else {
+        a.loss[t] = 0.0f;
+        a.lse[t] = 0.0f;
+    }
+}
+
+__device__ __forceinline__ void copy_row(const LossArgs& a, int64_t t, int64_t p) {
+    const u32x4* from = reinterpret_cast<const u32x4*>(a.x + t * a.x_stride);
+    u32x4* to = reinterpret_cast<u32x4*>(a.xc + p * a.pitch * 2);
+    for (int c = threadIdx.x & 63; c < a.hidden / 8; c += 64) to[c] = from[c];
+}
+
+// Up to kGather tokens: a workgroup has four of them, a wave each, and looks at all the
+// others' targets itself, which is quicker than a launch before it.
+constexpr int kGather = 4096;
+__global__ __launch_bounds__(256) void loss_gather_kernel(LossArgs a) {
+    __shared__ int32_t wave_count[4], wave_before[4];
+    __shared__ float wave_most[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tokens = (int)a.tokens, mine = blockIdx.x * 4;
+    int32_t count = 0, before = 0;
+    float most = 0.0f;
+    for (int t0 = 0; t0 < tokens; t0 += 1024) {
+        int32_t target[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) target[i] = target_of(a, min(t0 + i * 256 + tid, tokens - 1));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + i * 256 + tid;
+            if (t >= tokens || target[i] < 0) continue;
+            ++count;
+            before += t < mine;
+            if (a.dloss != nullptr) most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        count += __shfl_xor(count, m);
+        before += __shfl_xor(before, m);
+        most = fmaxf(most, __shfl_xor(most, m));
+    }
+    if (lane == 0) {
+        wave_count[wave] = count;
+        wave_before[wave] = before;
+        wave_most[wave] = most;
+    }
+    __syncthreads();
+    count = before = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        count += wave_count[w];
+        before += wave_before[w];
+        most = fmaxf(most, wave_most[w]);
+    }
+    const Found found = found_of(a, count, most);
+    if (blockIdx.x == 0 && tid == 0) *a.found = found;
+    const int t = mine + wave;
+    if (t >= tokens) return;
+    for (int i = 0; i < wave; ++i) before += target_of(a, mine + i) >= 0;
+    const int32_t target = target_of(a, t);
+    if (lane == 0) put_token(a, found, t, target, before);
+    if (target < 0) return;
+    copy_row(a, t, before);
+    if (found.low > 0) copy_row(a, t, found.count + before);
+}
+
+// More tokens: one workgroup for which they are, then their rows.
 __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
     __shared__ int32_t wave_count[16];
     __shared__ float wave_most[16];
@@ -109,14 +200,7 @@ __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
         all += wave_count[w];
         most = fmaxf(most, wave_most[w]);
     }
-    // d is kept relative to the largest dloss: with one dloss for all tokens, a mean's, the
-    // target's entry of an unlikely token then is -1 in 16 bits, and not wherever that dloss
-    // falls between two numbers, for all tokens on the same side.  In fp16 times 2^13, as
-    // that holds 6e-8 to 65,504 and most entries are about one over the vocabulary's size.
-    const float unit = a.half ? 8192.0f : 1.0f;
-    const bool fine = most > 0.0f && most < __builtin_inff();
-    const float largest = fine ? fminf(fmaxf(most, 0x1p-100f), 0x1p100f) : 1.0f;
-    const float up = unit / largest;
+    const Found found = found_of(a, all, most);
     for (int64_t t0 = begin; t0 < end; t0 += 64) {
         const int64_t t = t0 + lane;
         const int32_t target = t < end ? target_of(a, t) : -1;
@@ -124,32 +208,18 @@ __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
         const int32_t p = at + __popcll(some & ((1ull << lane) - 1));
         at += __popcll(some);
         if (t >= end) continue;
-        if (target >= 0) {
-            a.token[p] = (int32_t)t;
-            a.target[p] = target;
-            if (a.dloss != nullptr) {
-                a.grad[p] = a.dloss[t * a.dloss_stride] * a.scale * up;
-                a.lse_at[p] = a.lse_in[t];
-                a.place[t] = p;
-            }
-        } else if (a.dloss != nullptr) {
-            a.place[t] = -1;
-        } else {
-            a.loss[t] = 0.0f;
-            a.lse[t] = 0.0f;
-        }
+        put_token(a, found, t, target, p);
     }
-    if (tid == 0) *a.found = Found{all, up, largest / unit, a.dloss != nullptr && all <= kLowTokens ? all : 0};
+    if (tid == 0) *a.found = found;
 }
 
 // Their rows, one a wave.
 __global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
     const int64_t p = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int count = a.found->count;
-    if (p >= count + a.found->low) return;
-    const u32x4* from = reinterpret_cast<const u32x4*>(a.x + (int64_t)a.token[p < count ? p : p - count] * a.x_stride);
-    u32x4* to = reinterpret_cast<u32x4*>(a.xc + p * a.pitch * 2);
-    for (int c = threadIdx.x & 63; c < a.hidden / 8; c += 64) to[c] = from[c];
+    const Found found = *a.found;
+    if (p >= found.count) return;
+    copy_row(a, a.token[p], p);
+    if (found.low > 0) copy_row(a, a.token[p], found.count + p);
 }
 
 // ---------------------------------------------------------------------------
@@ -764,6 +834,17 @@ void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
     });
 }
 
+// Which tokens take part, and their rows together.
+void launch_tokens(const LossArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)((a.tokens + 3) / 4));
+    if (a.tokens > 0 && a.tokens <= kGather) {
+        loss_gather_kernel<<<grid, dim3(256), 0, s>>>(a);
+        return;
+    }
+    loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
+    if (a.tokens > 0) loss_rows_kernel<<<grid, dim3(256), 0, s>>>(a);
+}
+
 template <typename T>
 hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
     if (p.few) {
@@ -771,8 +852,7 @@ hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
         loss_few_join_kernel<<<dim3((unsigned)a.tokens), dim3(1024), 0, s>>>(a, (int)p.row_tiles);
         return hipGetLastError();
     }
-    loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
-    loss_rows_kernel<<<dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, s>>>(a);
+    launch_tokens(a, s);
     a.row0 = 0;
     a.piece = (int32_t)a.rows;
     launch_logits<T, false>(a, a.rows, p.tile, s);
@@ -783,9 +863,7 @@ hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_stride, hipStream_t s) {
     const uint64_t slabs = (a.hidden + 255) / 256;
-    loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
-    if (a.tokens > 0)
-        loss_rows_kernel<<<dim3((unsigned)((a.tokens + std::min<int64_t>(a.tokens, kLowTokens) + 3) / 4)), dim3(256), 0, s>>>(a);
+    launch_tokens(a, s);
     for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
         a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
         a.first = a.row0 == 0;

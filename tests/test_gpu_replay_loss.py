@@ -79,6 +79,43 @@ def test_ignored_tokens():
         assert torch.equal(alone[name].cpu(), got[name].cpu()[~gone])
 
 
+@pytest.mark.parametrize("T", [128, 129, 500, 4096, 4097, 6000])
+def test_few_of_many_take_part(T):
+    """The number of tokens that take part decides what is kept of them, not T: 1, 64, 65,
+    128 and 129 of them."""
+    H, V = 72, 300
+    x, weight, targets, dloss = _inputs(T, H, V, BF16, seed=10)
+    for n in (1, 64, 65, 128, 129):
+        if n > T:
+            continue
+        print("CASE", T, n, flush=True)
+        some = torch.randperm(T, generator=torch.Generator().manual_seed(n))[:n].sort()[0]
+        left = torch.full_like(targets, -1)
+        left[some] = targets[some]
+        got = _both(x, weight, left, dloss)
+        want = plain.vocab_loss(x[some], weight, targets[some], 1.0, dloss[some])
+        for name in ("loss", "lse", "dx"):
+            rest = torch.ones((T,), dtype=torch.bool)
+            rest[some] = False
+            assert bool((got[name].cpu()[rest] == 0).all()), name
+            got[name] = got[name][some.to(DEV)]
+        _compare(got, want, f"{T} {n}")
+
+
+def test_rounding_of_few_tokens():
+    """Up to 128 tokens d is kept twice over, and dx takes the target's entry in full: both
+    gradients then are off by little more than rounding the result, half a step of each
+    element, and not by the rounding of one large entry of d in all of a row."""
+    for T, names in ((1, ("dx", "dweight")), (7, ("dx", "dweight")), (128, ("dx", "dweight")), (700, ("dx",))):
+        v = _inputs(T, 256, 3000, BF16, seed=11)
+        got, want = _both(*v), plain.vocab_loss(*v[:3], 1.0, v[3])
+        for name in names:
+            value = want[name][0]
+            rounded = (value.to(BF16).double() - value).norm()
+            off = (got[name].cpu().double() - value).norm()
+            assert float(off) <= 1.1 * float(rounded), (T, name, float(off / rounded))
+
+
 def test_all_ignored_and_none():
     x, weight, targets, dloss = _inputs(40, 64, 300, BF16, seed=4)
     got = _both(torch.full_like(x, float("nan")), weight, torch.full_like(targets, -1), dloss)
