@@ -739,8 +739,9 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     p.grad = take(4 * T);
     p.lse_at = take(4 * T);
     p.low_target = take(4 * T);
-    p.piece = std::min(up(a->rows, kPieceRows),
-                       std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows));
+    // and no more than that 256 rows of d stay within 31 bits of bytes
+    p.piece = std::min({up(a->rows, kPieceRows), (int64_t)(1 << 22) - kPieceRows,
+                        std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows)});
     p.d = take(2 * with_low * p.piece);
     p.tile = tile_size(p.piece, T);
     p.dx_rows = T <= kLowDx ? 2 * T : std::max<int64_t>(T, 2 * kLowDx);
@@ -780,8 +781,9 @@ LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, c
     a.x = static_cast<const char*>(x);
     a.weight = static_cast<const char*>(weight);
     a.targets = targets;
-    a.x_stride = c->x_stride * 2;
-    a.weight_stride = c->weight_stride * 2;
+    // the stride of a single row says nothing
+    a.x_stride = (c->tokens > 1 ? c->x_stride : c->hidden) * 2;
+    a.weight_stride = (c->rows > 1 ? c->weight_stride : c->hidden) * 2;
     a.tokens = c->tokens;
     a.rows = c->rows;
     a.hidden = (int32_t)c->hidden;

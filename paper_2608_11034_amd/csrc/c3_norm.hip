@@ -107,10 +107,13 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* parts, in
     sums[(int64_t)kind * hidden + c] = sum;
 }
 
-// Workgroups of the gradient: sixteen waves a compute unit.
+// Workgroups of the gradient, all of which the device holds at once: two a compute unit of
+// up to eight waves, one of sixteen.  Three or four smaller ones a unit were slower (8,191
+// gated tokens of 2,048: 122 us forward and back with 1,024 workgroups, 117 with 512): the
+// registers of the gated forms leave no room for the fourth.
 int64_t grad_blocks(int64_t tokens, int64_t hidden) {
     const int t = norm_grad_threads(hidden), rpb = std::max(1, 256 / t);
-    return std::min<int64_t>((tokens + rpb - 1) / rpb, 262144 / std::max(256, t));
+    return std::min<int64_t>((tokens + rpb - 1) / rpb, t <= 512 ? 512 : 256);
 }
 int64_t grad_groups(int64_t tokens, int64_t hidden) {
     return grad_blocks(tokens, hidden) * std::max(1, 256 / norm_grad_threads(hidden));
@@ -119,7 +122,7 @@ int64_t grad_groups(int64_t tokens, int64_t hidden) {
 template <typename R, typename B, bool WIDE, int TPR, int PK>
 hipError_t launch(const NormArgs& a, hipStream_t s) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR, RPB = rows_of_block<TPR>();
-    residual_norm_kernel<R, B, WIDE, TPR, PK><<<wide_grid((uint64_t)(a.tokens + RPB - 1) / RPB), dim3(kBlock), 0, s>>>(a);
+    residual_norm_kernel<R, B, WIDE, TPR, PK><<<wide_grid((uint64_t)(a.tokens + RPB - 1) / RPB, kBlock), dim3(kBlock), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -48,8 +48,8 @@ struct FastDiv {
 // A launch dimension holds fewer than 2^32 threads, and one with more is cut off without
 // an error.  So grids that may pass that have two dimensions; the last workgroups of
 // the second may have nothing to do.
-inline dim3 wide_grid(uint64_t blocks) {
-    constexpr uint64_t kRow = 1u << 22;         // workgroups of 256 threads
+inline dim3 wide_grid(uint64_t blocks, unsigned threads = 256) {
+    const uint64_t kRow = (1u << 30) / threads;
     return blocks <= kRow ? dim3((unsigned)blocks) : dim3((unsigned)kRow, (unsigned)((blocks + kRow - 1) / kRow));
 }
 __device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }

@@ -565,6 +565,16 @@ def expert_dispatch_grad(dsorted, order: ExpertOrder, *, out=None, stream=None):
 # ---------------------------------------------------------------------------
 # embedding
 # ---------------------------------------------------------------------------
+def _result(t, name, beside, shape, dtype, stream):
+    """The caller's result tensor, checked, or a new one on the device of ``beside`` in
+    memory of the stream that the call runs on (new_empty takes half the time of empty)."""
+    if t is not None:
+        return _out(t, name, shape, dtype, beside.device, stream)
+    if stream is None:
+        return beside.new_empty(shape, dtype=dtype)
+    return _new(shape, dtype, beside.device, stream)
+
+
 def _ids(t, name, device=None):
     _dev_tensor(t, name)
     if t.dtype not in (torch.int32, torch.int64) or t.dim() != 1:
@@ -592,7 +602,7 @@ def embedding(ids, table, *, scale: float = 1.0, out=None, stream=None):
     _rows(table, "table", dim=(2,))
     _ids(ids, "ids", table.device)
     rows, hidden = table.shape
-    out = _out(out, "out", torch.Size((ids.numel(), hidden)), table.dtype, table.device, stream)
+    out = _result(out, "out", table, torch.Size((ids.numel(), hidden)), table.dtype, stream)
     a = _embedding_args(ids, table.dtype, rows, hidden, out, table, scale)
     _check(_lib().c3_embedding(a, _ptr(ids), _ptr(table), _ptr(out), _handle(stream, table.device)),
            "c3_embedding")
@@ -616,7 +626,7 @@ def embedding_grad(dout, ids, rows: int, *, scale: float = 1.0, dtype=None, dtab
         raise C3Error("dtable must have the dtype of dout or be fp32")
     if accumulate and dtable is None:
         raise C3Error("accumulate needs a dtable to add to")
-    dtable = _out(dtable, "dtable", torch.Size((rows, dout.shape[1])), dtype, dout.device, stream)
+    dtable = _result(dtable, "dtable", dout, torch.Size((rows, dout.shape[1])), dtype, stream)
     a = _embedding_args(ids, dout.dtype, rows, dout.shape[1], dout, dtable, scale)
     ws = _workspace(_lib().c3_embedding_grad_workspace_size(a), workspace, dout.device, "embedding_grad", stream)
     _check(_lib().c3_embedding_grad(a, _ptr(dout), _ptr(ids), _ptr(dtable), _CODE[dtype], int(bool(accumulate)),
@@ -682,14 +692,15 @@ def residual_norm(x, y, weight, *, post=None, gate=None, scale: float = 1.0, eps
     of x's dtype; all else has weight's.  ``h`` may be x.  stats fp32 [T, 2] goes to
     ``residual_norm_grad``.  hidden up to 16,384."""
     a, _ = _norm_args(x, y, weight, post, gate, scale, eps)
-    n = _out(n, "n", x.shape, weight.dtype, x.device, stream)
+    n = _result(n, "n", x, x.shape, weight.dtype, stream)
     if y is None:
         if h is not None and h is not x:
             raise C3Error("without y, h is x")
         h = x
     else:
-        h = _out(h, "h", x.shape, x.dtype, x.device, stream)
-    stats = _new((x.shape[0], 2), torch.float32, x.device, stream) if stats is None else _stats(stats, x)
+        h = _result(h, "h", x, x.shape, x.dtype, stream)
+    stats = (_result(None, "stats", x, (x.shape[0], 2), torch.float32, stream) if stats is None
+             else _stats(stats, x))
     rc = _lib().c3_residual_norm(a, _at(x), _at(y), None if gate is None else _gate(gate), _ptr(weight), _ptr(post),
                                  _at(h), _at(n), _ptr(stats), _handle(stream, x.device))
     _check(rc, "c3_residual_norm")
@@ -723,17 +734,17 @@ def residual_norm_grad(dn, dh, x, y, weight, stats, *, post=None, gate=None, sca
         _rows(t, name, like.dtype, x.device, (2,))
         if t.shape != x.shape:
             raise C3Error(f"{name} must have the shape of x")
-    dx = _out(dx, "dx", x.shape, x.dtype, x.device, stream)
+    dx = _result(dx, "dx", x, x.shape, x.dtype, stream)
     if y is None:
         if dy is not None:
             raise C3Error("dy needs y")
     else:
-        dy = _out(dy, "dy", x.shape, weight.dtype, x.device, stream)
+        dy = _result(dy, "dy", x, x.shape, weight.dtype, stream)
     if kind == GATE_TOKENS:
-        dgate = _out(dgate, "dgate", x.shape, weight.dtype, x.device, stream)
+        dgate = _result(dgate, "dgate", x, x.shape, weight.dtype, stream)
     elif dgate is not None:
         raise C3Error("dgate as rows needs such a gate")
-    sums = _new((3, x.shape[1]), torch.float32, x.device, stream)
+    sums = _result(None, "sums", x, (3, x.shape[1]), torch.float32, stream)
     ws = _workspace(_lib().c3_residual_norm_grad_workspace_size(a), workspace, x.device, "residual_norm_grad",
                     stream)
     rc = _lib().c3_residual_norm_grad(a, _at(dn), _at(dh), _at(x), _at(y), None if gate is None else _gate(gate),
@@ -763,7 +774,7 @@ def _loss_args(x, weight, targets, scale):
 def _tokens(t, name, x, stream):
     """fp32 [tokens], the caller's or new."""
     if t is None:
-        return _new((x.shape[0],), torch.float32, x.device, stream)
+        return _result(None, name, x, (x.shape[0],), torch.float32, stream)
     _dev_tensor(t, name)
     if t.requires_grad:
         _no_graph(name)
@@ -804,8 +815,8 @@ def vocab_loss_grad(dloss, x, weight, targets, lse, *, scale: float = 1.0, dx=No
     if lse is None:
         raise C3Error("lse must be that of vocab_loss")
     lse = _tokens(lse, "lse", x, stream)
-    dx = _out(dx, "dx", x.shape, x.dtype, x.device, stream)
-    dweight = _out(dweight, "dweight", weight.shape, x.dtype, x.device, stream)
+    dx = _result(dx, "dx", x, x.shape, x.dtype, stream)
+    dweight = _result(dweight, "dweight", x, weight.shape, x.dtype, stream)
     ws = _workspace(_lib().c3_vocab_loss_grad_workspace_size(a), workspace, x.device, "vocab_loss_grad", stream)
     rc = _lib().c3_vocab_loss_grad(a, _ptr(dloss), dloss.stride(0), _ptr(x), _ptr(weight), _ptr(targets), _ptr(lse),
                                    _ptr(dx), dx.stride(0), _ptr(dweight), dweight.stride(0), _ptr(ws),

@@ -154,6 +154,34 @@ def test_strides_and_types_of_targets():
         assert bool((big == 77.0).all())
 
 
+def test_stride_of_a_single_row():
+    """Nothing goes by it."""
+    x, weight, targets, dloss = (t.to(DEV) for t in _inputs(1, 72, 1, BF16, seed=12))
+    want = _both(x, weight, targets, dloss)
+    for n in (0, 8, 4096):
+        odd = [t.as_strided(t.shape, (n, 1)) for t in (x, weight)]
+        got = _both(odd[0], odd[1], targets, dloss)
+        assert all(torch.equal(got[name], t) for name, t in want.items()), n
+
+
+def test_more_rows_than_a_piece():
+    """5,000,000 rows for two tokens: d of 2^22 rows at most."""
+    V, H = 5_000_000, 8
+    g = torch.Generator(device=DEV).manual_seed(13)
+    weight = torch.randn((V, H), generator=g, device=DEV).to(BF16)
+    x = torch.randn((2, H), generator=g, device=DEV).to(BF16)
+    targets = torch.tensor([V - 1, 2 ** 22 + 5], device=DEV)
+    dloss = torch.ones((2,), device=DEV)
+    got = _both(x, weight, targets, dloss)
+    z = torch.mm(x.double(), weight.double().t())
+    lse = torch.logsumexp(z, 1)
+    assert float((got["lse"].double() - lse).abs().max()) <= 2e-5
+    p = (z - lse[:, None]).exp()
+    p[torch.arange(2, device=DEV), targets] -= 1
+    for name, want in (("dx", torch.mm(p, weight.double())), ("dweight", torch.mm(p.t(), x.double()))):
+        assert float((got[name].double() - want).norm() / want.norm()) <= 2.0 ** -8, name
+
+
 @pytest.mark.parametrize("factor", [2.0 ** -20, 2.0 ** 12])
 def test_gradients_of_any_size_in_fp16(factor):
     """dx and dweight scale with dloss: a power of two on it is one on them, as long as
