@@ -49,10 +49,8 @@ __device__ __forceinline__ void load8(const Rows& r, int64_t row, int at, int hi
     expand8(fetch8<T, WIDE>(r, row, at, hidden), x);
 }
 
-// past: past the caches.
 template <typename T, bool WIDE>
-__device__ __forceinline__ void store8(const Rows& r, int64_t row, int at, int hidden, const float (&x)[E],
-                                       bool past = false) {
+__device__ __forceinline__ void store8(const Rows& r, int64_t row, int at, int hidden, const float (&x)[E]) {
     T* p = reinterpret_cast<T*>(r.p) + row * r.stride;
     if constexpr (WIDE) {
         constexpr int V = 16 / sizeof(T);
@@ -62,11 +60,7 @@ __device__ __forceinline__ void store8(const Rows& r, int64_t row, int at, int h
             AlignedPack<T, V> v;
 #pragma unroll
             for (int j = 0; j < V; ++j) v.v[j] = from_f32<T>(x[i + j]);
-            u32x4 word;
-            __builtin_memcpy(&word, &v, 16);
-            u32x4* to = reinterpret_cast<u32x4*>(p + at + i);
-            if (past) __builtin_nontemporal_store(word, to);
-            else *to = word;
+            *reinterpret_cast<AlignedPack<T, V>*>(p + at + i) = v;
         }
     } else {
 #pragma unroll
@@ -104,7 +98,6 @@ struct NormArgs {
     int64_t groups;                             // of rows walked together, for the parts
     int hidden, gate_kind;
     float scale, eps;
-    bool past;                                  // results go past the caches
 };
 
 template <int TPR>

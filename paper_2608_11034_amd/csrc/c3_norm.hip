@@ -162,9 +162,6 @@ int by_type(const c3_residual_norm_t* c, NormArgs& a, bool grad, hipStream_t s) 
         if ((uintptr_t)r->p % size != 0) return C3_E_ALIGN;
         wide = wide && (uintptr_t)r->p % 16 == 0 && (r->stride * size) % 16 == 0;
     }
-    // What a gradient of more than the caches' 256 MiB writes would push out what it has
-    // yet to read (16,384 x 4,096 in bf16, 805 MB: 164 us, and 153 past them).
-    a.past = grad && c->tokens * c->hidden * (3 * rs + 3 * es) > (256ll << 20);
     hipError_t e;
     if (c->dtype == C3_F32)
         e = by_kind<float, float>(a, grad, wide, s);

@@ -111,7 +111,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
             expand8(cur.dh[k], w);
 #pragma unroll
             for (int i = 0; i < E; ++i) d[k][i] = fmaf(rh, fmaf(-h[k][i], mean, d[k][i]), w[i]);
-            if (there) store8<R, WIDE>(a.dx, row, (k * TPR + tid) * E, a.hidden, d[k], a.past);
+            if (there) store8<R, WIDE>(a.dx, row, (k * TPR + tid) * E, a.hidden, d[k]);
         }
         if constexpr (BLOCK) {
             // d becomes the gradient of z, then of y
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
                         for (int i = 0; i < E; ++i)
                             if (there) s_gate[k][i] += dg[i];
                     } else if (there) {
-                        store8<B, WIDE>(a.dgate, row, at, a.hidden, dg, a.past);
+                        store8<B, WIDE>(a.dgate, row, at, a.hidden, dg);
                     }
                     gate_of(k, w);
 #pragma unroll
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
             }
             if (there)
 #pragma unroll
-                for (int k = 0; k < PK; ++k) store8<B, WIDE>(a.dy, row, (k * TPR + tid) * E, a.hidden, d[k], a.past);
+                for (int k = 0; k < PK; ++k) store8<B, WIDE>(a.dy, row, (k * TPR + tid) * E, a.hidden, d[k]);
         }
     }
     // the workgroup's parts
