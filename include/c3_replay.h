@@ -1,5 +1,6 @@
 /*
- * c3_replay.h -- operators of a replayed transformer layer on MI355X (gfx950).
+ * c3_replay.h -- operators of a replayed transformer layer, and of the model around
+ * it, on MI355X (gfx950).
  *
  * A replay runs a layer's forward and backward again on every replica and
  * votes on the outputs and gradients (SCOUT, arXiv 2608.11034, Sec. 6).  Exact
@@ -11,7 +12,8 @@
  * call enqueues work on `stream` and returns, errors are negative
  * c3_status_t, nothing is launched when an argument check fails, host arrays
  * are consumed before the call returns.  Strides count elements.  Element
- * types are C3_F32, C3_BF16 and C3_F16; attention takes the two 16-bit types.
+ * types are C3_F32, C3_BF16 and C3_F16; attention and the loss over a vocabulary take
+ * the two 16-bit types.
  * Sums, softmax statistics and norms are held in 32 bits.
  */
 #ifndef C3_REPLAY_H_
@@ -362,9 +364,9 @@ int c3_vocab_loss(const c3_vocab_loss_t *a, const void *x, const void *weight, c
  * elements apart (0: one number for all): with d = scale * dloss[t] * (exp(l - lse[t]) -
  * onehot(targets[t])), dx = d weight and dweight = d^T x.  d, relative to the largest
  * dloss, is rounded to 16 bits on its way into the products (up to 128 tokens twice, with
- * what rounding left as a second row; dx always has the target's entry in full); all sums
- * are fp32, in an order that the sizes and the number of tokens that take part
- * fix.  lse is that of c3_vocab_loss.  dx and dweight are of a->dtype; rows of dx whose
+ * what rounding left as a second row; dx always has the target's entry in full); in
+ * C3_F16 steps of d are no smaller than 2^-37 of the largest dloss.  All sums are fp32, in
+ * an order that the sizes and the number of tokens that take part fix.  lse is that of c3_vocab_loss.  dx and dweight are of a->dtype; rows of dx whose
  * token takes no part are zeros.  Results overlap neither inputs nor each other.
  * Workspace and errors as c3_vocab_loss.  Can be captured.
  */

@@ -2,10 +2,18 @@
 // epilogue of their own behind: acc[n][m] = sum over k of a(m, k) b(n, k).
 //
 // A workgroup holds TM x TN sums in registers, each wave MB x NB blocks of 32 x 32.
-// Tiles of kInner inner indices come into LDS straight from memory, STAGES of each operand
-// in turn: all but one are on their way while that is multiplied.  An operand lies in
-// memory along the inner index (rows of k) or across it (rows of m or n); the latter is
-// turned by the reads from LDS, so that no operand is copied in another order first.
+// Tiles of kInner inner indices come into LDS straight from memory, two of each operand in
+// turn: one is on its way while the other is multiplied.  An operand lies in memory along
+// the inner index (rows of k) or across it (rows of m or n); the latter is turned by the
+// reads from LDS, so that no operand is copied in another order first.
+//
+// What bounds it is the matrix units at the clock that the card's power leaves them: 8,192
+// x 4,096 by 131,072 x 4,096 in bf16 with the epilogue of the forward loss take 6.9 ms,
+// 1,270 TFLOP/s at 1.73 GHz with the units busy 69% of the cycles and LDS 26%, without bank
+// conflicts; a large library product reaches 1,310 there.  Eight waves of 128 x 64 sums:
+// four of 128 x 128 read a third less of LDS, but nothing is left to run while one of them
+// waits (7.14 ms against 6.75); tiles of 32 inner indices, four in turn, read half lines
+// (7.55 on those four).
 #pragma once
 
 #include "c3_replay_types.h"
@@ -66,26 +74,24 @@ struct Operand {
     int outer, inner;
 };
 
-// A tile of R outer by INNER inner indices in LDS.
-//   ALONG: R rows of 2 INNER bytes; the 16-byte pieces of a row change places with bits
+// A tile of R outer by kInner inner indices in LDS.
+//   ALONG: R rows of 2 kInner bytes; the 16-byte pieces of a row change places with bits
 //   of the row, so that 16 rows' reads of one piece spread over all banks.
-//   Across: for each 128 outer indices INNER rows of 256 bytes; the pieces of a row
+//   Across: for each 128 outer indices kInner rows of 256 bytes; the pieces of a row
 //   change places with its low four bits, so that a turned read's four rows, 64 bytes of
 //   each, do too.
-template <int R, bool ALONG, int WAVES, int INNER, bool ONCE = false>
+template <int R, bool ALONG, int WAVES, bool ONCE = false>
 struct Tile {
-    static constexpr int kLoads = R * INNER / 512 / WAVES;      // of a wave, 1 KiB each
-    static constexpr int kBytes = R * INNER * 2;
-    static constexpr int kPieces = INNER / 8;                   // of a row, ALONG
-    static constexpr int kTurns = INNER / 32;
-    static_assert(kLoads * WAVES * 512 == R * INNER && (ALONG || R % 128 == 0) && (INNER == 64 || INNER == 128),
-                  "rows of a tile");
+    static constexpr int kLoads = R * kInner / 512 / WAVES;     // of a wave, 1 KiB each
+    static constexpr int kBytes = R * kInner * 2;
+    static constexpr int kPieces = kInner / 8;                  // of a row, ALONG
+    static constexpr int kTurns = kInner / 32;
+    static_assert(kLoads * WAVES * 512 == R * kInner && (ALONG || R % 128 == 0), "rows of a tile");
     uint32_t at[kLoads];        // byte offset of a lane's piece
     int piece[ALONG ? kTurns : 1];      // ALONG: which piece, in every kTurns-th load
     int read, read2;            // byte offsets of a lane's reads
 
     static __device__ __forceinline__ int swap_along(int row) {
-        if constexpr (INNER == 128) return row & 15;
         return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
     }
     static __device__ __forceinline__ int swap_across(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
@@ -105,15 +111,15 @@ struct Tile {
                 const int row = row_of(load), q = (lane & (kPieces - 1)) ^ swap_along(row);
                 at[n] = row < x.outer ? (uint32_t)(row * x.stride) + q * 16 : kNowhere;
             } else {
-                const int row = load % (INNER / 4) * 4 + lane / 16;
-                const int col = load / (INNER / 4) * 128 + ((lane & 15) ^ swap_across(row)) * 8;
+                const int row = load % (kInner / 4) * 4 + lane / 16;
+                const int col = load / (kInner / 4) * 128 + ((lane & 15) ^ swap_across(row)) * 8;
                 at[n] = col < x.outer ? (uint32_t)(row * x.stride) + col * 2 : kNowhere;
             }
         }
         if constexpr (ALONG) {
 #pragma unroll
             for (int n = 0; n < kTurns; ++n) piece[n] = (lane & (kPieces - 1)) ^ swap_along(row_of(wave * kLoads + n));
-            read = c * INNER * 2 + ((h ^ swap_along(c)) << 4);
+            read = c * kInner * 2 + ((h ^ swap_along(c)) << 4);
             read2 = 0;
         } else {
             const int row = h * 8 + (i >> 2), q = g * 2 + ((i & 3) >> 1);
@@ -124,7 +130,7 @@ struct Tile {
 
     // Loads the tile that begins at inner index k; zeros behind the last one.
     __device__ __forceinline__ void load(const Operand& x, int k, char* lds, int wave) const {
-        const int left = max(min(x.inner - k, INNER), 0);
+        const int left = max(min(x.inner - k, kInner), 0);
         if constexpr (ALONG) {
             const char* base = scalar(x.p + (int64_t)k * 2);
             const uint32_t bytes = scalar(left > 0 ? (uint32_t)((int64_t)(min(x.outer, R) - 1) * x.stride) + (left + 7) / 8 * 16 : 0);
@@ -143,9 +149,9 @@ struct Tile {
     // matrix unit, lane's outer index lane & 31, inner ones (lane >> 5) * 8 ...
     __device__ __forceinline__ u32x4 operand(const char* lds, int b, int ks) const {
         if constexpr (ALONG) {
-            return *reinterpret_cast<const u32x4*>(lds + b * 64 * INNER + (read ^ (ks << 5)));
+            return *reinterpret_cast<const u32x4*>(lds + b * 64 * kInner + (read ^ (ks << 5)));
         } else {
-            const char* p = lds + (b >> 2) * (INNER * 256) + ks * 4096;
+            const char* p = lds + (b >> 2) * (kInner * 256) + ks * 4096;
             const u32x2 lo = read_turned(p + (read ^ ((b & 3) << 6))), hi = read_turned(p + (read2 ^ ((b & 3) << 6)));
             return u32x4{lo.x, lo.y, hi.x, hi.y};
         }
@@ -160,13 +166,12 @@ __device__ __forceinline__ char* lds_object() {
     return bytes;
 }
 
-template <typename T, int WM, int WN, int MB, int NB, int STAGES, bool A_ALONG, bool B_ALONG>
+template <typename T, int WM, int WN, int MB, int NB, bool A_ALONG, bool B_ALONG>
 struct Product {
-    static_assert(STAGES == 2 || STAGES == 4, "stages");
     static constexpr int kWM = WM, kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TM = WM * MB * 32, TN = WN * NB * 32;
-    using TileA = Tile<TM, A_ALONG, kWaves, kInner>;
-    using TileB = Tile<TN, B_ALONG, kWaves, kInner>;
+    using TileA = Tile<TM, A_ALONG, kWaves>;
+    using TileB = Tile<TN, B_ALONG, kWaves>;
     static constexpr int kLoads = TileA::kLoads + TileB::kLoads;       // of a wave and stage
 
     // Block mb, nb of the wave, register i: m and n inside the tile.
@@ -239,31 +244,21 @@ struct Product {
                 __builtin_amdgcn_sched_barrier(0);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            landed<(STAGES - 2) * kLoads>();
-            load(k + STAGES * kInner, la, lb);
+            landed<0>();
+            load(k + 2 * kInner, la, lb);
             read(f[0], next_a, next_b, 0);
             multiply(acc, f[1]);
             __builtin_amdgcn_sched_barrier(0);
         };
         load(0, lds_a<0>(), lds_b<0>());
         load(kInner, lds_a<1>(), lds_b<1>());
-        if constexpr (STAGES == 4) {
-            load(2 * kInner, lds_a<2>(), lds_b<2>());
-            load(3 * kInner, lds_a<3>(), lds_b<3>());
-        }
-        landed<(STAGES - 1) * kLoads>();
+        landed<kLoads>();
         read(f[0], lds_a<0>(), lds_b<0>(), 0);
         __builtin_amdgcn_sched_barrier(0);
-        // all stages in a turn; zeros behind the last tile
-        for (int k = 0; k < inner; k += STAGES * kInner) {
+        // both stages in a turn; zeros behind the last tile
+        for (int k = 0; k < inner; k += 2 * kInner) {
             step(k, lds_a<0>(), lds_b<0>(), lds_a<1>(), lds_b<1>());
-            if constexpr (STAGES == 2) {
-                step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<0>(), lds_b<0>());
-            } else {
-                step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<2>(), lds_b<2>());
-                step(k + 2 * kInner, lds_a<2>(), lds_b<2>(), lds_a<3>(), lds_b<3>());
-                step(k + 3 * kInner, lds_a<3>(), lds_b<3>(), lds_a<0>(), lds_b<0>());
-            }
+            step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<0>(), lds_b<0>());
         }
         landed<0>();
     }

@@ -162,6 +162,30 @@ def test_many_tokens():
     assert bool((total.abs() <= 2.0 ** -8 * size).all())
 
 
+def test_most_tokens_of_a_loss():
+    """2^24 workgroups of 256 threads for the rows that take part: more than one launch
+    dimension holds.  Logits of 8 products: bounds as in replay_ends_plain, |z| below 64."""
+    T, H, V = (1 << 26) - 1, 8, 5
+    print("CASE", T, H, V, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(13)
+    x = torch.randn((T, H), generator=g, device=DEV, dtype=BF16)
+    weight = torch.randn((V, H), generator=g, device=DEV, dtype=BF16)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    targets[5:9] = -1
+    loss, lse = replay.vocab_loss(x, weight, targets)
+    at = torch.cat((torch.arange(0, 12, device=DEV), torch.arange(T // 2, T // 2 + 12, device=DEV),
+                    torch.arange(T - 12, T, device=DEV)))
+    z = torch.mm(x[at].double(), weight.double().t())
+    assert float(z.abs().max()) < 64
+    kept = targets[at] >= 0
+    want = torch.where(kept, torch.logsumexp(z, 1), 0.0)
+    picked = torch.where(kept, z.gather(1, targets[at].long().clamp(min=0)[:, None])[:, 0], 0.0)
+    # a logit is off by (8 + 8) 2^-24 of 8 products below 64 in all, exp's argument by as much
+    bound = 4 * 16 * 64 * 2.0 ** -24
+    assert float((lse[at].double() - want).abs().max()) <= bound
+    assert float((loss[at].double() - (want - picked)).abs().max()) <= bound
+
+
 def test_refusals():
     v = _inputs(11)
     T, H = v["y"].shape

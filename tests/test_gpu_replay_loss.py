@@ -196,6 +196,15 @@ def test_gradients_of_any_size_in_fp16(factor):
         assert torch.equal(a[fine], b[fine]), name
 
 
+def test_dloss_up_to_the_largest_of_fp32_in_fp16():
+    """Columns where the weights are zero have zeros in dx, and nothing is NaN."""
+    x, weight, targets, _ = _inputs(100, 64, 500, F16, seed=9)
+    weight[:, ::2] = 0
+    got = _both(x, weight, targets, torch.full((100,), 2.0 ** 127))
+    assert int((got["dx"][:, ::2] != 0).sum()) == 0
+    assert not bool(got["dx"].isnan().any()) and not bool(got["dweight"].isnan().any())
+
+
 def test_sure_and_far_logits():
     """Logits of a few hundred: one row takes all of the sum, or the target has none."""
     T, H, V = 64, 64, 1000
