@@ -1,7 +1,7 @@
-"""Operators of a replayed transformer layer (include/c3_replay.h) for torch
-tensors on a ROCm device.
+"""Operators of a replayed transformer layer and of the model around it
+(include/c3_replay.h) for torch tensors on a ROCm device.
 
-A replay runs a layer again on every replica and votes on outputs and
+A replay runs a model again on every replica and votes on outputs and
 gradients bit by bit, so each operator's bits depend on its inputs alone: no
 atomics, sums in an order that the sizes fix.  Argument marshalling only;
 every step runs in the HIP kernels of libc3.so and there is no CPU fallback.
