@@ -231,13 +231,11 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
 // ---------------------------------------------------------------------------
 // logits
 // ---------------------------------------------------------------------------
+// Tokens from n0 on by the rows of tile tm.
 template <typename T, bool GRAD, int WM, int WN, int MB, int NB>
-__global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
+__device__ __forceinline__ void logits_tile(const LossArgs& a, int count, uint32_t tm, int n0) {
     using P = Product<T, WM, WN, MB, NB, true, true>;
-    uint32_t tm, tn;
-    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
-    if (!tile_of((uint32_t)((a.piece + P::TM - 1) / P::TM), (uint32_t)((count + P::TN - 1) / P::TN), kTileGroup, tm, tn)) return;
-    const int n0 = tn * P::TN, m0 = tm * P::TM;
+    const int m0 = tm * P::TM;
     const int64_t row0 = a.row0 + m0;
     const int rows = (int)min((int64_t)P::TM, a.rows - row0);       // of the vocabulary, left in the tile
     f32x16 acc[MB][NB] = {};
@@ -332,6 +330,30 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
                 [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] - to_f32(from_f32<T>(acc[i][j][r]))); },
                 [&](int n) { return row_of(n, count); });
     }
+}
+
+// Where the last round of 256 by 256 tiles has work for half of a die's 32 compute units
+// at most, two take a tile of it, 128 tokens each, which costs three quarters of a round:
+// 233 of 333 fp16 tokens over 32,000 rows of 1,000 are 125 tiles, 32.7 us, and 25.7 so;
+// 2,047 over 50,001 of 2,048 six rounds and 32 tiles, 399 us, and 386 so.  How many tokens
+// take part is known here only.
+constexpr uint32_t kUnitsOfDie = 32;
+template <typename T, bool GRAD, int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
+    constexpr int TM = WM * MB * 32, TN = WN * NB * 32;
+    const int count = __builtin_amdgcn_readfirstlane(a.found->count);
+    const uint32_t first = (a.piece + TM - 1) / TM, second = (count + TN - 1) / TN, v = blockIdx.x / 8;
+    uint32_t tm, tn;
+    if constexpr (TN == 256) {
+        const uint32_t each = (first * second + 7) / 8, whole = each / kUnitsOfDie * kUnitsOfDie;
+        if (v >= whole && each - whole <= kUnitsOfDie / 2) {
+            const int n1 = (v - whole) % 2 * (TN / 2);
+            if (tile_at(first, second, kTileGroup, whole + (v - whole) / 2, tm, tn) && (int)tn * TN + n1 < count)
+                logits_tile<T, GRAD, 4, 2, 2, 2>(a, count, tm, tn * TN + n1);
+            return;
+        }
+    }
+    if (tile_at(first, second, kTileGroup, v, tm, tn)) logits_tile<T, GRAD, WM, WN, MB, NB>(a, count, tm, tn * TN);
 }
 
 // The forward pass of few tokens is bound by reading the weights once.  A workgroup has
@@ -837,8 +859,9 @@ template <typename T, bool GRAD>
 void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
     by_tile(tile, [&](auto shape) {
         using S = decltype(shape);
-        loss_logits_kernel<T, GRAD, S::WM, S::WN, S::MB, S::NB>
-            <<<dim3(tile_blocks(tiles(rows, tile), tiles(a.tokens, tile))), dim3(S::kThreads), 0, s>>>(a);
+        // whole rounds, as the last one's tiles may be halved
+        const unsigned blocks = (unsigned)up(tile_blocks(tiles(rows, tile), tiles(a.tokens, tile)), 8 * kUnitsOfDie);
+        loss_logits_kernel<T, GRAD, S::WM, S::WN, S::MB, S::NB><<<dim3(blocks), dim3(S::kThreads), 0, s>>>(a);
     });
 }
 

@@ -307,15 +307,19 @@ __device__ __forceinline__ void store_rows(int m_left, Value value, Row row) {
 // run of the tiles of its own, in which `group` tiles of the first index run fastest, so
 // that the tiles that a die works on at one time share their operands.
 constexpr uint32_t kTileGroup = 4;
-__device__ __forceinline__ bool tile_of(uint32_t first, uint32_t second, uint32_t group_size, uint32_t& i, uint32_t& j) {
+__device__ __forceinline__ bool tile_at(uint32_t first, uint32_t second, uint32_t group_size, uint32_t v, uint32_t& i,
+                                        uint32_t& j) {      // the v-th of the workgroup's die
     const uint32_t total = first * second, each = (total + 7) / 8;
-    const uint32_t t = blockIdx.x % 8 * each + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= each || t >= total) return false;
+    const uint32_t t = blockIdx.x % 8 * each + v;
+    if (v >= each || t >= total) return false;
     const uint32_t group = t / (group_size * second), in = t - group * group_size * second;
     const uint32_t high = min(group_size, first - group * group_size);
     i = group * group_size + in % high;
     j = in / high;
     return true;
+}
+__device__ __forceinline__ bool tile_of(uint32_t first, uint32_t second, uint32_t group_size, uint32_t& i, uint32_t& j) {
+    return tile_at(first, second, group_size, blockIdx.x / 8, i, j);
 }
 inline unsigned tile_blocks(int64_t first, int64_t second) { return (unsigned)((first * second + 7) / 8 * 8); }
 

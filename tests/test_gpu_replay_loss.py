@@ -59,6 +59,14 @@ def test_pieces(dtype):
     _compare(_both(*v), plain.vocab_loss(*v[:3], 1.0, v[3]))
 
 
+@pytest.mark.parametrize("T,H,V,ignored", [(333, 64, 32000, 0.4), (880, 72, 20000, 0.0), (1010, 8, 20001, 0.01)])
+def test_last_round(T, H, V, ignored):
+    """Tiles in whole rounds of the device and a few more, which two workgroups share."""
+    print("CASE", T, H, V, flush=True)
+    v = _inputs(T, H, V, BF16, ignored, seed=10)
+    _compare(_both(*v), plain.vocab_loss(*v[:3], 1.0, v[3]))
+
+
 def test_ignored_tokens():
     """What an ignored token holds enters nothing, and the others' bits do not go by it."""
     T, H, V = 300, 136, 500
