@@ -15,10 +15,10 @@
 // Writing a whole table of zeros is most of the gradient's bytes.  It needs no sorted
 // list, so it runs beside the sort, on compute units that have no part in that.
 //
-// 16,384 bf16 tokens into 32,000 rows of 4,096: 22 us for the sort's three launches, 60
+// 16,384 bf16 tokens into 32,000 rows of 4,096: 22 us for the sort's three launches, 57
 // for the sums and what is left of the zeros (HBM), 9 to join.  4,095 fp16 tokens into
-// 131,072 fp32 rows of 1,000: 22 us for one workgroup's sort and a fifth of 520 MB of
-// zeros beside it, 81 for the sums and the others at 5.3 TB/s, 5 to join.
+// 131,072 fp32 rows of 1,000: 28 us for one workgroup's sort and 151 of 520 MB of zeros
+// beside it, 63 for the sums and the others at 6 TB/s, 5 to join.
 #include <algorithm>
 
 #include "c3_internal.h"
@@ -203,14 +203,13 @@ struct Zeros {
     int64_t stride, row0, row1;
     const uint8_t* present;
     FastDiv units;                          // of a row
-    uint32_t each;                          // rows of a workgroup: 32 KiB or one
+    uint32_t each;                          // rows of a workgroup
     int first;
-    static Zeros of(void* table, int64_t stride, int64_t hidden) {
+    static Zeros of(void* table, int64_t stride, int64_t hidden) {      // `each` is set for a launch
         Zeros z{};
         z.table = static_cast<D*>(table);
         z.stride = stride;
         z.units = FastDiv((uint32_t)(hidden / kUnit));
-        z.each = (uint32_t)std::max<int64_t>(1, 32768 / (int64_t)sizeof(D) / hidden);
         return z;
     }
     int64_t blocks() const { return (row1 - row0 + each - 1) / each; }
@@ -555,28 +554,32 @@ hipError_t launch_grad(const GradCall& g) {
     int32_t* source = reinterpret_cast<int32_t*>(g.ws + p.source);
     uint8_t* present = reinterpret_cast<uint8_t*>(g.ws + p.present);
     // The sort's launches leave most of the device idle for some microseconds, in which
-    // kBeside bytes of zeros are written; the rest comes beside the sums, without the rows
-    // that have one.
-    constexpr int64_t kBeside = 24 << 20;
+    // kBeside bytes of zeros are written, or kBesideOne where one workgroup sorts for 20 us;
+    // the rest comes beside the sums, without the rows that have one.  A workgroup writes
+    // rows of 32 KiB, or beside the sums, where it has a quarter of the threads, 16 (4,095
+    // tokens into 131,072 fp32 rows of 1,000: 106 us with 32 there and 96 MiB beside the
+    // sort, 100 with 16, 114 with 8; 97 with 16 and 144 MiB).
+    constexpr int64_t kBeside = 24 << 20, kBesideOne = 144 << 20;
     const int passes = (key_bits + kMostBits - 1) / kMostBits;
     Zeros<D, V> z = Zeros<D, V>::of(g.table, g.table_stride, g.hidden);
     z.row1 = g.accumulate ? g.rows : 0;
     // the grid of a launch with `blocks` workgroups of its own that takes `bytes` of the zeros
-    const auto with_zeros = [&](int64_t blocks, int64_t bytes) {
+    const auto with_zeros = [&](int64_t blocks, int64_t bytes, int64_t of_block) {
+        z.each = (uint32_t)std::max<int64_t>(1, of_block / (int64_t)sizeof(D) / g.hidden);
         z.first = (int)blocks;
         z.row0 = z.row1;
         z.row1 = std::min(g.rows, z.row0 + bytes / (g.hidden * (int64_t)sizeof(D)) / z.each * z.each);
         return wide_grid((uint64_t)(blocks + z.blocks()));
     };
-    constexpr int64_t kAll = (int64_t)1 << 62;
+    constexpr int64_t kAll = (int64_t)1 << 62, kOfSort = 32768, kOfSum = 16384;
     if (g.n == 0) {
-        const dim3 grid = with_zeros(0, kAll);
+        const dim3 grid = with_zeros(0, kAll, kOfSum);
         embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
                                                                   static_cast<D*>(g.table), z);
         return hipGetLastError();
     }
     if (p.one) {
-        const dim3 grid = with_zeros(1, 4 * kBeside);      // one workgroup sorts for 20 us
+        const dim3 grid = with_zeros(1, kBesideOne, kOfSort);
         sort_one_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits, keys, source,
                                                                    present, z);
     } else {
@@ -592,7 +595,7 @@ hipError_t launch_grad(const GradCall& g) {
         q.runs = (int)((g.n - 1) >> q.run_shift) + 1;
         q.passes = passes;
         q.key_bits = key_bits;
-        dim3 grid = with_zeros(q.runs, kBeside);
+        dim3 grid = with_zeros(q.runs, kBeside, kOfSort);
         sort_count_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         for (q.pass = 0; q.pass < passes; ++q.pass) {
             // the last pass writes to the first pair of lists
@@ -603,11 +606,11 @@ hipError_t launch_grad(const GradCall& g) {
             q.in_source = to_first ? s2 : source;
             q.keys = to_first ? keys : k2;
             q.source = to_first ? source : s2;
-            grid = with_zeros(q.runs, kBeside);
+            grid = with_zeros(q.runs, kBeside, kOfSort);
             sort_place_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         }
     }
-    const dim3 grid = with_zeros((a.chunks * a.slabs + 3) / 4, kAll);
+    const dim3 grid = with_zeros((a.chunks * a.slabs + 3) / 4, kAll, kOfSum);
     z.present = present;
     embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
                                                               static_cast<D*>(g.table), z);
@@ -717,7 +720,7 @@ int c3_embedding_grad(const c3_embedding_t* a, const void* dout, const void* ids
         return C3_E_WORKSPACE;
     // the sums' workgroups are counted in 31 bits, the zeros' in a grid's 2^22 by 2^16
     const int64_t row_bytes = a->hidden * replay_elem_size(table_dtype);
-    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34) || a->rows / std::max<int64_t>(1, 32768 / row_bytes) >= (1ll << 37))
+    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34) || a->rows / std::max<int64_t>(1, 16384 / row_bytes) >= (1ll << 37))
         return C3_E_UNSUPPORTED;
     const GradCall g{{ids, a->id_bytes == 8}, a->tokens, a->rows, a->hidden, a->row_stride, a->table_stride, dout,
                      dtable, a->scale, accumulate != 0, static_cast<char*>(ws), reinterpret_cast<hipStream_t>(stream)};
