@@ -52,12 +52,25 @@ struct Ids {
     }
 };
 
+// V elements in memory.  WIDE: on their own size; else on an element's, which the memory
+// units take too (the gradient of 16,384 bf16 tokens of 4,097 into 32,000 rows: 113 us,
+// and 226 element by element).  A row's last piece then begins V elements before its end,
+// and what it shares with the piece before is written twice, with the same bits.
+template <typename T, int V, bool WIDE>
+struct alignas(WIDE ? sizeof(T) * V : sizeof(T)) Piece {
+    T v[V];
+};
+template <int V, bool WIDE>
+__device__ __forceinline__ int64_t column(int64_t piece, int64_t hidden) {
+    return WIDE ? piece * V : min(piece * V, hidden - V);
+}
+
 // ---------------------------------------------------------------------------
 // lookup
 // ---------------------------------------------------------------------------
-template <typename T, int V, int U>
-__global__ __launch_bounds__(256) void embedding_kernel(Ids ids, int64_t tokens, uint32_t rows, int64_t pieces,
-                                                        uint32_t parts, const T* table, int64_t table_stride,
+template <typename T, int V, bool WIDE, int U>
+__global__ __launch_bounds__(256) void embedding_kernel(Ids ids, int64_t tokens, uint32_t rows, int64_t hidden,
+                                                        int64_t pieces, uint32_t parts, const T* table, int64_t table_stride,
                                                         T* out, int64_t out_stride, float scale) {
     const int lane = threadIdx.x & 63;
     const int64_t w = wide_block() * 4 + (threadIdx.x >> 6);
@@ -65,18 +78,19 @@ __global__ __launch_bounds__(256) void embedding_kernel(Ids ids, int64_t tokens,
     if (token >= tokens) return;
     const uint32_t id = ids.key(token, rows);
     const T* row = table + (int64_t)(id < rows ? id : 0) * table_stride;
-    AlignedPack<T, V> p[U];
+    using Pack = Piece<T, V, WIDE>;
+    Pack p[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)             // behind the row's end the last piece again
-        p[u] = *reinterpret_cast<const AlignedPack<T, V>*>(row + min(c0 + u * 64, pieces - 1) * V);
+        p[u] = *reinterpret_cast<const Pack*>(row + column<V, WIDE>(min(c0 + u * 64, pieces - 1), hidden));
     T* to = out + token * out_stride;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (c0 + u * 64 >= pieces) continue;
-        AlignedPack<T, V> y;
+        Pack y;
 #pragma unroll
         for (int j = 0; j < V; ++j) y.v[j] = from_f32<T>(id < rows ? to_f32(p[u].v[j]) * scale : 0.0f);
-        *reinterpret_cast<AlignedPack<T, V>*>(to + (c0 + u * 64) * V) = y;
+        *reinterpret_cast<Pack*>(to + column<V, WIDE>(c0 + u * 64, hidden)) = y;
     }
 }
 
@@ -196,20 +210,23 @@ constexpr int kOneSortWords = (kSortWaves << kMostBits) + kSortWaves + kOneSort 
 // those that `present` (null: none) marks.  They go past the caches, in whole lines: what
 // the sums read stays there (16,384 tokens into 32,000 rows of 4,096 in bf16: 112 us, and
 // 95 so).
-template <typename D, int V>
+template <typename D, int V, bool WIDE>
 struct Zeros {
     static constexpr int kUnit = V == 1 ? 1 : 16 / (int)sizeof(D);     // elements of a store
+    typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
     D* table;
     int64_t stride, row0, row1;
     const uint8_t* present;
-    FastDiv units;                          // of a row
+    FastDiv units;                          // of a row, the last as a last Piece
+    int64_t hidden;
     uint32_t each;                          // rows of a workgroup
     int first;
     static Zeros of(void* table, int64_t stride, int64_t hidden) {      // `each` is set for a launch
         Zeros z{};
         z.table = static_cast<D*>(table);
         z.stride = stride;
-        z.units = FastDiv((uint32_t)(hidden / kUnit));
+        z.units = FastDiv((uint32_t)((hidden + kUnit - 1) / kUnit));
+        z.hidden = hidden;
         return z;
     }
     int64_t blocks() const { return (row1 - row0 + each - 1) / each; }
@@ -223,24 +240,25 @@ struct Zeros {
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) {
                 const uint32_t i = min(i0 + q * blockDim.x, all - 1), r = units.quot(i), c = i - r * units.d;
-                to[q] = table + (at + r) * stride + (int64_t)c * kUnit;
+                to[q] = table + (at + r) * stride + column<kUnit, WIDE>(c, hidden);
                 mark[q] = present != nullptr ? present[at + r] : 0;
             }
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) {
                 if (mark[q] != 0 || i0 + q * blockDim.x >= all) continue;
                 if constexpr (V == 1) *to[q] = (D)0.0f;
-                else __builtin_nontemporal_store(u32x4{}, reinterpret_cast<u32x4*>(to[q]));
+                else if constexpr (WIDE) __builtin_nontemporal_store(u32x4{}, reinterpret_cast<u32x4*>(to[q]));
+                else __builtin_nontemporal_store(Loose{}, reinterpret_cast<Loose*>(to[q]));
             }
         }
     }
 };
 
 // Workgroup 0 sorts, the others write zeros.
-template <typename D, int V>
+template <typename D, int V, bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_one_kernel(Ids ids, int n, uint32_t rows, int key_bits,
                                                                 uint32_t* keys, int32_t* source, uint8_t* present,
-                                                                Zeros<D, V> z) {
+                                                                Zeros<D, V, WIDE> z) {
     __shared__ int32_t lds[kOneSortWords];
     if (wide_block() < z.first)
         sort_one(ids, n, rows, key_bits, keys, source, present, lds);
@@ -274,8 +292,8 @@ struct SortPass {
     }
 };
 
-template <typename D, int V>
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Zeros<D, V> z) {
+template <typename D, int V, bool WIDE>
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Zeros<D, V, WIDE> z) {
     __shared__ int32_t lds[1 << kMostBits];
     if (wide_block() >= z.first) {
         z.write();
@@ -293,8 +311,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Ze
     p.count(0, blockIdx.x)[threadIdx.x] = lds[threadIdx.x];
 }
 
-template <typename D, int V>
-__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Zeros<D, V> z) {
+template <typename D, int V, bool WIDE>
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Zeros<D, V, WIDE> z) {
     __shared__ int32_t lds[(kSortWaves << kMostBits) + kSortWaves];
     __shared__ int32_t next[kNextCounts];
     if (wide_block() >= z.first) {
@@ -359,10 +377,18 @@ struct SumArgs {
     int32_t accumulate;
 };
 
-template <typename D, int V>
-__device__ __forceinline__ void write_row(const SumArgs& a, D* table, uint32_t row, int64_t c, const float* sum) {
-    AlignedPack<D, V>* to = reinterpret_cast<AlignedPack<D, V>*>(table + (int64_t)row * a.table_stride + c * V);
-    AlignedPack<D, V> y;
+// skip: elements that the piece before adds to.
+template <typename D, int V, bool WIDE>
+__device__ __forceinline__ void write_row(const SumArgs& a, D* table, uint32_t row, int64_t col, int skip, const float* sum) {
+    using Pack = Piece<D, V, WIDE>;
+    Pack* to = reinterpret_cast<Pack*>(table + (int64_t)row * a.table_stride + col);
+    Pack y;
+    if (!WIDE && a.accumulate && skip != 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j >= skip) to->v[j] = from_f32<D>(fmaf(sum[j], a.scale, to_f32(to->v[j])));
+        return;
+    }
     if (a.accumulate) y = *to;
 #pragma unroll
     for (int j = 0; j < V; ++j) y.v[j] = from_f32<D>(a.accumulate ? fmaf(sum[j], a.scale, to_f32(y.v[j])) : sum[j] * a.scale);
@@ -370,8 +396,8 @@ __device__ __forceinline__ void write_row(const SumArgs& a, D* table, uint32_t r
 }
 
 // A wave: the places of one chunk, 64 pieces of the width.
-template <typename S, typename D, int V>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* dout, D* table, Zeros<D, V> z) {
+template <typename S, typename D, int V, bool WIDE>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* dout, D* table, Zeros<D, V, WIDE> z) {
     if (wide_block() >= z.first) {
         z.write();
         return;
@@ -389,14 +415,15 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* 
     const uint32_t before = begin > 0 ? a.keys[begin - 1] : a.rows;
     const uint32_t behind = begin + count < a.n ? a.keys[begin + count] : a.rows;
     const bool in = c < a.pieces;
-    const int64_t col = (in ? c : 0) * V;
+    const int64_t col = column<V, WIDE>(in ? c : 0, a.width);
+    const int skip = in ? (int)(c * V - col) : 0;
     float sum[V] = {};
     bool whole = (uint32_t)__builtin_amdgcn_readlane(my_key, 0) != before;      // the run began here
     for (int i0 = 0; i0 < count; i0 += kSumRows) {
-        AlignedPack<S, V> p[kSumRows];
+        Piece<S, V, WIDE> p[kSumRows];
 #pragma unroll
         for (int i = 0; i < kSumRows; ++i)  // the rows stand without a branch between the loads
-            p[i] = *reinterpret_cast<const AlignedPack<S, V>*>(
+            p[i] = *reinterpret_cast<const Piece<S, V, WIDE>*>(
                 dout + (int64_t)__builtin_amdgcn_readlane(my_token, min(i0 + i, count - 1)) * a.dout_stride + col);
 #pragma unroll
         for (int i = 0; i < kSumRows; ++i) {
@@ -410,9 +437,9 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* 
             if (next == key && at + 1 < count) continue;
             if (in) {
                 if (whole && next != key) {
-                    write_row<D, V>(a, table, key, c, sum);
+                    write_row<D, V, WIDE>(a, table, key, col, skip, sum);
                 } else {
-                    float* to = a.parts + (chunk * 2 + whole) * a.width + c * V;
+                    float* to = a.parts + (chunk * 2 + whole) * a.width + col;
 #pragma unroll
                     for (int j = 0; j < V; ++j) to[j] = sum[j];
                 }
@@ -426,7 +453,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const S* 
 
 // A workgroup: the parts of the run that begins in one chunk and goes on, 64 pieces of
 // the width.  Its four waves take a quarter of the parts each.
-template <typename D, int V>
+template <typename D, int V, bool WIDE>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, D* table) {
     __shared__ float quarter[3][V][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -447,18 +474,19 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, D* table
     }
     const int64_t last = lo / a.chunk, count = last - chunk + 1, each = (count + 3) / 4;
     const bool in = c < a.pieces;
-    const int64_t col = (in ? c : 0) * V;
+    const int64_t col = column<V, WIDE>(in ? c : 0, a.width);
+    const int skip = in ? (int)(c * V - col) : 0;
     float sum[V] = {};
     const int64_t end = min(count, (wave + 1) * each);
     for (int64_t i0 = wave * each; i0 < end; i0 += 8) {
-        AlignedPack<float, V == 1 ? 1 : 4> p[8][V == 1 ? 1 : V / 4];
+        Piece<float, V == 1 ? 1 : 4, WIDE> p[8][V == 1 ? 1 : V / 4];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t at = min(i0 + i, end - 1);
             const float* from = a.parts + ((chunk + at) * 2 + (at == 0)) * a.width + col;
 #pragma unroll
             for (int j = 0; j < (V == 1 ? 1 : V / 4); ++j)
-                p[i][j] = *reinterpret_cast<const AlignedPack<float, V == 1 ? 1 : 4>*>(from + j * 4);
+                p[i][j] = *reinterpret_cast<const Piece<float, V == 1 ? 1 : 4, WIDE>*>(from + j * 4);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -473,7 +501,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, D* table
     if (wave > 0 || !in) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = sum[j] + quarter[0][j][lane] + quarter[1][j][lane] + quarter[2][j][lane];
-    write_row<D, V>(a, table, key, c, sum);
+    write_row<D, V, WIDE>(a, table, key, col, skip, sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -531,7 +559,7 @@ struct GradCall {
     hipStream_t s;
 };
 
-template <typename S, typename D, int V>
+template <typename S, typename D, int V, bool WIDE>
 hipError_t launch_grad(const GradCall& g) {
     const GradPlan p = grad_plan(g.n, g.rows, g.hidden);
     SumArgs a{};
@@ -539,7 +567,7 @@ hipError_t launch_grad(const GradCall& g) {
     a.source = reinterpret_cast<int32_t*>(g.ws + p.source);
     a.parts = reinterpret_cast<float*>(g.ws + p.parts);
     a.n = g.n;
-    a.pieces = g.hidden / V;
+    a.pieces = (g.hidden + V - 1) / V;
     a.width = g.hidden;
     a.dout_stride = g.dout_stride;
     a.table_stride = g.table_stride;
@@ -561,7 +589,7 @@ hipError_t launch_grad(const GradCall& g) {
     // sort, 100 with 16, 114 with 8; 97 with 16 and 144 MiB).
     constexpr int64_t kBeside = 24 << 20, kBesideOne = 144 << 20;
     const int passes = (key_bits + kMostBits - 1) / kMostBits;
-    Zeros<D, V> z = Zeros<D, V>::of(g.table, g.table_stride, g.hidden);
+    Zeros<D, V, WIDE> z = Zeros<D, V, WIDE>::of(g.table, g.table_stride, g.hidden);
     z.row1 = g.accumulate ? g.rows : 0;
     // the grid of a launch with `blocks` workgroups of its own that takes `bytes` of the zeros
     const auto with_zeros = [&](int64_t blocks, int64_t bytes, int64_t of_block) {
@@ -574,13 +602,13 @@ hipError_t launch_grad(const GradCall& g) {
     constexpr int64_t kAll = (int64_t)1 << 62, kOfSort = 32768, kOfSum = 16384;
     if (g.n == 0) {
         const dim3 grid = with_zeros(0, kAll, kOfSum);
-        embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
+        embedding_sum_kernel<S, D, V, WIDE><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
                                                                   static_cast<D*>(g.table), z);
         return hipGetLastError();
     }
     if (p.one) {
         const dim3 grid = with_zeros(1, kBesideOne, kOfSort);
-        sort_one_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits, keys, source,
+        sort_one_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits, keys, source,
                                                                    present, z);
     } else {
         SortPass q{};
@@ -596,7 +624,7 @@ hipError_t launch_grad(const GradCall& g) {
         q.passes = passes;
         q.key_bits = key_bits;
         dim3 grid = with_zeros(q.runs, kBeside, kOfSort);
-        sort_count_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
+        sort_count_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         for (q.pass = 0; q.pass < passes; ++q.pass) {
             // the last pass writes to the first pair of lists
             const bool to_first = (passes - 1 - q.pass) % 2 == 0;
@@ -607,15 +635,15 @@ hipError_t launch_grad(const GradCall& g) {
             q.keys = to_first ? keys : k2;
             q.source = to_first ? source : s2;
             grid = with_zeros(q.runs, kBeside, kOfSort);
-            sort_place_kernel<D, V><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
+            sort_place_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         }
     }
     const dim3 grid = with_zeros((a.chunks * a.slabs + 3) / 4, kAll, kOfSum);
     z.present = present;
-    embedding_sum_kernel<S, D, V><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
+    embedding_sum_kernel<S, D, V, WIDE><<<grid, dim3(256), 0, g.s>>>(a, static_cast<const S*>(g.dout),
                                                               static_cast<D*>(g.table), z);
     if (a.chunks > 1)
-        embedding_join_kernel<D, V><<<wide_grid((uint64_t)(a.chunks - 1) * a.slabs), dim3(256), 0, g.s>>>(
+        embedding_join_kernel<D, V, WIDE><<<wide_grid((uint64_t)(a.chunks - 1) * a.slabs), dim3(256), 0, g.s>>>(
             a, static_cast<D*>(g.table));
     return hipGetLastError();
 }
@@ -626,7 +654,8 @@ hipError_t grad_of(const GradCall& g) {
     // a piece is 16 bytes of dout, and of the table 16 or, in fp32 for a 16-bit dout, 32
     const bool wide = g.hidden % V == 0 && g.dout_stride % V == 0 && g.table_stride % V == 0 &&
                       (uintptr_t)g.dout % 16 == 0 && (uintptr_t)g.table % (V * sizeof(D)) == 0;
-    return wide ? launch_grad<S, D, V>(g) : launch_grad<S, D, 1>(g);
+    if (wide) return launch_grad<S, D, V, true>(g);
+    return g.hidden >= V ? launch_grad<S, D, V, false>(g) : launch_grad<S, D, 1, true>(g);
 }
 
 struct LookupCall {
@@ -638,19 +667,19 @@ struct LookupCall {
     hipStream_t s;
 };
 
-template <typename T, int V>
+template <typename T, int V, bool WIDE>
 hipError_t launch_lookup(const LookupCall& g) {
-    const int64_t pieces = g.hidden / V;
+    const int64_t pieces = (g.hidden + V - 1) / V;
     // four pieces a lane, or one where that leaves the device waves to spare
     const bool few = g.n * ((pieces + 255) / 256) < 4096;
     const uint32_t parts = (uint32_t)(few ? (pieces + 63) / 64 : (pieces + 255) / 256);
     const dim3 grid = wide_grid((uint64_t)(g.n * parts + 3) / 4);
     if (few)
-        embedding_kernel<T, V, 1><<<grid, dim3(256), 0, g.s>>>(g.ids, g.n, (uint32_t)g.rows, pieces, parts,
+        embedding_kernel<T, V, WIDE, 1><<<grid, dim3(256), 0, g.s>>>(g.ids, g.n, (uint32_t)g.rows, g.hidden, pieces, parts,
                                                               static_cast<const T*>(g.table), g.table_stride,
                                                               static_cast<T*>(g.out), g.out_stride, g.scale);
     else
-        embedding_kernel<T, V, 4><<<grid, dim3(256), 0, g.s>>>(g.ids, g.n, (uint32_t)g.rows, pieces, parts,
+        embedding_kernel<T, V, WIDE, 4><<<grid, dim3(256), 0, g.s>>>(g.ids, g.n, (uint32_t)g.rows, g.hidden, pieces, parts,
                                                               static_cast<const T*>(g.table), g.table_stride,
                                                               static_cast<T*>(g.out), g.out_stride, g.scale);
     return hipGetLastError();
@@ -661,7 +690,8 @@ hipError_t lookup_of(const LookupCall& g) {
     constexpr int V = 16 / sizeof(T);
     const bool wide = g.hidden % V == 0 && g.table_stride % V == 0 && g.out_stride % V == 0 &&
                       (uintptr_t)g.table % 16 == 0 && (uintptr_t)g.out % 16 == 0;
-    return wide ? launch_lookup<T, V>(g) : launch_lookup<T, 1>(g);
+    if (wide) return launch_lookup<T, V, true>(g);
+    return g.hidden >= V ? launch_lookup<T, V, false>(g) : launch_lookup<T, 1, true>(g);
 }
 
 // What both calls ask of their sizes.

@@ -88,7 +88,9 @@ def test_gradient(dtype, n, rows, hidden, hot, out):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,rows,hidden,hot,out", [(1, 3, 8, 0, 0), (100, 7, 40, 0.4, 0.3), (5000, 9000, 520, 0.3, 0.1),
-                                                   (17000, 50, 24, 0.3, 0.1)])
+                                                   (17000, 50, 24, 0.3, 0.1), (50, 7, 9, 0.3, 0.1),
+                                                   (600, 300, 513, 0.3, 0.1), (4100, 900, 257, 0.3, 0.1),
+                                                   (5000, 100, 1021, 0.3, 0.1)])
 def test_accumulated(dtype, n, rows, hidden, hot, out):
     print("CASE", dtype, n, rows, hidden, flush=True)
     ids, dout, old = _ids(5, n, rows, hot, out), _randn(6, n, hidden, dtype=dtype), _randn(7, rows, hidden, dtype=dtype)
