@@ -17,8 +17,8 @@
 //
 // 16,384 bf16 tokens into 32,000 rows of 4,096: 22 us for the sort's three launches, 57
 // for the sums and what is left of the zeros (HBM), 9 to join.  4,095 fp16 tokens into
-// 131,072 fp32 rows of 1,000: 28 us for one workgroup's sort and 151 of 520 MB of zeros
-// beside it, 63 for the sums and the others at 6 TB/s, 5 to join.
+// 131,072 fp32 rows of 1,000: 24 us for one workgroup's sort and 151 of 520 MB of zeros
+// beside it, 66 for the sums and the others at 5.8 TB/s, 5 to join.
 #include <algorithm>
 
 #include "c3_internal.h"
@@ -233,7 +233,7 @@ struct Zeros {
     __device__ __forceinline__ void write() const {
         const int64_t at = row0 + (wide_block() - first) * each;
         const uint32_t all = (uint32_t)max((int64_t)0, min((int64_t)each, row1 - at)) * units.d;
-        constexpr int kAhead = 8;           // marks on their way together, without a branch between them
+        constexpr int kAhead = 4;           // marks on their way together, without a branch between them
         for (uint32_t i0 = threadIdx.x; i0 < all; i0 += blockDim.x * kAhead) {
             D* to[kAhead];
             uint8_t mark[kAhead];
@@ -586,7 +586,8 @@ hipError_t launch_grad(const GradCall& g) {
     // the rest comes beside the sums, without the rows that have one.  A workgroup writes
     // rows of 32 KiB, or beside the sums, where it has a quarter of the threads, 16 (4,095
     // tokens into 131,072 fp32 rows of 1,000: 106 us with 32 there and 96 MiB beside the
-    // sort, 100 with 16, 114 with 8; 97 with 16 and 144 MiB).
+    // sort, 100 with 16, 114 with 8; 97 with 16 and 144 MiB, 94 with four marks ahead and
+    // not eight).
     constexpr int64_t kBeside = 24 << 20, kBesideOne = 144 << 20;
     const int passes = (key_bits + kMostBits - 1) / kMostBits;
     Zeros<D, V, WIDE> z = Zeros<D, V, WIDE>::of(g.table, g.table_stride, g.hidden);
