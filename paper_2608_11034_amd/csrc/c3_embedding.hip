@@ -348,7 +348,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Ze
     for (int64_t i0 = wb; i0 < we; i0 += 64) {
         const int64_t i = i0 + lane;
         const uint32_t k = i < we ? p.key(i) : 0;
-        const bool repeats = lane > 0 && __shfl_up(k, 1) == k;     // a mark for each lane would crowd a frequent row's
+        // a mark for each lane would crowd a frequent row's; every lane takes part in the shuffle
+        const uint32_t lower = __shfl_up(k, 1);
+        const bool repeats = lane > 0 && lower == k;
         const int32_t at = place_of((k >> lo) & (digits - 1), i < we, bits, mine);
         if (at < 0) continue;
         p.keys[at] = k;

@@ -142,3 +142,47 @@ def test_same_bits_every_time():
     first = replay.embedding_grad(dout, ids, 500)
     for _ in range(3):
         assert torch.equal(replay.embedding_grad(dout, ids, 500), first)
+
+
+@pytest.mark.parametrize("dtype,to", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32),
+                                      (torch.float32, torch.float32)])
+@pytest.mark.parametrize("n,rows,hidden", [(5000, 32000, 4097), (5000, 32000, 4096), (4097, 10000, 4099),
+                                           (300, 40000, 4097), (20000, 100000, 1021)])
+def test_zeros_beside_the_sums(dtype, to, n, rows, hidden):
+    """Tables of more zeros than the sort's launches take (72 MiB in 16 bits, or 144 MiB for up to
+    4,096 tokens): the sums' launch leaves out the rows that the sort has marked.  Rows with a
+    token and rows without, over the whole table, which holds something else before."""
+    print("CASE", dtype, to, n, rows, hidden, flush=True)
+    ids, dout = _ids(14, n, rows, 0.05, 0.1).to(DEV), _randn(15, n, hidden, dtype=dtype).to(DEV)
+    ids[:2] = torch.tensor([1, 0], device=DEV)
+    kept = (ids >= 0) & (ids < rows)
+    at, part = ids[kept], dout[kept].double()
+    want = torch.zeros((rows, hidden), dtype=torch.float64, device=DEV).index_add_(0, at, part)
+    mag = torch.zeros((rows, hidden), dtype=torch.float64, device=DEV).index_add_(0, at, part.abs_())
+    count = torch.bincount(at, minlength=rows)
+    assert int((count > 0).sum()) > 100 and int((count == 0).sum()) > 100
+    got = torch.full((rows, hidden), 77.0, dtype=to, device=DEV)
+    replay.embedding_grad(dout, ids, rows, dtable=got)
+    assert bool((got[count == 0] == 0).all())
+    # bounds as of the plain 64-bit form: the sum's order, then the rounding to the result's type
+    half = torch.finfo(to).eps / 2
+    bound = want.abs() * half * 1.01 + mag.mul_((count[:, None] + 3) * 2.0 ** -24) + plain.TINY[to]
+    assert bool(((got.double() - want).abs_() <= bound).all())
+
+
+def test_marks_of_rows_wider_than_the_zeros_beside_the_sort():
+    """Rows of more than 24 MiB are all left to the sums' launch, also row 0, whose only token
+    stands second in its wave behind another row's."""
+    n, hidden = 4097, 6_291_464
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("dout takes 52 GB")
+    dout = torch.empty((n, hidden), dtype=torch.bfloat16, device=DEV)
+    dout[:2] = torch.tensor([[1.0], [2.0]], device=DEV)
+    ids = torch.full((n,), -100, dtype=torch.int64, device=DEV)
+    ids[:2] = torch.tensor([1, 0], device=DEV)
+    got = torch.full((3, hidden), 77.0, device=DEV)
+    replay.embedding_grad(dout, ids, 3, dtable=got)
+    for row, value in enumerate((2.0, 1.0, 0.0)):
+        assert bool((got[row] == value).all()), row
+    del dout
+    torch.cuda.empty_cache()
