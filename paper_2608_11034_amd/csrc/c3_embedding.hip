@@ -21,36 +21,15 @@
 // beside it, 66 for the sums and the others at 5.8 TB/s, 5 to join.
 #include <algorithm>
 
-#include "c3_internal.h"
-#include "c3_replay_types.h"
+#include "c3_sort.h"
 
 namespace c3 {
 namespace {
 
-constexpr int kSortThreads = 1024;
-constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kOneSort = 4096;              // tokens that one workgroup sorts in LDS
 constexpr int kPerThread = kOneSort / kSortThreads;
-constexpr int kMostBits = 10;               // of a digit
-constexpr int kMostPasses = 4;              // keys have 32 bits at most
-constexpr int kMostRuns = 64;
-constexpr int kNextCounts = 16384;          // runs times digits at most: they are counted in LDS
 constexpr int kMostChunk = 64;
 constexpr int kSumRows = 16;                // rows that a wave has in flight
-
-struct Ids {
-    const void* p;
-    int wide;                               // 8-byte numbers
-    // The row that a token reads; `rows`, behind all of them, for none.
-    __device__ __forceinline__ uint32_t key(int64_t t, uint32_t rows) const {
-        if (wide) {
-            const int64_t i = static_cast<const int64_t*>(p)[t];
-            return (uint64_t)i < rows ? (uint32_t)i : rows;
-        }
-        const int32_t i = static_cast<const int32_t*>(p)[t];
-        return (uint32_t)i < rows ? (uint32_t)i : rows;
-    }
-};
 
 // V elements in memory.  WIDE: on their own size; else on an element's, which the memory
 // units take too (the gradient of 16,384 bf16 tokens of 4,097 into 32,000 rows: 113 us,
@@ -97,52 +76,6 @@ __global__ __launch_bounds__(256) void embedding_kernel(Ids ids, int64_t tokens,
 // ---------------------------------------------------------------------------
 // sort
 // ---------------------------------------------------------------------------
-// One step of a stable sort by `bits` bits of the key: the places of 64 keys in a row,
-// given the wave's next place of every digit (`mine`), which it moves on.
-__device__ __forceinline__ int32_t place_of(uint32_t digit, bool there, int bits, int32_t* mine) {
-    const int lane = threadIdx.x & 63;
-    uint64_t same = __ballot(there);
-    for (int b = 0; b < bits; ++b) {
-        const bool bit = (digit >> b) & 1;
-        const uint64_t m = __ballot(bit);
-        same &= bit ? m : ~m;
-    }
-    int32_t place = -1;
-    if (there) place = mine[digit] + __popcll(same & ((1ull << lane) - 1));
-    __builtin_amdgcn_wave_barrier();
-    if (there && (same >> lane) == 1) mine[digit] = place + 1;     // the last lane of its digit
-    __builtin_amdgcn_wave_barrier();
-    return place;
-}
-
-// lds[w][digit] holds wave w's number of keys with the digit: turns it into the wave's
-// first place of the digit, of which a thread has one.  total, before: keys with the
-// digit in all workgroups, and in those before this one.
-template <typename Counted>
-__device__ __forceinline__ void first_places(int32_t* lds, int32_t* wave_sum, int digits, Counted counted) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t total = 0, before = 0;
-    if (tid < digits) counted(tid, total, before);
-    int32_t sum = total;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int32_t up = __shfl_up(sum, d);
-        if (lane >= d) sum += up;
-    }
-    if (lane == 63) wave_sum[wave] = sum;
-    __syncthreads();
-    int32_t at = sum - total + before;
-    for (int w = 0; w < wave; ++w) at += wave_sum[w];
-    if (tid < digits) {
-#pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int32_t c = lds[w * digits + tid];
-            lds[w * digits + tid] = at;
-            at += c;
-        }
-    }
-    __syncthreads();
-}
-
 // Up to kOneSort tokens: the keys stay in registers between the passes and change
 // places through LDS.
 __device__ void sort_one(const Ids& ids, int n, uint32_t rows, int key_bits, uint32_t* keys, int32_t* source,
@@ -266,102 +199,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_one_kernel(Ids ids, int n, 
         z.write();
 }
 
-// More tokens: a launch counts the lowest digits of every run of tokens, and one for each
-// digit places them.  A placed key counts its next digit for the run that it comes to;
-// these are integers, so their order does not matter.  A workgroup counts in LDS first:
-// one by one a frequent digit's counts would wait for each other in memory (10 us of 18
-// with 16,384 tokens of which half have one high digit).
-struct SortPass {
-    Ids ids;                // of the first pass, whose keys and tokens are not written down
-    const uint32_t* in_keys;
-    const int32_t* in_source;
-    uint32_t* keys;
-    int32_t* source;
-    int32_t* counts;        // [passes][runs][1 << kMostBits]
-    uint8_t* present;       // 1 for each row of the table that has a token: stores of one
-                            // value, where bits would be atomics on few words
-    int64_t n;
-    uint32_t rows;
-    int run_shift;          // log2 of a run's length
-    int runs, pass, passes, key_bits;
-    __device__ __forceinline__ uint32_t key(int64_t i) const { return pass == 0 ? ids.key(i, rows) : in_keys[i]; }
-    __device__ __forceinline__ int lo(int p) const { return key_bits * p / passes; }
-    __device__ __forceinline__ int bits(int p) const { return lo(p + 1) - lo(p); }
-    __device__ __forceinline__ int32_t* count(int p, int64_t r) const {
-        return counts + (((int64_t)p * runs + r) << kMostBits);
-    }
-};
-
+// More tokens: a launch that counts, and one for each digit.
 template <typename D, int V, bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass p, Zeros<D, V, WIDE> z) {
-    __shared__ int32_t lds[1 << kMostBits];
-    if (wide_block() >= z.first) {
-        z.write();
-        return;
-    }
-    const int digits = 1 << p.bits(0);
-    lds[threadIdx.x] = 0;
-    for (int q = 1; q < p.passes; ++q) p.count(q, blockIdx.x)[threadIdx.x] = 0;
-    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i <= p.rows / 4; i += (int64_t)p.runs * kSortThreads)
-        reinterpret_cast<uint32_t*>(p.present)[i] = 0;
-    __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x << p.run_shift, end = min(begin + (1ll << p.run_shift), p.n);
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&lds[p.key(i) & (digits - 1)], 1);
-    __syncthreads();
-    p.count(0, blockIdx.x)[threadIdx.x] = lds[threadIdx.x];
+    if (wide_block() >= z.first) z.write();
+    else sort_count(p);
 }
-
 template <typename D, int V, bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortPass p, Zeros<D, V, WIDE> z) {
-    __shared__ int32_t lds[(kSortWaves << kMostBits) + kSortWaves];
-    __shared__ int32_t next[kNextCounts];
-    if (wide_block() >= z.first) {
-        z.write();
-        return;
-    }
-    const int lo = p.lo(p.pass), bits = p.bits(p.pass), digits = 1 << bits;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t* wave_sum = lds + kSortWaves * digits;
-    const int64_t begin = (int64_t)blockIdx.x << p.run_shift, end = min(begin + (1ll << p.run_shift), p.n);
-    const int64_t part = (1ll << p.run_shift) / kSortWaves, wb = begin + wave * part, we = min(wb + part, end);
-    const bool last = p.pass == p.passes - 1;
-    const int next_lo = p.lo(p.pass + 1), next_bits = last ? 0 : p.bits(p.pass + 1);
-    for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortThreads) lds[i] = 0;
-    if (!last)
-        for (int i = threadIdx.x; i < p.runs << next_bits; i += kSortThreads) next[i] = 0;
-    __syncthreads();
-    int32_t* mine = lds + wave * digits;
-    for (int64_t i = wb + lane; i < we; i += 64) atomicAdd(&mine[(p.key(i) >> lo) & (digits - 1)], 1);
-    __syncthreads();
-    first_places(lds, wave_sum, digits, [&](int d, int32_t& total, int32_t& before) {
-        for (int b = 0; b < p.runs; b += 16) {          // sixteen loads in flight
-            int32_t c[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) c[j] = p.count(p.pass, min(b + j, p.runs - 1))[d];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                before += b + j < (int)blockIdx.x ? c[j] : 0;
-                total += b + j < p.runs ? c[j] : 0;
-            }
-        }
-    });
-    for (int64_t i0 = wb; i0 < we; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const uint32_t k = i < we ? p.key(i) : 0;
-        // a mark for each lane would crowd a frequent row's; every lane takes part in the shuffle
-        const uint32_t lower = __shfl_up(k, 1);
-        const bool repeats = lane > 0 && lower == k;
-        const int32_t at = place_of((k >> lo) & (digits - 1), i < we, bits, mine);
-        if (at < 0) continue;
-        p.keys[at] = k;
-        p.source[at] = p.pass == 0 ? (int32_t)i : p.in_source[i];
-        if (last && k < p.rows && !repeats) p.present[k] = 1;
-        if (!last) atomicAdd(&next[((at >> p.run_shift) << next_bits) + ((k >> next_lo) & ((1 << next_bits) - 1))], 1);
-    }
-    if (last) return;
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.runs << next_bits; i += kSortThreads)
-        if (next[i] != 0) atomicAdd(&p.count(p.pass + 1, i >> next_bits)[i & ((1 << next_bits) - 1)], next[i]);
+    if (wide_block() >= z.first) z.write();
+    else sort_place(p);
 }
 
 // ---------------------------------------------------------------------------
@@ -509,12 +356,6 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, D* table
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-int key_bits_of(int64_t rows) {             // keys are 0 .. rows
-    int bits = 1;
-    while ((rows >> bits) != 0) ++bits;
-    return bits;
-}
-
 // Places of a wave: 16 to 64, as many as leave 4,096 waves.  The sizes alone decide, not
 // the alignment: the order of the sums goes by it.
 int chunk_of(int64_t n, int64_t hidden) {
@@ -542,7 +383,7 @@ GradPlan grad_plan(int64_t n, int64_t rows, int64_t hidden) {
     if (!p.one) {
         p.keys2 = take(4 * n);
         p.source2 = take(4 * n);
-        p.counts = take(4 * (int64_t)kMostPasses * kMostRuns << kMostBits);
+        p.counts = take(kSortCountBytes);
     }
     const int chunk = chunk_of(n, hidden);
     p.parts = take(4 * 2 * ((n + chunk - 1) / chunk) * hidden);
@@ -579,7 +420,6 @@ hipError_t launch_grad(const GradCall& g) {
     a.chunks = (g.n + a.chunk - 1) / a.chunk;
     a.scale = g.scale;
     a.accumulate = g.accumulate;
-    const int key_bits = key_bits_of(g.rows);
     uint32_t* keys = reinterpret_cast<uint32_t*>(g.ws + p.keys);
     int32_t* source = reinterpret_cast<int32_t*>(g.ws + p.source);
     uint8_t* present = reinterpret_cast<uint8_t*>(g.ws + p.present);
@@ -591,7 +431,6 @@ hipError_t launch_grad(const GradCall& g) {
     // sort, 100 with 16, 114 with 8; 97 with 16 and 144 MiB, 94 with four marks ahead and
     // not eight).
     constexpr int64_t kBeside = 24 << 20, kBesideOne = 144 << 20;
-    const int passes = (key_bits + kMostBits - 1) / kMostBits;
     Zeros<D, V, WIDE> z = Zeros<D, V, WIDE>::of(g.table, g.table_stride, g.hidden);
     z.row1 = g.accumulate ? g.rows : 0;
     // the grid of a launch with `blocks` workgroups of its own that takes `bytes` of the zeros
@@ -611,32 +450,16 @@ hipError_t launch_grad(const GradCall& g) {
     }
     if (p.one) {
         const dim3 grid = with_zeros(1, kBesideOne, kOfSort);
-        sort_one_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits, keys, source,
+        sort_one_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(g.ids, (int)g.n, a.rows, key_bits_of(g.rows), keys, source,
                                                                    present, z);
     } else {
-        SortPass q{};
-        q.ids = g.ids;
-        q.counts = reinterpret_cast<int32_t*>(g.ws + p.counts);
-        q.present = present;
-        q.n = g.n;
-        q.rows = a.rows;
-        q.run_shift = 10;
-        const int most_runs = std::min(kMostRuns, kNextCounts >> ((key_bits + passes - 1) / passes));
-        while (((g.n - 1) >> q.run_shift) >= most_runs) ++q.run_shift;
-        q.runs = (int)((g.n - 1) >> q.run_shift) + 1;
-        q.passes = passes;
-        q.key_bits = key_bits;
+        SortPass q = sort_of(g.ids, g.n, a.rows, reinterpret_cast<int32_t*>(g.ws + p.counts), present);
+        const SortLists lists{keys, source, reinterpret_cast<uint32_t*>(g.ws + p.keys2),
+                              reinterpret_cast<int32_t*>(g.ws + p.source2)};
         dim3 grid = with_zeros(q.runs, kBeside, kOfSort);
         sort_count_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
-        for (q.pass = 0; q.pass < passes; ++q.pass) {
-            // the last pass writes to the first pair of lists
-            const bool to_first = (passes - 1 - q.pass) % 2 == 0;
-            uint32_t* k2 = reinterpret_cast<uint32_t*>(g.ws + p.keys2);
-            int32_t* s2 = reinterpret_cast<int32_t*>(g.ws + p.source2);
-            q.in_keys = to_first ? k2 : keys;
-            q.in_source = to_first ? s2 : source;
-            q.keys = to_first ? keys : k2;
-            q.source = to_first ? source : s2;
+        for (int pass = 0; pass < q.passes; ++pass) {
+            set_pass(q, pass, lists);
             grid = with_zeros(q.runs, kBeside, kOfSort);
             sort_place_kernel<D, V, WIDE><<<grid, dim3(kSortThreads), 0, g.s>>>(q, z);
         }
