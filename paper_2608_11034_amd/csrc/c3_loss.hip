@@ -18,6 +18,7 @@
 
 #include "c3_internal.h"
 #include "c3_product.h"
+#include "c3_sort.h"
 
 namespace c3 {
 namespace {
@@ -31,12 +32,17 @@ struct Found {
 
 // d is rounded to 16 bits, and where one entry outweighs a token's others, as its target's
 // does, so does that one's rounding: as large as rounding the result, but the same way in
-// all of a row.  Over many tokens it averages out to 1.4 times the result's; over few it
-// may be twice that.  So up to kLowTokens tokens have a second row of d each, with what
-// rounding left of the first, and their rows of x twice: dweight's sums run over both.  dx
-// takes both up to kLowDx tokens, which no tile is fuller for; of more it takes what was
-// left of the target's entry times its row of the weights, in fp32.
-constexpr int kLowTokens = 128, kLowDx = 64;
+// all of a row.  So what rounding left of it is kept as well.
+//   Up to kLowTokens tokens have a second row of d each, with what rounding left of all of
+// the first, and their rows of x twice: dweight's sums run over both, and dx takes both up
+// to kLowDx tokens, which no tile is fuller for.
+//   Of more tokens only what was left of the target's entry counts.  dx takes it times its
+// row of the weights, in fp32.  For dweight tokens stand in the order of their targets, so
+// that those of one tile of the vocabulary are neighbours, and what was left of their
+// entries, kLowCols columns of zeros and one number for each token, is a second operand,
+// behind the first: few inner indices for most tiles, and never more than once as many.
+constexpr int kLowTokens = 128, kLowDx = 64, kLowCols = 256, kBlockRows = 128;
+constexpr int kPieceRows = 256;             // a piece of the vocabulary is a multiple of
 
 struct LossArgs {
     const char* x;
@@ -73,6 +79,10 @@ struct LossArgs {
     char* out;                  // dweight
     int64_t out_stride;
     float* w_parts;             // [splits][piece][pitch] fp32
+    // beyond kLowTokens
+    char* low_d;                // [tokens][kLowCols] the same as columns of d; null: not kept
+    int32_t* block_first;       // with low_d: the first place of each kBlockRows rows, and behind the last
+    Found* run_found;           // of each run of the sort, for more tokens than kGather: count, and in raise the largest dloss
 };
 
 __device__ __forceinline__ int32_t target_of(const LossArgs& a, int64_t t) {
@@ -97,16 +107,18 @@ __device__ __forceinline__ Found found_of(const LossArgs& a, int count, float mo
     return Found{count, up, largest / unit, a.dloss != nullptr && count <= kLowTokens ? count : 0};
 }
 
+__device__ __forceinline__ void put_grad(const LossArgs& a, const Found& found, int64_t t, int32_t p) {
+    a.grad[p] = a.dloss[t * a.dloss_stride] * a.scale * found.raise;
+    a.lse_at[p] = a.lse_in[t];
+    a.place[t] = p;
+}
+
 // Token t, which takes part at place p or, target < 0, does not.
 __device__ __forceinline__ void put_token(const LossArgs& a, const Found& found, int64_t t, int32_t target, int32_t p) {
     if (target >= 0) {
         a.token[p] = (int32_t)t;
         a.target[p] = target;
-        if (a.dloss != nullptr) {
-            a.grad[p] = a.dloss[t * a.dloss_stride] * a.scale * found.raise;
-            a.lse_at[p] = a.lse_in[t];
-            a.place[t] = p;
-        }
+        if (a.dloss != nullptr) put_grad(a, found, t, p);
     } else if (a.dloss != nullptr) {
         a.place[t] = -1;
     } else {
@@ -121,15 +133,35 @@ __device__ __forceinline__ void copy_row(const LossArgs& a, int64_t t, int64_t p
     for (int c = threadIdx.x & 63; c < a.hidden / 8; c += 64) to[c] = from[c];
 }
 
+// For low_d, by the wave of the token with `target` at place p, behind one with `before`
+// (-1: none): zeros, and the blocks that begin there.
+__device__ __forceinline__ void start_low(const LossArgs& a, int32_t before, int32_t target, int32_t p, int32_t count) {
+    const int lane = threadIdx.x & 63;
+    static_assert(kLowCols * 2 == 64 * 8, "eight bytes a lane");
+    reinterpret_cast<u32x2*>(a.low_d + (int64_t)p * kLowCols * 2)[lane] = u32x2{};
+    const int32_t mine = target / kBlockRows, end = (int32_t)((a.rows + kBlockRows - 1) / kBlockRows);
+    for (int32_t b = (before < 0 ? 0 : before / kBlockRows + 1) + lane; b <= mine; b += 64) a.block_first[b] = p;
+    if (p == count - 1)
+        for (int32_t b = mine + 1 + lane; b <= end; b += 64) a.block_first[b] = count;
+}
+
 // Up to kGather tokens: a workgroup has four of them, a wave each, and looks at all the
-// others' targets itself, which is quicker than a launch before it.
+// others' targets itself, which is quicker than a launch before it.  SORTED: places in the
+// order of the targets, for low_d; else in that of the tokens.
 constexpr int kGather = 4096;
+template <bool SORTED>
 __global__ __launch_bounds__(256) void loss_gather_kernel(LossArgs a) {
-    __shared__ int32_t wave_count[4], wave_before[4];
+    constexpr int N = SORTED ? 4 : 1;
+    __shared__ int32_t wave_count[4], wave_before[4][N], wave_lower[4][N];
     __shared__ float wave_most[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int tokens = (int)a.tokens, mine = blockIdx.x * 4;
-    int32_t count = 0, before = 0;
+    int32_t count = 0, before[N] = {}, lower[N], own[N];        // lower: the target of the place before
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        lower[n] = -1;
+        own[n] = SORTED ? target_of(a, min(mine + n, tokens - 1)) : 0;
+    }
     float most = 0.0f;
     for (int t0 = 0; t0 < tokens; t0 += 1024) {
         int32_t target[4];
@@ -140,73 +172,79 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(LossArgs a) {
             const int t = t0 + i * 256 + tid;
             if (t >= tokens || target[i] < 0) continue;
             ++count;
-            before += t < mine;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const bool ahead = SORTED ? target[i] < own[n] || (target[i] == own[n] && t < mine + n) : t < mine;
+                before[n] += ahead;
+                if (SORTED && ahead) lower[n] = max(lower[n], target[i]);
+            }
             if (a.dloss != nullptr) most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
         }
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
         count += __shfl_xor(count, m);
-        before += __shfl_xor(before, m);
         most = fmaxf(most, __shfl_xor(most, m));
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            before[n] += __shfl_xor(before[n], m);
+            if constexpr (SORTED) lower[n] = max(lower[n], __shfl_xor(lower[n], m));
+        }
     }
     if (lane == 0) {
         wave_count[wave] = count;
-        wave_before[wave] = before;
         wave_most[wave] = most;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            wave_before[wave][n] = before[n];
+            wave_lower[wave][n] = lower[n];
+        }
     }
     __syncthreads();
-    count = before = 0;
+    const int n = SORTED ? wave : 0;
+    int32_t place = 0, below = -1;
+    count = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         count += wave_count[w];
-        before += wave_before[w];
         most = fmaxf(most, wave_most[w]);
+        place += wave_before[w][n];
+        below = max(below, wave_lower[w][n]);
     }
     const Found found = found_of(a, count, most);
     if (blockIdx.x == 0 && tid == 0) *a.found = found;
     const int t = mine + wave;
     if (t >= tokens) return;
-    for (int i = 0; i < wave; ++i) before += target_of(a, mine + i) >= 0;
+    if constexpr (!SORTED)
+        for (int i = 0; i < wave; ++i) place += target_of(a, mine + i) >= 0;
     const int32_t target = target_of(a, t);
-    if (lane == 0) put_token(a, found, t, target, before);
+    if (lane == 0) put_token(a, found, t, target, place);
     if (target < 0) return;
-    copy_row(a, t, before);
-    if (found.low > 0) copy_row(a, t, found.count + before);
+    copy_row(a, t, place);
+    if (found.low > 0) copy_row(a, t, found.count + place);
+    if constexpr (SORTED) start_low(a, below, target, place, count);
 }
 
-// More tokens: one workgroup for which they are, then their rows.
+// The forward pass of more tokens (and the gradient of none): one workgroup for which they
+// are, then their rows.
 __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
     __shared__ int32_t wave_count[16];
-    __shared__ float wave_most[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // a wave's tokens: whole steps of 64 in a row
     const int64_t each = (a.tokens + 1023) / 1024 * 64;
     const int64_t begin = wave * each, end = min(a.tokens, begin + each);
     int32_t count = 0;
-    float most = 0.0f;
-    for (int64_t t = begin + lane; t < end; t += 64) {
-        if (target_of(a, t) < 0) continue;
-        ++count;
-        if (a.dloss != nullptr) most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
-    }
+    for (int64_t t = begin + lane; t < end; t += 64) count += target_of(a, t) >= 0;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        count += __shfl_xor(count, m);
-        most = fmaxf(most, __shfl_xor(most, m));
-    }
-    if (lane == 0) {
-        wave_count[wave] = count;
-        wave_most[wave] = most;
-    }
+    for (int m = 1; m < 64; m <<= 1) count += __shfl_xor(count, m);
+    if (lane == 0) wave_count[wave] = count;
     __syncthreads();
     int32_t at = 0, all = 0;
     for (int w = 0; w < 16; ++w) {
         if (w < wave) at += wave_count[w];
         all += wave_count[w];
-        most = fmaxf(most, wave_most[w]);
     }
-    const Found found = found_of(a, all, most);
+    const Found found = found_of(a, all, 0.0f);
     for (int64_t t0 = begin; t0 < end; t0 += 64) {
         const int64_t t = t0 + lane;
         const int32_t target = t < end ? target_of(a, t) : -1;
@@ -222,10 +260,68 @@ __global__ __launch_bounds__(1024) void loss_tokens_kernel(LossArgs a) {
 // Their rows, one a wave.
 __global__ __launch_bounds__(256) void loss_rows_kernel(LossArgs a) {
     const int64_t p = wide_block() * 4 + (threadIdx.x >> 6);
-    const Found found = *a.found;
-    if (p >= found.count) return;
-    copy_row(a, a.token[p], p);
-    if (found.low > 0) copy_row(a, a.token[p], found.count + p);
+    if (p < a.found->count) copy_row(a, a.token[p], p);
+}
+
+// The gradient of more tokens: a sort by their targets, whose first launch also finds how
+// many take part and the largest dloss, and whose lists are a.target and a.token; then, a
+// wave a place, what belongs there.
+__global__ __launch_bounds__(kSortThreads) void loss_count_kernel(LossArgs a, SortPass q) {
+    __shared__ int32_t wave_count[kSortWaves];
+    __shared__ float wave_most[kSortWaves];
+    sort_count(q);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t begin = (int64_t)blockIdx.x << q.run_shift, end = min(begin + (1ll << q.run_shift), q.n);
+    int32_t count = 0;
+    float most = 0.0f;
+    for (int64_t t = begin + tid; t < end; t += kSortThreads) {
+        if (target_of(a, t) < 0) continue;
+        ++count;
+        most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        count += __shfl_xor(count, m);
+        most = fmaxf(most, __shfl_xor(most, m));
+    }
+    if (lane == 0) {
+        wave_count[wave] = count;
+        wave_most[wave] = most;
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < kSortWaves; ++w) {
+        count += wave_count[w];
+        most = fmaxf(most, wave_most[w]);
+    }
+    a.run_found[blockIdx.x] = Found{count, most, 0.0f, 0};
+}
+
+__global__ __launch_bounds__(kSortThreads) void loss_place_kernel(SortPass q) { sort_place(q); }
+
+__global__ __launch_bounds__(256) void loss_sorted_rows_kernel(LossArgs a, int runs) {
+    const int64_t p = wide_block() * 4 + (threadIdx.x >> 6);
+    if (p >= a.tokens) return;
+    static_assert(kMostRuns <= 64, "a run a lane");
+    const int lane = threadIdx.x & 63;
+    int32_t count = lane < runs ? a.run_found[lane].count : 0;
+    float most = lane < runs ? a.run_found[lane].raise : 0.0f;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        count += __shfl_xor(count, m);
+        most = fmaxf(most, __shfl_xor(most, m));
+    }
+    const Found found = found_of(a, count, most);
+    if (p == 0 && lane == 0) *a.found = found;
+    const int32_t token = a.token[p];
+    if (p >= count) {                       // behind all rows' tokens
+        if (lane == 0) a.place[token] = -1;
+        return;
+    }
+    if (lane == 0) put_grad(a, found, token, (int32_t)p);
+    copy_row(a, token, p);
+    if (found.low > 0) copy_row(a, token, count + p);
+    start_low(a, p > 0 ? a.target[p - 1] : -1, a.target[p], (int32_t)p, count);
 }
 
 // ---------------------------------------------------------------------------
@@ -311,12 +407,22 @@ __device__ __forceinline__ void logits_tile(const LossArgs& a, int count, uint32
                     acc[i][j][r] = m < rows ? p * g : 0.0f;
                 }
             if (!here) continue;
+            // the target's entry, if the lane has it
+            bool mine = false;
+            float entry = 0.0f;
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (P::m_of(i, r) == target && n < count)
-                        a.low_target[n] = acc[i][j][r] - to_f32(from_f32<T>(acc[i][j][r]));
+                for (int r = 0; r < 16; ++r) {
+                    const bool this_one = P::m_of(i, r) == target;
+                    mine = mine || this_one;
+                    entry = this_one ? acc[i][j][r] : entry;
+                }
+            if (!mine || n >= count) continue;
+            const float low = entry - to_f32(from_f32<T>(entry));
+            a.low_target[n] = low;
+            if (a.low_d != nullptr)
+                reinterpret_cast<T*>(a.low_d)[(int64_t)n * kLowCols + a.target[n] % kLowCols] = from_f32<T>(low);
         }
         const auto row_of = [&](int n, int first) {
             return n0 + n < count ? reinterpret_cast<T*>(a.d) + (int64_t)(first + n0 + n) * a.d_pitch + m0 : nullptr;
@@ -607,7 +713,8 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
     store_parts<P>(acc, to, a.pitch, count - n0, a.hidden - m0, a.first == 0);
 }
 
-// dweight's rows of the piece, or with SPLIT a share of their sums.  With few inner indices
+// dweight's rows of the piece, or with SPLIT a share of their sums.  Behind the tokens' d
+// the tile's own low_d, of which a split has a share too.  With few inner indices
 // writing them is what counts: then a row's tiles run one after the other (262 MB for 8
 // tokens: 79 us in groups of four, 73 so).
 constexpr uint32_t kWholeRows = 4096;
@@ -620,11 +727,26 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) 
         return;
     const int count = __builtin_amdgcn_readfirstlane(a.found->count + a.found->low);
     const int n0 = tn * P::TN, m0 = tm * P::TM, k0 = SPLIT ? blockIdx.y * a.split_len : 0;
+    int low0 = 0, low1 = 0;                 // places
+    if (a.low_d != nullptr && a.found->low == 0 && count > 0) {
+        static_assert(P::TN % kBlockRows == 0 && kLowCols % P::TN == 0 && kPieceRows % kLowCols == 0, "blocks of a tile");
+        const int64_t block = (a.row0 + n0) / kBlockRows, end = (a.rows + kBlockRows - 1) / kBlockRows;
+        low0 = __builtin_amdgcn_readfirstlane(a.block_first[block]);
+        low1 = __builtin_amdgcn_readfirstlane(a.block_first[min(end, block + P::TN / kBlockRows)]);
+        if constexpr (SPLIT) {
+            const int share = ((low1 - low0 + (int)gridDim.y - 1) / (int)gridDim.y + kInner - 1) / kInner * kInner;
+            low0 = min(low1, low0 + (int)blockIdx.y * share);
+            low1 = min(low1, low0 + share);
+        }
+    }
     const int inner = SPLIT ? min(a.split_len, count - k0) : count;
     f32x16 acc[MB][NB] = {};
     const Operand x{a.xc + ((int64_t)k0 * a.pitch + m0) * 2, (int64_t)a.pitch * 2, a.hidden - m0, inner};
     const Operand d{a.d + ((int64_t)k0 * a.d_pitch + n0) * 2, (int64_t)a.d_pitch * 2, a.d_pitch - n0, inner};
-    P::run(acc, x, d);
+    const Operand low_x{a.xc + ((int64_t)low0 * a.pitch + m0) * 2, (int64_t)a.pitch * 2, a.hidden - m0, low1 - low0};
+    const Operand low_d{a.low_d + ((int64_t)low0 * kLowCols + n0 % kLowCols) * 2, kLowCols * 2, kLowCols - n0 % kLowCols,
+                        low1 - low0};
+    P::template run<true>(acc, x, d, low_x, low_d);
     const int n_left = a.piece - n0;
     if constexpr (SPLIT) {
         float* to = a.w_parts + ((int64_t)blockIdx.y * a.piece + n0) * a.pitch + m0;
@@ -702,7 +824,6 @@ __global__ __launch_bounds__(256) void loss_dx_finish_kernel(LossArgs a, char* d
 // host
 // ---------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = 512ll << 20;        // of d
-constexpr int kPieceRows = 256;                     // a piece is a multiple of
 constexpr int kFewTokens = 64;
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -719,6 +840,7 @@ int tile_size(int64_t first, int64_t second) {
 
 struct LossPlan {
     int64_t found, token, place, target, grad, lse_at, low_target, xc, parts, picked, d, dx_parts, w_parts, bytes;
+    int64_t low_d, block_first, token2, target2, counts, run_found;
     int64_t dx_rows, pitch, piece, row_tiles, splits, split_len, w_splits, w_split_len;
     int tile, dx_tile, w_tile;
     bool few;
@@ -767,6 +889,16 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     p.grad = take(4 * T);
     p.lse_at = take(4 * T);
     p.low_target = take(4 * T);
+    if (T > kLowTokens) {
+        p.low_d = take(2 * T * kLowCols);
+        p.block_first = take(4 * (tiles(a->rows, kBlockRows) + 1));
+    }
+    if (T > kGather) {
+        p.token2 = take(4 * T);
+        p.target2 = take(4 * T);
+        p.counts = take(kSortCountBytes);
+        p.run_found = take(kMostRuns * sizeof(Found));
+    }
     // and no more than that 256 rows of d stay within 31 bits of bytes
     p.piece = std::min({up(a->rows, kPieceRows), (int64_t)(1 << 22) - kPieceRows,
                         std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows)});
@@ -825,6 +957,10 @@ LossArgs loss_args(const c3_vocab_loss_t* c, const LossPlan& p, const void* x, c
     a.grad = reinterpret_cast<float*>(ws + p.grad);
     a.lse_at = reinterpret_cast<float*>(ws + p.lse_at);
     a.low_target = reinterpret_cast<float*>(ws + p.low_target);
+    // the loss itself, and the gradient of few tokens, have no such thing
+    a.low_d = p.low_d > 0 ? ws + p.low_d : nullptr;
+    a.block_first = reinterpret_cast<int32_t*>(ws + p.block_first);
+    a.run_found = reinterpret_cast<Found*>(ws + p.run_found);
     a.dx_rows = p.dx_rows;
     a.xc = ws + p.xc;
     a.parts = reinterpret_cast<float2*>(ws + p.parts);
@@ -866,10 +1002,24 @@ void launch_logits(const LossArgs& a, int64_t rows, int tile, hipStream_t s) {
 }
 
 // Which tokens take part, and their rows together.
-void launch_tokens(const LossArgs& a, hipStream_t s) {
+void launch_tokens(const LossArgs& a, const LossPlan& p, char* ws, hipStream_t s) {
     const uint64_t blocks = (uint64_t)(a.tokens + 3) / 4;
     if (a.tokens > 0 && a.tokens <= kGather) {
-        loss_gather_kernel<<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a);
+        if (a.low_d != nullptr) loss_gather_kernel<true><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a);
+        else loss_gather_kernel<false><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a);
+        return;
+    }
+    if (a.tokens > 0 && a.dloss != nullptr) {
+        SortPass q = sort_of(Ids{a.targets, a.wide_targets}, a.tokens, (uint32_t)a.rows,
+                             reinterpret_cast<int32_t*>(ws + p.counts), nullptr);
+        const SortLists lists{reinterpret_cast<uint32_t*>(a.target), a.token, reinterpret_cast<uint32_t*>(ws + p.target2),
+                              reinterpret_cast<int32_t*>(ws + p.token2)};
+        loss_count_kernel<<<dim3((unsigned)q.runs), dim3(kSortThreads), 0, s>>>(a, q);
+        for (int pass = 0; pass < q.passes; ++pass) {
+            set_pass(q, pass, lists);
+            loss_place_kernel<<<dim3((unsigned)q.runs), dim3(kSortThreads), 0, s>>>(q);
+        }
+        loss_sorted_rows_kernel<<<wide_grid(blocks), dim3(256), 0, s>>>(a, q.runs);
         return;
     }
     loss_tokens_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
@@ -877,13 +1027,13 @@ void launch_tokens(const LossArgs& a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
+hipError_t launch_loss(LossArgs a, const LossPlan& p, char* ws, hipStream_t s) {
     if (p.few) {
         launch_few<T, false>(a, a.rows, s);
         loss_few_join_kernel<<<dim3((unsigned)a.tokens), dim3(1024), 0, s>>>(a, (int)p.row_tiles);
         return hipGetLastError();
     }
-    launch_tokens(a, s);
+    launch_tokens(a, p, ws, s);
     a.row0 = 0;
     a.piece = (int32_t)a.rows;
     launch_logits<T, false>(a, a.rows, p.tile, s);
@@ -892,9 +1042,9 @@ hipError_t launch_loss(LossArgs a, const LossPlan& p, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_grad(LossArgs a, const LossPlan& p, char* dx, int64_t dx_stride, hipStream_t s) {
+hipError_t launch_grad(LossArgs a, const LossPlan& p, char* ws, char* dx, int64_t dx_stride, hipStream_t s) {
     const uint64_t slabs = (a.hidden + 255) / 256;
-    launch_tokens(a, s);
+    launch_tokens(a, p, ws, s);
     for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
         a.piece = (int32_t)std::min(p.piece, a.rows - a.row0);
         a.first = a.row0 == 0;
@@ -957,7 +1107,8 @@ int c3_vocab_loss(const c3_vocab_loss_t* a, const void* x, const void* weight, c
     k.loss = loss;
     k.lse = lse;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const hipError_t e = a->dtype == C3_BF16 ? launch_loss<__bf16>(k, p, s) : launch_loss<_Float16>(k, p, s);
+    const hipError_t e = a->dtype == C3_BF16 ? launch_loss<__bf16>(k, p, static_cast<char*>(ws), s)
+                                             : launch_loss<_Float16>(k, p, static_cast<char*>(ws), s);
     return e == hipSuccess ? C3_OK : C3_E_HIP;
 }
 
@@ -987,8 +1138,8 @@ int c3_vocab_loss_grad(const c3_vocab_loss_t* a, const float* dloss, int64_t dlo
     k.out = static_cast<char*>(dweight);
     k.out_stride = dweight_stride * 2;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const hipError_t e = a->dtype == C3_BF16 ? launch_grad<__bf16>(k, p, static_cast<char*>(dx), dx_stride * 2, s)
-                                             : launch_grad<_Float16>(k, p, static_cast<char*>(dx), dx_stride * 2, s);
+    const hipError_t e = a->dtype == C3_BF16 ? launch_grad<__bf16>(k, p, static_cast<char*>(ws), static_cast<char*>(dx), dx_stride * 2, s)
+                                             : launch_grad<_Float16>(k, p, static_cast<char*>(ws), static_cast<char*>(dx), dx_stride * 2, s);
     return e == hipSuccess ? C3_OK : C3_E_HIP;
 }
 

@@ -214,16 +214,33 @@ struct Product {
     }
 
     // Adds the product over the operands' inner indices (both have the same).  LDS is free
-    // to use behind it.
-    static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b) {
+    // to use behind it.  With MORE, that of a second pair of operands across the inner index
+    // behind it in the same loop: a2 with a's outer indices and stride, b2 with any.
+    template <bool MORE = false>
+    static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b,
+                                               const Operand& a2 = {}, const Operand& b2 = {}) {
+        static_assert(!MORE || (!A_ALONG && !B_ALONG), "operands across the inner index");
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int am = wave % WM * MB, bn = wave / WM * NB, inner = a.inner;
+        const int am = wave % WM * MB, bn = wave / WM * NB;
+        const int first = MORE ? (max(a.inner, 0) + kInner - 1) / kInner * kInner : a.inner;
+        const int inner = MORE ? first + max(a2.inner, 0) : first;
         const TileA ta(a, wave);
-        const TileB tb(b, wave);
+        const TileB tb(b, wave), tb2(MORE ? b2 : b, wave);
         if (inner <= 0) return;
         const auto load = [&](int k, char* la, char* lb) {
-            ta.load(a, k, la, wave);
-            tb.load(b, k, lb, wave);
+            if constexpr (MORE) {           // without a branch between the loads and what runs beside them
+                const bool more = k >= first;
+                const Operand oa{more ? a2.p : a.p, a.stride, a.outer, more ? a2.inner : a.inner};
+                const Operand ob{more ? b2.p : b.p, more ? b2.stride : b.stride, more ? b2.outer : b.outer, oa.inner};
+                TileB t = tb;
+#pragma unroll
+                for (int n = 0; n < TileB::kLoads; ++n) t.at[n] = more ? tb2.at[n] : tb.at[n];
+                ta.load(oa, more ? k - first : k, la, wave);
+                t.load(ob, more ? k - first : k, lb, wave);
+            } else {
+                ta.load(a, k, la, wave);
+                tb.load(b, k, lb, wave);
+            }
         };
         Operands f[2];
         const auto read = [&](Operands& to, const char* la, const char* lb, int ks) {
@@ -255,11 +272,14 @@ struct Product {
         landed<kLoads>();
         read(f[0], lds_a<0>(), lds_b<0>(), 0);
         __builtin_amdgcn_sched_barrier(0);
-        // both stages in a turn; zeros behind the last tile
-        for (int k = 0; k < inner; k += 2 * kInner) {
+        // both stages in a turn; zeros behind the last tile, or with MORE, where one more tile
+        // is the rule, half a turn for the last
+        int k = 0;
+        for (; k < (MORE ? inner - kInner : inner); k += 2 * kInner) {
             step(k, lds_a<0>(), lds_b<0>(), lds_a<1>(), lds_b<1>());
             step(k + kInner, lds_a<1>(), lds_b<1>(), lds_a<0>(), lds_b<0>());
         }
+        if (MORE && k < inner) step(k, lds_a<0>(), lds_b<0>(), lds_a<1>(), lds_b<1>());
         landed<0>();
     }
 };
