@@ -91,9 +91,23 @@ __device__ __forceinline__ int32_t target_of(const LossArgs& a, int64_t t) {
     return (uint64_t)v < (uint64_t)a.rows ? (int32_t)v : -1;
 }
 
+// What rounding leaves of an entry of d; nothing of one that is not finite.
+template <typename T>
+__device__ __forceinline__ float left_of(float d) {
+    const float rounded = to_f32(from_f32<T>(d));
+    return fabsf(rounded) < __builtin_inff() ? d - rounded : 0.0f;
+}
+
 // ---------------------------------------------------------------------------
 // which tokens take part
 // ---------------------------------------------------------------------------
+// The size of a token's dloss if it is finite: one that is not makes infinities of its own
+// row, and is no measure of the others.
+__device__ __forceinline__ float size_of(const LossArgs& a, int64_t t) {
+    const float size = fabsf(a.dloss[t * a.dloss_stride] * a.scale);
+    return size < __builtin_inff() ? size : 0.0f;
+}
+
 __device__ __forceinline__ Found found_of(const LossArgs& a, int count, float most) {
     // d is kept relative to the largest dloss: with one dloss for all tokens, a mean's, the
     // target's entry of an unlikely token then is -1 in 16 bits, and not wherever that dloss
@@ -101,8 +115,7 @@ __device__ __forceinline__ Found found_of(const LossArgs& a, int count, float mo
     // that holds 6e-8 to 65,504 and most entries are about one over the vocabulary's size.
     // The bounds keep `up` and `lower` normal numbers.
     const float unit = a.half ? 8192.0f : 1.0f;
-    const bool fine = most > 0.0f && most < __builtin_inff();
-    const float largest = fine ? fminf(fmaxf(most, 0x1p-100f), 0x1p126f) : 1.0f;
+    const float largest = most > 0.0f ? fminf(fmaxf(most, 0x1p-100f), 0x1p126f) : 1.0f;
     const float up = unit / largest;
     return Found{count, up, largest / unit, a.dloss != nullptr && count <= kLowTokens ? count : 0};
 }
@@ -178,7 +191,7 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(LossArgs a) {
                 before[n] += ahead;
                 if (SORTED && ahead) lower[n] = max(lower[n], target[i]);
             }
-            if (a.dloss != nullptr) most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
+            if (a.dloss != nullptr) most = fmaxf(most, size_of(a, t));
         }
     }
 #pragma unroll
@@ -277,7 +290,7 @@ __global__ __launch_bounds__(kSortThreads) void loss_count_kernel(LossArgs a, So
     for (int64_t t = begin + tid; t < end; t += kSortThreads) {
         if (target_of(a, t) < 0) continue;
         ++count;
-        most = fmaxf(most, fabsf(a.dloss[t * a.dloss_stride] * a.scale));
+        most = fmaxf(most, size_of(a, t));
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -419,7 +432,7 @@ __device__ __forceinline__ void logits_tile(const LossArgs& a, int count, uint32
                     entry = this_one ? acc[i][j][r] : entry;
                 }
             if (!mine || n >= count) continue;
-            const float low = entry - to_f32(from_f32<T>(entry));
+            const float low = left_of<T>(entry);
             a.low_target[n] = low;
             if (a.low_d != nullptr)
                 reinterpret_cast<T*>(a.low_d)[(int64_t)n * kLowCols + a.target[n] % kLowCols] = from_f32<T>(low);
@@ -433,7 +446,7 @@ __device__ __forceinline__ void logits_tile(const LossArgs& a, int count, uint32
         if (a.found->low > 0)
             store_rows<P, T, MB, NB>(
                 a.d_pitch - m0,
-                [&](int j, int i, int r) { return from_f32<T>(acc[i][j][r] - to_f32(from_f32<T>(acc[i][j][r]))); },
+                [&](int j, int i, int r) { return from_f32<T>(left_of<T>(acc[i][j][r])); },
                 [&](int n) { return row_of(n, count); });
     }
 }
@@ -582,7 +595,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void loss_few_kernel(LossArgs a) {
                         if (m == target) p -= 1.0f;
                         const float d = m < rows ? p * g : 0.0f;
                         v.v[r] = from_f32<T>(d);
-                        low.v[r] = from_f32<T>(d - to_f32(v.v[r]));
+                        low.v[r] = from_f32<T>(left_of<T>(d));
                     }
                     *reinterpret_cast<AlignedPack<T, 4>*>(to + m_of(i, 4 * q)) = v;
                     *reinterpret_cast<AlignedPack<T, 4>*>(to + (int64_t)tokens * a.d_pitch + m_of(i, 4 * q)) = low;

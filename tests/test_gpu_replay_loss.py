@@ -291,3 +291,27 @@ def test_targets_in_one_place(T, V):
         x, weight, targets, dloss = _inputs(T, 72, V, BF16, 0.1, seed=15)
         targets = torch.where((targets >= 0) & (targets < V), share.long(), targets)
         _compare(_both(x, weight, targets, dloss), plain.vocab_loss(x, weight, targets, 1.0, dloss), f"{T} {V} {n}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("T", [7, 100, 129, 300, 5000])
+def test_dloss_that_is_not_finite(dtype, T):
+    """An infinite dloss makes its token's share of dweight infinite, and the other tokens' rows
+    of dx are what they are without it, also in fp16 where dloss is past what it holds."""
+    x, weight, targets, dloss = _inputs(T, 72, 300, dtype, seed=16)
+    weight = weight * 2.0 ** -6             # dx within fp16
+    dloss = dloss * (100.0 / dloss.max())
+    dloss[3] = float("inf")
+    print("CASE", dtype, T, flush=True)
+    got = _both(x, weight, targets, dloss)
+    rest = torch.arange(T) != 3
+    want, bound = plain.vocab_loss(x[rest], weight, targets[rest], 1.0, dloss[rest])["dx"]
+    within(got["dx"].cpu()[rest], want, bound, "dx")
+    sign = torch.ones((300, 1))
+    sign[targets[3]] = -1.0
+    share = sign * x[3].float() * float("inf")
+    assert torch.equal(got["dweight"].cpu().float()[:, x[3] != 0], share[:, x[3] != 0])
+    dloss[3] = float("nan")
+    got = _both(x, weight, targets, dloss)
+    within(got["dx"].cpu()[rest], want, bound, "dx")
+    assert bool(got["dx"][3].isnan().all()) and bool(got["dweight"].isnan().all())
