@@ -315,3 +315,17 @@ def test_dloss_that_is_not_finite(dtype, T):
     got = _both(x, weight, targets, dloss)
     within(got["dx"].cpu()[rest], want, bound, "dx")
     assert bool(got["dx"][3].isnan().all()) and bool(got["dweight"].isnan().all())
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -20, 2.0 ** -14])
+def test_small_gradients_in_fp16(factor):
+    """As test_gradients_of_any_size_in_fp16, from gradients so large that fp16 holds a part of
+    the small ones in full."""
+    x, weight, targets, dloss = _inputs(200, 64, 3000, F16, seed=6)
+    one = _both(x, weight, targets, dloss * 2.0 ** 14)
+    other = _both(x, weight, targets, dloss * (2.0 ** 14 * factor))
+    for name in ("dx", "dweight"):
+        a, b = one[name].double() * factor, other[name].double()
+        fine = (a.abs() > 2.0 ** -14) & (one[name].double().abs() < 60000)
+        assert int(fine.sum()) > 100, (name, int(fine.sum()))
+        assert torch.equal(a[fine], b[fine]), name
