@@ -341,7 +341,8 @@ typedef struct {
 } c3_vocab_loss_t;
 
 /* Device workspace bytes of c3_vocab_loss and of c3_vocab_loss_grad (256 at least; 0 if
- * invalid). */
+ * invalid).  The gradient's holds d for a piece of the vocabulary: up to 512 MiB, or beyond
+ * 131,072 tokens 4 KiB a token. */
 size_t c3_vocab_loss_workspace_size(const c3_vocab_loss_t *a);
 size_t c3_vocab_loss_grad_workspace_size(const c3_vocab_loss_t *a);
 

@@ -836,7 +836,7 @@ __global__ __launch_bounds__(256) void loss_dx_finish_kernel(LossArgs a, char* d
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-constexpr int64_t kPieceBytes = 512ll << 20;        // of d
+constexpr int64_t kPieceBytes = 512ll << 20;        // of d, up to 131,072 tokens
 constexpr int kFewTokens = 64;
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -912,9 +912,10 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
         p.counts = take(kSortCountBytes);
         p.run_found = take(kMostRuns * sizeof(Found));
     }
-    // and no more than that 256 rows of d stay within 31 bits of bytes
+    // d of kPieceBytes, second rows with it, but 2,048 rows of the vocabulary at least; and no
+    // more than that 256 rows of d stay within 31 bits of bytes
     p.piece = std::min({up(a->rows, kPieceRows), (int64_t)(1 << 22) - kPieceRows,
-                        std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(T, 1) / kPieceRows * kPieceRows)});
+                        std::max<int64_t>(2048, kPieceBytes / 2 / std::max<int64_t>(with_low, 1) / kPieceRows * kPieceRows)});
     p.d = take(2 * with_low * p.piece);
     p.tile = tile_size(p.piece, T);
     p.dx_rows = T <= kLowDx ? 2 * T : std::max<int64_t>(T, 2 * kLowDx);

@@ -803,8 +803,10 @@ def vocab_loss_grad(dloss, x, weight, targets, lse, *, scale: float = 1.0, dx=No
                     workspace=None, stream=None):
     """(dx, dweight) of ``vocab_loss`` with the same arguments, from its ``lse`` and the
     gradient dloss fp32 [T] of its losses, which may be one number expanded to [T].  Rows
-    of dx whose token takes no part are zeros.  The workspace holds the softmax of up to
-    512 MiB of tokens by vocabulary at a time."""
+    of dx whose token takes no part are zeros.  The workspace holds the softmax of tokens by a
+    piece of the vocabulary: up to 512 MiB, or beyond 131,072 tokens 4 KiB a token.  In fp16
+    entries of the softmax's difference times dloss that are below 2^-37 of the largest dloss
+    are lost: a token whose dloss is a small part of the largest keeps its large entries only."""
     a = _loss_args(x, weight, targets, scale)
     if not isinstance(dloss, torch.Tensor) or not dloss.is_cuda:
         raise C3Error("dloss must be a tensor on a ROCm GPU device")

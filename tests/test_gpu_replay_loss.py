@@ -329,3 +329,36 @@ def test_small_gradients_in_fp16(factor):
         fine = (a.abs() > 2.0 ** -14) & (one[name].double().abs() < 60000)
         assert int(fine.sum()) > 100, (name, int(fine.sum()))
         assert torch.equal(a[fine], b[fine]), name
+
+
+def _against_plain_on_the_device(x, weight, targets, dloss, some, row_parts):
+    """dx of the tokens `some` and dweight's parts in 64 bits: d is rounded once and the results
+    once, half a step of each, so an error in the norm is below 2 half steps."""
+    got = _both(x, weight, targets, dloss)
+    W, dw = weight.double(), torch.zeros(weight.shape, dtype=torch.float64, device=DEV)
+    for at in torch.arange(len(x), device=DEV).split(max(1, 2 ** 28 // len(weight))):
+        p = torch.mm(x[at].double(), W.t())
+        p = (p - torch.logsumexp(p, 1, keepdim=True)).exp()
+        p[torch.arange(len(at), device=DEV), targets[at].long()] -= 1.0
+        p *= dloss[at].double()[:, None]
+        dw += torch.mm(p.t(), x[at].double())
+        mine = some[(some >= at[0]) & (some <= at[-1])]
+        want = torch.mm(p[mine - at[0]], W)
+        off = (got["dx"][mine].double() - want).norm(dim=1) / want.norm(dim=1)
+        assert bool((off <= 2 * 2.0 ** -8).all()), (mine, off)
+    for part in row_parts:
+        off = (got["dweight"][part].double() - dw[part]).norm() / dw[part].norm()
+        assert float(off) <= 2 * 2.0 ** -8, (part, float(off))
+
+
+def test_second_rows_of_d_in_pieces():
+    """100 tokens, each with two rows of d, over 3,000,000 rows: three pieces."""
+    T, H, V = 100, 8, 3_000_000
+    print("CASE", T, H, V, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(17)
+    weight = torch.randn((V, H), generator=g, device=DEV).to(BF16)
+    x = torch.randn((T, H), generator=g, device=DEV).to(BF16)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV)
+    targets[:2] = torch.tensor([V - 1, 0], device=DEV)
+    _against_plain_on_the_device(x, weight, targets, torch.ones((T,), device=DEV), torch.arange(T, device=DEV),
+                                 [targets, slice(0, 1 << 20), slice(1 << 20, 2 << 20), slice(2 << 20, V)])

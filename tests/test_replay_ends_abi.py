@@ -194,6 +194,19 @@ def test_loss_workspace_holds_a_piece():
     assert (512 << 20) < some < (900 << 20)
 
 
+def test_loss_workspace_of_few_and_many_tokens():
+    """512 MiB of d with the second rows that up to 128 tokens have, and beyond 131,072 tokens
+    2,048 rows of the vocabulary: 4 KiB a token."""
+    def size(tokens, rows):
+        return _loss(True, size=True, tokens=tokens, hidden=16, rows=rows)
+    for tokens in (64, 127, 128):
+        assert size(tokens, 3_000_000) <= (512 << 20) + (1 << 20), tokens
+    for tokens in (129, 1000, 131_072):
+        assert size(tokens, 1_000_000) <= (512 << 20) + 2048 * tokens + (64 << 20), tokens
+    for tokens in (200_000, 1 << 20):
+        assert 4096 * tokens < size(tokens, 8000) <= (4096 + 2048) * tokens + (64 << 20), tokens
+
+
 def test_cpu_tensors_and_graphs_are_refused():
     x = torch.zeros((4, 16), dtype=torch.bfloat16)
     ids, w = torch.zeros((4,), dtype=torch.int64), torch.ones((16,), dtype=torch.bfloat16)
