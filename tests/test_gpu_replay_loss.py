@@ -362,3 +362,18 @@ def test_second_rows_of_d_in_pieces():
     targets[:2] = torch.tensor([V - 1, 0], device=DEV)
     _against_plain_on_the_device(x, weight, targets, torch.ones((T,), device=DEV), torch.arange(T, device=DEV),
                                  [targets, slice(0, 1 << 20), slice(1 << 20, 2 << 20), slice(2 << 20, V)])
+
+
+def test_d_past_32_bits():
+    """2^20 + 77 tokens: pieces of 2,048 rows, d of more than 2^31 elements in each."""
+    T, H, V = (1 << 20) + 77, 8, 5000
+    print("CASE", T, H, V, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(18)
+    weight = torch.randn((V, H), generator=g, device=DEV).to(BF16)
+    x = torch.randn((T, H), generator=g, device=DEV).to(BF16)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV)
+    dloss = 0.5 + torch.rand((T,), generator=g, device=DEV)
+    order = targets.argsort()
+    some = torch.cat((torch.tensor([0, 1, T // 2, T - 2, T - 1], device=DEV), order[:3], order[-3:])).unique()
+    _against_plain_on_the_device(x, weight, targets, dloss, some,
+                                 [slice(0, 2048), slice(2048, 4096), slice(4096, V), slice(V - 100, V)])
