@@ -761,8 +761,12 @@ def residual_norm_grad(dn, dh, x, y, weight, stats, *, post=None, gate=None, sca
 # ---------------------------------------------------------------------------
 def _loss_args(x, weight, targets, scale):
     _rows(x, "x", dim=(2,))
+    if x.dtype == torch.float32:
+        raise C3Error("x and weight must be bf16 or fp16, which the products take")
     _rows(weight, "weight", x.dtype, x.device, (2,))
     _ids(targets, "targets", x.device)
+    if x.shape[1] % 8:
+        raise C3Error("hidden must be a multiple of 8")
     if weight.shape[1] != x.shape[1]:
         raise C3Error("x and weight must have the same hidden size")
     if targets.numel() != x.shape[0]:

@@ -243,3 +243,17 @@ def test_refusals():
     refuse(lambda: lg(v["dloss"], v["y"], v["table"], v["targets"], lse, dx=v["y"]))
     refuse(lambda: lg(v["dloss"], v["y"], v["table"], v["targets"], lse, dweight=v["table"]))
     refuse(lambda: lg(v["dloss"].clone().requires_grad_(), v["y"], v["table"], v["targets"], lse))
+
+
+def test_what_the_loss_refuses_it_names():
+    v = _inputs(12)
+    y, table, targets = v["y"], v["table"], v["targets"]
+    lse = torch.zeros((len(y),), device=DEV)
+    for call in (lambda a, b: replay.vocab_loss(a, b, targets),
+                 lambda a, b: replay.vocab_loss_grad(v["dloss"], a, b, targets, lse)):
+        with pytest.raises(replay.C3Error, match="bf16 or fp16"):
+            call(y.float(), table.float())
+        with pytest.raises(replay.C3Error, match="multiple of 8"):
+            call(y[:, :60], table[:, :60])
+        with pytest.raises(replay.C3Error, match="same hidden size"):
+            call(y, table[:, :128])
