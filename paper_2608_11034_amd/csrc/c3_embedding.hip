@@ -544,7 +544,7 @@ int c3_embedding(const c3_embedding_t* a, const void* ids, const void* table, vo
     if ((a->tokens > 1 && a->row_stride < a->hidden) || (a->rows > 1 && a->table_stride < a->hidden)) return C3_E_INVAL;
     const int es = replay_elem_size(a->dtype);
     if ((uintptr_t)ids % a->id_bytes != 0 || (uintptr_t)table % es != 0 || (uintptr_t)out % es != 0) return C3_E_ALIGN;
-    // waves are counted in 32 bits
+    // a grid has 2^22 by 2^16 workgroups, of four waves
     if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 36)) return C3_E_UNSUPPORTED;
     const LookupCall g{{ids, a->id_bytes == 8}, a->tokens, a->rows, a->hidden, a->table_stride, a->row_stride, table,
                        out, a->scale, reinterpret_cast<hipStream_t>(stream)};
@@ -574,10 +574,8 @@ int c3_embedding_grad(const c3_embedding_t* a, const void* dout, const void* ids
         return C3_E_ALIGN;
     if (ws == nullptr || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)grad_plan(a->tokens, a->rows, a->hidden).bytes)
         return C3_E_WORKSPACE;
-    // the sums' workgroups are counted in 31 bits, the zeros' in a grid's 2^22 by 2^16
-    const int64_t row_bytes = a->hidden * replay_elem_size(table_dtype);
-    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34) || a->rows / std::max<int64_t>(1, 16384 / row_bytes) >= (1ll << 37))
-        return C3_E_UNSUPPORTED;
+    // the sums' workgroups are counted in 31 bits; the zeros' are no more than rows
+    if (a->tokens * ((a->hidden + 63) / 64) >= (1ll << 34)) return C3_E_UNSUPPORTED;
     const GradCall g{{ids, a->id_bytes == 8}, a->tokens, a->rows, a->hidden, a->row_stride, a->table_stride, dout,
                      dtable, a->scale, accumulate != 0, static_cast<char*>(ws), reinterpret_cast<hipStream_t>(stream)};
     hipError_t e;
