@@ -895,7 +895,8 @@ LossPlan loss_plan(const c3_vocab_loss_t* a, bool grad) {
     }
     p.token = take(4 * T);
     p.target = take(4 * T);
-    const int64_t with_low = T + (grad ? std::min<int64_t>(T, kLowTokens) : 0);
+    // second rows are there only where no more than kLowTokens take part
+    const int64_t with_low = grad ? std::max<int64_t>(T, 2 * std::min<int64_t>(T, kLowTokens)) : T;
     p.xc = take(2 * with_low * H);
     if (!grad) return p;
     p.place = take(4 * T);
