@@ -364,14 +364,13 @@ int c3_vocab_loss(const c3_vocab_loss_t *a, const void *x, const void *weight, c
  * c3_vocab_loss_grad -- gradients of c3_vocab_loss for dloss fp32 [tokens], dloss_stride
  * elements apart (0: one number for all): with d = scale * dloss[t] * (exp(l - lse[t]) -
  * onehot(targets[t])), dx = d weight and dweight = d^T x.  d, relative to the largest
- * finite dloss, is rounded to 16 bits on its way into the products; what rounding leaves of the
- * target's entry, and up to 128 tokens of all of a token's, enters both results as well.
- * In C3_F16 steps of d are no smaller than 2^-37 of that.  All sums are fp32,
- * in an order that the sizes and the targets fix: from 129 tokens on dweight's run over the
- * tokens in the order of their targets.  lse is that of c3_vocab_loss.  dx and dweight are
- * of a->dtype; rows of dx whose
- * token takes no part are zeros.  Results overlap neither inputs nor each other.
- * Workspace and errors as c3_vocab_loss.  Can be captured.
+ * finite dloss, is rounded to 16 bits on its way into the products; what rounding leaves
+ * of the target's entry, and up to 128 tokens of all of a token's, enters both results as
+ * well.  In C3_F16 steps of d are no smaller than 2^-37 of that dloss.  All sums are fp32,
+ * in an order that the sizes and the targets fix: from 129 tokens on dweight's run over
+ * the tokens in the order of their targets.  lse is that of c3_vocab_loss.  dx and dweight
+ * are of a->dtype; rows of dx whose token takes no part are zeros.  Results overlap
+ * neither inputs nor each other.  Workspace and errors as c3_vocab_loss.  Can be captured.
  */
 int c3_vocab_loss_grad(const c3_vocab_loss_t *a, const float *dloss, int64_t dloss_stride,
                        const void *x, const void *weight, const void *targets, const float *lse,

@@ -9,10 +9,12 @@
 // Tokens whose target is no row of the vocabulary take no part: the others are copied
 // together first, so that neither their time nor what they hold enters anything.
 //
-// 8,192 tokens over 131,072 rows of 4,096 in bf16: 6.9 ms forward; back 1.85 ms for the
-// logits, 1.65 for dx and 1.64 for dweight of each quarter of the vocabulary, so that all
+// 8,192 tokens over 131,072 rows of 4,096 in bf16: 6.7 ms forward; back 1.79 ms for the
+// logits, 1.63 for dx and 1.67 for dweight of each quarter of the vocabulary, so that all
 // four products run at 1,300 TFLOP/s, as a large library product does (c3_product.h has
-// what bounds them).  8 tokens over 32,000 rows: bound by the weights, 262 MB in 43 us.
+// what bounds them).  8 tokens over 32,000 rows: bound by the weights, 262 MB in 43 us
+// forward; back 46 us for the logits, 52 for dx, which reads the weights again, and 63 for
+// 262 MB of dweight.
 #include <algorithm>
 #include <type_traits>
 
@@ -453,9 +455,10 @@ __device__ __forceinline__ void logits_tile(const LossArgs& a, int count, uint32
 
 // Where the last round of 256 by 256 tiles has work for half of a die's 32 compute units
 // at most, two take a tile of it, 128 tokens each, which costs three quarters of a round:
-// 233 of 333 fp16 tokens over 32,000 rows of 1,000 are 125 tiles, 32.7 us, and 25.7 so;
-// 2,047 over 50,001 of 2,048 six rounds and 32 tiles, 399 us, and 386 so.  How many tokens
-// take part is known here only.
+// 233 of 333 fp16 tokens over 32,000 rows of 1,000 are 125 tiles, 30.6 us, and 24.3 so;
+// 2,047 over 50,001 of 2,048 six rounds and 32 tiles, 388 us, and 377 so (medians of 600
+// launches: the first forty go through a dip of the clock to 500).  How many tokens take
+// part is known here only.
 constexpr uint32_t kUnitsOfDie = 32;
 template <typename T, bool GRAD, int WM, int WN, int MB, int NB>
 __global__ __launch_bounds__(WM * WN * 64) void loss_logits_kernel(LossArgs a) {
@@ -729,7 +732,7 @@ __global__ __launch_bounds__(WM * WN * 64) void loss_dx_kernel(LossArgs a) {
 // dweight's rows of the piece, or with SPLIT a share of their sums.  Behind the tokens' d
 // the tile's own low_d, of which a split has a share too.  With few inner indices
 // writing them is what counts: then a row's tiles run one after the other (262 MB for 8
-// tokens: 79 us in groups of four, 73 so).
+// tokens: 69 us in groups of four, 63 so).
 constexpr uint32_t kWholeRows = 4096;
 template <typename T, bool SPLIT, int WM, int WN, int MB, int NB>
 __global__ __launch_bounds__(WM * WN * 64) void loss_dweight_kernel(LossArgs a) {

@@ -8,8 +8,8 @@
 // reads from LDS, so that no operand is copied in another order first.
 //
 // What bounds it is the matrix units at the clock that the card's power leaves them: 8,192
-// x 4,096 by 131,072 x 4,096 in bf16 with the epilogue of the forward loss take 6.9 ms,
-// 1,270 TFLOP/s at 1.73 GHz with the units busy 69% of the cycles and LDS 26%, without bank
+// x 4,096 by 131,072 x 4,096 in bf16 with the epilogue of the forward loss take 6.8 ms,
+// 1,290 TFLOP/s at 1.77 GHz with the units busy 70% of the cycles and LDS 26%, without bank
 // conflicts; a large library product reaches 1,310 there.  Eight waves of 128 x 64 sums:
 // four of 128 x 128 read a third less of LDS, but nothing is left to run while one of them
 // waits (7.14 ms against 6.75); tiles of 32 inner indices, four in turn, read half lines
@@ -215,7 +215,10 @@ struct Product {
 
     // Adds the product over the operands' inner indices (both have the same).  LDS is free
     // to use behind it.  With MORE, that of a second pair of operands across the inner index
-    // behind it in the same loop: a2 with a's outer indices and stride, b2 with any.
+    // behind it in the same loop: a2 with a's outer indices and stride, b2 with any.  Which
+    // pair a load takes is chosen without a branch, which would part the loads from what runs
+    // beside them (dweight of 8,192 tokens, 32,768 rows of 4,096: 1,590 us without a second
+    // pair, 1,660 with one of a tile as a rule, 1,860 with the branch).
     template <bool MORE = false>
     static __device__ __forceinline__ void run(f32x16 (&acc)[MB][NB], const Operand& a, const Operand& b,
                                                const Operand& a2 = {}, const Operand& b2 = {}) {
@@ -228,7 +231,7 @@ struct Product {
         const TileB tb(b, wave), tb2(MORE ? b2 : b, wave);
         if (inner <= 0) return;
         const auto load = [&](int k, char* la, char* lb) {
-            if constexpr (MORE) {           // without a branch between the loads and what runs beside them
+            if constexpr (MORE) {
                 const bool more = k >= first;
                 const Operand oa{more ? a2.p : a.p, a.stride, a.outer, more ? a2.inner : a.inner};
                 const Operand ob{more ? b2.p : b.p, more ? b2.stride : b.stride, more ? b2.outer : b.outer, oa.inner};
@@ -289,7 +292,7 @@ struct Product {
 // of MB * 64 bytes.  value(j, i, r): element of block i, j, register r as T; row(n): where
 // m = 0 of the tile's row n is, or null; elements from m_left on (a multiple of 8) are not
 // there.  The rows go past the caches, which hold the operands that other workgroups share
-// (the gradient of the loss of 8 tokens over 32,000 rows of 4,096: 265 us, and 228 so).
+// (the loss of 8 tokens over 32,000 rows of 4,096, forward and back: 252 us, and 220 so).
 // Behind Product::run.
 template <typename P, typename T, int MB, int NB, typename Value, typename Row>
 __device__ __forceinline__ void store_rows(int m_left, Value value, Row row) {
