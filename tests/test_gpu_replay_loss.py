@@ -377,3 +377,18 @@ def test_d_past_32_bits():
     some = torch.cat((torch.tensor([0, 1, T // 2, T - 2, T - 1], device=DEV), order[:3], order[-3:])).unique()
     _against_plain_on_the_device(x, weight, targets, dloss, some,
                                  [slice(0, 2048), slice(2048, 4096), slice(4096, V), slice(V - 100, V)])
+
+
+@pytest.mark.parametrize("T", [129, 4096, 5000])
+def test_targets_of_none_and_of_four_bytes(T):
+    """Tokens placed by their targets: none takes part, or targets are int32 and dloss is one
+    number for all."""
+    print("CASE", T, flush=True)
+    x, weight, targets, _ = (t.to(DEV) for t in _inputs(T, 72, 300, BF16, 0.1, seed=19))
+    one = torch.full((1,), 0.25, device=DEV)
+    _, lse = replay.vocab_loss(x, weight, targets)
+    for t in replay.vocab_loss_grad(one.expand(T), x, weight, torch.full_like(targets, 300), lse):
+        assert bool((t == 0).all())
+    want = replay.vocab_loss_grad(one.expand(T).contiguous(), x, weight, targets, lse)
+    got = replay.vocab_loss_grad(one.expand(T), x, weight, targets.to(torch.int32), lse)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
